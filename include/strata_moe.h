@@ -54,12 +54,18 @@ typedef enum {
 
 typedef enum {
     STRATA_BF16 = 0,               /* dispatch copies bf16 rows bit for bit           */
-    STRATA_FP8_E4M3_B128 = 1       /* dispatch quantises to e4m3, one fp32 scale per
+    STRATA_FP8_E4M3_B128 = 1,      /* dispatch quantises to e4m3, one fp32 scale per
                                       token per block of 128 columns                  */
+    STRATA_Q8_ROW = 2              /* rows that are already 8-bit codes, H bytes, followed by
+                                      STRATA_Q8_TRAILER bytes that start with the row's fp32
+                                      scale: dispatch copies them bit for bit         */
 } strata_dtype;
+/* Bytes behind the H codes of a STRATA_Q8_ROW row (one 32-byte sector, so that rows of H % 32 == 0 stay
+ * sector-aligned): the scale travels with its row, and dispatch moves half the bytes of bf16. */
+#define STRATA_Q8_TRAILER 32
 
 /* Problem shape.  Requirements: R,T,H,E,K > 0; E % R == 0; E <= 1024; K <= 32;
- * H % 8 == 0 (rows are whole 16-byte vectors); H % 128 == 0 for FP8;
+ * H % 8 == 0 (rows are whole 16-byte vectors); H % 128 == 0 for FP8; H % 16 == 0 for Q8_ROW;
  * R*T*K + E*(segment_align-1) < 2^31.
  * Two production variants of the layout (zero = off, the packed strict layout):
  *  segment_align A > 1: every expert segment starts at a multiple of A rows (what a grouped GEMM
@@ -277,6 +283,9 @@ strata_status strata_moe_layout_noalloc(const strata_moe_shape *shape, const int
  *        per token and block of 128 columns: amax = max|x|, scale = amax/448 (IEEE binary32
  *        division), q = e4m3_rne_satfinite(x / (amax == 0 ? 1 : scale)); codes and the stored
  *        scale (amax/448) go to each of the token's K rows.
+ * Q8_ROW: x is uint8 [R,T,H+STRATA_Q8_TRAILER] (what strata_norm writes with q = x, q_stride = H + STRATA_Q8_TRAILER and
+ *        the scale of row n at byte H of the row), recv uint8 [capacity_rows, H+STRATA_Q8_TRAILER]; rows are copied
+ *        bit for bit; recv_scale must be NULL.
  * recv (and recv_scale) must lie inside a registered region (NOT_REGISTERED otherwise); x and recv
  * must be 16-byte aligned, recv_scale 4-byte aligned; capacity_rows >= strata_moe_recv_rows (CAPACITY
  * otherwise).  Items with dst_row = -1 are skipped silently; any other dst_row outside

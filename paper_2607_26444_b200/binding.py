@@ -30,6 +30,8 @@ STRATA_ERR_BAD_ROW = 10
 
 STRATA_BF16 = 0
 STRATA_FP8_E4M3_B128 = 1
+STRATA_Q8_ROW = 2
+STRATA_Q8_TRAILER = 32               # bytes behind the codes of a Q8_ROW row; the first four are its scale
 STRATA_FLAG_ALLOW_UNROUTED = 1
 
 EXPORTS = [
@@ -44,7 +46,14 @@ EXPORTS = [
     "strata_moe_mask_ragged", "strata_moe_expert_affine_inplace", "strata_ctx_set_x_early",
     "strata_allgather", "strata_alltoall", "strata_broadcast", "strata_reducescatter", "strata_allreduce",
     "strata_p2p", "strata_alltoallv",
+    "strata_moe_route", "strata_moe_route_grad", "strata_norm", "strata_norm_grad_scratch_bytes", "strata_norm_grad",
+    "strata_quantize_rows", "strata_moe_expert_matmul",
 ]
+
+# element types and modes of the layer operators (include/strata_layer.h)
+STRATA_T_BF16, STRATA_T_F32, STRATA_T_INT8, STRATA_T_E4M3 = 0, 1, 2, 3
+STRATA_SCORE_SOFTMAX, STRATA_SCORE_SIGMOID = 0, 1
+STRATA_GROUP_MAX, STRATA_GROUP_TOP2 = 0, 1
 
 
 class strata_moe_shape(ctypes.Structure):
@@ -86,6 +95,48 @@ class strata_partition_t(ctypes.Structure):
                 ("core_load", ctypes.c_void_p), ("scratch", ctypes.c_void_p), ("task_stripe", ctypes.c_void_p)]
 
 
+class strata_route_params(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("renormalise", ctypes.c_int32), ("n_group", ctypes.c_int32),
+                ("topk_group", ctypes.c_int32), ("group_score", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
+class strata_norm_args(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("weight_type", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("q_type", ctypes.c_int32), ("x", ctypes.c_void_p),
+                ("residual", ctypes.c_void_p), ("weight", ctypes.c_void_p), ("residual_out", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("q", ctypes.c_void_p), ("q_scale", ctypes.c_void_p),
+                ("x_stride", ctypes.c_int64), ("residual_stride", ctypes.c_int64),
+                ("residual_out_stride", ctypes.c_int64), ("out_stride", ctypes.c_int64), ("q_stride", ctypes.c_int64),
+                ("q_scale_stride", ctypes.c_int64)]
+
+
+class strata_norm_grad_args(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("cols", ctypes.c_int32), ("weight_type", ctypes.c_int32),
+                ("eps", ctypes.c_float), ("reserved", ctypes.c_int32), ("dy", ctypes.c_void_p), ("h", ctypes.c_void_p),
+                ("weight", ctypes.c_void_p), ("dresidual", ctypes.c_void_p), ("dx", ctypes.c_void_p),
+                ("dweight", ctypes.c_void_p), ("scratch", ctypes.c_void_p), ("scratch_bytes", ctypes.c_size_t),
+                ("dy_stride", ctypes.c_int64), ("h_stride", ctypes.c_int64), ("dresidual_stride", ctypes.c_int64),
+                ("dx_stride", ctypes.c_int64)]
+
+
+class strata_matmul_args(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("gated", ctypes.c_int32), ("inner", ctypes.c_int32),
+                ("channels", ctypes.c_int32), ("a_rows", ctypes.c_int64), ("a", ctypes.c_void_p),
+                ("a_scale", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("a_stride", ctypes.c_int64), ("a_scale_stride", ctypes.c_int64),
+                ("out_stride", ctypes.c_int64)]
+
+
+def make_route(score: str = "softmax", renormalise: bool = True, scale: float = 1.0, n_group: int = 1,
+               topk_group: int = 1, group_score: str = "max") -> strata_route_params:
+    """score: "softmax" or "sigmoid"; group_score: "max" or "top2" (read if n_group > 1)."""
+    scores = {"softmax": STRATA_SCORE_SOFTMAX, "sigmoid": STRATA_SCORE_SIGMOID}
+    groups = {"max": STRATA_GROUP_MAX, "top2": STRATA_GROUP_TOP2}
+    if score not in scores or group_score not in groups:
+        raise ValueError(f"unknown score {score!r} or group score {group_score!r}")
+    return strata_route_params(scores[score], int(renormalise), n_group, topk_group, groups[group_score], scale)
+
+
 def make_policy(tiers, g0: int = 1, g1: int = 1) -> strata_partition_policy:
     """tiers: list of (alpha, beta, unit_rows, fanout_cap), at most 3."""
     p = strata_partition_policy()
@@ -113,7 +164,7 @@ def lib() -> ctypes.CDLL:
         raise RuntimeError(f"{LIB_PATH} is missing: build it with "
                            f"`python -m paper_2607_26444_b200.build` (there is no CPU fallback)")
     L = ctypes.CDLL(LIB_PATH)
-    vp, sz, i32, u64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint64
+    vp, sz, i32, u64, i64 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int, ctypes.c_uint64, ctypes.c_int64
     P = ctypes.POINTER
     L.strata_status_string.restype = ctypes.c_char_p
     L.strata_status_string.argtypes = [i32]
@@ -155,6 +206,13 @@ def lib() -> ctypes.CDLL:
         "strata_alltoallv": [vp, i32, vp, sz, vp, sz, vp, vp, vp, vp],
         "strata_reducescatter": [vp, i32, vp, vp, sz, vp],
         "strata_allreduce": [vp, i32, vp, vp, sz, vp],
+        "strata_moe_route": [vp, P(strata_route_params), vp, i32, i64, vp, vp, vp, vp],
+        "strata_moe_route_grad": [vp, P(strata_route_params), vp, i32, i64, vp, vp, vp, i64, vp],
+        "strata_norm": [vp, P(strata_norm_args), vp],
+        "strata_norm_grad_scratch_bytes": [vp, i64, i32, P(sz)],
+        "strata_norm_grad": [vp, P(strata_norm_grad_args), vp],
+        "strata_quantize_rows": [vp, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp],
+        "strata_moe_expert_matmul": [vp, P(strata_moe_layout_t), P(strata_matmul_args), vp],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -353,11 +411,110 @@ def strata_allreduce(ctx, R: int, src: int, dst: int, elems: int, stream: int) -
     return lib().strata_allreduce(ctx, R, src, dst, elems, stream)
 
 
+def strata_moe_route(ctx, params: strata_route_params, logits: int, logits_type: int, logits_stride: int,
+                     bias: Optional[int], topk_ids: int, topk_w: int, stream: int) -> int:
+    return lib().strata_moe_route(ctx, ctypes.byref(params), logits, logits_type, logits_stride, bias, topk_ids, topk_w,
+                                  stream)
+
+
+def strata_moe_route_grad(ctx, params: strata_route_params, logits: int, logits_type: int, logits_stride: int,
+                          topk_ids: int, dtopk_w: int, dlogits: int, dlogits_stride: int, stream: int) -> int:
+    return lib().strata_moe_route_grad(ctx, ctypes.byref(params), logits, logits_type, logits_stride, topk_ids, dtopk_w,
+                                       dlogits, dlogits_stride, stream)
+
+
+def strata_norm(ctx, args: strata_norm_args, stream: int) -> int:
+    return lib().strata_norm(ctx, ctypes.byref(args), stream)
+
+
+def strata_norm_grad_scratch_bytes(ctx, rows: int, cols: int) -> Tuple[int, int]:
+    n = ctypes.c_size_t()
+    rc = lib().strata_norm_grad_scratch_bytes(ctx, rows, cols, ctypes.byref(n))
+    return rc, n.value
+
+
+def strata_norm_grad(ctx, args: strata_norm_grad_args, stream: int) -> int:
+    return lib().strata_norm_grad(ctx, ctypes.byref(args), stream)
+
+
+def strata_quantize_rows(ctx, x: int, x_stride: int, rows: int, cols: int, q_type: int, q: int, q_stride: int,
+                         q_scale: int, q_scale_stride: int, n_valid: Optional[int], stream: int) -> int:
+    return lib().strata_quantize_rows(ctx, x, x_stride, rows, cols, q_type, q, q_stride, q_scale, q_scale_stride,
+                                      n_valid, stream)
+
+
+def strata_moe_expert_matmul(ctx, layout: strata_moe_layout_t, args: strata_matmul_args, stream: int) -> int:
+    return lib().strata_moe_expert_matmul(ctx, ctypes.byref(layout), ctypes.byref(args), stream)
+
+
 # ---- convenience wrapper over torch tensors (memory + streams only) ---------
 
 def _check(rc: int, where: str) -> None:
     if rc != STRATA_OK:
         raise StrataError(rc, where)
+
+
+def _strides(t):
+    """(rows, columns, row stride in elements) of a tensor [..., columns] whose rows are evenly spaced."""
+    if t.dim() == 2:
+        (rows, cols), (stride, last) = t.shape, t.stride()
+    else:
+        cols, last = t.shape[-1], t.stride(-1)
+        stride, rows = (t.stride(-2), 1) if t.dim() > 1 else (cols, 1)
+        for d in range(t.dim() - 2, -1, -1):
+            if t.shape[d] > 1 and rows > 1 and t.stride(d) != rows * stride:
+                raise ValueError("rows are not evenly spaced: pass a contiguous tensor")
+            if t.shape[d] > 1 and rows == 1:
+                stride = t.stride(d)
+            rows *= t.shape[d]
+    if last != 1 and cols > 1:
+        raise ValueError("the last dimension is not contiguous")
+    return rows, cols, stride if rows > 1 else max(stride, cols)
+
+
+def _scale_stride(t, rows: int) -> int:
+    """Distance of a row's scale to the next one's."""
+    if t.dim() != 1:
+        n, one, stride = _strides(t[..., None])
+        if n < rows:
+            raise ValueError("one scale per row is needed")
+        return stride
+    if t.shape[0] < rows:
+        raise ValueError("one scale per row is needed")
+    return max(1, t.stride(0))
+
+
+def _code_type(t) -> int:
+    import torch
+    if t.dtype == torch.int8:
+        return STRATA_T_INT8
+    if t.dtype == torch.float8_e4m3fn:
+        return STRATA_T_E4M3
+    raise ValueError(f"8-bit codes are torch.int8 or torch.float8_e4m3fn, not {t.dtype}")
+
+
+def _float_type(t) -> int:
+    """bf16 (also as 16-bit patterns) or fp32."""
+    import torch
+    if t.dtype == torch.float32:
+        return STRATA_T_F32
+    if t.dtype in (torch.bfloat16, torch.int16):
+        return STRATA_T_BF16
+    raise ValueError(f"bf16 or fp32 is needed, not {t.dtype}")
+
+
+def _need(ok: bool, what: str) -> None:
+    if not ok:
+        raise ValueError(what)
+
+
+def q8_rows(buf, code_dtype):
+    """The two views of a uint8 buffer [..., H + STRATA_Q8_TRAILER] of STRATA_Q8_ROW rows: codes [..., H] of code_dtype
+    and scales [...] (float)."""
+    import torch
+    h = buf.shape[-1] - STRATA_Q8_TRAILER
+    scale = buf.view(torch.float32)[..., h // 4]
+    return buf[..., :h].view(code_dtype), scale
 
 
 class Layout:
@@ -498,6 +655,109 @@ class MoEContext:
         _check(strata_moe_expert_affine_inplace(self.h, layout.c, recv.data_ptr(), recv.shape[0], scale.data_ptr(),
                                                 bias.data_ptr(), tile_rows, self._stream()),
                "strata_moe_expert_affine_inplace")
+
+    # the layer around the routing path ------------------------------------------------------------
+    def route(self, params: strata_route_params, logits, ids, w, bias=None) -> None:
+        """Router logits [.., E] (bf16 or fp32) -> ids int32 [.., K] and gate weights fp32 [.., K]; bias fp32 [E] takes part
+        in the choice only."""
+        rows, cols, stride = _strides(logits)
+        _need(rows == self.n_tok and cols == self.E, "logits are [R, T, E]")
+        _need(ids.numel() == self.n_items and w.numel() == self.n_items and ids.is_contiguous() and w.is_contiguous(),
+              "ids and w are contiguous [R, T, K]")
+        _check(strata_moe_route(self.h, params, logits.data_ptr(), _float_type(logits), stride,
+                                bias.data_ptr() if bias is not None else None, ids.data_ptr(), w.data_ptr(),
+                                self._stream()), "strata_moe_route")
+
+    def route_grad(self, params: strata_route_params, logits, ids, dw, dlogits) -> None:
+        """Gradient of the logits (in their type) from the gradient dw [.., K] of the gate weights."""
+        rows, cols, stride = _strides(logits)
+        drows, dcols, dstride = _strides(dlogits)
+        _need(rows == self.n_tok and cols == self.E and (drows, dcols) == (rows, cols) and dlogits.dtype == logits.dtype,
+              "logits and dlogits are [R, T, E] of one type")
+        _need(ids.numel() == self.n_items and dw.numel() == self.n_items and ids.is_contiguous() and dw.is_contiguous(),
+              "ids and dw are contiguous [R, T, K]")
+        _check(strata_moe_route_grad(self.h, params, logits.data_ptr(), _float_type(logits), stride, ids.data_ptr(),
+                                     dw.data_ptr(), dlogits.data_ptr(), dstride, self._stream()), "strata_moe_route_grad")
+
+    def norm(self, x, weight, eps: float, out=None, residual=None, residual_out=None, q=None, q_scale=None) -> None:
+        """h = x + residual (stored in residual_out), then h * rsqrt(mean(h^2) + eps) * weight to `out` (bf16) and / or
+        to 8-bit codes `q` (torch.int8 or torch.float8_e4m3fn) with one fp32 scale per row."""
+        a = strata_norm_args()
+        a.rows, a.cols, a.x_stride = _strides(x)
+        shape = (a.rows, a.cols)
+        _need(weight.numel() == a.cols and weight.is_contiguous(), "weight is [cols]")
+        a.weight_type, a.eps = _float_type(weight), eps
+        a.x, a.weight = x.data_ptr(), weight.data_ptr()
+        if residual is not None:
+            _need(residual_out is not None, "residual needs residual_out")
+            r, c, a.residual_stride = _strides(residual)
+            ro, co, a.residual_out_stride = _strides(residual_out)
+            _need((r, c) == shape and (ro, co) == shape, "residual and residual_out have the shape of x")
+            a.residual, a.residual_out = residual.data_ptr(), residual_out.data_ptr()
+        if out is not None:
+            r, c, a.out_stride = _strides(out)
+            _need((r, c) == shape, "out has the shape of x")
+            a.out = out.data_ptr()
+        if q is not None:
+            r, c, a.q_stride = _strides(q)
+            _need((r, c) == shape and q_scale is not None, "q has the shape of x and comes with q_scale")
+            a.q, a.q_type = q.data_ptr(), _code_type(q)
+            a.q_scale, a.q_scale_stride = q_scale.data_ptr(), _scale_stride(q_scale, a.rows)
+        _check(strata_norm(self.h, a, self._stream()), "strata_norm")
+
+    def norm_grad_scratch(self, rows: int, cols: int):
+        """Scratch of norm_grad for this many rows and columns."""
+        import torch
+        rc, n = strata_norm_grad_scratch_bytes(self.h, rows, cols)
+        _check(rc, "strata_norm_grad_scratch_bytes")
+        return torch.empty(max(n, 16), dtype=torch.uint8, device=self.device)
+
+    def norm_grad(self, dy, h, weight, eps: float, dx, dweight, dresidual=None, scratch=None) -> None:
+        """Gradients of norm's bf16 output: dx (of x and of residual alike, dresidual added) and dweight (fp32 [cols])."""
+        import torch
+        a = strata_norm_grad_args()
+        a.rows, a.cols, a.dy_stride = _strides(dy)
+        shape = (a.rows, a.cols)
+        r, c, a.h_stride = _strides(h)
+        rx, cx, a.dx_stride = _strides(dx)
+        _need((r, c) == shape and (rx, cx) == shape, "dy, h and dx have one shape")
+        _need(weight.numel() == a.cols and weight.is_contiguous() and dweight.numel() == a.cols
+              and dweight.is_contiguous() and dweight.dtype == torch.float32, "weight and dweight (fp32) are [cols]")
+        if dresidual is not None:
+            r, c, a.dresidual_stride = _strides(dresidual)
+            _need((r, c) == shape, "dresidual has the shape of dy")
+            a.dresidual = dresidual.data_ptr()
+        if scratch is None:
+            scratch = self.norm_grad_scratch(a.rows, a.cols)
+        a.weight_type, a.eps = _float_type(weight), eps
+        a.dy, a.h, a.weight, a.dx = dy.data_ptr(), h.data_ptr(), weight.data_ptr(), dx.data_ptr()
+        a.dweight, a.scratch, a.scratch_bytes = dweight.data_ptr(), scratch.data_ptr(), scratch.numel()
+        _check(strata_norm_grad(self.h, a, self._stream()), "strata_norm_grad")
+
+    def quantize_rows(self, x, q, q_scale, layout: Optional[Layout] = None) -> None:
+        """bf16 rows -> 8-bit codes with one fp32 scale per row; with a layout, only the rows it has in use."""
+        rows, cols, stride = _strides(x)
+        r, c, q_stride = _strides(q)
+        _need((r, c) == (rows, cols), "q has the shape of x")
+        n_valid = layout.expert_offset.data_ptr() + 4 * self.E if layout is not None else None
+        _check(strata_quantize_rows(self.h, x.data_ptr(), stride, rows, cols, _code_type(q), q.data_ptr(), q_stride,
+                                    q_scale.data_ptr(), _scale_stride(q_scale, rows), n_valid, self._stream()),
+               "strata_quantize_rows")
+
+    def expert_matmul(self, layout: Layout, a, a_scale, w, w_scale, out, gated: bool = False) -> None:
+        """out[r] = (a[r] . w[e]) * a_scale[r] * w_scale[e] for the rows of every expert's segment; gated: silu(first half
+        of the channels) * second half.  a [rows, inner] and w [E, channels, inner]: torch.int8 or torch.float8_e4m3fn."""
+        m = strata_matmul_args()
+        m.a_rows, m.inner, m.a_stride = _strides(a)
+        rows, cols, m.out_stride = _strides(out)
+        m.type, m.gated, m.channels = _code_type(a), 1 if gated else 0, w.shape[1]
+        _need(w.dim() == 3 and w.dtype == a.dtype and w.is_contiguous() and w.shape[0] == self.E
+              and w.shape[2] == m.inner, "w is contiguous [E, channels, inner] of a's type")
+        _need(w_scale.is_contiguous() and w_scale.numel() == self.E * m.channels, "w_scale is contiguous [E, channels]")
+        _need(rows == m.a_rows and cols == (m.channels // 2 if gated else m.channels), "out is [rows, channels (/ 2)]")
+        m.a, m.w, m.w_scale, m.out = a.data_ptr(), w.data_ptr(), w_scale.data_ptr(), out.data_ptr()
+        m.a_scale, m.a_scale_stride = a_scale.data_ptr(), _scale_stride(a_scale, m.a_rows)
+        _check(strata_moe_expert_matmul(self.h, layout.c, m, self._stream()), "strata_moe_expert_matmul")
 
     def row_experts(self, layout: Layout, out=None):
         """int32 [recv_rows]: the expert of every occupied receive row, -1 for padding and empty rows."""

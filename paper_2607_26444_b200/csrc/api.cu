@@ -1,44 +1,17 @@
 // C ABI: context, registration pool, argument validation and kernel launches.
 // Host-side only; every device-side step lives in layout.cu / dispatch.cu / combine.cu.
 #include <algorithm>
-#include <mutex>
 #include <new>
-#include <vector>
 
-#include "common.cuh"
+#include "ctx.cuh"
 
 namespace strata {
 cudaError_t configure_layout_kernels();
 cudaError_t configure_dispatch_kernels();
 cudaError_t configure_partition_kernels();
 cudaError_t configure_collective_kernels();
+cudaError_t configure_matmul_kernels();
 }  // namespace strata
-
-struct strata_region {
-    uint64_t id;
-    uintptr_t base;
-    size_t bytes;
-    size_t used;      // bump pointer of strata_pool_carve
-};
-
-struct strata_ctx {
-    strata_moe_shape shape;
-    int device;
-    int n_sm;             // SMs the persistent kernels size their grids for (the device's, or the caller's budget)
-    int n_sm_device;
-    int x_early;          // the caller's promise about x (strata_ctx_set_x_early)
-    int* ws;              // device workspace (header + tile counts)
-    size_t ws_bytes;
-    uint64_t next_region;
-    uint64_t launches;
-    strata::TraceBuf trace;
-    // host round trip only: copy streams and events, created on first use (no device memory)
-    cudaStream_t s_in = nullptr, s_out = nullptr;
-    std::vector<cudaEvent_t> ev_in, ev_done;
-    cudaEvent_t ev_entry = nullptr, ev_out = nullptr;
-    std::vector<strata_region> regions;
-    std::mutex mu;
-};
 
 namespace {
 
@@ -50,12 +23,25 @@ strata_status check_shape(const strata_moe_shape* s)
     if (s->H <= 0 || s->H % 8 != 0) return STRATA_ERR_SHAPE;
     const strata_status st = check_layout_shape(*s);
     if (st != STRATA_OK) return st;
-    if (s->dispatch_dtype != STRATA_BF16 && s->dispatch_dtype != STRATA_FP8_E4M3_B128) return STRATA_ERR_SHAPE;
+    if (s->dispatch_dtype != STRATA_BF16 && s->dispatch_dtype != STRATA_FP8_E4M3_B128 &&
+        s->dispatch_dtype != STRATA_Q8_ROW)
+        return STRATA_ERR_SHAPE;
+    if (s->dispatch_dtype == STRATA_Q8_ROW && s->H % 16 != 0) return STRATA_ERR_SHAPE;
     if (s->dispatch_dtype == STRATA_FP8_E4M3_B128 && s->H % 128 != 0) return STRATA_ERR_SHAPE;
     // Dispatch and combine number their work units (a token, or a column piece of one never shorter than
     // 1 KB) with 32-bit counters whose top values are reserved.
     if ((long long)s->R * s->T * (((long long)s->H * 2 + 1023) / 1024) >= (1ll << 32) - (1ll << 20)) return STRATA_ERR_SHAPE;
     return STRATA_OK;
+}
+
+// bytes of one row of the receive buffer
+size_t recv_row_bytes(const strata_moe_shape& s)
+{
+    switch (s.dispatch_dtype) {
+        case STRATA_FP8_E4M3_B128: return (size_t)s.H;
+        case STRATA_Q8_ROW: return (size_t)s.H + STRATA_Q8_TRAILER;
+        default: return (size_t)s.H * 2;
+    }
 }
 
 size_t workspace_bytes(const strata_moe_shape& s)
@@ -68,31 +54,6 @@ size_t workspace_bytes(const strata_moe_shape& s)
 WorkQueue dispatch_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 2}; }
 WorkQueue combine_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 4}; }
 WorkQueue collective_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 6}; }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = true;
-    explicit DeviceGuard(int dev)
-    {
-        if (cudaGetDevice(&prev) != cudaSuccess) { ok = false; return; }
-        if (prev != dev && cudaSetDevice(dev) != cudaSuccess) ok = false;
-        if (prev == dev) prev = -1;
-    }
-    ~DeviceGuard()
-    {
-        if (prev >= 0) cudaSetDevice(prev);
-    }
-};
-
-bool region_contains(const strata_ctx* c, const void* p, size_t bytes)
-{
-    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
-    for (const strata_region& r : c->regions)
-        if (a >= r.base && bytes <= r.bytes && a - r.base <= r.bytes - bytes) return true;
-    return false;
-}
 
 strata_status check_layout_ptrs(const strata_moe_layout_t* L, bool need_all)
 {
@@ -143,7 +104,8 @@ strata_status strata_ctx_create(strata_ctx** out, const strata_moe_shape* shape,
         if (cudaDeviceGetAttribute(&n_sm, cudaDevAttrMultiProcessorCount, device) != cudaSuccess)
             return STRATA_ERR_CUDA;
         if (configure_layout_kernels() != cudaSuccess || configure_dispatch_kernels() != cudaSuccess ||
-            configure_partition_kernels() != cudaSuccess || configure_collective_kernels() != cudaSuccess) {
+            configure_partition_kernels() != cudaSuccess || configure_collective_kernels() != cudaSuccess ||
+            configure_matmul_kernels() != cudaSuccess) {
             cudaGetLastError();
             return STRATA_ERR_CUDA;
         }
@@ -416,7 +378,9 @@ strata_status strata_moe_dispatch(strata_ctx* ctx, const strata_moe_layout_t* la
     if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     const size_t n_rows = (size_t)recv_rows(s);
     if (capacity_rows < n_rows) return STRATA_ERR_CAPACITY;
-    const size_t row_bytes = fp8 ? (size_t)s.H : (size_t)s.H * 2;
+    const size_t row_bytes = recv_row_bytes(s);
+    strata_moe_shape copied = s;                        // rows that are copied bit for bit, in units of two bytes
+    copied.H = (int32_t)(row_bytes / 2);
     {
         std::lock_guard<std::mutex> lk(ctx->mu);
         if (!region_contains(ctx, recv, capacity_rows * row_bytes)) return STRATA_ERR_NOT_REGISTERED;
@@ -429,7 +393,7 @@ strata_status strata_moe_dispatch(strata_ctx* ctx, const strata_moe_layout_t* la
     cudaError_t err =
         fp8 ? launch_dispatch_fp8(s, layout->dst_row, x, recv, recv_scale, capacity_rows, ctx->ws, dispatch_queue(ctx),
                                   ctx->n_sm, ctx->trace, ctx->x_early != 0, static_cast<cudaStream_t>(stream))
-            : launch_dispatch_bf16(s, layout->dst_row, x, recv, capacity_rows, ctx->ws, dispatch_queue(ctx), ctx->n_sm,
+            : launch_dispatch_bf16(copied, layout->dst_row, x, recv, capacity_rows, ctx->ws, dispatch_queue(ctx), ctx->n_sm,
                                    ctx->trace, ctx->x_early != 0, static_cast<cudaStream_t>(stream));
     {
         std::lock_guard<std::mutex> lk(ctx->mu);
@@ -778,7 +742,7 @@ strata_status strata_moe_recv_view(strata_ctx* ctx, const int32_t* h_rank_offset
     if (rank < 0 || rank >= s.R) return STRATA_ERR_INVALID_ARG;
     const int64_t lo = h_rank_offset[rank], hi = h_rank_offset[rank + 1];
     if (lo < 0 || hi < lo) return STRATA_ERR_INVALID_ARG;
-    const size_t row_bytes = s.dispatch_dtype == STRATA_FP8_E4M3_B128 ? (size_t)s.H : (size_t)s.H * 2;
+    const size_t row_bytes = recv_row_bytes(s);
     *rank_base = static_cast<unsigned char*>(recv) + (size_t)lo * row_bytes;
     *rows = hi - lo;
     return STRATA_OK;
