@@ -76,15 +76,17 @@ strata_status strata_moe_route_grad(strata_ctx *ctx, const strata_route_params *
  * h = bf16(x + residual) if residual is given (written to residual_out, which may be residual itself), else x
  * y = (h * weight) * rstd,  rstd = 1 / sqrt(mean(h^2) + eps): the mean is of h as it is stored
  * out  (bf16) = bf16(y), if given
- * q (8 bits)  = codes of y / scale, q_scale[row] = max|y| / 127 (int8) or / 448 (e4m3), if given; codes of an
- *               all-zero row are zero with scale 0; e4m3 saturates.  Codes are of y, not of bf16(y).
+ * q (8 bits)  = codes of y * limit / max|y|, q_scale[row] = max|y| / limit, limit = 127 (int8) or 448 (e4m3), if
+ *               given: y is about code * q_scale.  The quotient is one correctly rounded binary32 value before it
+ *               becomes a code, so half-way cases go to the even code.  Codes of an all-zero row are zero with scale 0.
+ *               Codes are of y, not of bf16(y); they do not depend on rstd, which cancels.
  * NaN and infinities follow the formula in `out`; codes and scale of a row that holds one are unspecified.
  * x, residual, residual_out, out: device bf16, 16-byte aligned, strides multiples of 8; weight: device bf16 or float
  * [cols], 16-byte aligned; q: 8-byte aligned, stride a multiple of 8; q_scale: element `row` at q_scale[row *
  * q_scale_stride].  cols: a multiple of 8, at most 32768.  rows may be 0 (nothing is launched, row
  * tensors may be NULL).  One of out and q is
  * required.  residual and residual_out come together.  eps >= 0.  Outputs may alias no input, except residual_out
- * = residual or x, and out = x. */
+ * = residual or x, and out = x.  Needs a workspace (the status word).  One launch. */
 typedef struct {
     int64_t rows;
     int32_t cols;
@@ -128,9 +130,9 @@ strata_status strata_norm_grad_scratch_bytes(strata_ctx *ctx, int64_t rows, int3
 strata_status strata_norm_grad(strata_ctx *ctx, const strata_norm_grad_args *args, void *stream);
 
 /* ---- rows to 8 bits -----------------------------------------------------------------------------------------
- * q = codes of x / scale, q_scale[row] = max|x| / 127 or / 448, as in strata_norm.  n_valid: device int32, or NULL;
+ * q = codes of x * limit / max|x|, q_scale[row] = max|x| / limit, as in strata_norm.  n_valid: device int32, or NULL;
  * if given, only rows below *n_valid are read and written (expert_offset + E of a layout: the rows in use of a
- * receive buffer).  Alignments, strides and limits as in strata_norm.  One launch. */
+ * receive buffer).  Alignments, strides and limits as in strata_norm.  Needs a workspace (the status word).  One launch. */
 strata_status strata_quantize_rows(strata_ctx *ctx, const void *x, int64_t x_stride, int64_t rows, int32_t cols,
                                    int32_t q_type, void *q, int64_t q_stride, float *q_scale, int64_t q_scale_stride,
                                    const int32_t *n_valid, void *stream);

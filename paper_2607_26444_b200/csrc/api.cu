@@ -11,6 +11,7 @@ cudaError_t configure_dispatch_kernels();
 cudaError_t configure_partition_kernels();
 cudaError_t configure_collective_kernels();
 cudaError_t configure_matmul_kernels();
+cudaError_t configure_norm_kernels();
 }  // namespace strata
 
 namespace {
@@ -105,7 +106,7 @@ strata_status strata_ctx_create(strata_ctx** out, const strata_moe_shape* shape,
             return STRATA_ERR_CUDA;
         if (configure_layout_kernels() != cudaSuccess || configure_dispatch_kernels() != cudaSuccess ||
             configure_partition_kernels() != cudaSuccess || configure_collective_kernels() != cudaSuccess ||
-            configure_matmul_kernels() != cudaSuccess) {
+            configure_matmul_kernels() != cudaSuccess || configure_norm_kernels() != cudaSuccess) {
             cudaGetLastError();
             return STRATA_ERR_CUDA;
         }

@@ -107,10 +107,11 @@ strata_status strata_norm(strata_ctx* ctx, const strata_norm_args* a, void* stre
     if (a->out) STRATA_CHECK(check_rows16(a->out, a->out_stride, a->cols));
     if (a->q) STRATA_CHECK(check_codes(a->q, a->q_stride, a->q_scale, a->q_scale_stride, a->q_type, a->cols));
     if (!on(a->weight, 16)) return STRATA_ERR_ALIGNMENT;
+    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
-    return launched(ctx, launch_norm(*a, ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+    return launched(ctx, launch_norm(*a, ctx->ws, ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_norm_grad_scratch_bytes(strata_ctx* ctx, int64_t rows, int32_t cols, size_t* bytes)
@@ -155,11 +156,12 @@ strata_status strata_quantize_rows(strata_ctx* ctx, const void* x, int64_t x_str
     STRATA_CHECK(check_rows16(x, x_stride, cols));
     STRATA_CHECK(check_codes(q, q_stride, q_scale, q_scale_stride, q_type, cols));
     if (!on(n_valid, 4)) return STRATA_ERR_ALIGNMENT;
+    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     return launched(ctx, launch_quantize(x, x_stride, rows, cols, q_type, q, q_stride, q_scale, q_scale_stride, n_valid,
-                                         ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+                                         ctx->ws, ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_t* layout, const strata_matmul_args* a,

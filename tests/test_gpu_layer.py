@@ -7,7 +7,7 @@ Tolerances, derived before the first run (u = 2^-24, the unit roundoff of binary
   divisions: relative 2u * (E/32 + 5 + K + 8 + max|l|);
 - bf16 results: half an ulp (8 significant bits: 2^-8 of the value's power of two), plus a few binary32 roundings
   (2^-18 relative of the terms);
-- 8-bit codes of the quantiser: bit-exact against the same IEEE binary32 divisions; those of the norm: half a step
+- 8-bit codes of the quantiser: bit-exact against the correctly rounded binary32 quotient; those of the norm: half a step
   around the 64-bit value (1 + 2^-10 for the binary32 value's own error);
 - int8 products are exact sums, scaled: half a bf16 ulp + 2^-18 relative; e4m3 products are summed by the matrix unit in binary32
   storage with at least 13 fraction bits kept in each alignment: 2^-13 * sum|a w|;
@@ -300,10 +300,12 @@ def test_norm_against_64_bits(rows, cols, residual, out):
 
 
 def ieee_codes(x, kind):
-    """The quantiser's definition in binary32: max/limit, then a division per element."""
+    """The quantiser's definition: scale = max / limit, codes of the correctly rounded binary32 quotient x * limit / max."""
     x = x.astype(np.float32)
-    scale = (np.abs(x).max(1) / np.float32(ref.CODE_MAX[kind])).astype(np.float32)
-    units = (x / np.where(scale == 0, np.float32(1), scale)[:, None]).astype(np.float32)
+    top = np.abs(x).max(1)
+    scale = (top / np.float32(ref.CODE_MAX[kind])).astype(np.float32)
+    # exact product and one division in 64 bits: far enough beyond binary32 to round as the quotient itself
+    units = (x.astype(np.float64) * ref.CODE_MAX[kind] / np.where(top == 0, 1, top)[:, None].astype(np.float64)).astype(np.float32)
     if kind == "int8":
         return np.rint(units).astype(np.int8).view(np.uint8), scale
     return torch.from_numpy(np.clip(units, -448, 448)).to(torch.float8_e4m3fn).view(torch.uint8).numpy(), scale
