@@ -456,56 +456,81 @@ def _check(rc: int, where: str) -> None:
 
 def _strides(t):
     """(rows, columns, row stride in elements) of a tensor [..., columns] whose rows are evenly spaced."""
-    if t.dim() == 2:
-        (rows, cols), (stride, last) = t.shape, t.stride()
-    else:
-        cols, last = t.shape[-1], t.stride(-1)
-        stride, rows = (t.stride(-2), 1) if t.dim() > 1 else (cols, 1)
-        for d in range(t.dim() - 2, -1, -1):
-            if t.shape[d] > 1 and rows > 1 and t.stride(d) != rows * stride:
-                raise ValueError("rows are not evenly spaced: pass a contiguous tensor")
-            if t.shape[d] > 1 and rows == 1:
+    cols = t.size(-1)
+    if t.is_contiguous():
+        return (t.numel() // cols if cols else 0), cols, cols
+    stride, rows = cols, 1
+    for d in range(t.dim() - 2, -1, -1):
+        if t.shape[d] > 1:
+            if rows == 1:
                 stride = t.stride(d)
-            rows *= t.shape[d]
-    if last != 1 and cols > 1:
+            elif t.stride(d) != rows * stride:
+                raise ValueError("rows are not evenly spaced: pass a contiguous tensor")
+        rows *= t.shape[d]
+    if t.stride(-1) != 1 and cols > 1:
         raise ValueError("the last dimension is not contiguous")
-    return rows, cols, stride if rows > 1 else max(stride, cols)
+    return rows, cols, stride
+
+
+def _stride(t, rows: int, cols: int, what: str) -> int:
+    """Row stride of a tensor that must hold rows x cols."""
+    r, c, stride = _strides(t)
+    if r != rows or c != cols:
+        raise ValueError(f"{what}: {rows} rows of {cols} are needed, not {r} of {c}")
+    return stride
 
 
 def _scale_stride(t, rows: int) -> int:
     """Distance of a row's scale to the next one's."""
-    if t.dim() != 1:
-        n, one, stride = _strides(t[..., None])
-        if n < rows:
-            raise ValueError("one scale per row is needed")
-        return stride
-    if t.shape[0] < rows:
+    n = t.numel()
+    if t.dim() == 1 or t.is_contiguous():
+        stride = t.stride(-1) if t.dim() else 1
+    else:
+        stride = _strides(t[..., None])[2]
+    if n < rows:
         raise ValueError("one scale per row is needed")
-    return max(1, t.stride(0))
+    return max(1, stride)
+
+
+class _Types(dict):
+    """Element types by torch dtype, filled on first use (torch is imported by the callers that need it)."""
+
+    def __missing__(self, dtype):
+        import torch
+        self.update({torch.float32: STRATA_T_F32, torch.bfloat16: STRATA_T_BF16, torch.int16: STRATA_T_BF16,
+                     torch.int8: STRATA_T_INT8, torch.float8_e4m3fn: STRATA_T_E4M3})
+        return self.setdefault(dtype, -1)
+
+
+_types = _Types()
 
 
 def _code_type(t) -> int:
-    import torch
-    if t.dtype == torch.int8:
-        return STRATA_T_INT8
-    if t.dtype == torch.float8_e4m3fn:
-        return STRATA_T_E4M3
-    raise ValueError(f"8-bit codes are torch.int8 or torch.float8_e4m3fn, not {t.dtype}")
+    code = _types[t.dtype]
+    if code != STRATA_T_INT8 and code != STRATA_T_E4M3:
+        raise ValueError(f"8-bit codes are torch.int8 or torch.float8_e4m3fn, not {t.dtype}")
+    return code
 
 
 def _float_type(t) -> int:
     """bf16 (also as 16-bit patterns) or fp32."""
-    import torch
-    if t.dtype == torch.float32:
-        return STRATA_T_F32
-    if t.dtype in (torch.bfloat16, torch.int16):
-        return STRATA_T_BF16
-    raise ValueError(f"bf16 or fp32 is needed, not {t.dtype}")
+    code = _types[t.dtype]
+    if code != STRATA_T_BF16 and code != STRATA_T_F32:
+        raise ValueError(f"bf16 or fp32 is needed, not {t.dtype}")
+    return code
 
 
-def _need(ok: bool, what: str) -> None:
-    if not ok:
-        raise ValueError(what)
+def _bf16(*tensors) -> None:
+    for t in tensors:
+        if t is not None and _types[t.dtype] != STRATA_T_BF16:
+            raise ValueError(f"bf16 is needed, not {t.dtype}")
+
+
+def _flat(t, dtype_bytes: int, n: int, what: str) -> int:
+    """Address of a contiguous tensor of n elements."""
+    if t.numel() != n or not t.is_contiguous() or t.element_size() != dtype_bytes:
+        raise ValueError(f"{what}: {n} contiguous elements of {dtype_bytes} bytes are needed")
+    return t.data_ptr()
 
 
 def q8_rows(buf, code_dtype):
@@ -576,6 +601,9 @@ class MoEContext:
         self.fp8 = dispatch_dtype == STRATA_FP8_E4M3_B128
         self.n_tok, self.n_items = R * T, R * T * K
         self.device = torch.device("cuda", device)
+        self._c = lib()
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (
+            lambda index: torch.cuda.current_stream(index).cuda_stream)
         rc, h = strata_ctx_create(self.shape, device)
         _check(rc, "strata_ctx_create")
         self.h = h
@@ -598,10 +626,9 @@ class MoEContext:
         except Exception:
             pass
 
-    @staticmethod
-    def _stream() -> int:
-        import torch
-        return torch.cuda.current_stream().cuda_stream
+    def _stream(self) -> int:
+        """The current stream of the context's device (the raw handle: building a Stream object costs a microsecond)."""
+        return self._raw_stream(self.device.index)
 
     # pool -----------------------------------------------------------------
     def register(self, tensor) -> int:
@@ -660,50 +687,44 @@ class MoEContext:
     def route(self, params: strata_route_params, logits, ids, w, bias=None) -> None:
         """Router logits [.., E] (bf16 or fp32) -> ids int32 [.., K] and gate weights fp32 [.., K]; bias fp32 [E] takes part
         in the choice only."""
-        rows, cols, stride = _strides(logits)
-        _need(rows == self.n_tok and cols == self.E, "logits are [R, T, E]")
-        _need(ids.numel() == self.n_items and w.numel() == self.n_items and ids.is_contiguous() and w.is_contiguous(),
-              "ids and w are contiguous [R, T, K]")
-        _check(strata_moe_route(self.h, params, logits.data_ptr(), _float_type(logits), stride,
-                                bias.data_ptr() if bias is not None else None, ids.data_ptr(), w.data_ptr(),
-                                self._stream()), "strata_moe_route")
+        n = self.n_items
+        _check(self._c.strata_moe_route(
+            self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, self.n_tok, self.E, "logits"),
+            None if bias is None else _flat(bias, 4, self.E, "bias"), _flat(ids, 4, n, "ids"), _flat(w, 4, n, "w"),
+            self._stream()), "strata_moe_route")
 
     def route_grad(self, params: strata_route_params, logits, ids, dw, dlogits) -> None:
         """Gradient of the logits (in their type) from the gradient dw [.., K] of the gate weights."""
-        rows, cols, stride = _strides(logits)
-        drows, dcols, dstride = _strides(dlogits)
-        _need(rows == self.n_tok and cols == self.E and (drows, dcols) == (rows, cols) and dlogits.dtype == logits.dtype,
-              "logits and dlogits are [R, T, E] of one type")
-        _need(ids.numel() == self.n_items and dw.numel() == self.n_items and ids.is_contiguous() and dw.is_contiguous(),
-              "ids and dw are contiguous [R, T, K]")
-        _check(strata_moe_route_grad(self.h, params, logits.data_ptr(), _float_type(logits), stride, ids.data_ptr(),
-                                     dw.data_ptr(), dlogits.data_ptr(), dstride, self._stream()), "strata_moe_route_grad")
+        n = self.n_items
+        if dlogits.dtype != logits.dtype:
+            raise ValueError("dlogits has the type of logits")
+        _check(self._c.strata_moe_route_grad(
+            self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, self.n_tok, self.E, "logits"),
+            _flat(ids, 4, n, "ids"), _flat(dw, 4, n, "dw"), dlogits.data_ptr(),
+            _stride(dlogits, self.n_tok, self.E, "dlogits"), self._stream()), "strata_moe_route_grad")
 
     def norm(self, x, weight, eps: float, out=None, residual=None, residual_out=None, q=None, q_scale=None) -> None:
         """h = x + residual (stored in residual_out), then h * rsqrt(mean(h^2) + eps) * weight to `out` (bf16) and / or
         to 8-bit codes `q` (torch.int8 or torch.float8_e4m3fn) with one fp32 scale per row."""
-        a = strata_norm_args()
-        a.rows, a.cols, a.x_stride = _strides(x)
-        shape = (a.rows, a.cols)
-        _need(weight.numel() == a.cols and weight.is_contiguous(), "weight is [cols]")
-        a.weight_type, a.eps = _float_type(weight), eps
-        a.x, a.weight = x.data_ptr(), weight.data_ptr()
+        rows, cols, x_stride = _strides(x)
+        _bf16(x, residual, residual_out, out)
+        rp = hp = op = qp = sp = r_stride = h_stride = o_stride = q_stride = s_stride = q_type = 0
         if residual is not None:
-            _need(residual_out is not None, "residual needs residual_out")
-            r, c, a.residual_stride = _strides(residual)
-            ro, co, a.residual_out_stride = _strides(residual_out)
-            _need((r, c) == shape and (ro, co) == shape, "residual and residual_out have the shape of x")
-            a.residual, a.residual_out = residual.data_ptr(), residual_out.data_ptr()
+            if residual_out is None:
+                raise ValueError("residual needs residual_out")
+            rp, r_stride = residual.data_ptr(), _stride(residual, rows, cols, "residual")
+            hp, h_stride = residual_out.data_ptr(), _stride(residual_out, rows, cols, "residual_out")
         if out is not None:
-            r, c, a.out_stride = _strides(out)
-            _need((r, c) == shape, "out has the shape of x")
-            a.out = out.data_ptr()
+            op, o_stride = out.data_ptr(), _stride(out, rows, cols, "out")
         if q is not None:
-            r, c, a.q_stride = _strides(q)
-            _need((r, c) == shape and q_scale is not None, "q has the shape of x and comes with q_scale")
-            a.q, a.q_type = q.data_ptr(), _code_type(q)
-            a.q_scale, a.q_scale_stride = q_scale.data_ptr(), _scale_stride(q_scale, a.rows)
-        _check(strata_norm(self.h, a, self._stream()), "strata_norm")
+            if q_scale is None:
+                raise ValueError("q comes with q_scale")
+            qp, q_type, q_stride = q.data_ptr(), _code_type(q), _stride(q, rows, cols, "q")
+            sp, s_stride = q_scale.data_ptr(), _scale_stride(q_scale, rows)
+        wt = _float_type(weight)
+        _check(self._c.strata_norm(self.h, strata_norm_args(
+            rows, cols, wt, eps, q_type, x.data_ptr(), rp, _flat(weight, 4 if wt else 2, cols, "weight"), hp, op, qp, sp,
+            x_stride, r_stride, h_stride, o_stride, q_stride, s_stride), self._stream()), "strata_norm")
 
     def norm_grad_scratch(self, rows: int, cols: int):
         """Scratch of norm_grad for this many rows and columns."""
@@ -714,50 +735,42 @@ class MoEContext:
 
     def norm_grad(self, dy, h, weight, eps: float, dx, dweight, dresidual=None, scratch=None) -> None:
         """Gradients of norm's bf16 output: dx (of x and of residual alike, dresidual added) and dweight (fp32 [cols])."""
-        import torch
-        a = strata_norm_grad_args()
-        a.rows, a.cols, a.dy_stride = _strides(dy)
-        shape = (a.rows, a.cols)
-        r, c, a.h_stride = _strides(h)
-        rx, cx, a.dx_stride = _strides(dx)
-        _need((r, c) == shape and (rx, cx) == shape, "dy, h and dx have one shape")
-        _need(weight.numel() == a.cols and weight.is_contiguous() and dweight.numel() == a.cols
-              and dweight.is_contiguous() and dweight.dtype == torch.float32, "weight and dweight (fp32) are [cols]")
+        rows, cols, dy_stride = _strides(dy)
+        _bf16(dy, h, dx, dresidual)
+        rp = r_stride = 0
         if dresidual is not None:
-            r, c, a.dresidual_stride = _strides(dresidual)
-            _need((r, c) == shape, "dresidual has the shape of dy")
-            a.dresidual = dresidual.data_ptr()
+            rp, r_stride = dresidual.data_ptr(), _stride(dresidual, rows, cols, "dresidual")
         if scratch is None:
-            scratch = self.norm_grad_scratch(a.rows, a.cols)
-        a.weight_type, a.eps = _float_type(weight), eps
-        a.dy, a.h, a.weight, a.dx = dy.data_ptr(), h.data_ptr(), weight.data_ptr(), dx.data_ptr()
-        a.dweight, a.scratch, a.scratch_bytes = dweight.data_ptr(), scratch.data_ptr(), scratch.numel()
-        _check(strata_norm_grad(self.h, a, self._stream()), "strata_norm_grad")
+            scratch = self.norm_grad_scratch(rows, cols)
+        wt = _float_type(weight)
+        _check(self._c.strata_norm_grad(self.h, strata_norm_grad_args(
+            rows, cols, wt, eps, 0, dy.data_ptr(), h.data_ptr(), _flat(weight, 4 if wt else 2, cols, "weight"), rp,
+            dx.data_ptr(), _flat(dweight, 4, cols, "dweight"), scratch.data_ptr(), scratch.nbytes, dy_stride,
+            _stride(h, rows, cols, "h"), r_stride, _stride(dx, rows, cols, "dx")), self._stream()), "strata_norm_grad")
 
     def quantize_rows(self, x, q, q_scale, layout: Optional[Layout] = None) -> None:
         """bf16 rows -> 8-bit codes with one fp32 scale per row; with a layout, only the rows it has in use."""
         rows, cols, stride = _strides(x)
-        r, c, q_stride = _strides(q)
-        _need((r, c) == (rows, cols), "q has the shape of x")
+        _bf16(x)
         n_valid = layout.expert_offset.data_ptr() + 4 * self.E if layout is not None else None
-        _check(strata_quantize_rows(self.h, x.data_ptr(), stride, rows, cols, _code_type(q), q.data_ptr(), q_stride,
-                                    q_scale.data_ptr(), _scale_stride(q_scale, rows), n_valid, self._stream()),
-               "strata_quantize_rows")
+        _check(self._c.strata_quantize_rows(
+            self.h, x.data_ptr(), stride, rows, cols, _code_type(q), q.data_ptr(), _stride(q, rows, cols, "q"),
+            q_scale.data_ptr(), _scale_stride(q_scale, rows), n_valid, self._stream()), "strata_quantize_rows")
 
     def expert_matmul(self, layout: Layout, a, a_scale, w, w_scale, out, gated: bool = False) -> None:
         """out[r] = (a[r] . w[e]) * a_scale[r] * w_scale[e] for the rows of every expert's segment; gated: silu(first half
         of the channels) * second half.  a [rows, inner] and w [E, channels, inner]: torch.int8 or torch.float8_e4m3fn."""
-        m = strata_matmul_args()
-        m.a_rows, m.inner, m.a_stride = _strides(a)
-        rows, cols, m.out_stride = _strides(out)
-        m.type, m.gated, m.channels = _code_type(a), 1 if gated else 0, w.shape[1]
-        _need(w.dim() == 3 and w.dtype == a.dtype and w.is_contiguous() and w.shape[0] == self.E
-              and w.shape[2] == m.inner, "w is contiguous [E, channels, inner] of a's type")
-        _need(w_scale.is_contiguous() and w_scale.numel() == self.E * m.channels, "w_scale is contiguous [E, channels]")
-        _need(rows == m.a_rows and cols == (m.channels // 2 if gated else m.channels), "out is [rows, channels (/ 2)]")
-        m.a, m.w, m.w_scale, m.out = a.data_ptr(), w.data_ptr(), w_scale.data_ptr(), out.data_ptr()
-        m.a_scale, m.a_scale_stride = a_scale.data_ptr(), _scale_stride(a_scale, m.a_rows)
-        _check(strata_moe_expert_matmul(self.h, layout.c, m, self._stream()), "strata_moe_expert_matmul")
+        rows, inner, a_stride = _strides(a)
+        channels = w.size(1)
+        if w.dtype != a.dtype or w.dim() != 3:
+            raise ValueError("w is [E, channels, inner] of a's type")
+        _bf16(out)
+        wide = channels // 2 if gated else channels
+        _check(self._c.strata_moe_expert_matmul(self.h, layout.c, strata_matmul_args(
+            _code_type(a), 1 if gated else 0, inner, channels, rows, a.data_ptr(), a_scale.data_ptr(),
+            _flat(w, 1, self.E * channels * inner, "w"), _flat(w_scale, 4, self.E * channels, "w_scale"), out.data_ptr(),
+            a_stride, _scale_stride(a_scale, rows), _stride(out, rows, wide, "out")), self._stream()),
+            "strata_moe_expert_matmul")
 
     def row_experts(self, layout: Layout, out=None):
         """int32 [recv_rows]: the expert of every occupied receive row, -1 for padding and empty rows."""

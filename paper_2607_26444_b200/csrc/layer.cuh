@@ -7,7 +7,7 @@
 namespace strata {
 
 cudaError_t launch_route(const strata_moe_shape& s, const strata_route_params& r, const void* logits, int type,
-                         long long stride, const float* bias, int32_t* ids, float* w, cudaStream_t st);
+                         long long stride, const float* bias, int32_t* ids, float* w, int n_sm, cudaStream_t st);
 cudaError_t launch_route_grad(const strata_moe_shape& s, const strata_route_params& r, const void* logits, int type,
                               long long stride, const int32_t* ids, const float* dw, void* dlogits, long long dstride,
                               int* status, cudaStream_t st);

@@ -70,7 +70,7 @@ strata_status strata_moe_route(strata_ctx* ctx, const strata_route_params* param
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     return launched(ctx, launch_route(ctx->shape, *params, logits, logits_type, logits_stride, bias, topk_ids, topk_w,
-                                      static_cast<cudaStream_t>(stream)));
+                                      ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_moe_route_grad(strata_ctx* ctx, const strata_route_params* params, const void* logits,

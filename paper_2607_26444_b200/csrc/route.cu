@@ -19,6 +19,8 @@ struct RouteParams {
     int n_tok, E, K;
     int n_group, topk_group, group_size;
     int renormalise, top2;
+    int fast, fast_vec;    // fast = 0: every token takes the exact path
+    int lanes_per_group, run;
     int vec_ok;            // rows start on 16 bytes
     float scale;
 };
@@ -54,8 +56,8 @@ __device__ __forceinline__ float warp_max(float v)
     return v;
 }
 
-// VPL logits of experts e0 .. e0+VPL-1; experts beyond E, and NaN logits, read as -inf.
-template <int VPL, bool BF16>
+// VPL logits of experts e0 .. e0+VPL-1.  RAW: experts beyond E read as zero and NaN stays; otherwise both read as -inf.
+template <int VPL, bool BF16, bool RAW = false>
 __device__ __forceinline__ void load_logits(float (&l)[VPL], const void* base, long long row_off, int e0, int E, bool vec_ok)
 {
     constexpr int VW = BF16 ? 8 : 4;                              // logits in 16 bytes
@@ -76,36 +78,38 @@ __device__ __forceinline__ void load_logits(float (&l)[VPL], const void* base, l
             } else {
 #pragma unroll
                 for (int i = 0; i < VW; ++i)
-                    l[j + i] = e0 + j + i < E ? load_as_float<BF16>(base, row_off + e0 + j + i) : -INFINITY;
+                    l[j + i] = e0 + j + i < E ? load_as_float<BF16>(base, row_off + e0 + j + i) : RAW ? 0.0f : -INFINITY;
             }
         }
     } else {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) l[i] = e0 + i < E ? load_as_float<BF16>(base, row_off + e0 + i) : -INFINITY;
+        for (int i = 0; i < VPL; ++i)
+            l[i] = e0 + i < E ? load_as_float<BF16>(base, row_off + e0 + i) : RAW ? 0.0f : -INFINITY;
     }
+    if constexpr (!RAW) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+        for (int i = 0; i < VPL; ++i) l[i] = l[i] == l[i] ? l[i] : -INFINITY;
+    }
 }
 
-// Choice of the K largest of 32*VPL keys.  A direct selection (K rounds of: lane maxima, a warp-wide maximum, removal
-// of the winner from one lane's registers) issues about 40 instructions a round at VPL = 8.  Instead the K-th largest of
-// the 32 lane maxima is found first: it is a lower bound of the K-th largest key, and only about K + 2 keys
-// reach it; those are compacted in index order, one per lane, and each counts the keys that come before it.  Where more
-// than 32 reach it (many equal keys, K near 32), the direct selection runs.  At 65,536 tokens x 256 experts, sigmoid
-// scores in 4 of 8 groups, with the group choice below: see the measurements at the launcher.
+struct __align__(16) RouteSmem {          // of one warp
+    unsigned long long key[32];
+    uint32_t one[32], two[32];
+    float l[32];
+    int id[32];
+};
+
+// The whole choice of one token in exact arithmetic.  route_kernel below sends here what its shorter way does not decide:
+// masked or NaN logits, softmax scores compared as such, near-ties of groups, and more than 32 candidates.  Scores become ordered integer keys; the K-th largest of the 32 lane maxima bounds the K-th largest
+// key from below; the keys that reach it are compacted in index order and ranked; if more than 32 do, K
+// rounds of a warp-wide maximum take the winners one by one.  1,138 instructions per token at 256 experts in 4 of
+// 8 groups.
 template <int VPL, bool BF16, bool SIGMOID, bool BY_SCORE>
-__global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RouteParams p)
+__device__ __noinline__ void route_exact(const RouteParams& p, int tok, RouteSmem& sm, uint32_t* all)
 {
-    extern __shared__ uint32_t dyn_keys[];                        // [warps][E], only for groups that split a lane's run
-    __shared__ uint32_t s_key[kRouteWarps][32], s_two[kRouteWarps][32];
-    __shared__ float s_l[kRouteWarps][32];
-    __shared__ int s_id[kRouteWarps][32];
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int tok = (int)blockIdx.x * kRouteWarps + warp;
-    griddep_wait();
-    griddep_launch_dependents();
-    if (tok >= p.n_tok) return;
+    const int lane = (int)threadIdx.x & 31;
     const int e0 = lane * VPL;
+    __syncwarp();
 
     float l[VPL];
     load_logits<VPL, BF16>(l, p.logits, (long long)tok * p.stride, e0, p.E, p.vec_ok != 0);
@@ -156,18 +160,17 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RoutePara
                 a2 = max(a2, min(a1, key[i]));
                 a1 = max(a1, key[i]);
             }
-            s_key[warp][lane] = a1;
-            s_two[warp][lane] = a2;
+            sm.one[lane] = a1;
+            sm.two[lane] = a2;
             __syncwarp();
             const int lpg = gs / VPL;
             if (lane < p.n_group)
                 for (int q = lane * lpg; q < (lane + 1) * lpg; ++q) {
-                    const uint32_t b1 = s_key[warp][q];
-                    k2 = max(max(k2, min(k1, b1)), s_two[warp][q]);
+                    const uint32_t b1 = sm.one[q];
+                    k2 = max(max(k2, min(k1, b1)), sm.two[q]);
                     k1 = max(k1, b1);
                 }
         } else {
-            uint32_t* all = dyn_keys + (size_t)warp * p.E;
 #pragma unroll
             for (int i = 0; i < VPL; ++i)
                 if (e0 + i < p.E) all[e0 + i] = key[i];
@@ -230,19 +233,19 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RoutePara
 #pragma unroll
         for (int i = 0; i < VPL; ++i)
             if (key[i] >= bound) {
-                s_key[warp][at] = key[i];
-                s_id[warp][at] = e0 + i;
-                s_l[warp][at] = l[i];
+                sm.one[at] = key[i];
+                sm.id[at] = e0 + i;
+                sm.l[at] = l[i];
                 ++at;
             }
         __syncwarp();
         if (lane < total) {
-            const uint32_t k = s_key[warp][lane];
-            id = s_id[warp][lane];
-            lk = s_l[warp][lane];
+            const uint32_t k = sm.one[lane];
+            id = sm.id[lane];
+            lk = sm.l[lane];
             rank = 0;
             for (int j = 0; j < total; ++j) {
-                const uint32_t o = s_key[warp][j];
+                const uint32_t o = sm.one[j];
                 rank += (o > k || (o == k && j < lane)) ? 1 : 0;
             }
         }
@@ -296,6 +299,224 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_kernel(const RoutePara
         ids[lane] = -1;
         w[lane] = 0.0f;
     }
+}
+
+// redux.sync on floats: the largest over the warp, NaN never wins
+__device__ __forceinline__ float warp_redux_max(float v)
+{
+    float r;
+    asm("redux.sync.max.f32 %0, %1, 0xffffffff;" : "=f"(r) : "f"(v));
+    return r;
+}
+__device__ __forceinline__ float min_nan(float a, float b)         // NaN if either is
+{
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// 1 / (1 + exp(-l)) within 2^-22: the exponential is good to 2^-22 relative (its argument's rounding included, since
+// the slope t / (1 + t)^2 falls faster than |l| grows) and the slope is at most 1/4; reciprocal and sum add 2^-23;
+// results below 2^-126 flush to zero.
+__device__ __forceinline__ float sigmoid_approx(float l)
+{
+    float t, s;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t) : "f"(l * -1.44269504f));
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(s) : "f"(1.0f + t));
+    return s;
+}
+
+template <int N>
+struct TopTwo {                           // the two largest of N values
+    static __device__ __forceinline__ float2 of(const float* c)
+    {
+        const float2 a = TopTwo<N / 2>::of(c), b = TopTwo<N / 2>::of(c + N / 2);
+        return make_float2(fmaxf(a.x, b.x), fmaxf(fminf(a.x, b.x), fmaxf(a.y, b.y)));
+    }
+};
+template <>
+struct TopTwo<2> {
+    static __device__ __forceinline__ float2 of(const float* c) { return make_float2(fmaxf(c[0], c[1]), fminf(c[0], c[1])); }
+};
+template <>
+struct TopTwo<1> {
+    static __device__ __forceinline__ float2 of(const float* c) { return make_float2(c[0], -INFINITY); }
+};
+
+// The router is bound by instruction issue (in exact arithmetic throughout: 1,138 instructions per token at 256 experts,
+// 3.5 issued per cycle and SM, 75 us for 65,536 tokens, where reading the logits takes 11 us).  So the bulk of the work is
+// done on approximate choice values with a known error, and only the candidates, one per lane, are evaluated exactly:
+//  1. c ~ sigmoid + bias within err = 2^-21 + 2^-22 (1 + max|bias|), the roundings of the sum on both sides included
+//     (without a bias the logits themselves are compared, err = 0);
+//  2. groups: two largest per lane, merged over the lanes of a group; the topk_group best by warp-wide maxima.  If the
+//     last kept and the first dropped lie closer than their errors, or equal scores leave too many, the exact path decides;
+//  3. the K-th largest lane maximum, less twice the error, is a bound that every expert of the true choice reaches;
+//  4. the experts that reach it (about K + 2) are compacted; each lane evaluates one of them exactly, and its rank
+//     is the number of candidates with a larger choice value, or an equal one and a lower index.
+// A warp keeps its biases in registers from token to token and fetches the next token's logits ahead.
+constexpr int route_blocks_per_sm(int vpl) { return vpl <= 8 ? 4 : vpl == 16 ? 2 : 1; }
+template <int VPL, bool BF16, bool SIGMOID, bool BY_SCORE>
+__global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) route_kernel(const RouteParams p)
+{
+    extern __shared__ uint32_t dyn_keys[];                        // [warps][E], only for groups that split a lane's run
+    __shared__ RouteSmem s_route[kRouteWarps];
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int step = (int)gridDim.x * kRouteWarps;
+    int tok = (int)blockIdx.x * kRouteWarps + warp;
+    RouteSmem& sm = s_route[warp];
+    griddep_wait();
+    if (tok >= p.n_tok) return;
+    if (!p.fast) {
+        for (; tok < p.n_tok; tok += step)
+            route_exact<VPL, BF16, SIGMOID, BY_SCORE>(p, tok, sm, dyn_keys + (size_t)warp * p.E);
+        return;
+    }
+    // A group owns a power of two of lanes; a lane holds `run` (or fewer) experts of its group from e0 on.
+    const int lpg = p.lanes_per_group, in_group = (lane & (lpg - 1)) * p.run;
+    const int left = lane / lpg < p.n_group ? max(0, min(p.run, p.group_size - in_group)) : 0;
+    const int e0 = left > 0 ? lane / lpg * p.group_size + in_group : 0, end = e0 + left;
+    float bias[BY_SCORE ? VPL : 1], err = 0.0f;
+    if constexpr (BY_SCORE) {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            bias[i] = i >= left ? -INFINITY : p.bias ? p.bias[e0 + i] : 0.0f;
+            if (bias[i] != bias[i]) bias[i] = -INFINITY;
+            if (bias[i] > -INFINITY) err = fmaxf(err, fabsf(bias[i]));
+        }
+        err = 0x1p-21f + 0x1p-22f * (1.0f + warp_redux_max(err));
+    }
+    const bool padded = p.E != 32 * VPL;
+
+    float l[VPL];
+    load_logits<VPL, BF16, true>(l, p.logits, (long long)tok * p.stride, e0, end, p.fast_vec != 0);
+    while (true) {
+        const int next = tok + step;
+        float c[VPL], least = l[0];
+#pragma unroll
+        for (int i = 1; i < VPL; ++i) least = min_nan(least, l[i]);
+        bool exact = __any_sync(kFull, !(least > -INFINITY));
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) c[i] = BY_SCORE ? sigmoid_approx(l[i]) + bias[i] : l[i];
+        if (!BY_SCORE && padded) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i)
+                if (i >= left) c[i] = -INFINITY;
+        }
+        float m = 0.0f, sum = 1.0f;
+        if constexpr (!SIGMOID) {                                 // logits are compared (BY_SCORE softmax is never fast)
+            m = c[0];
+#pragma unroll
+            for (int i = 1; i < VPL; ++i) m = fmaxf(m, c[i]);
+            m = warp_redux_max(m);
+            if (!p.renormalise) {
+                float s = 0.0f;
+#pragma unroll
+                for (int i = 0; i < VPL; ++i) s += softmax_term(c[i], m);
+                sum = warp_sum(s);
+            }
+        }
+        // the next token's logits travel while this one is decided
+        if (next < p.n_tok) load_logits<VPL, BF16, true>(l, p.logits, (long long)next * p.stride, e0, end, p.fast_vec != 0);
+
+        float2 two = TopTwo<VPL>::of(c);
+        float lane_max = two.x;
+        bool kept = true;
+        if (p.n_group > 1) {
+            for (int o = 1; o < lpg; o <<= 1) {
+                const float bx = __shfl_xor_sync(kFull, two.x, o), by = __shfl_xor_sync(kFull, two.y, o);
+                two = make_float2(fmaxf(two.x, bx), fmaxf(fminf(two.x, bx), fmaxf(two.y, by)));
+            }
+            float g = p.top2 && two.y > -INFINITY ? two.x + two.y : two.x;
+            float last = 0.0f;
+            kept = false;
+#pragma unroll 4
+            for (int r = 0; r < p.topk_group; ++r) {
+                last = warp_redux_max(g);
+                if (g == last) {
+                    kept = g > -INFINITY;
+                    g = -INFINITY;
+                }
+            }
+            const float first_out = warp_redux_max(g);
+            const int n_kept = __popc(__ballot_sync(kFull, kept));
+            // no more groups than asked for may be kept; fewer only if no other has a member left
+            exact |= n_kept > p.topk_group * lpg || first_out >= last - 8.0f * err ||
+                     (n_kept < p.topk_group * lpg && first_out > -INFINITY);
+            lane_max = kept ? lane_max : -INFINITY;
+        }
+        float bound = -INFINITY;
+#pragma unroll 4
+        for (int r = 0; r < p.K; ++r) {
+            bound = warp_redux_max(lane_max);
+            if (lane_max == bound) lane_max = -INFINITY;
+        }
+        if constexpr (BY_SCORE) bound -= 4.0f * err;
+        bound = bound >= -3.402823466e38f ? bound : -3.402823466e38f;     // -inf (and the NaN of its margin): all finite ones
+        if (!kept) bound = INFINITY;
+        uint32_t flags = 0;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) flags |= c[i] >= bound ? 1u << i : 0u;
+        int at = __popc(flags);
+        const int mine = at;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int v = __shfl_up_sync(kFull, at, o);
+            if (lane >= o) at += v;
+        }
+        const int total = __shfl_sync(kFull, at, 31);
+        at -= mine;
+        __syncwarp();                                             // the last token's candidates have been read
+        if (total <= 32)
+            for (; flags; flags &= flags - 1) sm.id[at++] = e0 + __ffs(flags) - 1;
+        exact |= total > 32;
+        if (exact) {
+            route_exact<VPL, BF16, SIGMOID, BY_SCORE>(p, tok, sm, dyn_keys + (size_t)warp * p.E);
+        } else {
+            __syncwarp();
+            int id = -1, rank = p.K;
+            float lk = 0.0f, s = 0.0f;
+            unsigned long long key = 0;
+            if (lane < total) {
+                id = sm.id[lane];
+                lk = load_as_float<BF16>(p.logits, (long long)tok * p.stride + id);
+                float ck = lk;
+                if constexpr (SIGMOID) s = sigmoid_f(lk);
+                if constexpr (BY_SCORE) ck = __fadd_rn(s, p.bias ? p.bias[id] : 0.0f);
+                key = ((unsigned long long)key_of(ck) << 32) | (uint32_t)~id;
+            }
+            sm.key[lane] = key;
+            __syncwarp();
+            if (lane < total) {
+                rank = 0;
+                for (int j = 0; j < total; j += 4) {              // slots beyond the candidates hold the lowest key
+                    const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(&sm.key[j]);
+                    const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(&sm.key[j + 2]);
+                    rank += (a.x > key ? 1 : 0) + (a.y > key ? 1 : 0) + (b.x > key ? 1 : 0) + (b.y > key ? 1 : 0);
+                }
+            }
+            const bool sel = rank < p.K;
+            if constexpr (!SIGMOID) s = sel ? softmax_term(lk, m) : 0.0f;
+            float over = p.scale;
+            if (p.renormalise) {
+                const float d = warp_sum(sel ? s : 0.0f);
+                over = d > 0.0f ? p.scale * __frcp_rn(d) : 0.0f;
+            } else if (!SIGMOID) {
+                over = p.scale * __frcp_rn(sum);
+            }
+            int32_t* ids = p.ids + (long long)tok * p.K;
+            float* w = p.w + (long long)tok * p.K;
+            if (sel) {
+                ids[rank] = id;
+                w[rank] = s * over;
+            }
+            if (lane >= total && lane < p.K) {
+                ids[lane] = -1;
+                w[lane] = 0.0f;
+            }
+        }
+        if (next >= p.n_tok) break;
+        tok = next;
+    }
+    griddep_launch_dependents();
 }
 
 struct RouteGradParams {
@@ -399,18 +620,24 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
     store_row<VPL, BF16>(g, p.dlogits, (long long)tok * p.dstride, e0, p.E, p.dvec_ok != 0);
 }
 
-int lanes_width(int E)
+// registers per lane for runs of `lanes` lanes over `n` experts
+int lanes_width(int n, int lanes = 32)
 {
     int v = 1;
-    while (32 * v < E) v *= 2;
+    while (lanes * v < n) v *= 2;
     return v;
 }
 
 template <int VPL, bool BF16>
-cudaError_t route_vpl(const RouteParams& p, const strata_route_params& r, cudaStream_t st)
+cudaError_t route_vpl(RouteParams& p, const strata_route_params& r, int n_sm, cudaStream_t st)
 {
     const bool by_score = p.bias != nullptr || p.top2;
-    const unsigned grid = (unsigned)((p.n_tok + kRouteWarps - 1) / kRouteWarps);
+    constexpr int kVec = BF16 ? 8 : 4;                            // logits in 16 bytes
+    p.fast = !(by_score && r.score == STRATA_SCORE_SOFTMAX);
+    p.run = (p.group_size + p.lanes_per_group - 1) / p.lanes_per_group;
+    if (VPL >= kVec) p.run = (p.run + kVec - 1) / kVec * kVec;
+    p.fast_vec = p.vec_ok && p.run % kVec == 0 && p.group_size % kVec == 0;
+    const unsigned grid = (unsigned)min((p.n_tok + kRouteWarps - 1) / kRouteWarps, n_sm * route_blocks_per_sm(VPL));
     const size_t smem = p.n_group > 1 && p.group_size % VPL != 0 ? (size_t)kRouteWarps * p.E * sizeof(uint32_t) : 0;
     if (r.score == STRATA_SCORE_SIGMOID)
         return by_score ? launch_pdl(route_kernel<VPL, BF16, true, true>, grid, kRouteWarps * 32, smem, st, p)
@@ -439,7 +666,7 @@ bool rows_on_16(const void* base, long long stride, int type)
 }  // namespace
 
 cudaError_t launch_route(const strata_moe_shape& s, const strata_route_params& r, const void* logits, int type,
-                         long long stride, const float* bias, int32_t* ids, float* w, cudaStream_t st)
+                         long long stride, const float* bias, int32_t* ids, float* w, int n_sm, cudaStream_t st)
 {
     RouteParams p{};
     p.logits = logits;
@@ -453,18 +680,20 @@ cudaError_t launch_route(const strata_moe_shape& s, const strata_route_params& r
     p.n_group = r.n_group;
     p.topk_group = r.topk_group;
     p.group_size = s.E / r.n_group;
+    p.lanes_per_group = 32;
+    while (p.lanes_per_group * r.n_group > 32) p.lanes_per_group /= 2;
     p.renormalise = r.renormalise;
     p.top2 = r.n_group > 1 && r.group_score == STRATA_GROUP_TOP2;
     p.vec_ok = rows_on_16(logits, stride, type);
     p.scale = r.scale;
     const bool bf = type == STRATA_T_BF16;
-    switch (lanes_width(s.E)) {
-        case 1: return bf ? route_vpl<1, true>(p, r, st) : route_vpl<1, false>(p, r, st);
-        case 2: return bf ? route_vpl<2, true>(p, r, st) : route_vpl<2, false>(p, r, st);
-        case 4: return bf ? route_vpl<4, true>(p, r, st) : route_vpl<4, false>(p, r, st);
-        case 8: return bf ? route_vpl<8, true>(p, r, st) : route_vpl<8, false>(p, r, st);
-        case 16: return bf ? route_vpl<16, true>(p, r, st) : route_vpl<16, false>(p, r, st);
-        default: return bf ? route_vpl<32, true>(p, r, st) : route_vpl<32, false>(p, r, st);
+    switch (lanes_width(p.group_size, p.lanes_per_group)) {
+        case 1: return bf ? route_vpl<1, true>(p, r, n_sm, st) : route_vpl<1, false>(p, r, n_sm, st);
+        case 2: return bf ? route_vpl<2, true>(p, r, n_sm, st) : route_vpl<2, false>(p, r, n_sm, st);
+        case 4: return bf ? route_vpl<4, true>(p, r, n_sm, st) : route_vpl<4, false>(p, r, n_sm, st);
+        case 8: return bf ? route_vpl<8, true>(p, r, n_sm, st) : route_vpl<8, false>(p, r, n_sm, st);
+        case 16: return bf ? route_vpl<16, true>(p, r, n_sm, st) : route_vpl<16, false>(p, r, n_sm, st);
+        default: return bf ? route_vpl<32, true>(p, r, n_sm, st) : route_vpl<32, false>(p, r, n_sm, st);
     }
 }
 
