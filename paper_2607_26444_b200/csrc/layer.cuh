@@ -20,7 +20,7 @@ cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, i
                             int* status, int n_sm, cudaStream_t st);
 cudaError_t configure_matmul_kernels();
 cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_layout_t& L, const strata_matmul_args& a,
-                                 int* status, int n_sm, cudaStream_t st);
+                                 int* status, WorkQueue wq, int n_sm, cudaStream_t st);
 
 #ifdef __CUDACC__
 __device__ __forceinline__ void unpack_bf16x8(uint4 v, float* f)

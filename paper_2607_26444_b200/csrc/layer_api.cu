@@ -12,6 +12,8 @@ using namespace strata;
 constexpr int kMaxCols = 32768;          // longest row the norm and the quantiser hold in registers
 constexpr int kMaxInner = 131056;        // 2^31 / 128^2, less one: int8 sums cannot overflow int32
 
+WorkQueue matmul_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 8}; }
+
 bool on(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 strata_status check_route(const strata_ctx* ctx, const strata_route_params* r, int type, int64_t stride)
@@ -185,7 +187,7 @@ strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
-    return launched(ctx, launch_expert_matmul(s, *layout, *a, ctx->ws, ctx->n_sm, static_cast<cudaStream_t>(stream)));
+    return launched(ctx, launch_expert_matmul(s, *layout, *a, ctx->ws, matmul_queue(ctx), ctx->n_sm, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

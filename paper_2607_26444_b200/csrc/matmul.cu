@@ -13,20 +13,30 @@ namespace strata {
 
 namespace {
 
-constexpr int kM = 128;                 // weight rows of a tile (gated: 64 gate rows and 64 up rows, see kGateRows)
-constexpr int kGateRows = 16;           // gated: every 32 rows of the tile are 16 of the gate, then the same 16 of up
+constexpr int kM = 128;                 // channels of a matrix instruction
 constexpr int kKBytes = 128;            // inner extent of a stage: one swizzle span
 constexpr int kUmmaK = 32;              // bytes of K per matrix instruction
-constexpr int kThreads = 192;           // warp 0: loads, warp 1: matrix instructions, warps 2..5: epilogue
-constexpr int kAStage = kM * kKBytes;
+constexpr int kBlock = kM * kKBytes;    // one 128-row block of weights of a stage
 
-template <int BN>
+// A tile is MB blocks of 128 weight rows by up to BN rows of the N operand.
+//   MB = 1: one accumulator.  Gated: its rows 0..63 are 64 gate channels, rows 64..127 the same channels of up, and the
+//           epilogue warps of the two halves exchange columns through shared memory.
+//   MB = 2: two accumulators that share the N operand.  Gated: 128 gate channels and the same of up, which then meet in
+//           one thread; otherwise 256 channels.
+// Accumulators are doubled (one pair is filled while the other is read) wherever TMEM's 512 columns allow it.
+template <int MB, int BN>
 struct Tile {
     static constexpr int box_rows = BN >= 128 ? 64 : 32;            // rows of one TMA box of the N operand
-    static constexpr int b_stage = BN * kKBytes;
-    static constexpr int stages = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-    static constexpr int tmem_cols = 2 * BN;                        // two accumulators: one is filled while one is read
-    static constexpr size_t data_bytes = (size_t)stages * (kAStage + b_stage);
+    static constexpr int w_stage = MB * kBlock, a_stage = BN * kKBytes;
+    static constexpr int stages = 192 * 1024 / (w_stage + a_stage);
+    static constexpr int bufs = MB * BN * 2 <= 512 ? 2 : 1;
+    static constexpr int tmem_cols = bufs * MB * BN;
+    static constexpr int epi_warps = MB == 2 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
+    static constexpr int threads = 64 + 32 * epi_warps;             // warp 0: loads, warp 1: matrix instructions
+    static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
+    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 16 * 32 : 0;   // exchange of a gated tile
+    static constexpr size_t data_bytes = (size_t)stages * (w_stage + a_stage);
+    static_assert(stages <= 8 && tmem_cols <= 512 && data_bytes % 1024 == 0, "");
 };
 
 struct MatParams {
@@ -37,12 +47,17 @@ struct MatParams {
     const float* w_scale;
     uint16_t* out;
     int* status;
+    WorkQueue wq;
     long long a_rows, a_scale_stride, out_stride;
     int E, k_blocks, channels, m_tiles; // channels: rows of w per expert
 };
 
+constexpr int kClaims = 4;              // tiles that the loading warp may be ahead of the epilogue
+
 struct SmemTail {                       // behind the operand stages
     uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], drain;
+    uint64_t claim_full[kClaims], claim_empty[kClaims];
+    unsigned claim[kClaims];
     uint32_t tmem_base, issued;
     int dead, pad[3];
 };
@@ -116,18 +131,22 @@ __device__ __forceinline__ void mma_commit(uint64_t* bar)
     asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(smem_addr(bar))
                  : "memory");
 }
-__device__ __forceinline__ void tmem_ld32(uint32_t (&r)[32], uint32_t addr)
+__device__ __forceinline__ void tmem_ld16(uint32_t (&r)[16], uint32_t addr)
 {
     asm volatile(
-        "tcgen05.ld.sync.aligned.32x32b.x32.b32 "
-        "{%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
-        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];"
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
         : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
-          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
-          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
-          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
         : "r"(addr));
-    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+// the loaded registers are tied to the wait, so that no use of them moves in front of it
+__device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15])
+                 :
+                 : "memory");
 }
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
@@ -136,6 +155,8 @@ struct Work {
     int e, m, row0, rows;               // expert, channel tile, first receive row, rows of the tile
 };
 
+// Tiles are dealt by an ordered claim (common.cuh): their costs differ, since an expert's last row tile is partial, and
+// a static round robin left the SMs between 79 % and 100 % of the kernel's time at work (prefill chunk of 16,384 rows).
 // Tiles are numbered expert by expert, inside an expert channel tile by channel tile, row tiles fastest: CTAs that run
 // together read the same weights (once from HBM) and the same few row tiles.
 template <int BN>
@@ -160,17 +181,61 @@ __device__ __forceinline__ Work find_work(unsigned t, const int* s_base, const i
     return w;
 }
 
-template <bool INT8, bool GATED, int BN>
-__global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid_constant__ MatParams p)
+// Whether both warps of an exchanging pair go on: one vote for all 64 threads, so that neither waits for the other in vain.
+__device__ __forceinline__ bool pair_all(bool ok, int pair)
 {
-    using T = Tile<BN>;
+    uint32_t r;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
+        "bar.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+        : "=r"(r)
+        : "r"((uint32_t)ok), "r"(1 + pair)
+        : "memory");
+    return r != 0;
+}
+
+template <bool INT8>
+__device__ __forceinline__ float acc_value(uint32_t v)
+{
+    return INT8 ? __int2float_rn((int)v) : __uint_as_float(v);
+}
+__device__ __forceinline__ float gate_mul(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
+
+// N columns of 32 channels, lane = channel: neighbouring lanes exchange, so that one holds two channels of column c and
+// the other two channels of column c + 1, and each writes them with one 4-byte store (64 bytes per row and warp).
+template <int N>
+__device__ __forceinline__ void store_pairs(const float (&y)[N], int lane, uint16_t* out, long long stride, int rows, bool in)
+{
+    const int odd = lane & 1;
+    out += odd * stride;
+#pragma unroll
+    for (int c = 0; c < N; c += 2) {
+        const float other = __shfl_xor_sync(0xffffffffu, odd ? y[c] : y[c + 1], 1);
+        const uint32_t v = odd ? pack_bf16x2(other, y[c + 1]) : pack_bf16x2(y[c], other);
+        if (in && c + odd < rows) *reinterpret_cast<uint32_t*>(out + c * stride) = v;
+    }
+}
+
+// The n-th tile that the loading warp handed over.
+__device__ __forceinline__ bool next_tile(SmemTail& tail, uint32_t n, unsigned& t, volatile int* dead, int* status)
+{
+    if (!wait_or_dead(&tail.claim_full[n % kClaims], (n / kClaims) & 1, dead, status)) return false;
+    t = *reinterpret_cast<volatile unsigned*>(&tail.claim[n % kClaims]);
+    return true;
+}
+
+template <bool INT8, bool GATED, int MB, int BN>
+__global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel(const __grid_constant__ MatParams p)
+{
+    using T = Tile<MB, BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    unsigned char* s_w = smem;                                       // [stages][128][128]
-    unsigned char* s_a = smem + T::stages * kAStage;                 // [stages][BN][128]
+    unsigned char* s_w = smem;                                       // [stages][MB * 128][128]
+    unsigned char* s_a = smem + T::stages * T::w_stage;              // [stages][BN][128]
     SmemTail* tail = reinterpret_cast<SmemTail*>(smem + T::data_bytes);
-    float* s_scale = reinterpret_cast<float*>(tail + 1);             // [4][BN]
-    int* s_base = reinterpret_cast<int*>(s_scale + 4 * BN);          // [E + 1]
+    float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
+    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][2][16][32]
+    int* s_base = reinterpret_cast<int*>(s_swap + T::swap_floats);   // [E + 1]
     int* s_off = s_base + p.E + 1;                                   // [E]
     int* s_cnt = s_off + p.E;                                        // [E]
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
@@ -182,7 +247,11 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&tail->tmem_full[b], 1);
-            mbar_init(&tail->tmem_empty[b], 4);
+            mbar_init(&tail->tmem_empty[b], T::epi_warps);
+        }
+        for (int c = 0; c < kClaims; ++c) {
+            mbar_init(&tail->claim_full[c], 1);
+            mbar_init(&tail->claim_empty[c], 1 + T::epi_warps);
         }
         mbar_init(&tail->drain, 1);
         tail->dead = 0;
@@ -198,7 +267,7 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
     }
     griddep_wait();
     // segments, kept inside the buffer whatever the offsets hold
-    for (int e = (int)threadIdx.x; e < p.E; e += kThreads) {
+    for (int e = (int)threadIdx.x; e < p.E; e += T::threads) {
         const long long off = p.expert_offset[e];
         const long long cnt = p.expert_count ? (long long)p.expert_count[e] : (long long)p.expert_offset[e + 1] - off;
         const bool ok = off >= 0 && off <= p.a_rows;
@@ -231,11 +300,18 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
     if (warp == 0) {
         if (lane == 0) {
             uint32_t it = 0;
-            bool ok = true;
-            for (unsigned t = blockIdx.x; t < n_tiles && ok; t += gridDim.x) {
+            bool ok = true, exhausted = false;
+            unsigned t = blockIdx.x < n_tiles ? blockIdx.x : kNoUnit;
+            for (uint32_t n = 0; ok; ++n) {
+                // hand the tile to the other warps (kNoUnit ends their loops), then claim the next one
+                if (!wait_or_dead(&tail->claim_empty[n % kClaims], ((n / kClaims) & 1) ^ 1, dead, p.status)) break;
+                tail->claim[n % kClaims] = t;
+                mbar_arrive(&tail->claim_full[n % kClaims]);
+                if (t == kNoUnit) break;
+                const unsigned next = claim_unit(p.wq, n_tiles, gridDim.x, exhausted);
                 const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
                 const int boxes = (w.rows + T::box_rows - 1) / T::box_rows;
-                const uint32_t bytes = (uint32_t)(kAStage + boxes * T::box_rows * kKBytes);
+                const uint32_t bytes = (uint32_t)(T::w_stage + boxes * T::box_rows * kKBytes);
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                     const uint32_t s = it % T::stages;
                     if (!wait_or_dead(&tail->empty[s], ((it / T::stages) & 1) ^ 1, dead, p.status)) {
@@ -243,17 +319,22 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
                         break;
                     }
                     mbar_expect_tx(&tail->full[s], bytes);
-                    if constexpr (GATED) {
+                    unsigned char* dw = s_w + s * T::w_stage;
+                    if constexpr (GATED) {                           // [2E][channels / 2][inner]: gate, up
+                        constexpr int kRows = MB * kM / 2;
 #pragma unroll
-                        for (int b = 0; b < kM / kGateRows; ++b)
-                            tma_load_3d(s_w + s * kAStage + b * kGateRows * kKBytes, &p.map_w, kb * kKBytes,
-                                        w.m * (kM / 2) + (b >> 1) * kGateRows, 2 * w.e + (b & 1), &tail->full[s]);
-                    } else
-                        tma_load_2d(s_w + s * kAStage, &p.map_w, kb * kKBytes, w.e * p.channels + w.m * kM, &tail->full[s]);
+                        for (int g = 0; g < 2; ++g)
+                            tma_load_3d(dw + g * kRows * kKBytes, &p.map_w, kb * kKBytes, w.m * kRows, 2 * w.e + g, &tail->full[s]);
+                    } else {
+#pragma unroll
+                        for (int b = 0; b < MB; ++b)
+                            tma_load_3d(dw + b * kBlock, &p.map_w, kb * kKBytes, (w.m * MB + b) * kM, w.e, &tail->full[s]);
+                    }
                     for (int b = 0; b < boxes; ++b)
-                        tma_load_2d(s_a + s * T::b_stage + b * T::box_rows * kKBytes, &p.map_a, kb * kKBytes,
+                        tma_load_2d(s_a + s * T::a_stage + b * T::box_rows * kKBytes, &p.map_a, kb * kKBytes,
                                     w.row0 + b * T::box_rows, &tail->full[s]);
                 }
+                t = next;
             }
             tail->issued = it;
         }
@@ -261,13 +342,17 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
         if (lane == 0) {
             uint32_t it = 0, use = 0;
             bool ok = true;
-            for (unsigned t = blockIdx.x; t < n_tiles && ok; t += gridDim.x, ++use) {
+            for (; ok; ++use) {
+                unsigned t;
+                if (!next_tile(*tail, use, t, dead, p.status)) break;
+                mbar_arrive(&tail->claim_empty[use % kClaims]);
+                if (t == kNoUnit) break;
                 const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
                 const uint32_t idesc = instr_desc<INT8>((w.rows + 15) & ~15);
-                const uint32_t buf = use & 1;
-                if (!wait_or_dead(&tail->tmem_empty[buf], ((use >> 1) & 1) ^ 1, dead, p.status)) break;
+                const uint32_t buf = use % T::bufs;
+                if (!wait_or_dead(&tail->tmem_empty[buf], ((use / T::bufs) & 1) ^ 1, dead, p.status)) break;
                 tmem_fence_after();
-                const uint32_t d = tmem + buf * BN;
+                const uint32_t d = tmem + buf * MB * BN;
                 for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
                     const uint32_t s = it % T::stages;
                     if (!wait_or_dead(&tail->full[s], (it / T::stages) & 1, dead, p.status)) {
@@ -275,11 +360,14 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
                         break;
                     }
                     tmem_fence_after();
-                    const uint64_t da = smem_desc(smem_addr(s_w + s * kAStage));
-                    const uint64_t db = smem_desc(smem_addr(s_a + s * T::b_stage));
+                    const uint64_t dw = smem_desc(smem_addr(s_w + s * T::w_stage));
+                    const uint64_t da = smem_desc(smem_addr(s_a + s * T::a_stage));
 #pragma unroll
                     for (int k = 0; k < kKBytes / kUmmaK; ++k)
-                        mma<INT8>(d, da + k * (kUmmaK >> 4), db + k * (kUmmaK >> 4), idesc, (kb | k) != 0);
+#pragma unroll
+                        for (int b = 0; b < MB; ++b)
+                            mma<INT8>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4), idesc,
+                                      (kb | k) != 0);
                     mma_commit(&tail->empty[s]);
                 }
                 if (ok) mma_commit(&tail->tmem_full[buf]);
@@ -290,56 +378,106 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
             }
         }
     } else {
-        const int quad = warp & 3;                                   // TMEM lanes 32*quad .. of this warp
-        float* scale = s_scale + quad * BN;
+        const int ew = warp - 2, quad = warp & 3;                    // TMEM lanes 32*quad .. of this warp
+        const int col0 = (ew >> 2) * T::cols;                        // first column of this warp
+        float* scale = s_scale + ew * T::cols;
         const int half = p.channels / 2;
         uint32_t use = 0;
-        for (unsigned t = blockIdx.x; t < n_tiles; t += gridDim.x, ++use) {
-            const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
-            const uint32_t buf = use & 1;
-            // Channel of w that this lane holds.  Gated: lanes q and q + 16 hold gate and up of one output channel.
-            int ch, out_ch;
-            bool in;
-            if constexpr (GATED) {
-                out_ch = w.m * (kM / 2) + quad * kGateRows + (lane & 15);
-                in = out_ch < half;
-                ch = out_ch + (lane >> 4) * half;
-            } else {
-                ch = w.m * kM + quad * 32 + lane;
-                out_ch = ch & ~1;
-                in = ch < p.channels;
+        for (;; ++use) {
+            unsigned t;
+            const bool got = next_tile(*tail, use, t, dead, p.status);
+            if constexpr (GATED && MB == 1) {                        // the two warps of an exchange leave together
+                if (!pair_all(got, quad & 1)) break;
+            } else if (!__all_sync(0xffffffffu, got)) {
+                break;
             }
-            const float ws = in ? p.w_scale[(size_t)w.e * p.channels + ch] : 0.0f;
             __syncwarp();
-            for (int c = lane; c < BN; c += 32)
-                scale[c] = c < w.rows ? p.a_scale[(long long)(w.row0 + c) * p.a_scale_stride] : 0.0f;
-            __syncwarp();
-            const bool ok = wait_or_dead(&tail->tmem_full[buf], (use >> 1) & 1, dead, p.status);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            tmem_fence_after();
-            const uint32_t addr = tmem + buf * BN + ((uint32_t)(quad * 32) << 16);
-            constexpr int kPair = GATED ? 16 : 1;                    // the partner is lane ^ kPair
-            const int odd = (lane & kPair) ? 1 : 0;
-            uint16_t* out = p.out + out_ch;
-            for (int c0 = 0; c0 < w.rows; c0 += 32) {
-                uint32_t v[32];
-                tmem_ld32(v, addr + c0);
+            if (lane == 0) mbar_arrive(&tail->claim_empty[use % kClaims]);
+            if (t == kNoUnit) break;
+            const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
+            const uint32_t buf = use % T::bufs;
+            const int rows = min(T::cols, w.rows - col0);            // of this warp; may be negative
+            const float* ws = p.w_scale + (size_t)w.e * p.channels;
+            // channel(s) of w that this lane holds, and the first channel of out
+            int ch[2], out_ch[2];
+            if constexpr (GATED && MB == 1) {
+                out_ch[0] = w.m * (kM / 2) + (quad & 1) * 32 + lane;
+                ch[0] = out_ch[0] + (quad >> 1) * half;
+            } else if constexpr (GATED) {
+                out_ch[0] = ch[0] = w.m * kM + quad * 32 + lane;
+                ch[1] = ch[0] + half;
+            } else {
 #pragma unroll
-                for (int c = 0; c < 32; c += 2) {
-                    const float a0 = INT8 ? __int2float_rn((int)v[c]) : __uint_as_float(v[c]);
-                    const float a1 = INT8 ? __int2float_rn((int)v[c + 1]) : __uint_as_float(v[c + 1]);
-                    const float y0 = a0 * (scale[c0 + c] * ws), y1 = a1 * (scale[c0 + c + 1] * ws);
-                    // the two partners hold two channels (gated: gate and up of one channel) of rows c and c + 1;
-                    // after the exchange one has both of row c, the other both of row c + 1
-                    const float other = __shfl_xor_sync(0xffffffffu, odd ? y0 : y1, kPair);
-                    const float lo = odd ? other : y0, hi = odd ? y1 : other;
-                    const int col = c0 + c + odd;
-                    uint16_t* at = out + (long long)(w.row0 + col) * p.out_stride;
-                    if constexpr (GATED) {
-                        const float g = __fdividef(lo, 1.0f + __expf(-lo)) * hi;
-                        if (in && col < w.rows) *at = (uint16_t)pack_bf16x2(g, 0.0f);
-                    } else {
-                        if (in && col < w.rows) *reinterpret_cast<uint32_t*>(at) = pack_bf16x2(lo, hi);
+                for (int b = 0; b < MB; ++b) out_ch[b] = ch[b] = (w.m * MB + b) * kM + quad * 32 + lane;
+            }
+            const int limit = GATED ? half : p.channels;
+            float wsc[2];
+#pragma unroll
+            for (int b = 0; b < MB; ++b) wsc[b] = out_ch[GATED ? 0 : b] < limit ? ws[ch[b]] : 0.0f;
+            __syncwarp();
+            for (int c = lane; c < T::cols; c += 32)
+                scale[c] = c < rows ? p.a_scale[(long long)(w.row0 + col0 + c) * p.a_scale_stride] : 0.0f;
+            __syncwarp();
+            const bool ok = wait_or_dead(&tail->tmem_full[buf], (use / T::bufs) & 1, dead, p.status);
+            if constexpr (GATED && MB == 1) {
+                if (!pair_all(ok, quad & 1)) break;
+            } else if (!__all_sync(0xffffffffu, ok)) {
+                break;
+            }
+            tmem_fence_after();
+            const uint32_t addr = tmem + buf * MB * BN + ((uint32_t)(quad * 32) << 16) + col0;
+            uint16_t* out = p.out + (long long)(w.row0 + col0) * p.out_stride;
+            int phase = 0;
+            for (int c0 = 0; c0 < rows; c0 += 16, phase ^= 1) {
+                float sc[16];
+#pragma unroll
+                for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(&sc[c]) = *reinterpret_cast<const float4*>(&scale[c0 + c]);
+                if constexpr (GATED && MB == 1) {
+                    uint32_t v[16];
+                    tmem_ld16(v, addr + c0);
+                    tmem_ld_wait(v);
+                    float y[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) y[c] = acc_value<INT8>(v[c]) * (sc[c] * wsc[0]);
+                    // the gate's warp finishes columns 0..7, up's warp columns 8..15
+                    const bool up = quad >> 1;
+                    float* mine = s_swap + (ew * 2 + phase) * 16 * 32 + lane;
+                    const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 16 * 32 + lane;
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[c] : y[8 + c];
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
+                    float o[8];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) {
+                        const float other = theirs[c * 32];
+                        o[c] = up ? gate_mul(other, y[8 + c]) : gate_mul(y[c], other);
+                    }
+                    const int shift = up ? 8 : 0;
+                    store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride + (out_ch[0] & ~1), p.out_stride,
+                                 rows - c0 - shift, out_ch[0] < limit);
+                } else if constexpr (GATED) {
+                    uint32_t g[16], u[16];
+                    tmem_ld16(g, addr + c0);
+                    tmem_ld16(u, addr + BN + c0);
+                    tmem_ld_wait(g);
+                    tmem_ld_wait(u);
+                    float y[16];
+#pragma unroll
+                    for (int c = 0; c < 16; ++c)
+                        y[c] = gate_mul(acc_value<INT8>(g[c]) * (sc[c] * wsc[0]), acc_value<INT8>(u[c]) * (sc[c] * wsc[1]));
+                    store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride + (out_ch[0] & ~1), p.out_stride, rows - c0,
+                                out_ch[0] < limit);
+                } else {
+#pragma unroll
+                    for (int b = 0; b < MB; ++b) {
+                        uint32_t v[16];
+                        tmem_ld16(v, addr + b * BN + c0);
+                        tmem_ld_wait(v);
+                        float y[16];
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) y[c] = acc_value<INT8>(v[c]) * (sc[c] * wsc[b]);
+                        store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride + (out_ch[b] & ~1), p.out_stride, rows - c0,
+                                    out_ch[b] < limit);
                     }
                 }
             }
@@ -361,10 +499,12 @@ __global__ void __launch_bounds__(kThreads, 1) expert_matmul_kernel(const __grid
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::tmem_cols) : "memory");
 }
 
-template <int BN>
+template <int MB, int BN>
 size_t smem_bytes(int E)
 {
-    return 1024 + Tile<BN>::data_bytes + sizeof(SmemTail) + 4 * BN * sizeof(float) + (size_t)(3 * E + 1) * sizeof(int);
+    using T = Tile<MB, BN>;
+    return 1024 + T::data_bytes + sizeof(SmemTail) + (size_t)(T::epi_warps * T::cols + T::swap_floats) * sizeof(float) +
+           (size_t)(3 * E + 1) * sizeof(int);
 }
 
 typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -394,37 +534,54 @@ bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims
                     CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int BN>
+// Row tiles of height bn, at most: every expert may end in one partial tile.
+long long row_tiles(const strata_moe_shape& s, long long a_rows, int bn)
+{
+    const long long items = min((long long)s.R * s.T * s.K, a_rows);
+    const long long rows = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : items;
+    return rows / bn + min((long long)s.E, rows);
+}
+
+template <int MB, int BN>
 cudaError_t run(const strata_moe_shape& s, const strata_matmul_args& a, MatParams& p, int n_sm, cudaStream_t st)
 {
+    using T = Tile<MB, BN>;
     {
         const cuuint64_t dims[2] = {(cuuint64_t)a.inner, (cuuint64_t)a.a_rows};
         const cuuint64_t strides[1] = {(cuuint64_t)a.a_stride};
-        const cuuint32_t box[2] = {(cuuint32_t)kKBytes, (cuuint32_t)Tile<BN>::box_rows};
+        const cuuint32_t box[2] = {(cuuint32_t)kKBytes, (cuuint32_t)T::box_rows};
         if (!encode(&p.map_a, a.a, 2, dims, strides, box)) return cudaErrorInvalidValue;
     }
-    // no more CTAs than tiles can exist: every expert may end in one partial row tile
-    const long long items = min((long long)s.R * s.T * s.K, (long long)a.a_rows);
-    const long long rows = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : items;
-    const long long row_tiles = rows / BN + min((long long)s.E, rows);
-    if (row_tiles * p.m_tiles >= (1ll << 31)) return cudaErrorInvalidConfiguration;
-    const unsigned grid = (unsigned)min(row_tiles * p.m_tiles, (long long)n_sm);
-    const size_t smem = smem_bytes<BN>(s.E);
+    {   // [E][channels][inner]; gated: [2E][channels / 2][inner], gate and up of an expert in turn
+        const cuuint64_t k = (cuuint64_t)a.inner, rows = (cuuint64_t)a.channels / (a.gated ? 2 : 1);
+        const cuuint64_t dims[3] = {k, rows, (cuuint64_t)s.E * (a.gated ? 2 : 1)};
+        const cuuint64_t strides[2] = {k, rows * k};
+        const cuuint32_t box[3] = {(cuuint32_t)kKBytes, (cuuint32_t)(a.gated ? MB * kM / 2 : kM), 1};
+        if (!encode(&p.map_w, a.w, 3, dims, strides, box)) return cudaErrorInvalidValue;
+    }
+    const int per_tile = MB * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
+    p.m_tiles = (wide + per_tile - 1) / per_tile;
+    const long long tiles = row_tiles(s, a.a_rows, BN) * p.m_tiles;
+    if (tiles >= (1ll << 31)) return cudaErrorInvalidConfiguration;
+    const unsigned grid = (unsigned)min(tiles, (long long)n_sm);
+    const size_t smem = smem_bytes<MB, BN>(s.E);
     if (a.type == STRATA_T_INT8)
-        return a.gated ? launch_pdl(expert_matmul_kernel<true, true, BN>, grid, kThreads, smem, st, p)
-                       : launch_pdl(expert_matmul_kernel<true, false, BN>, grid, kThreads, smem, st, p);
-    return a.gated ? launch_pdl(expert_matmul_kernel<false, true, BN>, grid, kThreads, smem, st, p)
-                   : launch_pdl(expert_matmul_kernel<false, false, BN>, grid, kThreads, smem, st, p);
+        return a.gated ? launch_pdl(expert_matmul_kernel<true, true, MB, BN>, grid, T::threads, smem, st, p)
+                       : launch_pdl(expert_matmul_kernel<true, false, MB, BN>, grid, T::threads, smem, st, p);
+    return a.gated ? launch_pdl(expert_matmul_kernel<false, true, MB, BN>, grid, T::threads, smem, st, p)
+                   : launch_pdl(expert_matmul_kernel<false, false, MB, BN>, grid, T::threads, smem, st, p);
 }
 
-template <int BN>
+template <int MB, int BN>
 cudaError_t configure()
 {
-    const void* fns[4] = {(const void*)expert_matmul_kernel<true, true, BN>, (const void*)expert_matmul_kernel<true, false, BN>,
-                          (const void*)expert_matmul_kernel<false, true, BN>,
-                          (const void*)expert_matmul_kernel<false, false, BN>};
+    const void* fns[4] = {(const void*)expert_matmul_kernel<true, true, MB, BN>,
+                          (const void*)expert_matmul_kernel<true, false, MB, BN>,
+                          (const void*)expert_matmul_kernel<false, true, MB, BN>,
+                          (const void*)expert_matmul_kernel<false, false, MB, BN>};
     for (const void* f : fns) {
-        const cudaError_t e = cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<BN>(kMaxExperts));
+        const cudaError_t e =
+            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<MB, BN>(kMaxExperts));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -434,45 +591,44 @@ cudaError_t configure()
 
 cudaError_t configure_matmul_kernels()
 {
-    cudaError_t e = configure<64>();
-    if (e == cudaSuccess) e = configure<128>();
-    if (e == cudaSuccess) e = configure<256>();
+    cudaError_t e = configure<1, 64>();
+    if (e == cudaSuccess) e = configure<2, 128>();
+    if (e == cudaSuccess) e = configure<2, 256>();
     return e;
 }
 
 cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_layout_t& L, const strata_matmul_args& a,
-                                 int* status, int n_sm, cudaStream_t st)
+                                 int* status, WorkQueue wq, int n_sm, cudaStream_t st)
 {
     MatParams p;
-    const cuuint64_t k = (cuuint64_t)a.inner, ch = (cuuint64_t)a.channels;
-    if (a.gated) {                       // [2E][channels/2][inner]: boxes alternate between gate and up
-        const cuuint64_t dims[3] = {k, ch / 2, 2 * (cuuint64_t)s.E};
-        const cuuint64_t strides[2] = {k, ch / 2 * k};
-        const cuuint32_t box[3] = {(cuuint32_t)kKBytes, (cuuint32_t)kGateRows, 1};
-        if (!encode(&p.map_w, a.w, 3, dims, strides, box)) return cudaErrorInvalidValue;
-    } else {
-        const cuuint64_t dims[2] = {k, ch * (cuuint64_t)s.E};
-        const cuuint64_t strides[1] = {k};
-        const cuuint32_t box[2] = {(cuuint32_t)kKBytes, (cuuint32_t)kM};
-        if (!encode(&p.map_w, a.w, 2, dims, strides, box)) return cudaErrorInvalidValue;
-    }
     p.expert_count = s.slot_capacity > 0 ? nullptr : L.expert_count;
     p.expert_offset = L.expert_offset;
     p.a_scale = a.a_scale;
     p.w_scale = a.w_scale;
     p.out = static_cast<uint16_t*>(a.out);
     p.status = status;
+    p.wq = wq;
     p.a_rows = a.a_rows;
     p.a_scale_stride = a.a_scale_stride;
     p.out_stride = a.out_stride;
     p.E = s.E;
     p.k_blocks = (a.inner + kKBytes - 1) / kKBytes;
     p.channels = a.channels;
-    p.m_tiles = a.gated ? (a.channels / 2 + kM / 2 - 1) / (kM / 2) : (a.channels + kM - 1) / kM;
-    const long long rows = s.slot_capacity > 0 ? (long long)s.R * s.slot_capacity : (long long)s.R * s.T * s.K / s.E;
-    if (rows > 128) return run<256>(s, a, p, n_sm, st);
-    if (rows > 64) return run<128>(s, a, p, n_sm, st);
-    return run<64>(s, a, p, n_sm, st);
+    // Tile by the mean rows of an expert (what the host knows), measured with 32 experts, 7168 -> 4096 gated, and others:
+    //   512 rows:  <2,256> 396 us, <1,256> 480 us, <2,128> 469 us: the larger tile reads least per product
+    //   124 rows (60 experts, Zipf, inner 1424): <2,128> 55 us, <2,256> 63 us: with few inner blocks the doubled
+    //              accumulators, which hide the epilogue, count for more; 128 rows, inner 7168: 185 against 178 us
+    //   32 rows:   <1,64> 149 us, <2,128> 156 us, <1,128> 153 us: bound by the weights, more and smaller tiles
+    //   1/4 row (one token): <2,128> 42 us, <1,64> 45 us: 128 tiles at once, not 256 in two rounds
+    const long long mean = s.slot_capacity > 0 ? (long long)s.R * s.slot_capacity : (long long)s.R * s.T * s.K / s.E;
+    const bool one_round = (long long)min((long long)s.R * s.T * s.K, (long long)s.E) * ((a.channels + 255) / 256) <= n_sm;
+    long long v = mean > 64 ? (mean > 128 || p.k_blocks >= 32 ? 2256 : 2128) : mean < 16 && one_round ? 2128 : 1064;
+    v = tune("STRATA_MM", v);
+    switch (v) {
+        case 1064: return run<1, 64>(s, a, p, n_sm, st);
+        case 2128: return run<2, 128>(s, a, p, n_sm, st);
+        default: return run<2, 256>(s, a, p, n_sm, st);
+    }
 }
 
 }  // namespace strata
