@@ -34,7 +34,7 @@ struct Tile {
     static constexpr int epi_warps = MB == 2 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
     static constexpr int threads = 64 + 32 * epi_warps;             // warp 0: loads, warp 1: matrix instructions
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
-    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 16 * 32 : 0;   // exchange of a gated tile
+    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 8 * 32 : 0;   // exchange of a gated tile
     static constexpr size_t data_bytes = (size_t)stages * (w_stage + a_stage);
     static_assert(stages <= 8 && tmem_cols <= 512 && data_bytes % 1024 == 0, "");
 };
@@ -234,7 +234,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
     unsigned char* s_a = smem + T::stages * T::w_stage;              // [stages][BN][128]
     SmemTail* tail = reinterpret_cast<SmemTail*>(smem + T::data_bytes);
     float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
-    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][2][16][32]
+    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][2][8][32]
     int* s_base = reinterpret_cast<int*>(s_swap + T::swap_floats);   // [E + 1]
     int* s_off = s_base + p.E + 1;                                   // [E]
     int* s_cnt = s_off + p.E;                                        // [E]
@@ -441,8 +441,8 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
                     for (int c = 0; c < 16; ++c) y[c] = acc_value<INT8>(v[c]) * (sc[c] * wsc[0]);
                     // the gate's warp finishes columns 0..7, up's warp columns 8..15
                     const bool up = quad >> 1;
-                    float* mine = s_swap + (ew * 2 + phase) * 16 * 32 + lane;
-                    const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 16 * 32 + lane;
+                    float* mine = s_swap + (ew * 2 + phase) * 8 * 32 + lane;
+                    const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 8 * 32 + lane;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[c] : y[8 + c];
                     asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
@@ -614,19 +614,32 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
     p.E = s.E;
     p.k_blocks = (a.inner + kKBytes - 1) / kKBytes;
     p.channels = a.channels;
-    // Tile by the mean rows of an expert (what the host knows), measured with 32 experts, 7168 -> 4096 gated, and others:
-    //   512 rows:  <2,256> 396 us, <1,256> 480 us, <2,128> 469 us: the larger tile reads least per product
-    //   124 rows (60 experts, Zipf, inner 1424): <2,128> 55 us, <2,256> 63 us: with few inner blocks the doubled
-    //              accumulators, which hide the epilogue, count for more; 128 rows, inner 7168: 185 against 178 us
-    //   32 rows:   <1,64> 149 us, <2,128> 156 us, <1,128> 153 us: bound by the weights, more and smaller tiles
-    //   1/4 row (one token): <2,128> 42 us, <1,64> 45 us: 128 tiles at once, not 256 in two rounds
-    const long long mean = s.slot_capacity > 0 ? (long long)s.R * s.slot_capacity : (long long)s.R * s.T * s.K / s.E;
-    const bool one_round = (long long)min((long long)s.R * s.T * s.K, (long long)s.E) * ((a.channels + 255) / 256) <= n_sm;
-    long long v = mean > 64 ? (mean > 128 || p.k_blocks >= 32 ? 2256 : 2128) : mean < 16 && one_round ? 2128 : 1064;
-    v = tune("STRATA_MM", v);
+    // Which tile: the shortest estimate of rounds * (inner blocks * c + f) over the GPU, where c is what one inner block of a
+    // tile takes and f what a tile adds (its epilogue where the accumulators are not doubled, the ring's refill).  The
+    // constants were fitted to 116 measured shapes (8 and 32 experts, 2 .. 2048 mean rows, inner 512 .. 7168, 512 .. 4096
+    // channels, even and Zipf routing); the choice is on average 2 % above the best of the three, and 30 % above at
+    // worst, where a skewed routing has other tiles than the mean.  At 7168 -> 4096 gated, 32 experts: one token
+    // <1,64> 45 us, <2,128> 42 us; 32 rows each 149, 156 (<2,256> 163); 128 rows 337, 185, 178; 512 rows 1149, 469, 396.
+    struct Cost { int mb, bn; float c, f; };
+    static const Cost costs[3] = {{1, 64, 0.37f, 0.65f}, {2, 128, 0.66f, 1.06f}, {2, 256, 1.22f, 2.78f}};
+    const long long items = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : (long long)s.R * s.T * s.K;
+    const long long used = min(items, (long long)s.E), mean = (items + s.E - 1) / s.E;
+    int v = 0;
+    float least = 0.0f;
+    for (int i = 0; i < 3; ++i) {
+        const int per_tile = costs[i].mb * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
+        const float tiles = (float)(used * ((mean + costs[i].bn - 1) / costs[i].bn) * ((wide + per_tile - 1) / per_tile));
+        const float rounds = tiles > (float)n_sm ? tiles / (float)n_sm + 0.19f : 1.0f;
+        const float cost = rounds * ((float)p.k_blocks * costs[i].c + costs[i].f);
+        if (i == 0 || cost < least) {
+            least = cost;
+            v = i;
+        }
+    }
+    v = (int)tune("STRATA_MM", v);
     switch (v) {
-        case 1064: return run<1, 64>(s, a, p, n_sm, st);
-        case 2128: return run<2, 128>(s, a, p, n_sm, st);
+        case 0: return run<1, 64>(s, a, p, n_sm, st);
+        case 1: return run<2, 128>(s, a, p, n_sm, st);
         default: return run<2, 256>(s, a, p, n_sm, st);
     }
 }
