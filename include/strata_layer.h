@@ -109,7 +109,7 @@ strata_status strata_norm(strata_ctx *ctx, const strata_norm_args *args, void *s
  *   dweight[c] = sum over rows of dy * hat                 (float; the order of the sum is fixed)
  * h: the stored sum (residual_out of the forward pass, or x where there was no residual); dresidual: the gradient
  * that arrives at residual_out, or NULL.  dx may be dy or dresidual.  scratch: device, 16-byte aligned, of
- * strata_norm_grad_scratch_bytes.  rows = 0: dweight is zeroed.  Two launches. */
+ * strata_norm_grad_scratch_bytes.  rows = 0: dweight is zeroed.  Needs a workspace (the status word).  Two launches. */
 typedef struct {
     int64_t rows;
     int32_t cols;

@@ -14,6 +14,8 @@ constexpr int kMaxInner = 131056;        // 2^31 / 128^2, less one: int8 sums ca
 
 WorkQueue matmul_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 8}; }
 
+WorkQueue row_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 10}; }
+
 bool on(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 strata_status check_route(const strata_ctx* ctx, const strata_route_params* r, int type, int64_t stride)
@@ -113,7 +115,7 @@ strata_status strata_norm(strata_ctx* ctx, const strata_norm_args* a, void* stre
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
-    return launched(ctx, launch_norm(*a, ctx->ws, ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+    return launched(ctx, launch_norm(*a, ctx->ws, row_queue(ctx), ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_norm_grad_scratch_bytes(strata_ctx* ctx, int64_t rows, int32_t cols, size_t* bytes)
@@ -139,11 +141,12 @@ strata_status strata_norm_grad(strata_ctx* ctx, const strata_norm_grad_args* a, 
     const size_t need = norm_grad_scratch_bytes(a->rows, a->cols, ctx->n_sm_device);
     if (a->scratch_bytes < need) return STRATA_ERR_CAPACITY;
     if (need > 0 && !a->scratch) return STRATA_ERR_INVALID_ARG;
+    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     int n = 0;
-    const cudaError_t err = launch_norm_grad(*a, ctx->n_sm_device, static_cast<cudaStream_t>(stream), &n);
+    const cudaError_t err = launch_norm_grad(*a, ctx->ws, ctx->n_sm_device, static_cast<cudaStream_t>(stream), &n);
     return launched(ctx, err, (uint64_t)n);
 }
 
@@ -163,7 +166,7 @@ strata_status strata_quantize_rows(strata_ctx* ctx, const void* x, int64_t x_str
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     return launched(ctx, launch_quantize(x, x_stride, rows, cols, q_type, q, q_stride, q_scale, q_scale_stride, n_valid,
-                                         ctx->ws, ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+                                         ctx->ws, row_queue(ctx), ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_t* layout, const strata_matmul_args* a,

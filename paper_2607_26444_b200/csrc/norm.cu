@@ -9,9 +9,59 @@ namespace {
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kVpt = 4;                // 16-byte vectors of a row per thread
-constexpr int kGradCtasPerSm = 4;
+constexpr size_t kRingBytes = 200 * 1024;  // shared memory of an SM that rows in flight may take
 
 enum QKind { kNoCodes = 0, kInt8 = 1, kE4m3 = 2 };
+
+// Two binary32 values in one register pair: sm_100 multiplies and adds them with one instruction, and these kernels are
+// bound by instruction issue before they are bound by memory (the norm to e4m3 with scalar arithmetic and
+// the row widened element by element: 29 instructions per element, 590 us for 65,536 x 7168; 502 us are the bytes).
+using Pair = unsigned long long;
+__device__ __forceinline__ Pair make_pair(float lo, float hi)
+{
+    Pair d;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(lo), "f"(hi));
+    return d;
+}
+__device__ __forceinline__ float2 split(Pair p)
+{
+    float2 d;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(d.x), "=f"(d.y) : "l"(p));
+    return d;
+}
+__device__ __forceinline__ Pair mul2(Pair a, Pair b)
+{
+    Pair d;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+    return d;
+}
+__device__ __forceinline__ Pair fma2(Pair a, Pair b, Pair c)
+{
+    Pair d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(d) : "l"(a), "l"(b), "l"(c));
+    return d;
+}
+__device__ __forceinline__ Pair widen(uint32_t u) { return make_pair(__uint_as_float(u << 16), __uint_as_float(u & 0xffff0000u)); }
+__device__ __forceinline__ void widen8(uint4 v, Pair* p)
+{
+    p[0] = widen(v.x);
+    p[1] = widen(v.y);
+    p[2] = widen(v.z);
+    p[3] = widen(v.w);
+}
+__device__ __forceinline__ uint32_t narrow(Pair p)
+{
+    const float2 f = split(p);
+    return pack_bf16x2(f.x, f.y);
+}
+__device__ __forceinline__ uint4 narrow8(const Pair* p) { return make_uint4(narrow(p[0]), narrow(p[1]), narrow(p[2]), narrow(p[3])); }
+// bf16 sums, rounded once
+__device__ __forceinline__ uint32_t add_bf16x2(uint32_t a, uint32_t b)
+{
+    uint32_t d;
+    asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+    return d;
+}
 
 // coherent load (outputs may alias inputs row by row) that leaves L1 to the weights
 __device__ __forceinline__ uint4 ld_row16(const void* p)
@@ -24,22 +74,33 @@ __device__ __forceinline__ uint4 ld_row16(const void* p)
     return v;
 }
 
-__device__ __forceinline__ void load_weight8(const void* w, bool f32, int col, float* out)
+__device__ __forceinline__ void load_weight8(const void* w, bool f32, int col, Pair* out)
 {
     if (f32) {
-        const float4 a = *reinterpret_cast<const float4*>(static_cast<const float*>(w) + col);
-        const float4 b = *reinterpret_cast<const float4*>(static_cast<const float*>(w) + col + 4);
-        out[0] = a.x; out[1] = a.y; out[2] = a.z; out[3] = a.w;
-        out[4] = b.x; out[5] = b.y; out[6] = b.z; out[7] = b.w;
+        const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(static_cast<const float*>(w) + col);
+        const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(static_cast<const float*>(w) + col + 4);
+        out[0] = a.x;
+        out[1] = a.y;
+        out[2] = b.x;
+        out[3] = b.y;
     } else {
-        unpack_bf16x8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + col), out);
+        widen8(*reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(w) + col), out);
     }
+}
+
+// a load from shared memory that is not merged with an earlier one (to keep the registers free in between)
+__device__ __forceinline__ uint4 lds16(const void* p)
+{
+    uint4 v;
+    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_addr(p)) : "memory");
+    return v;
 }
 
 // Sum of a and maximum (or sum) of b over the threads of one row.  Rows of one warp need no barrier; otherwise the
 // partials of the warps meet in shared memory, in a buffer that alternates from row to row, so one barrier is enough.
+// Returns whether any of them wants to stop.
 template <bool B_IS_MAX>
-__device__ __forceinline__ void row_reduce(float& a, float& b, float2* buf, bool one_warp, int phase)
+__device__ __forceinline__ bool row_reduce(float& a, float& b, float2* buf, bool one_warp, int phase, bool stop = false)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -47,17 +108,18 @@ __device__ __forceinline__ void row_reduce(float& a, float& b, float2* buf, bool
         const float t = __shfl_xor_sync(kFull, b, o);
         b = B_IS_MAX ? fmaxf(b, t) : b + t;
     }
-    if (one_warp) return;
+    if (one_warp) return __any_sync(kFull, stop);
     const int warp = (int)threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
     float2* mine = buf + (phase & 1) * 32;
     if ((threadIdx.x & 31) == 0) mine[warp] = make_float2(a, b);
-    __syncthreads();
+    if (__syncthreads_or(stop)) return true;
     a = mine[0].x;
     b = mine[0].y;
     for (int q = 1; q < warps; ++q) {
         a += mine[q].x;
         b = B_IS_MAX ? fmaxf(b, mine[q].y) : b + mine[q].y;
     }
+    return false;
 }
 
 // 8 codes of y * limit / top (top = max|y| of the row), one correctly rounded binary32 quotient each, so that a
@@ -68,32 +130,29 @@ __device__ __forceinline__ void row_reduce(float& a, float& b, float2* buf, bool
 // with extreme magnitudes are moved into range by a power of two first (row_range), so the remainder stays exact.
 // Three instructions instead of the division's ten: the division made the quantiser bound by instruction issue.
 template <int QK>
-__device__ __forceinline__ uint2 codes8(const float* y, float range, float top, float inv)
+__device__ __forceinline__ uint2 codes8(const Pair* y, Pair factor, Pair neg_top, Pair inv)
 {
-    constexpr float kLimit = QK == kInt8 ? 127.0f : 448.0f;
-    const float f = kLimit * range;
-    float q[8];
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float n = y[i] * f;
-        const float q0 = n * inv;
-        q[i] = fmaf(fmaf(-q0, top, n), inv, q0);
-    }
     uint32_t w[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-        const float* p = q + 4 * h;
+        float2 q[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const Pair n = mul2(y[2 * h + i], factor);
+            const Pair q0 = mul2(n, inv);
+            q[i] = split(fma2(fma2(q0, neg_top, n), inv, q0));
+        }
         if constexpr (QK == kInt8) {
             // adding 1.5 * 2^23 rounds to an integer, ties to even, and leaves it in the low bits
             constexpr float kRound = 12582912.0f;
-            const uint32_t lo = __byte_perm(__float_as_uint(p[0] + kRound), __float_as_uint(p[1] + kRound), 0x0040);
-            const uint32_t hi = __byte_perm(__float_as_uint(p[2] + kRound), __float_as_uint(p[3] + kRound), 0x0040);
+            const uint32_t lo = __byte_perm(__float_as_uint(q[0].x + kRound), __float_as_uint(q[0].y + kRound), 0x0040);
+            const uint32_t hi = __byte_perm(__float_as_uint(q[1].x + kRound), __float_as_uint(q[1].y + kRound), 0x0040);
             w[h] = __byte_perm(lo, hi, 0x5410);
         } else {
             uint16_t lo, hi;
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(p[1]), "f"(p[0]));
-            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(p[3]), "f"(p[2]));
-            w[h] = (uint32_t)lo | ((uint32_t)hi << 16);
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(lo) : "f"(q[0].y), "f"(q[0].x));
+            asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(hi) : "f"(q[1].y), "f"(q[1].x));
+            asm("mov.b32 %0, {%1, %2};" : "=r"(w[h]) : "h"(lo), "h"(hi));
         }
     }
     return make_uint2(w[0], w[1]);
@@ -118,20 +177,33 @@ struct RowParams {
     int vecs;              // 16-byte vectors in a row
     int tpr;               // threads of one row: the whole block, or 32 (several rows per block)
     int stages;            // rows in flight per row group (ring)
+    int chunk;             // rows of one claim
+    WorkQueue wq;
     int weight_f32;
     float eps, inv_cols;
 };
 
+// y = h * weight for eight columns (vector c of the row)
+__device__ __forceinline__ void weigh8(const RowParams& p, int c, Pair* y)
+{
+    Pair w[4];
+    load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], w[i]);
+}
+
 constexpr int kMaxStages = 4, kMaxGroups = 8;
 
-// A wait that runs out marks the block dead: later waits return at once, the block finishes its rows with whatever its
-// buffers hold and the status tells that the results are void.
-__device__ __forceinline__ void ring_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status)
+// False if the wait ran out, here or in another thread of the block: the status tells that the results are void.
+__device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status)
 {
-    for (uint32_t it = 0; it < (uint32_t)(STRATA_WAIT_LIMIT); ++it)
-        if (mbar_try_wait(bar, parity) || *dead) return;
+    for (uint32_t it = 0; it < (uint32_t)(STRATA_WAIT_LIMIT); ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*dead) return false;
+    }
     *dead = 1;
     report_status(status, STRATA_ERR_TIMEOUT);
+    return false;
 }
 
 // Forward pass.  NORM: y = (h * w) * rstd; otherwise y = x (row quantiser).  max|y| follows from max|h * w|, because
@@ -139,15 +211,15 @@ __device__ __forceinline__ void ring_wait(uint64_t* bar, uint32_t parity, volati
 //
 // A row belongs to one block (rows of up to 1024 columns: to one warp of eight), which keeps it packed in registers
 // between the two passes.  RING: bulk copies keep the next rows of the group in flight in shared memory whatever the
-// threads do (a stage is free again after the reduction's barrier); without it, two blocks of 224 threads held too
-// few loads in flight: 837 us for 65,536 x 7168 with residual to e4m3.  Launches with one row per group at most load
+// threads do (a stage is free again after the reduction's barrier).  Launches with one row per group at most load
 // directly: there is nothing to run ahead of.
 template <bool NORM, bool RES, int QK, bool RING, int MAXT>
-__global__ void __launch_bounds__(MAXT) row_kernel(const RowParams p)
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) row_kernel(const RowParams p)
 {
     extern __shared__ __align__(128) unsigned char ring[];            // [groups][stages][1 or 2 rows]
     __shared__ float2 s_part[64];
     __shared__ uint64_t s_full[kMaxGroups][kMaxStages];
+    __shared__ long long s_row[kMaxGroups][kMaxStages];               // the row in a stage, -1: no more
     __shared__ int s_dead;
     const bool one_warp = p.tpr == 32;
     const int sub = one_warp ? (int)threadIdx.x >> 5 : 0;            // row group inside the block
@@ -168,79 +240,112 @@ __global__ void __launch_bounds__(MAXT) row_kernel(const RowParams p)
     long long rows = p.rows;
     if (p.n_valid) rows = min(rows, (long long)max(0, *p.n_valid));
     const long long first = (long long)blockIdx.x * groups + sub, step = (long long)gridDim.x * groups;
-    auto fetch = [&](long long row, int stage) {
+    // Ring: the first thread of a group claims rows in order, a few at a time, `stages` ahead of the group.  The next claim is
+    // in flight while the rows of the last one are fetched, so nothing waits for the counter.
+    const unsigned units = (unsigned)((rows + p.chunk - 1) / p.chunk), claimers = (unsigned)step;
+    unsigned unit = (unsigned)first < units ? (unsigned)first : kNoUnit, drawn = 0;
+    long long ahead = 0, ahead_end = 0;
+    int issued = 0;
+    auto begin_unit = [&] {
+        ahead = (long long)unit * p.chunk;
+        ahead_end = min(rows, ahead + p.chunk);
+        if (claimers < units) drawn = atomicAdd(p.wq.next, 1u);
+    };
+    if (RING && tid == 0 && unit != kNoUnit) begin_unit();
+    auto fetch = [&](int stage) {
+        if (unit != kNoUnit && ahead == ahead_end) {
+            unit = claimers < units ? claimed_unit(p.wq, units, claimers, drawn) : kNoUnit;
+            if (unit != kNoUnit) begin_unit();
+        }
         uint64_t* bar = &s_full[sub][stage];
+        if (unit == kNoUnit) {
+            s_row[sub][stage] = -1;
+            asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
+            return;
+        }
+        const long long row = ahead++;
         unsigned char* dst = my_ring + (size_t)stage * stage_bytes;
+        s_row[sub][stage] = row;
         mbar_expect_tx(bar, stage_bytes);
         bulk_g2s_plain(dst, p.x + row * p.x_stride, row_bytes, bar);
         if constexpr (RES) bulk_g2s_plain(dst + row_bytes, p.res + row * p.res_stride, row_bytes, bar);
+        ++issued;
     };
     if (RING && tid == 0)
-        for (int s = 0; s < p.stages; ++s)
-            if (first + s * step < rows) fetch(first + s * step, s);
+        for (int s = 0; s < p.stages; ++s) fetch(s);
     int phase = 0, stage = 0;
     uint32_t parity = 0;
-    for (long long row = first; row < rows; row += step, ++phase) {
+    for (long long row = first; RING || row < rows; row += step, ++phase) {
         const unsigned char* src = my_ring + (size_t)stage * stage_bytes;
+        bool stop = false;
+        if constexpr (RING) {
+            row = -1;
+            if (ring_wait(&s_full[sub][stage], parity, &s_dead, p.status))
+                row = *reinterpret_cast<volatile long long*>(&s_row[sub][stage]);
+            stop = row < 0;
+        }
+        const int vecs = RING && stop ? 0 : p.vecs;
         uint4 h[kVpt];                                               // the row, as stored
         if constexpr (RING) {
-            ring_wait(&s_full[sub][stage], parity, &s_dead, p.status);
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
                 const int c = tid + j * p.tpr;
-                if (c < p.vecs) h[j] = *reinterpret_cast<const uint4*>(src + (size_t)c * 16);
+                if (c < vecs) h[j] = *reinterpret_cast<const uint4*>(src + (size_t)c * 16);
             }
         } else {
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
                 const int c = tid + j * p.tpr;
-                if (c < p.vecs) h[j] = ld_row16(p.x + row * p.x_stride + (size_t)c * 8);
+                if (c < vecs) h[j] = ld_row16(p.x + row * p.x_stride + (size_t)c * 8);
             }
         }
-        uint4 r[kVpt];
         if constexpr (RES) {
+            uint4 r[kVpt];
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
                 const int c = tid + j * p.tpr;
-                if (c < p.vecs)
+                if (c < vecs)
                     r[j] = RING ? *reinterpret_cast<const uint4*>(src + row_bytes + (size_t)c * 16)
                                 : ld_row16(p.res + row * p.res_stride + (size_t)c * 8);
             }
-        }
-        float sum = 0.0f, top = 0.0f;
 #pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
-            const int c = tid + j * p.tpr;
-            if (c < p.vecs) {
-                float f[8];
-                unpack_bf16x8(h[j], f);
-                if constexpr (RES) {
-                    float t[8];
-                    unpack_bf16x8(r[j], t);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] += t[i];
-                    h[j] = pack_bf16x8(f);
+            for (int j = 0; j < kVpt; ++j) {
+                const int c = tid + j * p.tpr;
+                if (c < vecs) {                                    // what is stored is what is normed
+                    h[j] = make_uint4(add_bf16x2(h[j].x, r[j].x), add_bf16x2(h[j].y, r[j].y), add_bf16x2(h[j].z, r[j].z),
+                                      add_bf16x2(h[j].w, r[j].w));
                     *reinterpret_cast<uint4*>(p.res_out + row * p.res_out_stride + (size_t)c * 8) = h[j];
-                    unpack_bf16x8(h[j], f);                          // what is stored is what is normed
-                }
-                if constexpr (NORM) {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) sum = fmaf(f[i], f[i], sum);
-                    if constexpr (QK != kNoCodes) {
-                        float w[8];
-                        load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i] * w[i]));
-                    }
-                } else {
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(f[i]));
                 }
             }
         }
-        row_reduce<true>(sum, top, s_part, one_warp, phase);
+        Pair squares = 0;
+        float top = 0.0f;
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) {
+            const int c = tid + j * p.tpr;
+            if (c < vecs) {
+                Pair y[4];
+                widen8(h[j], y);
+                if constexpr (NORM) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) squares = fma2(y[i], y[i], squares);
+                    if constexpr (QK != kNoCodes) weigh8(p, c, y);
+                }
+                if constexpr (QK != kNoCodes) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const float2 f = split(y[i]);
+                        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                    }
+                }
+            }
+        }
+        const float2 sq = split(squares);
+        float sum = sq.x + sq.y;
+        const bool ends = row_reduce<true>(sum, top, s_part, one_warp, phase, stop);
         if constexpr (RING) {
-            if (tid == 0 && row + p.stages * step < rows) fetch(row + p.stages * step, stage);
+            if (ends) break;
+            if (tid == 0) fetch(stage);
             if (++stage == p.stages) {
                 stage = 0;
                 parity ^= 1;
@@ -249,25 +354,23 @@ __global__ void __launch_bounds__(MAXT) row_kernel(const RowParams p)
         float rstd = 1.0f;
         if constexpr (NORM) rstd = __frcp_rn(__fsqrt_rn(fmaf(sum, p.inv_cols, p.eps)));
         const float range = row_range(top), in_range = top == 0.0f ? 1.0f : top * range, inv = __frcp_rn(in_range);
+        const float factor = (QK == kInt8 ? 127.0f : 448.0f) * range;
+        const Pair factor2 = make_pair(factor, factor), neg_top2 = make_pair(-in_range, -in_range), inv2 = make_pair(inv, inv);
+        const Pair rstd2 = make_pair(rstd, rstd);
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) {
-                float f[8];
-                unpack_bf16x8(h[j], f);
-                if constexpr (NORM) {
-                    float w[8];
-                    load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) f[i] *= w[i];
-                }
+                Pair y[4];
+                widen8(h[j], y);
+                if constexpr (NORM) weigh8(p, c, y);
                 if constexpr (QK != kNoCodes)
-                    *reinterpret_cast<uint2*>(p.q + row * p.q_stride + (size_t)c * 8) = codes8<QK>(f, range, in_range, inv);
+                    *reinterpret_cast<uint2*>(p.q + row * p.q_stride + (size_t)c * 8) = codes8<QK>(y, factor2, neg_top2, inv2);
                 if constexpr (NORM) {
                     if (QK == kNoCodes || p.out) {
 #pragma unroll
-                        for (int i = 0; i < 8; ++i) f[i] *= rstd;
-                        *reinterpret_cast<uint4*>(p.out + row * p.out_stride + (size_t)c * 8) = pack_bf16x8(f);
+                        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], rstd2);
+                        *reinterpret_cast<uint4*>(p.out + row * p.out_stride + (size_t)c * 8) = narrow8(y);
                     }
                 }
             }
@@ -278,11 +381,8 @@ __global__ void __launch_bounds__(MAXT) row_kernel(const RowParams p)
     griddep_launch_dependents();
     if constexpr (RING) {                                            // a block that gave up lets its copies land first
         if (tid == 0 && s_dead)
-            for (int s = 0; s < p.stages; ++s) {
-                const long long last = rows > first ? (rows - 1 - first) / step : -1;       // uses of the ring: 0 .. last
-                const long long use = last - ((last - s) % p.stages + p.stages) % p.stages;
-                if (use >= 0) mbar_wait_bounded(&s_full[sub][s], (uint32_t)(use / p.stages) & 1u);
-            }
+            for (int u = max(0, issued - p.stages); u < issued; ++u)
+                mbar_wait_bounded(&s_full[sub][u % p.stages], (uint32_t)(u / p.stages) & 1u);
     }
 }
 
@@ -293,96 +393,162 @@ struct GradParams {
     const uint16_t* dres;
     uint16_t* dx;
     float* part;           // [gridDim.x * rows per block, 8 * vecs]
+    int* status;
     long long dy_stride, h_stride, dres_stride, dx_stride;
     long long rows;
-    int vecs, tpr, weight_f32;
+    int vecs, tpr, stages, weight_f32;
     float eps, inv_cols;
 };
 
 // Backward pass.  A thread keeps the same columns for every row it meets, so its share of dweight stays in
-// registers; each row-owner writes one partial row, and a second kernel adds the partial rows in a fixed order.
-template <bool RES, int MAXT>
-__global__ void __launch_bounds__(MAXT) norm_grad_kernel(const GradParams p)
+// registers; each row group writes one partial row, and a second kernel adds the partial rows in a fixed order.
+// (Rows are dealt in equal shares: with claims the order of the sum would change from call to call.)
+// RING: as in the forward pass, but a stage is read in both passes; it is refilled after the next row's reduction, whose
+// barrier every thread reaches only when it is done with the stage.
+template <bool RES, bool RING, bool WF32, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(const GradParams p)
 {
+    extern __shared__ __align__(128) unsigned char ring[];            // [groups][stages][2 or 3 rows]: h, dy, dresidual
     __shared__ float2 s_part[64];
+    __shared__ uint64_t s_full[kMaxGroups][kMaxStages];
+    __shared__ int s_dead;
     const bool one_warp = p.tpr == 32;
     const int sub = one_warp ? (int)threadIdx.x >> 5 : 0;
     const int tid = one_warp ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const int rows_per_block = one_warp ? (int)blockDim.x >> 5 : 1;
+    const int groups = one_warp ? (int)blockDim.x >> 5 : 1;
+    const uint32_t row_bytes = (uint32_t)p.vecs * 16u, stage_bytes = (RES ? 3u : 2u) * row_bytes;
+    unsigned char* my_ring = ring + (size_t)sub * p.stages * stage_bytes;
+    if constexpr (RING) {
+        if (threadIdx.x == 0) {
+            s_dead = 0;
+            for (int g = 0; g < groups; ++g)
+                for (int s = 0; s < p.stages; ++s) mbar_init(&s_full[g][s], 1);
+            mbar_fence_init();
+        }
+        __syncthreads();
+    }
     griddep_wait();
-    float dw[kVpt][8];
+    Pair dw[kVpt][4];
 #pragma unroll
     for (int j = 0; j < kVpt; ++j)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) dw[j][i] = 0.0f;
-    const long long owner = (long long)blockIdx.x * rows_per_block + sub, owners = (long long)gridDim.x * rows_per_block;
-    int phase = 0;
-    for (long long row = owner; row < p.rows; row += owners, ++phase) {
-        uint4 hv[kVpt], dv[kVpt], rv[kVpt];
+        for (int i = 0; i < 4; ++i) dw[j][i] = 0;
+    uint4 wv[kVpt];                                                  // bf16 weights stay in registers, as they come
+    if constexpr (!WF32) {
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
             const int c = tid + j * p.tpr;
-            if (c < p.vecs) {
-                hv[j] = ld_row16(p.h + row * p.h_stride + (size_t)c * 8);
-                dv[j] = ld_row16(p.dy + row * p.dy_stride + (size_t)c * 8);
-            }
+            if (c < p.vecs) wv[j] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.weight) + c * 8);
         }
-        if constexpr (RES) {
+    }
+    const long long owner = (long long)blockIdx.x * groups + sub, owners = (long long)gridDim.x * groups;
+    int fetched = 0;
+    auto fetch = [&] {
+        const long long row = owner + fetched * owners;
+        if (row >= p.rows) return;
+        const int stage = fetched % p.stages;
+        uint64_t* bar = &s_full[sub][stage];
+        unsigned char* dst = my_ring + (size_t)stage * stage_bytes;
+        mbar_expect_tx(bar, stage_bytes);
+        bulk_g2s_plain(dst, p.h + row * p.h_stride, row_bytes, bar);
+        bulk_g2s_plain(dst + row_bytes, p.dy + row * p.dy_stride, row_bytes, bar);
+        if constexpr (RES) bulk_g2s_plain(dst + 2 * row_bytes, p.dres + row * p.dres_stride, row_bytes, bar);
+        ++fetched;
+    };
+    if (RING && tid == 0)
+        for (int s = 0; s < p.stages; ++s) fetch();
+    int phase = 0, stage = 0;
+    uint32_t parity = 0;
+    for (long long row = owner; row < p.rows; row += owners, ++phase) {
+        const unsigned char* src = my_ring + (size_t)stage * stage_bytes;
+        uint4 hv[kVpt], dv[kVpt], rv[kVpt];                          // without a ring; with one they are read where they lie
+        if constexpr (RING) {
+            ring_wait(&s_full[sub][stage], parity, &s_dead, p.status);
+        } else {
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
                 const int c = tid + j * p.tpr;
-                if (c < p.vecs) rv[j] = ld_row16(p.dres + row * p.dres_stride + (size_t)c * 8);
+                if (c < p.vecs) {
+                    hv[j] = ld_row16(p.h + row * p.h_stride + (size_t)c * 8);
+                    dv[j] = ld_row16(p.dy + row * p.dy_stride + (size_t)c * 8);
+                    if constexpr (RES) rv[j] = ld_row16(p.dres + row * p.dres_stride + (size_t)c * 8);
+                }
             }
         }
-        float sum = 0.0f, dot = 0.0f;
+        Pair squares = 0, dots = 0;
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) {
-                float h[8], d[8], w[8];
-                unpack_bf16x8(hv[j], h);
-                unpack_bf16x8(dv[j], d);
-                load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
+                if constexpr (RING) {
+                    hv[j] = *reinterpret_cast<const uint4*>(src + (size_t)c * 16);
+                    dv[j] = *reinterpret_cast<const uint4*>(src + row_bytes + (size_t)c * 16);
+                }
+                Pair h[4], d[4], w[4];
+                widen8(hv[j], h);
+                widen8(dv[j], d);
+                if constexpr (WF32) load_weight8(p.weight, true, c * 8, w);
+                else widen8(wv[j], w);
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    sum = fmaf(h[i], h[i], sum);
-                    dot = fmaf(d[i] * w[i], h[i], dot);
+                for (int i = 0; i < 4; ++i) {
+                    squares = fma2(h[i], h[i], squares);
+                    dots = fma2(mul2(d[i], w[i]), h[i], dots);
                 }
             }
         }
+        const float2 sq = split(squares), dt = split(dots);
+        float sum = sq.x + sq.y, dot = dt.x + dt.y;
         row_reduce<false>(sum, dot, s_part, one_warp, phase);
-        const float rstd = __frcp_rn(__fsqrt_rn(fmaf(sum, p.inv_cols, p.eps)));
+        if (RING && tid == 0 && phase > 0) fetch();                  // into the stage of the row before this one
+        const float rstd = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
         const float mean = dot * rstd * p.inv_cols;                  // mean(g * hat)
+        const Pair rstd2 = make_pair(rstd, rstd), neg_mean2 = make_pair(-mean, -mean);
 #pragma unroll
         for (int j = 0; j < kVpt; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) {
-                float h[8], d[8], w[8], o[8];
-                unpack_bf16x8(hv[j], h);
-                unpack_bf16x8(dv[j], d);
-                load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
-                if constexpr (RES) unpack_bf16x8(rv[j], o);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float hat = h[i] * rstd;
-                    dw[j][i] = fmaf(d[i], hat, dw[j][i]);
-                    const float t = fmaf(-hat, mean, d[i] * w[i]);
-                    o[i] = RES ? fmaf(rstd, t, o[i]) : rstd * t;
+                if constexpr (RING) {
+                    hv[j] = lds16(src + (size_t)c * 16);
+                    dv[j] = lds16(src + row_bytes + (size_t)c * 16);
+                    if constexpr (RES) rv[j] = *reinterpret_cast<const uint4*>(src + 2 * row_bytes + (size_t)c * 16);
                 }
-                *reinterpret_cast<uint4*>(p.dx + row * p.dx_stride + (size_t)c * 8) = pack_bf16x8(o);
+                Pair h[4], d[4], w[4], o[4];
+                widen8(hv[j], h);
+                widen8(dv[j], d);
+                if constexpr (WF32) load_weight8(p.weight, true, c * 8, w);
+                else widen8(wv[j], w);
+                if constexpr (RES) widen8(rv[j], o);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const Pair hat = mul2(h[i], rstd2);
+                    dw[j][i] = fma2(d[i], hat, dw[j][i]);
+                    const Pair t = fma2(hat, neg_mean2, mul2(d[i], w[i]));
+                    o[i] = RES ? fma2(rstd2, t, o[i]) : mul2(rstd2, t);
+                }
+                *reinterpret_cast<uint4*>(p.dx + row * p.dx_stride + (size_t)c * 8) = narrow8(o);
             }
         }
+        if constexpr (RING)
+            if (++stage == p.stages) {
+                stage = 0;
+                parity ^= 1;
+            }
     }
 #pragma unroll
     for (int j = 0; j < kVpt; ++j) {
         const int c = tid + j * p.tpr;
         if (c < p.vecs) {
-            float4* o = reinterpret_cast<float4*>(p.part + (size_t)owner * p.vecs * 8 + (size_t)c * 8);
-            o[0] = make_float4(dw[j][0], dw[j][1], dw[j][2], dw[j][3]);
-            o[1] = make_float4(dw[j][4], dw[j][5], dw[j][6], dw[j][7]);
+            ulonglong2* o = reinterpret_cast<ulonglong2*>(p.part + (size_t)owner * p.vecs * 8 + (size_t)c * 8);
+            o[0] = make_ulonglong2(dw[j][0], dw[j][1]);
+            o[1] = make_ulonglong2(dw[j][2], dw[j][3]);
         }
     }
     griddep_launch_dependents();
+    if constexpr (RING) {
+        if (tid == 0 && s_dead)
+            for (int u = max(0, fetched - p.stages); u < fetched; ++u)
+                mbar_wait_bounded(&s_full[sub][u % p.stages], (uint32_t)(u / p.stages) & 1u);
+    }
 }
 
 // dweight[c] = sum of the partial rows: 8 columns x 32 row lanes per block, each lane adding every 32nd partial row,
@@ -427,23 +593,28 @@ cudaError_t run_rows(RowParams& p, const RowGeom& g, int n_sm, cudaStream_t st)
     const long long blocks = (p.rows + g.groups - 1) / g.groups;
     const size_t row = (size_t)p.vecs * (RES ? 32 : 16) * (size_t)g.groups;       // bytes a block reads per round
     // blocks per SM: up to 1,024 threads, with two rows per group in flight in 200 KB of shared memory
-    constexpr size_t kRing = 200 * 1024;
-    const int per_sm = (int)max(1ll, min((long long)(1024 / g.threads), (long long)(kRing / (2 * row))));
+    const int per_sm = (int)max(1ll, min((long long)(1024 / g.threads), (long long)(kRingBytes / (2 * row))));
     if (blocks <= (long long)n_sm * per_sm) {
         return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, false, 256>, (unsigned)blocks, g.threads, 0, st, p)
                                 : launch_pdl(row_kernel<NORM, RES, QK, false, 1024>, (unsigned)blocks, g.threads, 0, st, p);
     }
-    p.stages = (int)max(1ll, min((long long)kMaxStages, (long long)(kRing / (per_sm * row))));
+    p.stages = (int)max(1ll, min((long long)kMaxStages, (long long)(kRingBytes / (per_sm * row))));
+    // claims on one counter complete at about one per 3.5 ns: few enough of them to stay below the bytes' time
+    // (64 KB: 65,536 x 7168 with residual 523 us, 553 us with equal shares; 8 KB claims took 214 us, not 136, at 2048 columns)
+    p.chunk = (int)max((size_t)1, (size_t)65536 / ((size_t)p.vecs * (RES ? 32 : 16)));
     const size_t smem = row * p.stages;
-    const unsigned grid = (unsigned)(n_sm * per_sm);
+    const unsigned grid = (unsigned)min(blocks, (long long)n_sm * per_sm);
     return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, true, 256>, grid, g.threads, smem, st, p)
                             : launch_pdl(row_kernel<NORM, RES, QK, true, 1024>, grid, g.threads, smem, st, p);
 }
 
-long long grad_owners(long long rows, const RowGeom& g, int n_sm)
+// Row groups of the backward pass: up to four blocks per SM, as long as two rounds of rows (three operands) of each fit
+// the ring; more groups mean more partial rows, fewer mean less in flight.
+long long grad_owners(long long rows, const RowGeom& g, int cols, int n_sm)
 {
-    const long long blocks = min((rows + g.groups - 1) / g.groups, (long long)n_sm * kGradCtasPerSm);
-    return blocks * g.groups;
+    const long long round = (long long)cols * 6 * g.groups;
+    const long long per_sm = max(1ll, min(4ll, (long long)kRingBytes / (2 * round)));
+    return min((rows + g.groups - 1) / g.groups, (long long)n_sm * per_sm) * g.groups;
 }
 
 }  // namespace
@@ -454,16 +625,43 @@ template <bool NORM, bool RES, int QK>
 cudaError_t configure_rows()
 {
     cudaError_t e = cudaFuncSetAttribute(row_kernel<NORM, RES, QK, true, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         200 * 1024);
+                                         (int)kRingBytes);
     if (e == cudaSuccess)
         e = cudaFuncSetAttribute(row_kernel<NORM, RES, QK, true, 1024>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 200 * 1024);
+                                 (int)kRingBytes);
     return e;
+}
+template <bool RES>
+cudaError_t configure_grad()
+{
+    const void* f[6] = {(const void*)norm_grad_kernel<RES, true, true, 128>,  (const void*)norm_grad_kernel<RES, true, true, 512>,
+                        (const void*)norm_grad_kernel<RES, true, true, 1024>, (const void*)norm_grad_kernel<RES, true, false, 128>,
+                        (const void*)norm_grad_kernel<RES, true, false, 512>, (const void*)norm_grad_kernel<RES, true, false, 1024>};
+    cudaError_t e = cudaSuccess;
+    for (int i = 0; i < 6 && e == cudaSuccess; ++i)
+        e = cudaFuncSetAttribute(f[i], cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kRingBytes);
+    return e;
+}
+
+template <bool RES, bool RING, bool WF32>
+cudaError_t run_grad_w(const GradParams& p, const RowGeom& g, unsigned grid, size_t smem, cudaStream_t st)
+{
+    if (g.threads <= 128) return launch_pdl(norm_grad_kernel<RES, RING, WF32, 128>, grid, g.threads, smem, st, p);
+    if (g.threads <= 512) return launch_pdl(norm_grad_kernel<RES, RING, WF32, 512>, grid, g.threads, smem, st, p);
+    return launch_pdl(norm_grad_kernel<RES, RING, WF32, 1024>, grid, g.threads, smem, st, p);
+}
+template <bool RES, bool RING>
+cudaError_t run_grad(const GradParams& p, const RowGeom& g, unsigned grid, size_t smem, cudaStream_t st)
+{
+    return p.weight_f32 ? run_grad_w<RES, RING, true>(p, g, grid, smem, st) : run_grad_w<RES, RING, false>(p, g, grid, smem, st);
 }
 }  // namespace
 cudaError_t configure_norm_kernels()
 {
-    cudaError_t e = configure_rows<true, true, kNoCodes>();
+    cudaError_t e = cudaSuccess;
+    e = configure_grad<true>();
+    if (e == cudaSuccess) e = configure_grad<false>();
+    if (e == cudaSuccess) e = configure_rows<true, true, kNoCodes>();
     if (e == cudaSuccess) e = configure_rows<true, true, kInt8>();
     if (e == cudaSuccess) e = configure_rows<true, true, kE4m3>();
     if (e == cudaSuccess) e = configure_rows<true, false, kNoCodes>();
@@ -474,7 +672,7 @@ cudaError_t configure_norm_kernels()
     return e;
 }
 
-cudaError_t launch_norm(const strata_norm_args& a, int* status, int n_sm, cudaStream_t st)
+cudaError_t launch_norm(const strata_norm_args& a, int* status, WorkQueue wq, int n_sm, cudaStream_t st)
 {
     const RowGeom g = row_geom(a.cols);
     RowParams p{};
@@ -492,6 +690,7 @@ cudaError_t launch_norm(const strata_norm_args& a, int* status, int n_sm, cudaSt
     p.q_stride = a.q_stride;
     p.q_scale_stride = a.q_scale_stride;
     p.status = status;
+    p.wq = wq;
     p.rows = a.rows;
     p.vecs = a.cols / 8;
     p.tpr = g.tpr;
@@ -510,7 +709,7 @@ cudaError_t launch_norm(const strata_norm_args& a, int* status, int n_sm, cudaSt
 
 cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, int cols, int q_type, void* q,
                             long long q_stride, float* q_scale, long long q_scale_stride, const int32_t* n_valid,
-                            int* status, int n_sm, cudaStream_t st)
+                            int* status, WorkQueue wq, int n_sm, cudaStream_t st)
 {
     const RowGeom g = row_geom(cols);
     RowParams p{};
@@ -519,6 +718,7 @@ cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, i
     p.q_scale = q_scale;
     p.n_valid = n_valid;
     p.status = status;
+    p.wq = wq;
     p.x_stride = x_stride;
     p.q_stride = q_stride;
     p.q_scale_stride = q_scale_stride;
@@ -531,13 +731,13 @@ cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, i
 
 size_t norm_grad_scratch_bytes(long long rows, int cols, int n_sm)
 {
-    return (size_t)grad_owners(rows, row_geom(cols), n_sm) * (size_t)cols * sizeof(float);
+    return (size_t)grad_owners(rows, row_geom(cols), cols, n_sm) * (size_t)cols * sizeof(float);
 }
 
-cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int n_sm, cudaStream_t st, int* n_launches)
+cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_sm, cudaStream_t st, int* n_launches)
 {
     const RowGeom g = row_geom(a.cols);
-    const long long owners = grad_owners(a.rows, g, n_sm);
+    const long long owners = grad_owners(a.rows, g, a.cols, n_sm);
     GradParams p{};
     p.dy = static_cast<const uint16_t*>(a.dy);
     p.h = static_cast<const uint16_t*>(a.h);
@@ -559,11 +759,14 @@ cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int n_sm, cudaStrea
     cudaError_t err = cudaSuccess;
     if (owners > 0) {
         const unsigned grid = (unsigned)(owners / g.groups);
-#define STRATA_GRAD(MAXT)                                                                                              \
-    (a.dresidual ? launch_pdl(norm_grad_kernel<true, MAXT>, grid, g.threads, 0, st, p)                                 \
-                 : launch_pdl(norm_grad_kernel<false, MAXT>, grid, g.threads, 0, st, p))
-        err = g.threads <= 256 ? STRATA_GRAD(256) : g.threads <= 512 ? STRATA_GRAD(512) : STRATA_GRAD(1024);
-#undef STRATA_GRAD
+        p.status = status;
+        const size_t round = (size_t)p.vecs * 16 * (a.dresidual ? 3 : 2) * (size_t)g.groups;     // bytes of a block's rows
+        const int per_sm = (int)((grid + n_sm - 1) / n_sm);
+        p.stages = (int)min((long long)kMaxStages, (long long)(kRingBytes / (per_sm * round)));
+        const bool use_ring = p.stages >= 2 && a.rows > owners;
+        const size_t smem = use_ring ? round * p.stages : 0;
+        err = a.dresidual ? (use_ring ? run_grad<true, true>(p, g, grid, smem, st) : run_grad<true, false>(p, g, grid, smem, st))
+                          : (use_ring ? run_grad<false, true>(p, g, grid, smem, st) : run_grad<false, false>(p, g, grid, smem, st));
         *n_launches = 1;
         if (err != cudaSuccess) return err;
     }

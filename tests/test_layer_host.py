@@ -149,6 +149,7 @@ def test_operators_need_a_workspace():
     h = make_ctx(workspace=False)
     assert B.strata_norm(h, B.strata_norm_args(**NORM), None) == WS
     assert B.strata_quantize_rows(h, P, 104, 7, 104, B.STRATA_T_E4M3, P, 104, P, 1, None, None) == WS
+    assert B.strata_norm_grad(h, B.strata_norm_grad_args(**GRAD), None) == WS
     lay = B.strata_moe_layout_t(P, P, P, P, None, P, None)
     assert B.strata_moe_expert_matmul(h, lay, B.strata_matmul_args(**MATMUL), None) == WS
     B.strata_ctx_destroy(h)
