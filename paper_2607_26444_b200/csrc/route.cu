@@ -43,6 +43,9 @@ __device__ __forceinline__ float sigmoid_f(float l) { return __frcp_rn(__fadd_rn
 // exp(l - m) for l <= m; infinities at the maximum count as equal to it
 __device__ __forceinline__ float softmax_term(float l, float m) { return l == m ? 1.0f : expf(l - m); }
 
+// the same through the hardware's power of two: 2^-22 relative and the rounding of its argument, for gradients
+__device__ __forceinline__ float softmax_fast(float l, float m) { return l == m ? 1.0f : __expf(l - m); }
+
 __device__ __forceinline__ float warp_sum(float v)
 {
 #pragma unroll
@@ -93,7 +96,6 @@ __device__ __forceinline__ void load_logits(float (&l)[VPL], const void* base, l
 }
 
 struct __align__(16) RouteSmem {          // of one warp
-    unsigned long long key[32];
     uint32_t one[32], two[32];
     float l[32];
     int id[32];
@@ -474,25 +476,27 @@ __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) ro
             __syncwarp();
             int id = -1, rank = p.K;
             float lk = 0.0f, s = 0.0f;
-            unsigned long long key = 0;
+            uint32_t key = 0;
             if (lane < total) {
                 id = sm.id[lane];
                 lk = load_as_float<BF16>(p.logits, (long long)tok * p.stride + id);
                 float ck = lk;
                 if constexpr (SIGMOID) s = sigmoid_f(lk);
                 if constexpr (BY_SCORE) ck = __fadd_rn(s, p.bias ? p.bias[id] : 0.0f);
-                key = ((unsigned long long)key_of(ck) << 32) | (uint32_t)~id;
+                key = key_of(ck);
             }
-            sm.key[lane] = key;
+            sm.one[lane] = key;
             __syncwarp();
             if (lane < total) {
                 rank = 0;
                 for (int j = 0; j < total; j += 4) {              // slots beyond the candidates hold the lowest key
-                    const ulonglong2 a = *reinterpret_cast<const ulonglong2*>(&sm.key[j]);
-                    const ulonglong2 b = *reinterpret_cast<const ulonglong2*>(&sm.key[j + 2]);
-                    rank += (a.x > key ? 1 : 0) + (a.y > key ? 1 : 0) + (b.x > key ? 1 : 0) + (b.y > key ? 1 : 0);
+                    const uint4 o = *reinterpret_cast<const uint4*>(&sm.one[j]);
+                    rank += (o.x > key ? 1 : 0) + (o.y > key ? 1 : 0) + (o.z > key ? 1 : 0) + (o.w > key ? 1 : 0);
                 }
             }
+            // equal keys share a rank; candidates lie in index order, so those in front go first
+            if (__popc(__reduce_or_sync(kFull, lane < total ? 1u << rank : 0u)) != total)
+                for (int j = 0; j < total; ++j) rank += lane < total && j < lane && sm.one[j] == key ? 1 : 0;
             const bool sel = rank < p.K;
             if constexpr (!SIGMOID) s = sel ? softmax_term(lk, m) : 0.0f;
             float over = p.scale;
@@ -565,7 +569,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
     const bool live = lk > -INFINITY;
     if (!live) dw = 0.0f;
 
-    float l[VPL], m = 0.0f, sum = 1.0f, mean = 0.0f, d;
+    float l[VPL], m = 0.0f, inv = 0.0f, mean = 0.0f, d;
     if constexpr (kFullRow) {
         load_logits<VPL, BF16>(l, p.logits, base, e0, p.E, p.vec_ok != 0);
         m = l[0];
@@ -575,12 +579,13 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            l[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
+            l[i] = l[i] == -INFINITY ? 0.0f : softmax_fast(l[i], m);
             s += l[i];
         }
-        sum = warp_sum(s);
+        s = warp_sum(s);
+        inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
         d = p.scale * dw;
-        mean = warp_sum(live ? d * __fdiv_rn(softmax_term(lk, m), sum) : 0.0f);
+        mean = warp_sum(live ? d * softmax_fast(lk, m) * inv : 0.0f);
     } else if constexpr (MODE == kGradSigmoid) {
         const float s = live ? sigmoid_f(lk) : 0.0f;
         const float slope = live ? s * sigmoid_f(-lk) : 0.0f;     // s * (1 - s) without the cancellation
@@ -601,21 +606,29 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
         d = live ? p.scale * t * (dw - dot) : 0.0f;
     }
     if (!live) d = 0.0f;
-    float add = 0.0f;
-    for (int k = 0; k < p.K; ++k) {
-        const int ik = __shfl_sync(kFull, id, k);
-        const float dk = __shfl_sync(kFull, d, k);
-        if (ik == id) add += dk;
+    __syncwarp();
+    float* slot = row + (id % VPL) * 32 + id / VPL;               // register i of lane q, without bank conflicts
+    if (id >= 0) *slot = __int_as_float(lane);
+    __syncwarp();
+    // an expert that stands twice in a token: its slots add up, in slot order
+    if (__any_sync(kFull, id >= 0 && __float_as_int(*slot) != lane)) {
+        float add = 0.0f;
+        for (int k = 0; k < p.K; ++k) {
+            const int ik = __shfl_sync(kFull, id, k);
+            const float dk = __shfl_sync(kFull, d, k);
+            if (ik == id) add += dk;
+        }
+        d = add;
     }
     __syncwarp();
-    if (id >= 0) row[(id % VPL) * 32 + id / VPL] = add;           // register i of lane q, without bank conflicts
+    if (id >= 0) *slot = d;
     __syncwarp();
 
     float g[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
         g[i] = row[i * 32 + lane];
-        if constexpr (kFullRow) g[i] = sum > 0.0f ? __fdiv_rn(l[i], sum) * (g[i] - mean) : 0.0f;
+        if constexpr (kFullRow) g[i] = l[i] * inv * (g[i] - mean);
     }
     store_row<VPL, BF16>(g, p.dlogits, (long long)tok * p.dstride, e0, p.E, p.dvec_ok != 0);
 }
