@@ -102,7 +102,7 @@ struct __align__(16) RouteSmem {          // of one warp
 };
 
 // The whole choice of one token in exact arithmetic.  route_kernel below sends here what its shorter way does not decide:
-// masked or NaN logits, softmax scores compared as such, near-ties of groups, and more than 32 candidates.  Scores become ordered integer keys; the K-th largest of the 32 lane maxima bounds the K-th largest
+// masked or NaN logits, softmax scores compared as such, near-ties of groups, and more than CAP candidates.  Scores become ordered integer keys; the K-th largest of the 32 lane maxima bounds the K-th largest
 // key from below; the keys that reach it are compacted in index order and ranked; if more than 32 do, K
 // rounds of a warp-wide maximum take the winners one by one.  1,138 instructions per token at 256 experts in 4 of
 // 8 groups.
@@ -354,9 +354,10 @@ struct TopTwo<1> {
 //  3. the K-th largest lane maximum, less twice the error, is a bound that every expert of the true choice reaches;
 //  4. the experts that reach it (about K + 2) are compacted; each lane evaluates one of them exactly, and its rank
 //     is the number of candidates with a larger choice value, or an equal one and a lower index.
-// A warp keeps its biases in registers from token to token and fetches the next token's logits ahead.
+// A warp keeps its biases in registers from token to token and fetches the next token's logits ahead.  Step 4 takes CAP
+// lanes: with CAP = 16 (at most eight slots) the candidates of two tokens are evaluated together.
 constexpr int route_blocks_per_sm(int vpl) { return vpl <= 8 ? 4 : vpl == 16 ? 2 : 1; }
-template <int VPL, bool BF16, bool SIGMOID, bool BY_SCORE>
+template <int VPL, bool BF16, bool SIGMOID, bool BY_SCORE, int CAP>
 __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) route_kernel(const RouteParams p)
 {
     extern __shared__ uint32_t dyn_keys[];                        // [warps][E], only for groups that split a lane's run
@@ -390,135 +391,156 @@ __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) ro
 
     float l[VPL];
     load_logits<VPL, BF16, true>(l, p.logits, (long long)tok * p.stride, e0, end, p.fast_vec != 0);
-    while (true) {
-        const int next = tok + step;
-        float c[VPL], least = l[0];
-#pragma unroll
-        for (int i = 1; i < VPL; ++i) least = min_nan(least, l[i]);
-        bool exact = __any_sync(kFull, !(least > -INFINITY));
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) c[i] = BY_SCORE ? sigmoid_approx(l[i]) + bias[i] : l[i];
-        if (!BY_SCORE && padded) {
-#pragma unroll
-            for (int i = 0; i < VPL; ++i)
-                if (i >= left) c[i] = -INFINITY;
-        }
-        float m = 0.0f, sum = 1.0f;
-        if constexpr (!SIGMOID) {                                 // logits are compared (BY_SCORE softmax is never fast)
-            m = c[0];
-#pragma unroll
-            for (int i = 1; i < VPL; ++i) m = fmaxf(m, c[i]);
-            m = warp_redux_max(m);
-            if (!p.renormalise) {
-                float s = 0.0f;
-#pragma unroll
-                for (int i = 0; i < VPL; ++i) s += softmax_term(c[i], m);
-                sum = warp_sum(s);
+    constexpr int kBatch = 32 / CAP;                              // tokens whose candidates share the warp
+    const int sub = lane & (CAP - 1), mine_b = lane / CAP;        // place among the candidates of token mine_b of the batch
+    for (; tok < p.n_tok; tok += kBatch * step) {
+        int total = 0;                                            // of token mine_b: candidates, and its softmax statistics
+        float m_sel = 0.0f, sum_sel = 1.0f;
+        unsigned redo = 0;                                        // tokens of the batch that the exact path decides
+        __syncwarp();                                             // the last batch's candidates have been read
+#pragma unroll 1
+        for (int b = 0; b < kBatch; ++b) {
+            const int t = tok + b * step;
+            if (t >= p.n_tok) {
+                if (mine_b == b) total = -1;
+                break;
             }
-        }
-        // the next token's logits travel while this one is decided
-        if (next < p.n_tok) load_logits<VPL, BF16, true>(l, p.logits, (long long)next * p.stride, e0, end, p.fast_vec != 0);
+            float c[VPL], least = l[0];
+#pragma unroll
+            for (int i = 1; i < VPL; ++i) least = min_nan(least, l[i]);
+            bool exact = __any_sync(kFull, !(least > -INFINITY));
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) c[i] = BY_SCORE ? sigmoid_approx(l[i]) + bias[i] : l[i];
+            if (!BY_SCORE && padded) {
+#pragma unroll
+                for (int i = 0; i < VPL; ++i)
+                    if (i >= left) c[i] = -INFINITY;
+            }
+            float m = 0.0f, sum = 1.0f;
+            if constexpr (!SIGMOID) {                                 // logits are compared (BY_SCORE softmax is never fast)
+                m = c[0];
+#pragma unroll
+                for (int i = 1; i < VPL; ++i) m = fmaxf(m, c[i]);
+                m = warp_redux_max(m);
+                if (!p.renormalise) {
+                    float s = 0.0f;
+#pragma unroll
+                    for (int i = 0; i < VPL; ++i) s += softmax_term(c[i], m);
+                    sum = warp_sum(s);
+                }
+            }
+            // the next token's logits travel while this one is decided
+            if (t + step < p.n_tok) load_logits<VPL, BF16, true>(l, p.logits, (long long)(t + step) * p.stride, e0, end, p.fast_vec != 0);
 
-        float2 two = TopTwo<VPL>::of(c);
-        float lane_max = two.x;
-        bool kept = true;
-        if (p.n_group > 1) {
-            for (int o = 1; o < lpg; o <<= 1) {
-                const float bx = __shfl_xor_sync(kFull, two.x, o), by = __shfl_xor_sync(kFull, two.y, o);
-                two = make_float2(fmaxf(two.x, bx), fmaxf(fminf(two.x, bx), fmaxf(two.y, by)));
-            }
-            float g = p.top2 && two.y > -INFINITY ? two.x + two.y : two.x;
-            float last = 0.0f;
-            kept = false;
-#pragma unroll 4
-            for (int r = 0; r < p.topk_group; ++r) {
-                last = warp_redux_max(g);
-                if (g == last) {
-                    kept = g > -INFINITY;
-                    g = -INFINITY;
+            float2 two = TopTwo<VPL>::of(c);
+            float lane_max = two.x;
+            bool kept = true;
+            if (p.n_group > 1) {
+                for (int o = 1; o < lpg; o <<= 1) {
+                    const float bx = __shfl_xor_sync(kFull, two.x, o), by = __shfl_xor_sync(kFull, two.y, o);
+                    two = make_float2(fmaxf(two.x, bx), fmaxf(fminf(two.x, bx), fmaxf(two.y, by)));
                 }
-            }
-            const float first_out = warp_redux_max(g);
-            const int n_kept = __popc(__ballot_sync(kFull, kept));
-            // no more groups than asked for may be kept; fewer only if no other has a member left
-            exact |= n_kept > p.topk_group * lpg || first_out >= last - 8.0f * err ||
-                     (n_kept < p.topk_group * lpg && first_out > -INFINITY);
-            lane_max = kept ? lane_max : -INFINITY;
-        }
-        float bound = -INFINITY;
+                float g = p.top2 && two.y > -INFINITY ? two.x + two.y : two.x;
+                float last = 0.0f;
+                kept = false;
 #pragma unroll 4
-        for (int r = 0; r < p.K; ++r) {
-            bound = warp_redux_max(lane_max);
-            if (lane_max == bound) lane_max = -INFINITY;
-        }
-        if constexpr (BY_SCORE) bound -= 4.0f * err;
-        bound = bound >= -3.402823466e38f ? bound : -3.402823466e38f;     // -inf (and the NaN of its margin): all finite ones
-        if (!kept) bound = INFINITY;
-        uint32_t flags = 0;
-#pragma unroll
-        for (int i = 0; i < VPL; ++i) flags |= c[i] >= bound ? 1u << i : 0u;
-        int at = __popc(flags);
-        const int mine = at;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-            const int v = __shfl_up_sync(kFull, at, o);
-            if (lane >= o) at += v;
-        }
-        const int total = __shfl_sync(kFull, at, 31);
-        at -= mine;
-        __syncwarp();                                             // the last token's candidates have been read
-        if (total <= 32)
-            for (; flags; flags &= flags - 1) sm.id[at++] = e0 + __ffs(flags) - 1;
-        exact |= total > 32;
-        if (exact) {
-            route_exact<VPL, BF16, SIGMOID, BY_SCORE>(p, tok, sm, dyn_keys + (size_t)warp * p.E);
-        } else {
-            __syncwarp();
-            int id = -1, rank = p.K;
-            float lk = 0.0f, s = 0.0f;
-            uint32_t key = 0;
-            if (lane < total) {
-                id = sm.id[lane];
-                lk = load_as_float<BF16>(p.logits, (long long)tok * p.stride + id);
-                float ck = lk;
-                if constexpr (SIGMOID) s = sigmoid_f(lk);
-                if constexpr (BY_SCORE) ck = __fadd_rn(s, p.bias ? p.bias[id] : 0.0f);
-                key = key_of(ck);
-            }
-            sm.one[lane] = key;
-            __syncwarp();
-            if (lane < total) {
-                rank = 0;
-                for (int j = 0; j < total; j += 4) {              // slots beyond the candidates hold the lowest key
-                    const uint4 o = *reinterpret_cast<const uint4*>(&sm.one[j]);
-                    rank += (o.x > key ? 1 : 0) + (o.y > key ? 1 : 0) + (o.z > key ? 1 : 0) + (o.w > key ? 1 : 0);
+                for (int r = 0; r < p.topk_group; ++r) {
+                    last = warp_redux_max(g);
+                    if (g == last) {
+                        kept = g > -INFINITY;
+                        g = -INFINITY;
+                    }
                 }
+                const float first_out = warp_redux_max(g);
+                const int n_kept = __popc(__ballot_sync(kFull, kept));
+                // no more groups than asked for may be kept; fewer only if no other has a member left
+                exact |= n_kept > p.topk_group * lpg || first_out >= last - 8.0f * err ||
+                         (n_kept < p.topk_group * lpg && first_out > -INFINITY);
+                lane_max = kept ? lane_max : -INFINITY;
             }
-            // equal keys share a rank; candidates lie in index order, so those in front go first
-            if (__popc(__reduce_or_sync(kFull, lane < total ? 1u << rank : 0u)) != total)
-                for (int j = 0; j < total; ++j) rank += lane < total && j < lane && sm.one[j] == key ? 1 : 0;
-            const bool sel = rank < p.K;
-            if constexpr (!SIGMOID) s = sel ? softmax_term(lk, m) : 0.0f;
-            float over = p.scale;
-            if (p.renormalise) {
-                const float d = warp_sum(sel ? s : 0.0f);
-                over = d > 0.0f ? p.scale * __frcp_rn(d) : 0.0f;
-            } else if (!SIGMOID) {
-                over = p.scale * __frcp_rn(sum);
+            float bound = -INFINITY;
+#pragma unroll 4
+            for (int r = 0; r < p.K; ++r) {
+                bound = warp_redux_max(lane_max);
+                if (lane_max == bound) lane_max = -INFINITY;
             }
-            int32_t* ids = p.ids + (long long)tok * p.K;
-            float* w = p.w + (long long)tok * p.K;
-            if (sel) {
-                ids[rank] = id;
-                w[rank] = s * over;
+            if constexpr (BY_SCORE) bound -= 4.0f * err;
+            bound = bound >= -3.402823466e38f ? bound : -3.402823466e38f;     // -inf (and the NaN of its margin): all finite ones
+            if (!kept) bound = INFINITY;
+            uint32_t flags = 0;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) flags |= c[i] >= bound ? 1u << i : 0u;
+            int at = __popc(flags);
+            const int mine = at;
+#pragma unroll
+            for (int o = 1; o < 32; o <<= 1) {
+                const int v = __shfl_up_sync(kFull, at, o);
+                if (lane >= o) at += v;
             }
-            if (lane >= total && lane < p.K) {
-                ids[lane] = -1;
-                w[lane] = 0.0f;
+            const int found = __shfl_sync(kFull, at, 31);
+            at -= mine;
+            exact |= found > CAP;
+            if (found <= CAP)
+                for (at += b * CAP; flags; flags &= flags - 1) sm.id[at++] = e0 + __ffs(flags) - 1;
+            if (exact) redo |= 1u << b;
+            if (mine_b == b) {
+                total = exact ? -1 : found;
+                m_sel = m;
+                sum_sel = sum;
             }
         }
-        if (next >= p.n_tok) break;
-        tok = next;
+        __syncwarp();
+        const int my_tok = tok + mine_b * step;
+        int id = -1, rank = p.K;
+        float lk = 0.0f, s = 0.0f;
+        uint32_t key = 0;
+        if (sub < total) {
+            id = sm.id[lane];
+            lk = load_as_float<BF16>(p.logits, (long long)my_tok * p.stride + id);
+            float ck = lk;
+            if constexpr (SIGMOID) s = sigmoid_f(lk);
+            if constexpr (BY_SCORE) ck = __fadd_rn(s, p.bias ? p.bias[id] : 0.0f);
+            key = key_of(ck);
+        }
+        sm.one[lane] = key;
+        __syncwarp();
+        const uint32_t* keys = sm.one + mine_b * CAP;
+        if (sub < total) {
+            rank = 0;
+            for (int j = 0; j < total; j += 4) {                  // slots beyond the candidates hold the lowest key
+                const uint4 o = *reinterpret_cast<const uint4*>(keys + j);
+                rank += (o.x > key ? 1 : 0) + (o.y > key ? 1 : 0) + (o.z > key ? 1 : 0) + (o.w > key ? 1 : 0);
+            }
+        }
+        // equal keys share a rank; candidates lie in index order, so those in front go first
+        const uint32_t here = __ballot_sync(kFull, sub < total);
+        if (__reduce_or_sync(kFull, sub < total ? 1u << (rank + mine_b * CAP) : 0u) != here && sub < total)
+            for (int j = 0; j < sub; ++j) rank += keys[j] == key ? 1 : 0;
+        const bool sel = rank < p.K;
+        if constexpr (!SIGMOID) s = sel ? softmax_term(lk, m_sel) : 0.0f;
+        float over = p.scale;
+        if (p.renormalise) {
+            float d = sel ? s : 0.0f;
+#pragma unroll
+            for (int o = CAP / 2; o > 0; o >>= 1) d += __shfl_xor_sync(kFull, d, o);
+            over = d > 0.0f ? p.scale * __frcp_rn(d) : 0.0f;
+        } else if (!SIGMOID) {
+            over = p.scale * __frcp_rn(sum_sel);
+        }
+        const long long at0 = (long long)my_tok * p.K;
+        if (sel) {
+            p.ids[at0 + rank] = id;
+            p.w[at0 + rank] = s * over;
+        }
+        if (total >= 0 && sub >= total && sub < p.K) {
+            p.ids[at0 + sub] = -1;
+            p.w[at0 + sub] = 0.0f;
+        }
+        if (redo) {
+            for (int b = 0; b < kBatch; ++b)
+                if ((redo >> b) & 1u)
+                    route_exact<VPL, BF16, SIGMOID, BY_SCORE>(p, tok + b * step, sm, dyn_keys + (size_t)warp * p.E);
+        }
     }
     griddep_launch_dependents();
 }
@@ -652,11 +674,15 @@ cudaError_t route_vpl(RouteParams& p, const strata_route_params& r, int n_sm, cu
     p.fast_vec = p.vec_ok && p.run % kVec == 0 && p.group_size % kVec == 0;
     const unsigned grid = (unsigned)min((p.n_tok + kRouteWarps - 1) / kRouteWarps, n_sm * route_blocks_per_sm(VPL));
     const size_t smem = p.n_group > 1 && p.group_size % VPL != 0 ? (size_t)kRouteWarps * p.E * sizeof(uint32_t) : 0;
-    if (r.score == STRATA_SCORE_SIGMOID)
-        return by_score ? launch_pdl(route_kernel<VPL, BF16, true, true>, grid, kRouteWarps * 32, smem, st, p)
-                        : launch_pdl(route_kernel<VPL, BF16, true, false>, grid, kRouteWarps * 32, smem, st, p);
-    return by_score ? launch_pdl(route_kernel<VPL, BF16, false, true>, grid, kRouteWarps * 32, smem, st, p)
-                    : launch_pdl(route_kernel<VPL, BF16, false, false>, grid, kRouteWarps * 32, smem, st, p);
+    // two tokens per batch where their candidates (about K + 2) fit 16 lanes, and where a warp has two tokens at all
+    const bool pairs = VPL <= 8 && p.K <= 8 && p.n_tok > (int)grid * kRouteWarps;
+    constexpr int kPairCap = VPL <= 8 ? 16 : 32;
+#define STRATA_ROUTE(SIG, BY)                                                                                            \
+    (pairs ? launch_pdl(route_kernel<VPL, BF16, SIG, BY, kPairCap>, grid, kRouteWarps * 32, smem, st, p)                 \
+           : launch_pdl(route_kernel<VPL, BF16, SIG, BY, 32>, grid, kRouteWarps * 32, smem, st, p))
+    if (r.score == STRATA_SCORE_SIGMOID) return by_score ? STRATA_ROUTE(true, true) : STRATA_ROUTE(true, false);
+    return by_score ? STRATA_ROUTE(false, true) : STRATA_ROUTE(false, false);
+#undef STRATA_ROUTE
 }
 
 template <int VPL, bool BF16>

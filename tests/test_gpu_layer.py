@@ -72,6 +72,11 @@ ROUTES = [
     dict(n=12, E=1000, K=32, score="sigmoid", bias=False, G=1, kg=1, gs="max", renorm=True, scale=1.0, dt=torch.float32),
     dict(n=14, E=31, K=3, score="sigmoid", bias=True, G=1, kg=1, gs="max", renorm=True, scale=1.0, dt=torch.bfloat16),
     dict(n=21, E=64, K=7, score="softmax", bias=True, G=32, kg=9, gs="top2", renorm=False, scale=1.0, dt=torch.float32),
+    # more tokens than resident warps: a warp decides several, and up to eight slots two at a time
+    dict(n=9777, E=256, K=8, score="sigmoid", bias=True, G=8, kg=4, gs="top2", renorm=True, scale=2.5, dt=torch.float32),
+    dict(n=14211, E=64, K=6, score="softmax", bias=False, G=1, kg=1, gs="max", renorm=False, scale=1.0, dt=torch.bfloat16),
+    dict(n=5001, E=60, K=5, score="softmax", bias=False, G=6, kg=2, gs="max", renorm=True, scale=1.0, dt=torch.float32),
+    dict(n=5003, E=384, K=10, score="sigmoid", bias=True, G=8, kg=4, gs="max", renorm=False, scale=1.0, dt=torch.float32),
 ]
 
 
@@ -175,6 +180,34 @@ def test_route_masked_logits(score, bias, groups):
         assert 7 not in got[got >= 0]
 
 
+def test_route_many_tokens_with_ties_and_masks():
+    """Tokens that the shorter way decides and tokens that the exact one must (ties, masks, NaN) side by side in one warp."""
+    n, E, K = 9500, 128, 8
+    g = gen(51)
+    logits = (randn(g, n, E) * 4).round() / 4                    # few distinct values: ties everywhere
+    logits[::7] = randn(g, logits[::7].shape[0], E)
+    logits[3::11, ::2] = -float("inf")
+    logits[5::13] = 0.0
+    logits[6::17, 40] = float("nan")
+    ctx = B.MoEContext(1, n, 8, E, K)
+    for score, groups in (("softmax", (1, 1, "max")), ("sigmoid", (4, 2, "top2"))):
+        bias = None if score == "softmax" else torch.zeros(E, device=DEV)
+        ids = torch.empty((n, K), dtype=torch.int32, device=DEV)
+        w = torch.empty((n, K), device=DEV)
+        ctx.route(B.make_route(score, True, 1.0, *groups), logits, ids, w, bias=bias)
+        l64 = f64(logits)
+        # equal logits have equal binary32 scores: the order of the 64-bit scores, rounded, is the order to expect
+        choice = ref.route_choice(l64, score, None if bias is None else f64(bias), *groups)
+        if score == "softmax":
+            assert np.array_equal(ids.cpu().numpy(), ref.route_ids(choice, K))
+        else:
+            got, want = ids.cpu().numpy(), ref.route_ids(choice, K)
+            rows = [i for i in range(n) if i % 7 != 0]             # quarter steps: groups' sums are apart or equal
+            assert (got[rows] != want[rows]).mean() < 1e-3
+        ww = ref.route_weights(l64, ids.cpu().numpy(), score, True, 1.0)
+        np.testing.assert_allclose(f64(w), ww, rtol=2 * U * (E / 32 + 5 + K + 8 + 40), atol=1e-37)
+
+
 def test_route_ids_feed_the_layout():
     """Unrouted slots (-1) of the router are what the layout skips."""
     ctx = B.MoEContext(2, 8, 8, 16, 4, allow_unrouted=True)
@@ -261,6 +294,8 @@ def test_route_grad_skips_what_it_must():
 
 SHAPES = [(1, 8), (1, 7168), (3, 1000), (5, 1024), (7, 1032), (130, 4096), (300, 2048), (2, 8200), (33, 16384), (3, 32768),
           (4000, 64), (2500, 1544)]
+# more rows than the grid holds at once: rows claimed and fetched ahead, of one warp, of a block, of the longest kinds
+RING_SHAPES = [(9001, 64), (6003, 1024), (7000, 1544), (1501, 7168), (701, 16384), (401, 32768)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
@@ -299,6 +334,12 @@ def test_norm_against_64_bits(rows, cols, residual, out):
         assert bool((buf[:, cols + 4:] == 0x55).all())         # only the codes and the scale of a row are written
 
 
+@pytest.mark.parametrize("rows,cols", RING_SHAPES)
+@pytest.mark.parametrize("residual,out", [(False, "bf16"), (True, "both"), (True, "int8")])
+def test_norm_of_many_rows_against_64_bits(rows, cols, residual, out):
+    test_norm_against_64_bits(rows, cols, residual, out)
+
+
 def ieee_codes(x, kind):
     """The quantiser's definition: scale = max / limit, codes of the correctly rounded binary32 quotient x * limit / max."""
     x = x.astype(np.float32)
@@ -311,7 +352,7 @@ def ieee_codes(x, kind):
     return torch.from_numpy(np.clip(units, -448, 448)).to(torch.float8_e4m3fn).view(torch.uint8).numpy(), scale
 
 
-@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("rows,cols", SHAPES + RING_SHAPES)
 @pytest.mark.parametrize("kind", ["int8", "e4m3"])
 def test_quantize_rows_bit_exact(rows, cols, kind):
     g = gen(rows + cols)
@@ -372,7 +413,7 @@ def test_norm_in_place_zero_rows_and_streams():
     assert np.all(np.abs(f64(big) - want) <= half_ulp(want) + 2.0 ** -18 * np.abs(want))
 
 
-@pytest.mark.parametrize("rows,cols", SHAPES)
+@pytest.mark.parametrize("rows,cols", SHAPES + RING_SHAPES)
 @pytest.mark.parametrize("residual", [False, True])
 def test_norm_grad_against_64_bits(rows, cols, residual):
     g = gen(rows * 3 + cols)
