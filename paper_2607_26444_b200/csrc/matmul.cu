@@ -9,9 +9,19 @@
 
 #include "layer.cuh"
 
+#ifdef STRATA_TEST_HOOKS
+#include <atomic>
+#endif
+
 namespace strata {
 
 namespace {
+
+#ifdef STRATA_TEST_HOOKS
+// Test builds only: CTA 0 of the next launch expects 16 bytes more than its first loads deliver, so that its bounded wait runs
+// out and the error path runs without any fault, trap or unbounded spin.
+std::atomic<int> g_inject_short_load{0};
+#endif
 
 constexpr int kM = 128;                 // channels of a matrix instruction
 constexpr int kKBytes = 128;            // inner extent of a stage: one swizzle span
@@ -50,6 +60,9 @@ struct MatParams {
     WorkQueue wq;
     long long a_rows, a_scale_stride, out_stride;
     int E, k_blocks, channels, m_tiles; // channels: rows of w per expert
+#ifdef STRATA_TEST_HOOKS
+    int test_flags;
+#endif
 };
 
 constexpr int kClaims = 4;              // tiles that the loading warp may be ahead of the epilogue
@@ -318,7 +331,11 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
                         ok = false;
                         break;
                     }
-                    mbar_expect_tx(&tail->full[s], bytes);
+                    uint32_t expect = bytes;
+#ifdef STRATA_TEST_HOOKS
+                    if (p.test_flags && blockIdx.x == 0 && it == 0) expect += 16;
+#endif
+                    mbar_expect_tx(&tail->full[s], expect);
                     unsigned char* dw = s_w + s * T::w_stage;
                     if constexpr (GATED) {                           // [2E][channels / 2][inner]: gate, up
                         constexpr int kRows = MB * kM / 2;
@@ -608,6 +625,9 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
     p.out = static_cast<uint16_t*>(a.out);
     p.status = status;
     p.wq = wq;
+#ifdef STRATA_TEST_HOOKS
+    p.test_flags = g_inject_short_load.exchange(0);
+#endif
     p.a_rows = a.a_rows;
     p.a_scale_stride = a.a_scale_stride;
     p.out_stride = a.out_stride;
@@ -645,3 +665,7 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
 }
 
 }  // namespace strata
+
+#ifdef STRATA_TEST_HOOKS
+extern "C" void strata_test_inject_short_load(int on) { strata::g_inject_short_load.store(on); }
+#endif

@@ -3,9 +3,21 @@
 // once, its statistics are formed across the threads that hold it, and its results are written once.
 #include "layer.cuh"
 
+#ifdef STRATA_TEST_HOOKS
+#include <atomic>
+#endif
+
 namespace strata {
 
 namespace {
+
+#ifdef STRATA_TEST_HOOKS
+// Test builds only: block 0 of the next launch with a ring expects 16 bytes more than its first row delivers (see matmul.cu).
+std::atomic<int> g_inject_short_row{0};
+#define STRATA_TEST_EXTRA(first) (p.test_flags && blockIdx.x == 0 && (first) ? 16u : 0u)
+#else
+#define STRATA_TEST_EXTRA(first) 0u
+#endif
 
 constexpr unsigned kFull = 0xffffffffu;
 constexpr int kVpt = 4;                // 16-byte vectors of a row per thread
@@ -181,6 +193,9 @@ struct RowParams {
     WorkQueue wq;
     int weight_f32;
     float eps, inv_cols;
+#ifdef STRATA_TEST_HOOKS
+    int test_flags;
+#endif
 };
 
 // y = h * weight for eight columns (vector c of the row)
@@ -266,7 +281,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) row_kernel(const Ro
         const long long row = ahead++;
         unsigned char* dst = my_ring + (size_t)stage * stage_bytes;
         s_row[sub][stage] = row;
-        mbar_expect_tx(bar, stage_bytes);
+        mbar_expect_tx(bar, stage_bytes + STRATA_TEST_EXTRA(issued == 0));
         bulk_g2s_plain(dst, p.x + row * p.x_stride, row_bytes, bar);
         if constexpr (RES) bulk_g2s_plain(dst + row_bytes, p.res + row * p.res_stride, row_bytes, bar);
         ++issued;
@@ -398,6 +413,9 @@ struct GradParams {
     long long rows;
     int vecs, tpr, stages, weight_f32;
     float eps, inv_cols;
+#ifdef STRATA_TEST_HOOKS
+    int test_flags;
+#endif
 };
 
 // Backward pass.  A thread keeps the same columns for every row it meets, so its share of dweight stays in
@@ -449,7 +467,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
         const int stage = fetched % p.stages;
         uint64_t* bar = &s_full[sub][stage];
         unsigned char* dst = my_ring + (size_t)stage * stage_bytes;
-        mbar_expect_tx(bar, stage_bytes);
+        mbar_expect_tx(bar, stage_bytes + STRATA_TEST_EXTRA(fetched == 0));
         bulk_g2s_plain(dst, p.h + row * p.h_stride, row_bytes, bar);
         bulk_g2s_plain(dst + row_bytes, p.dy + row * p.dy_stride, row_bytes, bar);
         if constexpr (RES) bulk_g2s_plain(dst + 2 * row_bytes, p.dres + row * p.dres_stride, row_bytes, bar);
@@ -457,6 +475,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
     };
     if (RING && tid == 0)
         for (int s = 0; s < p.stages; ++s) fetch();
+    volatile int* dead = &s_dead;                                    // a block that gave up fetches nothing more
     int phase = 0, stage = 0;
     uint32_t parity = 0;
     for (long long row = owner; row < p.rows; row += owners, ++phase) {
@@ -499,7 +518,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
         const float2 sq = split(squares), dt = split(dots);
         float sum = sq.x + sq.y, dot = dt.x + dt.y;
         row_reduce<false>(sum, dot, s_part, one_warp, phase);
-        if (RING && tid == 0 && phase > 0) fetch();                  // into the stage of the row before this one
+        if (RING && tid == 0 && phase > 0 && !*dead) fetch();        // into the stage of the row before this one
         const float rstd = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
         const float mean = dot * rstd * p.inv_cols;                  // mean(g * hat)
         const Pair rstd2 = make_pair(rstd, rstd), neg_mean2 = make_pair(-mean, -mean);
@@ -599,6 +618,9 @@ cudaError_t run_rows(RowParams& p, const RowGeom& g, int n_sm, cudaStream_t st)
                                 : launch_pdl(row_kernel<NORM, RES, QK, false, 1024>, (unsigned)blocks, g.threads, 0, st, p);
     }
     p.stages = (int)max(1ll, min((long long)kMaxStages, (long long)(kRingBytes / (per_sm * row))));
+#ifdef STRATA_TEST_HOOKS
+    p.test_flags = g_inject_short_row.exchange(0);
+#endif
     // claims on one counter complete at about one per 3.5 ns: few enough of them to stay below the bytes' time
     // (64 KB: 65,536 x 7168 with residual 523 us, 553 us with equal shares; 8 KB claims took 214 us, not 136, at 2048 columns)
     p.chunk = (int)max((size_t)1, (size_t)65536 / ((size_t)p.vecs * (RES ? 32 : 16)));
@@ -765,6 +787,9 @@ cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_
         p.stages = (int)min((long long)kMaxStages, (long long)(kRingBytes / (per_sm * round)));
         const bool use_ring = p.stages >= 2 && a.rows > owners;
         const size_t smem = use_ring ? round * p.stages : 0;
+#ifdef STRATA_TEST_HOOKS
+        p.test_flags = use_ring ? g_inject_short_row.exchange(0) : 0;
+#endif
         err = a.dresidual ? (use_ring ? run_grad<true, true>(p, g, grid, smem, st) : run_grad<true, false>(p, g, grid, smem, st))
                           : (use_ring ? run_grad<false, true>(p, g, grid, smem, st) : run_grad<false, false>(p, g, grid, smem, st));
         *n_launches = 1;
@@ -776,3 +801,7 @@ cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_
 }
 
 }  // namespace strata
+
+#ifdef STRATA_TEST_HOOKS
+extern "C" void strata_test_inject_short_row(int on) { strata::g_inject_short_row.store(on); }
+#endif
