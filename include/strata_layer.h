@@ -86,7 +86,7 @@ strata_status strata_moe_route_grad(strata_ctx *ctx, const strata_route_params *
  * q_scale_stride].  cols: a multiple of 8, at most 32768.  rows may be 0 (nothing is launched, row
  * tensors may be NULL).  One of out and q is
  * required.  residual and residual_out come together.  eps >= 0.  Outputs may alias no input, except residual_out
- * = residual or x, and out = x.  Needs a workspace (the status word).  One launch. */
+ * = residual or x, and out = x.  One launch. */
 typedef struct {
     int64_t rows;
     int32_t cols;
@@ -132,7 +132,7 @@ strata_status strata_norm_grad(strata_ctx *ctx, const strata_norm_grad_args *arg
 /* ---- rows to 8 bits -----------------------------------------------------------------------------------------
  * q = codes of x * limit / max|x|, q_scale[row] = max|x| / limit, as in strata_norm.  n_valid: device int32, or NULL;
  * if given, only rows below *n_valid are read and written (expert_offset + E of a layout: the rows in use of a
- * receive buffer).  Alignments, strides and limits as in strata_norm.  Needs a workspace (the status word).  One launch. */
+ * receive buffer).  Alignments, strides and limits as in strata_norm.  One launch. */
 strata_status strata_quantize_rows(strata_ctx *ctx, const void *x, int64_t x_stride, int64_t rows, int32_t cols,
                                    int32_t q_type, void *q, int64_t q_stride, float *q_scale, int64_t q_scale_stride,
                                    const int32_t *n_valid, void *stream);
@@ -145,8 +145,9 @@ strata_status strata_quantize_rows(strata_ctx *ctx, const void *x, int64_t x_str
  *   out[r, n] = bf16(silu(y[r, n]) * y[r, channels/2 + n])                n < channels/2, if gated
  * a: 8-bit rows [a_rows, inner], 16-byte aligned, stride in bytes a multiple of 16, a_rows >= strata_moe_recv_rows;
  * a_scale of row r at a_scale[r * a_scale_stride]; w: [E, channels, inner] contiguous, 16-byte aligned; w_scale: float
- * [E, channels]; out: bf16, 4-byte aligned, out_stride even.  inner: a multiple of 16, at most 131056 (int32 sums cannot
- * overflow); channels: even, a multiple of 4 if gated.  Rows outside the segments (padding, unrouted) are not written.
+ * [E, channels]; out: bf16 (stored in pairs where out, out_stride and the channels of out are even multiples of two bytes,
+ * one by one otherwise).  inner: a multiple of 16, at most 131056 (int32 sums cannot overflow); channels: any number, an even
+ * one if gated.  Rows outside the segments (padding, unrouted) are not written.
  * Needs a workspace (the status word).  One launch. */
 typedef struct {
     int32_t type;                  /* STRATA_T_INT8 or STRATA_T_E4M3, of a and w alike        */

@@ -765,8 +765,8 @@ strata_status strata_device_status(strata_ctx* ctx, void* stream, strata_status*
     }
     if (word != 0) {
         // clear the status word; after an error also the ticket and the work-claim counters, which a
-        // kernel that gave up may have left non-zero (header words 0..11)
-        if (cudaMemsetAsync(ctx->ws, 0, 12 * sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+        // kernel that gave up may have left non-zero (header words 0..9)
+        if (cudaMemsetAsync(ctx->ws, 0, 10 * sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
             cudaGetLastError();
             return STRATA_ERR_CUDA;
         }

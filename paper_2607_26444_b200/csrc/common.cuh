@@ -14,7 +14,7 @@ namespace strata {
 // word 0: device status (a strata_status, first error wins)
 // word 1: ticket of the layout kernel (returns to 0 after every call)
 // word 2: work-claim counter of dispatch, word 4: of combine, word 6: of the collectives, word 8: of the experts'
-//         products, word 10: of the norm and the row quantiser (each returns to 0 inside the kernel)
+//         products (each returns to 0 inside the kernel)
 // bytes [256, ...): per-tile, per-expert counts, int32 [n_tiles, E]
 // the last collective_table_bytes() bytes: pair table of all-to-all-v
 constexpr int kWsHeaderBytes = 256;
@@ -307,17 +307,6 @@ __device__ __forceinline__ unsigned int claim_unit(const WorkQueue& q, unsigned 
     exhausted = true;
     // failed claims are numbered n_units-base .. n_units-base+gridDim.x-1; the last one re-arms the queue
     if (old == n_units - base + gridDim.x - 1) *q.next = 0;
-    return kNoUnit;
-}
-
-// The same in two steps and with a given number of claimers, the first `claimers` units being dealt statically, one to
-// each: a claimer draws a number (atomicAdd(next, 1)) when it begins a unit, so that the answer is there when the unit ends, and
-// turns it into the next unit here.  It draws until it is told kNoUnit; claimers < n_units.
-__device__ __forceinline__ unsigned int claimed_unit(const WorkQueue& q, unsigned int n_units, unsigned int claimers,
-                                                     unsigned int drawn)
-{
-    if (claimers + drawn < n_units) return claimers + drawn;
-    if (drawn == n_units - 1) *q.next = 0;      // failed draws are numbered n_units - claimers .. n_units - 1
     return kNoUnit;
 }
 

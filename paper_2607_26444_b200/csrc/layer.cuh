@@ -12,12 +12,12 @@ cudaError_t launch_route_grad(const strata_moe_shape& s, const strata_route_para
                               long long stride, const int32_t* ids, const float* dw, void* dlogits, long long dstride,
                               int* status, cudaStream_t st);
 cudaError_t configure_norm_kernels();
-cudaError_t launch_norm(const strata_norm_args& a, int* status, WorkQueue wq, int n_sm, cudaStream_t st);
+cudaError_t launch_norm(const strata_norm_args& a, cudaStream_t st);
 size_t norm_grad_scratch_bytes(long long rows, int cols, int n_sm);
 cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_sm, cudaStream_t st, int* n_launches);
 cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, int cols, int q_type, void* q,
                             long long q_stride, float* q_scale, long long q_scale_stride, const int32_t* n_valid,
-                            int* status, WorkQueue wq, int n_sm, cudaStream_t st);
+                            cudaStream_t st);
 cudaError_t configure_matmul_kernels();
 cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_layout_t& L, const strata_matmul_args& a,
                                  int* status, WorkQueue wq, int n_sm, cudaStream_t st);

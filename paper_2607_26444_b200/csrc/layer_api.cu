@@ -14,8 +14,6 @@ constexpr int kMaxInner = 131056;        // 2^31 / 128^2, less one: int8 sums ca
 
 WorkQueue matmul_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 8}; }
 
-WorkQueue row_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 10}; }
-
 bool on(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
 strata_status check_route(const strata_ctx* ctx, const strata_route_params* r, int type, int64_t stride)
@@ -49,7 +47,7 @@ strata_status check_codes(const void* q, int64_t q_stride, const float* q_scale,
 }
 bool bad_extent(int64_t rows, int32_t cols)
 {
-    return rows < 0 || rows >= (1ll << 40) || cols < 8 || cols % 8 != 0 || cols > kMaxCols;
+    return rows < 0 || rows >= (1ll << 31) || cols < 8 || cols % 8 != 0 || cols > kMaxCols;
 }
 
 #define STRATA_CHECK(call)                          \
@@ -111,11 +109,10 @@ strata_status strata_norm(strata_ctx* ctx, const strata_norm_args* a, void* stre
     if (a->out) STRATA_CHECK(check_rows16(a->out, a->out_stride, a->cols));
     if (a->q) STRATA_CHECK(check_codes(a->q, a->q_stride, a->q_scale, a->q_scale_stride, a->q_type, a->cols));
     if (!on(a->weight, 16)) return STRATA_ERR_ALIGNMENT;
-    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
-    return launched(ctx, launch_norm(*a, ctx->ws, row_queue(ctx), ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+    return launched(ctx, launch_norm(*a, static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_norm_grad_scratch_bytes(strata_ctx* ctx, int64_t rows, int32_t cols, size_t* bytes)
@@ -161,12 +158,11 @@ strata_status strata_quantize_rows(strata_ctx* ctx, const void* x, int64_t x_str
     STRATA_CHECK(check_rows16(x, x_stride, cols));
     STRATA_CHECK(check_codes(q, q_stride, q_scale, q_scale_stride, q_type, cols));
     if (!on(n_valid, 4)) return STRATA_ERR_ALIGNMENT;
-    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (ctx->device < 0) return STRATA_ERR_CUDA;
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     return launched(ctx, launch_quantize(x, x_stride, rows, cols, q_type, q, q_stride, q_scale, q_scale_stride, n_valid,
-                                         ctx->ws, row_queue(ctx), ctx->n_sm_device, static_cast<cudaStream_t>(stream)));
+                                         static_cast<cudaStream_t>(stream)));
 }
 
 strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_t* layout, const strata_matmul_args* a,
@@ -178,12 +174,12 @@ strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_
     if (a->gated != 0 && a->gated != 1) return STRATA_ERR_INVALID_ARG;
     const strata_moe_shape& s = ctx->shape;
     if (a->inner < 16 || a->inner % 16 != 0 || a->inner > kMaxInner) return STRATA_ERR_SHAPE;
-    if (a->channels < 2 || a->channels % (a->gated ? 4 : 2) != 0 || a->channels > (1 << 24)) return STRATA_ERR_SHAPE;
+    if (a->channels < 1 || (a->gated && a->channels % 2 != 0) || a->channels > (1 << 24)) return STRATA_ERR_SHAPE;
     if ((int64_t)a->channels * s.E >= (1ll << 31)) return STRATA_ERR_SHAPE;
     if (a->a_stride < a->inner || a->a_stride % 16 != 0 || a->a_stride >= (1ll << 40)) return STRATA_ERR_SHAPE;
     if (a->a_scale_stride < 1 || a->a_rows >= (1ll << 31)) return STRATA_ERR_SHAPE;
-    if (a->out_stride < a->channels / (a->gated ? 2 : 1) || a->out_stride % 2 != 0) return STRATA_ERR_SHAPE;
-    if (!on(a->a, 16) || !on(a->w, 16) || !on(a->a_scale, 4) || !on(a->w_scale, 4) || !on(a->out, 4))
+    if (a->out_stride < a->channels / (a->gated ? 2 : 1)) return STRATA_ERR_SHAPE;
+    if (!on(a->a, 16) || !on(a->w, 16) || !on(a->a_scale, 4) || !on(a->w_scale, 4) || !on(a->out, 2))
         return STRATA_ERR_ALIGNMENT;
     if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (a->a_rows < (int64_t)recv_rows(s)) return STRATA_ERR_CAPACITY;

@@ -60,6 +60,7 @@ struct MatParams {
     WorkQueue wq;
     long long a_rows, a_scale_stride, out_stride;
     int E, k_blocks, channels, m_tiles; // channels: rows of w per expert
+    int out_words;                      // pairs of channels of out lie on 4 bytes
 #ifdef STRATA_TEST_HOOKS
     int test_flags;
 #endif
@@ -214,18 +215,27 @@ __device__ __forceinline__ float acc_value(uint32_t v)
 }
 __device__ __forceinline__ float gate_mul(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
-// N columns of 32 channels, lane = channel: neighbouring lanes exchange, so that one holds two channels of column c and
-// the other two channels of column c + 1, and each writes them with one 4-byte store (64 bytes per row and warp).
+// N columns of 32 channels, lane = channel `ch`: neighbouring lanes exchange, so that one holds two channels of column c and
+// the other two channels of column c + 1, and each writes them with one 4-byte store (64 bytes per row and warp).  Where
+// rows of out do not all start on 4 bytes, or the channels are odd in number, the two are stored one by one.
 template <int N>
-__device__ __forceinline__ void store_pairs(const float (&y)[N], int lane, uint16_t* out, long long stride, int rows, bool in)
+__device__ __forceinline__ void store_pairs(const float (&y)[N], int lane, uint16_t* out, long long stride, int rows, int ch,
+                                            int limit, bool words)
 {
     const int odd = lane & 1;
-    out += odd * stride;
+    ch &= ~1;
+    out += odd * stride + ch;
 #pragma unroll
     for (int c = 0; c < N; c += 2) {
         const float other = __shfl_xor_sync(0xffffffffu, odd ? y[c] : y[c + 1], 1);
         const uint32_t v = odd ? pack_bf16x2(other, y[c + 1]) : pack_bf16x2(y[c], other);
-        if (in && c + odd < rows) *reinterpret_cast<uint32_t*>(out + c * stride) = v;
+        uint16_t* at = out + c * stride;
+        if (words) {
+            if (ch < limit && c + odd < rows) *reinterpret_cast<uint32_t*>(at) = v;
+        } else if (c + odd < rows) {
+            if (ch < limit) at[0] = (uint16_t)v;
+            if (ch + 1 < limit) at[1] = (uint16_t)(v >> 16);
+        }
     }
 }
 
@@ -428,6 +438,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
                 for (int b = 0; b < MB; ++b) out_ch[b] = ch[b] = (w.m * MB + b) * kM + quad * 32 + lane;
             }
             const int limit = GATED ? half : p.channels;
+            const bool words = p.out_words != 0;
             float wsc[2];
 #pragma unroll
             for (int b = 0; b < MB; ++b) wsc[b] = out_ch[GATED ? 0 : b] < limit ? ws[ch[b]] : 0.0f;
@@ -470,8 +481,8 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
                         o[c] = up ? gate_mul(other, y[8 + c]) : gate_mul(y[c], other);
                     }
                     const int shift = up ? 8 : 0;
-                    store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride + (out_ch[0] & ~1), p.out_stride,
-                                 rows - c0 - shift, out_ch[0] < limit);
+                    store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride, p.out_stride, rows - c0 - shift, out_ch[0],
+                                   limit, words);
                 } else if constexpr (GATED) {
                     uint32_t g[16], u[16];
                     tmem_ld16(g, addr + c0);
@@ -482,8 +493,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
 #pragma unroll
                     for (int c = 0; c < 16; ++c)
                         y[c] = gate_mul(acc_value<INT8>(g[c]) * (sc[c] * wsc[0]), acc_value<INT8>(u[c]) * (sc[c] * wsc[1]));
-                    store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride + (out_ch[0] & ~1), p.out_stride, rows - c0,
-                                out_ch[0] < limit);
+                    store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[0], limit, words);
                 } else {
 #pragma unroll
                     for (int b = 0; b < MB; ++b) {
@@ -493,8 +503,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
                         float y[16];
 #pragma unroll
                         for (int c = 0; c < 16; ++c) y[c] = acc_value<INT8>(v[c]) * (sc[c] * wsc[b]);
-                        store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride + (out_ch[b] & ~1), p.out_stride, rows - c0,
-                                    out_ch[b] < limit);
+                        store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[b], limit, words);
                     }
                 }
             }
@@ -634,6 +643,7 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
     p.E = s.E;
     p.k_blocks = (a.inner + kKBytes - 1) / kKBytes;
     p.channels = a.channels;
+    p.out_words = a.channels % (a.gated ? 4 : 2) == 0 && a.out_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
     // Which tile: the shortest estimate of rounds * (inner blocks * c + f) over the GPU, where c is what one inner block of a
     // tile takes and f what a tile adds (its epilogue where the accumulators are not doubled, the ring's refill).  The
     // constants were fitted to 116 measured shapes (8 and 32 experts, 2 .. 2048 mean rows, inner 512 .. 7168, 512 .. 4096

@@ -108,11 +108,11 @@ __device__ __forceinline__ uint4 lds16(const void* p)
     return v;
 }
 
-// Sum of a and maximum (or sum) of b over the threads of one row.  Rows of one warp need no barrier; otherwise the
-// partials of the warps meet in shared memory, in a buffer that alternates from row to row, so one barrier is enough.
-// Returns whether any of them wants to stop.
+// Sum of a and maximum (or sum) of b over the tpr threads of row group `sub`.  Rows of one warp need no barrier; otherwise the
+// partials of the warps meet in shared memory (the group's own part of buf, not reused before its next barrier but one:
+// callers with several rows alternate between two buffers), behind a barrier of the group.
 template <bool B_IS_MAX>
-__device__ __forceinline__ bool row_reduce(float& a, float& b, float2* buf, bool one_warp, int phase, bool stop = false)
+__device__ __forceinline__ void row_reduce(float& a, float& b, float2* buf, int sub, int tpr)
 {
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) {
@@ -120,18 +120,17 @@ __device__ __forceinline__ bool row_reduce(float& a, float& b, float2* buf, bool
         const float t = __shfl_xor_sync(kFull, b, o);
         b = B_IS_MAX ? fmaxf(b, t) : b + t;
     }
-    if (one_warp) return __any_sync(kFull, stop);
-    const int warp = (int)threadIdx.x >> 5, warps = (int)blockDim.x >> 5;
-    float2* mine = buf + (phase & 1) * 32;
-    if ((threadIdx.x & 31) == 0) mine[warp] = make_float2(a, b);
-    if (__syncthreads_or(stop)) return true;
+    if (tpr == 32) return;
+    const int warps = tpr >> 5, warp = (int)threadIdx.x >> 5;
+    if ((threadIdx.x & 31) == 0) buf[warp] = make_float2(a, b);
+    asm volatile("bar.sync %0, %1;" ::"r"(sub), "r"(tpr) : "memory");
+    const float2* mine = buf + sub * warps;
     a = mine[0].x;
     b = mine[0].y;
     for (int q = 1; q < warps; ++q) {
         a += mine[q].x;
         b = B_IS_MAX ? fmaxf(b, mine[q].y) : b + mine[q].y;
     }
-    return false;
 }
 
 // 8 codes of y * limit / top (top = max|y| of the row), one correctly rounded binary32 quotient each, so that a
@@ -183,19 +182,12 @@ struct RowParams {
     uint8_t* q;
     float* q_scale;
     const int32_t* n_valid;
-    int* status;
     long long x_stride, res_stride, res_out_stride, out_stride, q_stride, q_scale_stride;
     long long rows;
     int vecs;              // 16-byte vectors in a row
-    int tpr;               // threads of one row: the whole block, or 32 (several rows per block)
-    int stages;            // rows in flight per row group (ring)
-    int chunk;             // rows of one claim
-    WorkQueue wq;
+    int tpr;               // threads of one row, a multiple of 32; a block holds blockDim.x / tpr rows
     int weight_f32;
     float eps, inv_cols;
-#ifdef STRATA_TEST_HOOKS
-    int test_flags;
-#endif
 };
 
 // y = h * weight for eight columns (vector c of the row)
@@ -205,6 +197,102 @@ __device__ __forceinline__ void weigh8(const RowParams& p, int c, Pair* y)
     load_weight8(p.weight, p.weight_f32 != 0, c * 8, w);
 #pragma unroll
     for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], w[i]);
+}
+
+// Forward pass.  NORM: y = (h * w) * rstd; otherwise y = x (row quantiser).  max|y| follows from max|h * w|, because
+// multiplying by rstd keeps the order, so both statistics come out of one reduction, and the codes need no rstd at all.
+//
+// One row per group of threads, no loop: the hardware deals blocks of up to 256 threads to SMs as they free up, which keeps
+// every SM busy to the end.  h * w waits in registers between the two passes.  65,536 x 7168 with residual to e4m3: 487 us,
+// 520 once the power limit slows the clocks (6.3 TB/s); widening and weighing again in the second pass: 501 and 550;
+// persistent blocks with a ring of bulk copies and ordered claims: 526 and 569 (and 90, not 82 us, at 16,384 x 4096 to bf16).
+// Three blocks per SM (80 registers) with a residual, four (64) without: 178, not 200 us, at 65,536 x 4096 to e4m3.
+template <bool NORM, bool RES, int QK, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1) row_kernel(const RowParams p)
+{
+    __shared__ float2 s_part[32];
+    const int sub = (int)threadIdx.x / p.tpr, tid = (int)threadIdx.x - sub * p.tpr;
+    const long long row = (long long)blockIdx.x * ((int)blockDim.x / p.tpr) + sub;
+    griddep_wait();
+    griddep_launch_dependents();
+    if (row >= p.rows || (p.n_valid && row >= *p.n_valid)) return;
+    uint4 h[kVpt];                                                   // the row, as stored
+    {
+        const uint16_t* x = p.x + row * p.x_stride;
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) {
+            const int c = tid + j * p.tpr;
+            if (c < p.vecs) h[j] = ld_row16(x + (size_t)c * 8);
+        }
+    }
+    if constexpr (RES) {
+        const uint16_t* res = p.res + row * p.res_stride;
+        uint16_t* res_out = p.res_out + row * p.res_out_stride;
+        uint4 r[kVpt];
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) {
+            const int c = tid + j * p.tpr;
+            if (c < p.vecs) r[j] = ld_row16(res + (size_t)c * 8);
+        }
+#pragma unroll
+        for (int j = 0; j < kVpt; ++j) {
+            const int c = tid + j * p.tpr;
+            if (c < p.vecs) {                                        // what is stored is what is normed
+                h[j] = make_uint4(add_bf16x2(h[j].x, r[j].x), add_bf16x2(h[j].y, r[j].y), add_bf16x2(h[j].z, r[j].z),
+                                  add_bf16x2(h[j].w, r[j].w));
+                *reinterpret_cast<uint4*>(res_out + (size_t)c * 8) = h[j];
+            }
+        }
+    }
+    Pair squares = 0, kept[kVpt][4];
+    float top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < kVpt; ++j) {
+        const int c = tid + j * p.tpr;
+        if (c < p.vecs) {
+            Pair* y = kept[j];
+            widen8(h[j], y);
+            if constexpr (NORM) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) squares = fma2(y[i], y[i], squares);
+                weigh8(p, c, y);
+            }
+            if constexpr (QK != kNoCodes) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const float2 f = split(y[i]);
+                    top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
+                }
+            }
+        }
+    }
+    const float2 sq = split(squares);
+    float sum = sq.x + sq.y;
+    row_reduce<true>(sum, top, s_part, sub, p.tpr);
+    float rstd = 1.0f;
+    if constexpr (NORM) rstd = __frcp_rn(__fsqrt_rn(fmaf(sum, p.inv_cols, p.eps)));
+    const float range = row_range(top), in_range = top == 0.0f ? 1.0f : top * range, inv = __frcp_rn(in_range);
+    const float factor = (QK == kInt8 ? 127.0f : 448.0f) * range;
+    const Pair factor2 = make_pair(factor, factor), neg_top2 = make_pair(-in_range, -in_range), inv2 = make_pair(inv, inv);
+    const Pair rstd2 = make_pair(rstd, rstd);
+    uint8_t* q = p.q + row * p.q_stride;
+    uint16_t* out = p.out + row * p.out_stride;
+#pragma unroll
+    for (int j = 0; j < kVpt; ++j) {
+        const int c = tid + j * p.tpr;
+        if (c < p.vecs) {
+            Pair* y = kept[j];
+            if constexpr (QK != kNoCodes) *reinterpret_cast<uint2*>(q + (size_t)c * 8) = codes8<QK>(y, factor2, neg_top2, inv2);
+            if constexpr (NORM) {
+                if (QK == kNoCodes || p.out) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], rstd2);
+                    *reinterpret_cast<uint4*>(out + (size_t)c * 8) = narrow8(y);
+                }
+            }
+        }
+    }
+    if (QK != kNoCodes && tid == 0) p.q_scale[row * p.q_scale_stride] = __fdiv_rn(top * rstd, QK == kInt8 ? 127.0f : 448.0f);
 }
 
 constexpr int kMaxStages = 4, kMaxGroups = 8;
@@ -219,186 +307,6 @@ __device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, volati
     *dead = 1;
     report_status(status, STRATA_ERR_TIMEOUT);
     return false;
-}
-
-// Forward pass.  NORM: y = (h * w) * rstd; otherwise y = x (row quantiser).  max|y| follows from max|h * w|, because
-// multiplying by rstd keeps the order, so both statistics come out of one reduction, and the codes need no rstd at all.
-//
-// A row belongs to one block (rows of up to 1024 columns: to one warp of eight), which keeps it packed in registers
-// between the two passes.  RING: bulk copies keep the next rows of the group in flight in shared memory whatever the
-// threads do (a stage is free again after the reduction's barrier).  Launches with one row per group at most load
-// directly: there is nothing to run ahead of.
-template <bool NORM, bool RES, int QK, bool RING, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? 3 : 1) row_kernel(const RowParams p)
-{
-    extern __shared__ __align__(128) unsigned char ring[];            // [groups][stages][1 or 2 rows]
-    __shared__ float2 s_part[64];
-    __shared__ uint64_t s_full[kMaxGroups][kMaxStages];
-    __shared__ long long s_row[kMaxGroups][kMaxStages];               // the row in a stage, -1: no more
-    __shared__ int s_dead;
-    const bool one_warp = p.tpr == 32;
-    const int sub = one_warp ? (int)threadIdx.x >> 5 : 0;            // row group inside the block
-    const int tid = one_warp ? (int)threadIdx.x & 31 : (int)threadIdx.x;
-    const int groups = one_warp ? (int)blockDim.x >> 5 : 1;
-    const uint32_t row_bytes = (uint32_t)p.vecs * 16u, stage_bytes = RES ? 2u * row_bytes : row_bytes;
-    unsigned char* my_ring = ring + (size_t)sub * p.stages * stage_bytes;
-    if constexpr (RING) {
-        if (threadIdx.x == 0) {
-            s_dead = 0;
-            for (int g = 0; g < groups; ++g)
-                for (int s = 0; s < p.stages; ++s) mbar_init(&s_full[g][s], 1);
-            mbar_fence_init();
-        }
-        __syncthreads();
-    }
-    griddep_wait();
-    long long rows = p.rows;
-    if (p.n_valid) rows = min(rows, (long long)max(0, *p.n_valid));
-    const long long first = (long long)blockIdx.x * groups + sub, step = (long long)gridDim.x * groups;
-    // Ring: the first thread of a group claims rows in order, a few at a time, `stages` ahead of the group.  The next claim is
-    // in flight while the rows of the last one are fetched, so nothing waits for the counter.
-    const unsigned units = (unsigned)((rows + p.chunk - 1) / p.chunk), claimers = (unsigned)step;
-    unsigned unit = (unsigned)first < units ? (unsigned)first : kNoUnit, drawn = 0;
-    long long ahead = 0, ahead_end = 0;
-    int issued = 0;
-    auto begin_unit = [&] {
-        ahead = (long long)unit * p.chunk;
-        ahead_end = min(rows, ahead + p.chunk);
-        if (claimers < units) drawn = atomicAdd(p.wq.next, 1u);
-    };
-    if (RING && tid == 0 && unit != kNoUnit) begin_unit();
-    auto fetch = [&](int stage) {
-        if (unit != kNoUnit && ahead == ahead_end) {
-            unit = claimers < units ? claimed_unit(p.wq, units, claimers, drawn) : kNoUnit;
-            if (unit != kNoUnit) begin_unit();
-        }
-        uint64_t* bar = &s_full[sub][stage];
-        if (unit == kNoUnit) {
-            s_row[sub][stage] = -1;
-            asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");
-            return;
-        }
-        const long long row = ahead++;
-        unsigned char* dst = my_ring + (size_t)stage * stage_bytes;
-        s_row[sub][stage] = row;
-        mbar_expect_tx(bar, stage_bytes + STRATA_TEST_EXTRA(issued == 0));
-        bulk_g2s_plain(dst, p.x + row * p.x_stride, row_bytes, bar);
-        if constexpr (RES) bulk_g2s_plain(dst + row_bytes, p.res + row * p.res_stride, row_bytes, bar);
-        ++issued;
-    };
-    if (RING && tid == 0)
-        for (int s = 0; s < p.stages; ++s) fetch(s);
-    int phase = 0, stage = 0;
-    uint32_t parity = 0;
-    for (long long row = first; RING || row < rows; row += step, ++phase) {
-        const unsigned char* src = my_ring + (size_t)stage * stage_bytes;
-        bool stop = false;
-        if constexpr (RING) {
-            row = -1;
-            if (ring_wait(&s_full[sub][stage], parity, &s_dead, p.status))
-                row = *reinterpret_cast<volatile long long*>(&s_row[sub][stage]);
-            stop = row < 0;
-        }
-        const int vecs = RING && stop ? 0 : p.vecs;
-        uint4 h[kVpt];                                               // the row, as stored
-        if constexpr (RING) {
-#pragma unroll
-            for (int j = 0; j < kVpt; ++j) {
-                const int c = tid + j * p.tpr;
-                if (c < vecs) h[j] = *reinterpret_cast<const uint4*>(src + (size_t)c * 16);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < kVpt; ++j) {
-                const int c = tid + j * p.tpr;
-                if (c < vecs) h[j] = ld_row16(p.x + row * p.x_stride + (size_t)c * 8);
-            }
-        }
-        if constexpr (RES) {
-            uint4 r[kVpt];
-#pragma unroll
-            for (int j = 0; j < kVpt; ++j) {
-                const int c = tid + j * p.tpr;
-                if (c < vecs)
-                    r[j] = RING ? *reinterpret_cast<const uint4*>(src + row_bytes + (size_t)c * 16)
-                                : ld_row16(p.res + row * p.res_stride + (size_t)c * 8);
-            }
-#pragma unroll
-            for (int j = 0; j < kVpt; ++j) {
-                const int c = tid + j * p.tpr;
-                if (c < vecs) {                                    // what is stored is what is normed
-                    h[j] = make_uint4(add_bf16x2(h[j].x, r[j].x), add_bf16x2(h[j].y, r[j].y), add_bf16x2(h[j].z, r[j].z),
-                                      add_bf16x2(h[j].w, r[j].w));
-                    *reinterpret_cast<uint4*>(p.res_out + row * p.res_out_stride + (size_t)c * 8) = h[j];
-                }
-            }
-        }
-        Pair squares = 0;
-        float top = 0.0f;
-#pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
-            const int c = tid + j * p.tpr;
-            if (c < vecs) {
-                Pair y[4];
-                widen8(h[j], y);
-                if constexpr (NORM) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) squares = fma2(y[i], y[i], squares);
-                    if constexpr (QK != kNoCodes) weigh8(p, c, y);
-                }
-                if constexpr (QK != kNoCodes) {
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 f = split(y[i]);
-                        top = fmaxf(top, fmaxf(fabsf(f.x), fabsf(f.y)));
-                    }
-                }
-            }
-        }
-        const float2 sq = split(squares);
-        float sum = sq.x + sq.y;
-        const bool ends = row_reduce<true>(sum, top, s_part, one_warp, phase, stop);
-        if constexpr (RING) {
-            if (ends) break;
-            if (tid == 0) fetch(stage);
-            if (++stage == p.stages) {
-                stage = 0;
-                parity ^= 1;
-            }
-        }
-        float rstd = 1.0f;
-        if constexpr (NORM) rstd = __frcp_rn(__fsqrt_rn(fmaf(sum, p.inv_cols, p.eps)));
-        const float range = row_range(top), in_range = top == 0.0f ? 1.0f : top * range, inv = __frcp_rn(in_range);
-        const float factor = (QK == kInt8 ? 127.0f : 448.0f) * range;
-        const Pair factor2 = make_pair(factor, factor), neg_top2 = make_pair(-in_range, -in_range), inv2 = make_pair(inv, inv);
-        const Pair rstd2 = make_pair(rstd, rstd);
-#pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
-            const int c = tid + j * p.tpr;
-            if (c < p.vecs) {
-                Pair y[4];
-                widen8(h[j], y);
-                if constexpr (NORM) weigh8(p, c, y);
-                if constexpr (QK != kNoCodes)
-                    *reinterpret_cast<uint2*>(p.q + row * p.q_stride + (size_t)c * 8) = codes8<QK>(y, factor2, neg_top2, inv2);
-                if constexpr (NORM) {
-                    if (QK == kNoCodes || p.out) {
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) y[i] = mul2(y[i], rstd2);
-                        *reinterpret_cast<uint4*>(p.out + row * p.out_stride + (size_t)c * 8) = narrow8(y);
-                    }
-                }
-            }
-        }
-        if (QK != kNoCodes && tid == 0)
-            p.q_scale[row * p.q_scale_stride] = __fdiv_rn(top * rstd, QK == kInt8 ? 127.0f : 448.0f);
-    }
-    griddep_launch_dependents();
-    if constexpr (RING) {                                            // a block that gave up lets its copies land first
-        if (tid == 0 && s_dead)
-            for (int u = max(0, issued - p.stages); u < issued; ++u)
-                mbar_wait_bounded(&s_full[sub][u % p.stages], (uint32_t)(u / p.stages) & 1u);
-    }
 }
 
 struct GradParams {
@@ -517,7 +425,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
         }
         const float2 sq = split(squares), dt = split(dots);
         float sum = sq.x + sq.y, dot = dt.x + dt.y;
-        row_reduce<false>(sum, dot, s_part, one_warp, phase);
+        row_reduce<false>(sum, dot, s_part + (phase & 1) * 32, sub, p.tpr);
         if (RING && tid == 0 && phase > 0 && !*dead) fetch();        // into the stage of the row before this one
         const float rstd = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
         const float mean = dot * rstd * p.inv_cols;                  // mean(g * hat)
@@ -596,38 +504,24 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) weight_sum_kernel(const f
 struct RowGeom {
     int tpr, threads, groups;          // threads per row, threads per block, rows per block at a time
 };
-RowGeom row_geom(int cols)
+// Forward: blocks of 256 threads as far as whole rows fit; backward (`wide` false): one row per block, or eight rows of one warp.
+RowGeom row_geom(int cols, bool wide)
 {
     RowGeom g;
     const int vecs = cols / 8;
     g.tpr = ((vecs + kVpt - 1) / kVpt + 31) / 32 * 32;
-    g.groups = g.tpr == 32 ? kMaxGroups : 1;
+    g.groups = g.tpr == 32 ? kMaxGroups : wide && g.tpr <= 128 ? 256 / g.tpr : 1;
     g.threads = g.tpr * g.groups;
     return g;
 }
 
 template <bool NORM, bool RES, int QK>
-cudaError_t run_rows(RowParams& p, const RowGeom& g, int n_sm, cudaStream_t st)
+cudaError_t run_rows(const RowParams& p, const RowGeom& g, cudaStream_t st)
 {
     const long long blocks = (p.rows + g.groups - 1) / g.groups;
-    const size_t row = (size_t)p.vecs * (RES ? 32 : 16) * (size_t)g.groups;       // bytes a block reads per round
-    // blocks per SM: up to 1,024 threads, with two rows per group in flight in 200 KB of shared memory
-    const int per_sm = (int)max(1ll, min((long long)(1024 / g.threads), (long long)(kRingBytes / (2 * row))));
-    if (blocks <= (long long)n_sm * per_sm) {
-        return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, false, 256>, (unsigned)blocks, g.threads, 0, st, p)
-                                : launch_pdl(row_kernel<NORM, RES, QK, false, 1024>, (unsigned)blocks, g.threads, 0, st, p);
-    }
-    p.stages = (int)max(1ll, min((long long)kMaxStages, (long long)(kRingBytes / (per_sm * row))));
-#ifdef STRATA_TEST_HOOKS
-    p.test_flags = g_inject_short_row.exchange(0);
-#endif
-    // claims on one counter complete at about one per 3.5 ns: few enough of them to stay below the bytes' time
-    // (64 KB: 65,536 x 7168 with residual 523 us, 553 us with equal shares; 8 KB claims took 214 us, not 136, at 2048 columns)
-    p.chunk = (int)max((size_t)1, (size_t)65536 / ((size_t)p.vecs * (RES ? 32 : 16)));
-    const size_t smem = row * p.stages;
-    const unsigned grid = (unsigned)min(blocks, (long long)n_sm * per_sm);
-    return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, true, 256>, grid, g.threads, smem, st, p)
-                            : launch_pdl(row_kernel<NORM, RES, QK, true, 1024>, grid, g.threads, smem, st, p);
+    if (blocks >= (1ll << 31)) return cudaErrorInvalidConfiguration;
+    return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, 256>, (unsigned)blocks, g.threads, 0, st, p)
+                            : launch_pdl(row_kernel<NORM, RES, QK, 1024>, (unsigned)blocks, g.threads, 0, st, p);
 }
 
 // Row groups of the backward pass: up to four blocks per SM, as long as two rounds of rows (three operands) of each fit
@@ -643,16 +537,6 @@ long long grad_owners(long long rows, const RowGeom& g, int cols, int n_sm)
 
 // Attributes of the kernels that use more than 48 KB of shared memory.
 namespace {
-template <bool NORM, bool RES, int QK>
-cudaError_t configure_rows()
-{
-    cudaError_t e = cudaFuncSetAttribute(row_kernel<NORM, RES, QK, true, 256>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                         (int)kRingBytes);
-    if (e == cudaSuccess)
-        e = cudaFuncSetAttribute(row_kernel<NORM, RES, QK, true, 1024>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                 (int)kRingBytes);
-    return e;
-}
 template <bool RES>
 cudaError_t configure_grad()
 {
@@ -683,20 +567,12 @@ cudaError_t configure_norm_kernels()
     cudaError_t e = cudaSuccess;
     e = configure_grad<true>();
     if (e == cudaSuccess) e = configure_grad<false>();
-    if (e == cudaSuccess) e = configure_rows<true, true, kNoCodes>();
-    if (e == cudaSuccess) e = configure_rows<true, true, kInt8>();
-    if (e == cudaSuccess) e = configure_rows<true, true, kE4m3>();
-    if (e == cudaSuccess) e = configure_rows<true, false, kNoCodes>();
-    if (e == cudaSuccess) e = configure_rows<true, false, kInt8>();
-    if (e == cudaSuccess) e = configure_rows<true, false, kE4m3>();
-    if (e == cudaSuccess) e = configure_rows<false, false, kInt8>();
-    if (e == cudaSuccess) e = configure_rows<false, false, kE4m3>();
     return e;
 }
 
-cudaError_t launch_norm(const strata_norm_args& a, int* status, WorkQueue wq, int n_sm, cudaStream_t st)
+cudaError_t launch_norm(const strata_norm_args& a, cudaStream_t st)
 {
-    const RowGeom g = row_geom(a.cols);
+    const RowGeom g = row_geom(a.cols, true);
     RowParams p{};
     p.x = static_cast<const uint16_t*>(a.x);
     p.res = static_cast<const uint16_t*>(a.residual);
@@ -711,8 +587,6 @@ cudaError_t launch_norm(const strata_norm_args& a, int* status, WorkQueue wq, in
     p.out_stride = a.out_stride;
     p.q_stride = a.q_stride;
     p.q_scale_stride = a.q_scale_stride;
-    p.status = status;
-    p.wq = wq;
     p.rows = a.rows;
     p.vecs = a.cols / 8;
     p.tpr = g.tpr;
@@ -721,44 +595,42 @@ cudaError_t launch_norm(const strata_norm_args& a, int* status, WorkQueue wq, in
     p.inv_cols = 1.0f / (float)a.cols;
     const int qk = !a.q ? kNoCodes : a.q_type == STRATA_T_INT8 ? kInt8 : kE4m3;
     if (a.residual)
-        return qk == kNoCodes ? run_rows<true, true, kNoCodes>(p, g, n_sm, st)
-               : qk == kInt8  ? run_rows<true, true, kInt8>(p, g, n_sm, st)
-                              : run_rows<true, true, kE4m3>(p, g, n_sm, st);
-    return qk == kNoCodes ? run_rows<true, false, kNoCodes>(p, g, n_sm, st)
-           : qk == kInt8  ? run_rows<true, false, kInt8>(p, g, n_sm, st)
-                          : run_rows<true, false, kE4m3>(p, g, n_sm, st);
+        return qk == kNoCodes ? run_rows<true, true, kNoCodes>(p, g, st)
+               : qk == kInt8  ? run_rows<true, true, kInt8>(p, g, st)
+                              : run_rows<true, true, kE4m3>(p, g, st);
+    return qk == kNoCodes ? run_rows<true, false, kNoCodes>(p, g, st)
+           : qk == kInt8  ? run_rows<true, false, kInt8>(p, g, st)
+                          : run_rows<true, false, kE4m3>(p, g, st);
 }
 
 cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, int cols, int q_type, void* q,
                             long long q_stride, float* q_scale, long long q_scale_stride, const int32_t* n_valid,
-                            int* status, WorkQueue wq, int n_sm, cudaStream_t st)
+                            cudaStream_t st)
 {
-    const RowGeom g = row_geom(cols);
+    const RowGeom g = row_geom(cols, true);
     RowParams p{};
     p.x = static_cast<const uint16_t*>(x);
     p.q = static_cast<uint8_t*>(q);
     p.q_scale = q_scale;
     p.n_valid = n_valid;
-    p.status = status;
-    p.wq = wq;
     p.x_stride = x_stride;
     p.q_stride = q_stride;
     p.q_scale_stride = q_scale_stride;
     p.rows = rows;
     p.vecs = cols / 8;
     p.tpr = g.tpr;
-    return q_type == STRATA_T_INT8 ? run_rows<false, false, kInt8>(p, g, n_sm, st)
-                                   : run_rows<false, false, kE4m3>(p, g, n_sm, st);
+    return q_type == STRATA_T_INT8 ? run_rows<false, false, kInt8>(p, g, st)
+                                   : run_rows<false, false, kE4m3>(p, g, st);
 }
 
 size_t norm_grad_scratch_bytes(long long rows, int cols, int n_sm)
 {
-    return (size_t)grad_owners(rows, row_geom(cols), cols, n_sm) * (size_t)cols * sizeof(float);
+    return (size_t)grad_owners(rows, row_geom(cols, false), cols, n_sm) * (size_t)cols * sizeof(float);
 }
 
 cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_sm, cudaStream_t st, int* n_launches)
 {
-    const RowGeom g = row_geom(a.cols);
+    const RowGeom g = row_geom(a.cols, false);
     const long long owners = grad_owners(a.rows, g, a.cols, n_sm);
     GradParams p{};
     p.dy = static_cast<const uint16_t*>(a.dy);

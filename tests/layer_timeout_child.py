@@ -34,7 +34,7 @@ def matmul_call():
     return ctx, call
 
 
-def rows(cols, grad):
+def norm_grad_call(cols):
     g = torch.Generator(device=DEV)
     g.manual_seed(2)
     ctx = B.MoEContext(1, 1, 8, 1, 1)
@@ -43,12 +43,9 @@ def rows(cols, grad):
     w = torch.ones(cols, device=DEV)
 
     def call():
-        out, h, dw = torch.zeros_like(x), torch.zeros_like(x), torch.zeros(cols, device=DEV)
-        if grad:
-            ctx.norm_grad(x, r, w, 1e-6, out, dw, dresidual=r)
-            return torch.cat([out.float().sum(0), dw])
-        ctx.norm(x, w, 1e-6, out=out, residual=r, residual_out=h)
-        return out
+        dx, dw = torch.zeros_like(x), torch.zeros(cols, device=DEV)
+        ctx.norm_grad(x, r, w, 1e-6, dx, dw, dresidual=r)
+        return torch.cat([dx.float().sum(0), dw])
     return ctx, call
 
 
@@ -56,14 +53,14 @@ def main(kind):
     L = B.lib()
     hook = L.strata_test_inject_short_load if kind == "matmul" else L.strata_test_inject_short_row
     hook.argtypes, hook.restype = [ctypes.c_int], None
-    ctx, call = matmul_call() if kind == "matmul" else rows(512 if kind.endswith("warp") else 1544, "grad" in kind)
+    ctx, call = matmul_call() if kind == "matmul" else norm_grad_call(512 if kind.endswith("warp") else 1544)
     before = call()
     res = {"kind": kind, "status_before": ctx.device_status()}
     hook(1)
     call()
     res["status_after_injection"] = ctx.device_status()
     res["status_read_again"] = ctx.device_status()
-    res["header_words_after_recovery"] = ctx.workspace[:48].view(torch.int32).cpu().tolist()
+    res["header_words_after_recovery"] = ctx.workspace[:40].view(torch.int32).cpu().tolist()
     res["same_afterwards"] = bool(torch.equal(call(), before))
     res["status_after_normal_call"] = ctx.device_status()
     print(json.dumps(res), flush=True)

@@ -534,6 +534,8 @@ MATMULS = [
     dict(tokens=50, E=6, K=2, inner=256, channels=384, allow_unrouted=True),
     dict(tokens=2048, E=2, K=1, inner=64, channels=512),              # short inner extent, many tiles per CTA
     dict(tokens=3000, E=4, K=4, inner=32, channels=1200, skew=True),
+    dict(tokens=45, E=5, K=2, inner=160, channels=274),               # an odd number of gated channels: rows of out on two bytes
+    dict(tokens=300, E=3, K=2, inner=368, channels=510),
 ]
 
 
@@ -556,6 +558,16 @@ def test_expert_matmul_fixed_capacity(gated):
     ctx.expert_matmul(lay, a, a_scale, w, w_scale, out, gated=gated)
     assert ctx.device_status() == B.STRATA_OK
     check_products(lay, a, a_scale, w, w_scale, out, gated, "int8", count=np.full(4, 80))
+
+
+def test_expert_matmul_odd_channels_and_odd_strides():
+    for channels, stride in ((131, 131), (1, 1), (128, 129)):
+        ctx, lay, a, a_scale, w, w_scale, out = matmul_case(90, 3, 2, 128, channels, False, "int8", 23)
+        wide = torch.full((a.shape[0], stride), 99.0, dtype=torch.bfloat16, device=DEV)
+        out = wide[:, :channels]
+        ctx.expert_matmul(lay, a, a_scale, w, w_scale, out)
+        check_products(lay, a, a_scale, w, w_scale, out, False, "int8")
+        assert bool((wide[:, channels:] == 99.0).all())
 
 
 def test_expert_matmul_extreme_codes_are_exact():
