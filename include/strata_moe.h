@@ -314,8 +314,8 @@ strata_status strata_moe_combine(strata_ctx *ctx, const strata_moe_layout_t *lay
 strata_status strata_moe_mask_ragged(strata_ctx *ctx, const int32_t *tokens_per_rank, int32_t *topk_ids, void *stream);
 
 /* In-place consumer of the receive buffer (paper Sec. 2.2 / 8.1: the receive buffer is the input of the expert
- * computation, no staging copy).  The paper's expert is a grouped GEMM, which this library does not contain;
- * this call is the hand-over part of such a consumer with a per-expert affine map standing in for the GEMM.
+ * computation, no staging copy).  The paper's expert is a grouped GEMM (strata_moe_expert_matmul in strata_layer.h is one, in
+ * 8 bits); this call is the hand-over part of such a consumer with a per-expert affine map standing in for the GEMM.
  * It walks recv in tiles of tile_rows rows; every tile finds the expert e that owns it and its number of
  * occupied rows from expert_offset / expert_count as the layout call on the same stream left them, and
  * rewrites those rows in place:  recv[row][c] = bf16_rne(fma(f32(recv[row][c]), scale[e], bias[e]))

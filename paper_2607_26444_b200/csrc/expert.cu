@@ -1,6 +1,6 @@
 // In-place consumer of the receive buffer (paper Sec. 2.2 / 8.1: the buffer dispatch fills is the input of
-// the expert computation, with no staging copy in between).  The paper's expert is a grouped GEMM, which is
-// not part of this path; what is built here is the part of such a consumer that touches the hand-over: the
+// the expert computation, with no staging copy in between).  The paper's expert is a grouped GEMM (matmul.cu is
+// one, in 8 bits); what is built here is the part of such a consumer that touches the hand-over: the
 // walk over row tiles, each tile finding the expert that owns it from the layout's offsets (segments are
 // aligned to the tile height, so a tile never holds two experts) and the number of occupied rows in it,
 // with a per-expert affine map standing in for the GEMM:

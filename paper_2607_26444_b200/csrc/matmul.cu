@@ -650,8 +650,11 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
     // channels, even and Zipf routing); the choice is on average 2 % above the best of the three, and 30 % above at
     // worst, where a skewed routing has other tiles than the mean.  At 7168 -> 4096 gated, 32 experts: one token
     // <1,64> 45 us, <2,128> 42 us; 32 rows each 149, 156 (<2,256> 163); 128 rows 337, 185, 178; 512 rows 1149, 469, 396.
-    struct Cost { int mb, bn; float c, f; };
-    static const Cost costs[3] = {{1, 64, 0.37f, 0.65f}, {2, 128, 0.66f, 1.06f}, {2, 256, 1.22f, 2.78f}};
+    // Where the weights' way from HBM takes longer than that, smaller tiles spread it better over the SMs: 1.03, 1.08 and 1.13
+    // of the bytes at the measured copy rate (149, 156, 163 us against 144 us at 32 rows each).
+    struct Cost { int mb, bn; float c, f, hbm; };
+    static const Cost costs[3] = {{1, 64, 0.37f, 0.65f, 1.03f}, {2, 128, 0.66f, 1.06f, 1.08f}, {2, 256, 1.22f, 2.78f, 1.13f}};
+    constexpr float kHbmBytesPerUs = 6.55e6f;
     const long long items = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : (long long)s.R * s.T * s.K;
     const long long used = min(items, (long long)s.E), mean = (items + s.E - 1) / s.E;
     int v = 0;
@@ -660,7 +663,8 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
         const int per_tile = costs[i].mb * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
         const float tiles = (float)(used * ((mean + costs[i].bn - 1) / costs[i].bn) * ((wide + per_tile - 1) / per_tile));
         const float rounds = tiles > (float)n_sm ? tiles / (float)n_sm + 0.19f : 1.0f;
-        const float cost = rounds * ((float)p.k_blocks * costs[i].c + costs[i].f);
+        const float bytes_us = (float)used * (float)a.channels * (float)a.inner / kHbmBytesPerUs;
+        const float cost = max(rounds * ((float)p.k_blocks * costs[i].c + costs[i].f), bytes_us * costs[i].hbm);
         if (i == 0 || cost < least) {
             least = cost;
             v = i;

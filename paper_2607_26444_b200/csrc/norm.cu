@@ -26,8 +26,8 @@ constexpr size_t kRingBytes = 200 * 1024;  // shared memory of an SM that rows i
 enum QKind { kNoCodes = 0, kInt8 = 1, kE4m3 = 2 };
 
 // Two binary32 values in one register pair: sm_100 multiplies and adds them with one instruction, and these kernels are
-// bound by instruction issue before they are bound by memory (the norm to e4m3 with scalar arithmetic and
-// the row widened element by element: 29 instructions per element, 590 us for 65,536 x 7168; 502 us are the bytes).
+// bound by instruction issue before they are bound by memory (the norm of 65,536 x 7168 to e4m3 with scalar arithmetic took 206
+// warp instructions per 32 vectors and 590 us; with pairs 146, and the bytes at the copy rate are 502 us).
 using Pair = unsigned long long;
 __device__ __forceinline__ Pair make_pair(float lo, float hi)
 {
