@@ -203,12 +203,14 @@ __device__ __forceinline__ void weigh8(const RowParams& p, int c, Pair* y)
 // multiplying by rstd keeps the order, so both statistics come out of one reduction, and the codes need no rstd at all.
 //
 // One row per group of threads, no loop: the hardware deals blocks of up to 256 threads to SMs as they free up, which keeps
-// every SM busy to the end.  h * w waits in registers between the two passes.  65,536 x 7168 with residual to e4m3: 487 us,
-// 520 once the power limit slows the clocks (6.3 TB/s); widening and weighing again in the second pass: 501 and 550;
-// persistent blocks with a ring of bulk copies and ordered claims: 526 and 569 (and 90, not 82 us, at 16,384 x 4096 to bf16).
-// Three blocks per SM (80 registers) with a residual, four (64) without: 178, not 200 us, at 65,536 x 4096 to e4m3.
-template <bool NORM, bool RES, int QK, int MAXT>
-__global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1) row_kernel(const RowParams p)
+// every SM busy to the end.  The row waits in registers between the two passes, as h * w where the codes need that and the
+// registers allow it.  65,536 x 7168 with residual to e4m3: 487 us, 520 once the power limit slows the clocks (6.3 TB/s);
+// widening and weighing again in the second pass: 501 and 550; persistent blocks with a ring of bulk copies and ordered
+// claims: 526 and 569 (and 90, not 82 us, at 16,384 x 4096 to bf16); several rows per block, the next one fetched ahead:
+// 157 to 171 us, not 148, at 131,072 x 2048.  Three blocks per SM (80 registers) with a residual, four (64) without: 178,
+// not 200 us, at 65,536 x 4096 to e4m3.
+template <bool NORM, bool RES, int QK, int VPT, int MAXT>
+__global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : VPT == 8 || (NORM && RES) ? 3 : 4) row_kernel(const RowParams p)
 {
     __shared__ float2 s_part[32];
     const int sub = (int)threadIdx.x / p.tpr, tid = (int)threadIdx.x - sub * p.tpr;
@@ -216,11 +218,11 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1)
     griddep_wait();
     griddep_launch_dependents();
     if (row >= p.rows || (p.n_valid && row >= *p.n_valid)) return;
-    uint4 h[kVpt];                                                   // the row, as stored
+    uint4 h[VPT];                                                   // the row, as stored
     {
         const uint16_t* x = p.x + row * p.x_stride;
 #pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
+        for (int j = 0; j < VPT; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) h[j] = ld_row16(x + (size_t)c * 8);
         }
@@ -228,14 +230,14 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1)
     if constexpr (RES) {
         const uint16_t* res = p.res + row * p.res_stride;
         uint16_t* res_out = p.res_out + row * p.res_out_stride;
-        uint4 r[kVpt];
+        uint4 r[VPT];
 #pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
+        for (int j = 0; j < VPT; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) r[j] = ld_row16(res + (size_t)c * 8);
         }
 #pragma unroll
-        for (int j = 0; j < kVpt; ++j) {
+        for (int j = 0; j < VPT; ++j) {
             const int c = tid + j * p.tpr;
             if (c < p.vecs) {                                        // what is stored is what is normed
                 h[j] = make_uint4(add_bf16x2(h[j].x, r[j].x), add_bf16x2(h[j].y, r[j].y), add_bf16x2(h[j].z, r[j].z),
@@ -244,18 +246,19 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1)
             }
         }
     }
-    Pair squares = 0, kept[kVpt][4];
+    constexpr bool kKeep = QK != kNoCodes && VPT == 4;               // h * w waits in registers, not h
+    Pair squares = 0, kept[kKeep ? VPT : 1][4];
     float top = 0.0f;
 #pragma unroll
-    for (int j = 0; j < kVpt; ++j) {
+    for (int j = 0; j < VPT; ++j) {
         const int c = tid + j * p.tpr;
         if (c < p.vecs) {
-            Pair* y = kept[j];
+            Pair* y = kept[kKeep ? j : 0];
             widen8(h[j], y);
             if constexpr (NORM) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) squares = fma2(y[i], y[i], squares);
-                weigh8(p, c, y);
+                if constexpr (QK != kNoCodes) weigh8(p, c, y);
             }
             if constexpr (QK != kNoCodes) {
 #pragma unroll
@@ -278,10 +281,14 @@ __global__ void __launch_bounds__(MAXT, MAXT == 256 ? (NORM && RES ? 3 : 4) : 1)
     uint8_t* q = p.q + row * p.q_stride;
     uint16_t* out = p.out + row * p.out_stride;
 #pragma unroll
-    for (int j = 0; j < kVpt; ++j) {
+    for (int j = 0; j < VPT; ++j) {
         const int c = tid + j * p.tpr;
         if (c < p.vecs) {
-            Pair* y = kept[j];
+            Pair* y = kept[kKeep ? j : 0];
+            if constexpr (!kKeep) {
+                widen8(h[j], y);
+                if constexpr (NORM) weigh8(p, c, y);
+            }
             if constexpr (QK != kNoCodes) *reinterpret_cast<uint2*>(q + (size_t)c * 8) = codes8<QK>(y, factor2, neg_top2, inv2);
             if constexpr (NORM) {
                 if (QK == kNoCodes || p.out) {
@@ -504,24 +511,43 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) weight_sum_kernel(const f
 struct RowGeom {
     int tpr, threads, groups;          // threads per row, threads per block, rows per block at a time
 };
-// Forward: blocks of 256 threads as far as whole rows fit; backward (`wide` false): one row per block, or eight rows of one warp.
-RowGeom row_geom(int cols, bool wide)
+// Backward pass: one row per block, or eight rows of one warp each.
+RowGeom row_geom(int cols)
 {
     RowGeom g;
     const int vecs = cols / 8;
     g.tpr = ((vecs + kVpt - 1) / kVpt + 31) / 32 * 32;
-    g.groups = g.tpr == 32 ? kMaxGroups : wide && g.tpr <= 128 ? 256 / g.tpr : 1;
+    g.groups = g.tpr == 32 ? kMaxGroups : 1;
     g.threads = g.tpr * g.groups;
     return g;
 }
 
-template <bool NORM, bool RES, int QK>
-cudaError_t run_rows(const RowParams& p, const RowGeom& g, cudaStream_t st)
+template <bool NORM, bool RES, int QK, int VPT>
+cudaError_t run_rows_v(RowParams& p, cudaStream_t st)
 {
-    const long long blocks = (p.rows + g.groups - 1) / g.groups;
+    p.tpr = ((p.vecs + VPT - 1) / VPT + 31) / 32 * 32;
+    const int groups = p.tpr <= 128 ? 256 / p.tpr : 1, threads = p.tpr * groups;
+    const long long blocks = (p.rows + groups - 1) / groups;
     if (blocks >= (1ll << 31)) return cudaErrorInvalidConfiguration;
-    return g.threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, 256>, (unsigned)blocks, g.threads, 0, st, p)
-                            : launch_pdl(row_kernel<NORM, RES, QK, 1024>, (unsigned)blocks, g.threads, 0, st, p);
+    constexpr int kLong = VPT == 8 ? 512 : 1024;
+    return threads <= 256 ? launch_pdl(row_kernel<NORM, RES, QK, VPT, 256>, (unsigned)blocks, threads, 0, st, p)
+                          : launch_pdl(row_kernel<NORM, RES, QK, VPT, kLong>, (unsigned)blocks, threads, 0, st, p);
+}
+
+// Vectors per thread.  Eight put twice the loads of a thread in flight and need fewer warps per row (one up to 2048 columns), four
+// spread a row over more threads and leave room to keep h * w between the passes.  Measured, four against eight, us:
+//   quantiser 131,072 x 2048: 148, 119; 30,000 x 4096: 72, 58; 60,000 x 1024: 34, 36
+//   norm without residual to bf16, 30,000 x 4096: 83, 77; 16,384 x 7168: 86, 73; to e4m3, 30,000 x 4096: 84, 95
+//   norm with residual 30,000 x 4096 to bf16: 147, 150; 20,000 x 8800 (four take blocks of 288 threads): 232, 217
+//   128 rows of 7168 with residual to e4m3 (one wave of blocks, latency): 3.6, 5.3
+template <bool NORM, bool RES, int QK>
+cudaError_t run_rows(RowParams& p, cudaStream_t st)
+{
+    if constexpr (!NORM || RES || QK == kNoCodes) {
+        const int longer = RES ? 8192 / 8 : 1024 / 8;
+        if (p.vecs > longer && p.rows >= 2048) return run_rows_v<NORM, RES, QK, 8>(p, st);
+    }
+    return run_rows_v<NORM, RES, QK, 4>(p, st);
 }
 
 // Row groups of the backward pass: up to four blocks per SM, as long as two rounds of rows (three operands) of each fit
@@ -572,7 +598,6 @@ cudaError_t configure_norm_kernels()
 
 cudaError_t launch_norm(const strata_norm_args& a, cudaStream_t st)
 {
-    const RowGeom g = row_geom(a.cols, true);
     RowParams p{};
     p.x = static_cast<const uint16_t*>(a.x);
     p.res = static_cast<const uint16_t*>(a.residual);
@@ -589,25 +614,23 @@ cudaError_t launch_norm(const strata_norm_args& a, cudaStream_t st)
     p.q_scale_stride = a.q_scale_stride;
     p.rows = a.rows;
     p.vecs = a.cols / 8;
-    p.tpr = g.tpr;
     p.weight_f32 = a.weight_type == STRATA_T_F32;
     p.eps = a.eps;
     p.inv_cols = 1.0f / (float)a.cols;
     const int qk = !a.q ? kNoCodes : a.q_type == STRATA_T_INT8 ? kInt8 : kE4m3;
     if (a.residual)
-        return qk == kNoCodes ? run_rows<true, true, kNoCodes>(p, g, st)
-               : qk == kInt8  ? run_rows<true, true, kInt8>(p, g, st)
-                              : run_rows<true, true, kE4m3>(p, g, st);
-    return qk == kNoCodes ? run_rows<true, false, kNoCodes>(p, g, st)
-           : qk == kInt8  ? run_rows<true, false, kInt8>(p, g, st)
-                          : run_rows<true, false, kE4m3>(p, g, st);
+        return qk == kNoCodes ? run_rows<true, true, kNoCodes>(p, st)
+               : qk == kInt8  ? run_rows<true, true, kInt8>(p, st)
+                              : run_rows<true, true, kE4m3>(p, st);
+    return qk == kNoCodes ? run_rows<true, false, kNoCodes>(p, st)
+           : qk == kInt8  ? run_rows<true, false, kInt8>(p, st)
+                          : run_rows<true, false, kE4m3>(p, st);
 }
 
 cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, int cols, int q_type, void* q,
                             long long q_stride, float* q_scale, long long q_scale_stride, const int32_t* n_valid,
                             cudaStream_t st)
 {
-    const RowGeom g = row_geom(cols, true);
     RowParams p{};
     p.x = static_cast<const uint16_t*>(x);
     p.q = static_cast<uint8_t*>(q);
@@ -618,19 +641,18 @@ cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, i
     p.q_scale_stride = q_scale_stride;
     p.rows = rows;
     p.vecs = cols / 8;
-    p.tpr = g.tpr;
-    return q_type == STRATA_T_INT8 ? run_rows<false, false, kInt8>(p, g, st)
-                                   : run_rows<false, false, kE4m3>(p, g, st);
+    return q_type == STRATA_T_INT8 ? run_rows<false, false, kInt8>(p, st)
+                                   : run_rows<false, false, kE4m3>(p, st);
 }
 
 size_t norm_grad_scratch_bytes(long long rows, int cols, int n_sm)
 {
-    return (size_t)grad_owners(rows, row_geom(cols, false), cols, n_sm) * (size_t)cols * sizeof(float);
+    return (size_t)grad_owners(rows, row_geom(cols), cols, n_sm) * (size_t)cols * sizeof(float);
 }
 
 cudaError_t launch_norm_grad(const strata_norm_grad_args& a, int* status, int n_sm, cudaStream_t st, int* n_launches)
 {
-    const RowGeom g = row_geom(a.cols, false);
+    const RowGeom g = row_geom(a.cols);
     const long long owners = grad_owners(a.rows, g, a.cols, n_sm);
     GradParams p{};
     p.dy = static_cast<const uint16_t*>(a.dy);

@@ -294,8 +294,8 @@ def test_route_grad_skips_what_it_must():
 
 SHAPES = [(1, 8), (1, 7168), (3, 1000), (5, 1024), (7, 1032), (130, 4096), (300, 2048), (2, 8200), (33, 16384), (3, 32768),
           (4000, 64), (2500, 1544)]
-# more rows than the grid holds at once: rows claimed and fetched ahead, of one warp, of a block, of the longest kinds
-RING_SHAPES = [(9001, 64), (6003, 1024), (7000, 1544), (1501, 7168), (701, 16384), (401, 32768)]
+# more rows than the GPU holds at once, of one warp, of part of a block, of a block, of the longest kinds; rows fetched ahead
+RING_SHAPES = [(9001, 64), (6003, 1024), (7000, 1544), (1501, 7168), (701, 16384), (401, 32768), (2049, 8712), (2048, 16648)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
