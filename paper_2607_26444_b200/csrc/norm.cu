@@ -336,8 +336,9 @@ struct GradParams {
 // Backward pass.  A thread keeps the same columns for every row it meets, so its share of dweight stays in
 // registers; each row group writes one partial row, and a second kernel adds the partial rows in a fixed order.
 // (Rows are dealt in equal shares: with claims the order of the sum would change from call to call.)
-// RING: as in the forward pass, but a stage is read in both passes; it is refilled after the next row's reduction, whose
-// barrier every thread reaches only when it is done with the stage.
+// RING: rows arrive by bulk copies ahead of their turn.  A stage is read in both passes over its row; it is refilled after the next
+// row's reduction, behind a barrier of the row's threads (of the warp, where a row has one) that each reaches only when it
+// is done with the stage.
 template <bool RES, bool RING, bool WF32, int MAXT>
 __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(const GradParams p)
 {
@@ -433,7 +434,10 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
         const float2 sq = split(squares), dt = split(dots);
         float sum = sq.x + sq.y, dot = dt.x + dt.y;
         row_reduce<false>(sum, dot, s_part + (phase & 1) * 32, sub, p.tpr);
-        if (RING && tid == 0 && phase > 0 && !*dead) fetch();        // into the stage of the row before this one
+        if constexpr (RING) {
+            __syncwarp();                                            // a row of one warp has met no barrier, and shuffles order no memory
+            if (tid == 0 && phase > 0 && !*dead) fetch();            // into the stage of the row before this one
+        }
         const float rstd = rsqrtf(fmaf(sum, p.inv_cols, p.eps));
         const float mean = dot * rstd * p.inv_cols;                  // mean(g * hat)
         const Pair rstd2 = make_pair(rstd, rstd), neg_mean2 = make_pair(-mean, -mean);

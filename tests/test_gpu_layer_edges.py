@@ -1,0 +1,45 @@
+"""Edges of the layer operators on the GPU.  Helpers and tolerances are those of test_gpu_layer.py."""
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_26444_b200 import binding as B
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import layer_reference as ref  # noqa: E402
+import test_gpu_layer as base  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV, U = base.DEV, base.U
+
+
+# ---- norm --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("rows,cols", [(9001, 64), (9001, 1024), (7000, 1544)])
+@pytest.mark.parametrize("residual", [False, True])
+def test_norm_grad_in_place_with_rows_fetched_ahead(rows, cols, residual):
+    """More rows than the GPU holds at once, so that stages are refilled (in rows of one warp and of several): results that
+    overwrite an operand are those that go elsewhere, time after time, and both are the formula's."""
+    ctx = B.MoEContext(1, 1, 8, 1, 1)
+    g = base.gen(rows + cols)
+    h, dy, r = (base.randn(g, rows, cols).to(torch.bfloat16) for _ in range(3))
+    r = r if residual else None
+    w = 1 + 0.2 * base.randn(g, cols)
+    dx, dw = torch.empty_like(h), torch.empty(cols, device=DEV)
+    ctx.norm_grad(dy, h, w, 1e-6, dx, dw, dresidual=r)
+    want, dwant = ref.norm_grad(base.f64(dy), base.f64(h), base.f64(w), 1e-6, base.f64(r) if residual else None)
+    h64, dy64 = base.f64(h), base.f64(dy)
+    rstd = 1 / np.sqrt((h64 ** 2).mean(1, keepdims=True) + 1e-6)
+    hat, gg = h64 * rstd, np.abs(dy64 * base.f64(w))
+    terms = rstd * (gg + np.abs(hat) * (gg * np.abs(hat)).mean(1, keepdims=True)) + (np.abs(base.f64(r)) if residual else 0)
+    assert np.all(np.abs(base.f64(dx) - want) <= base.half_ulp(want) + 2.0 ** -18 * terms)
+    assert np.all(np.abs(base.f64(dw) - dwant) <= (rows + 8) * U * np.abs(dy64 * hat).sum(0) + 8 * U * np.abs(dwant))
+    for _ in range(8):
+        for target in ("dy", "r") if residual else ("dy",):
+            d2, r2, dw2 = dy.clone(), r.clone() if residual else None, torch.empty_like(dw)
+            out = d2 if target == "dy" else r2
+            ctx.norm_grad(d2, h, w, 1e-6, out, dw2, dresidual=r2)
+            assert torch.equal(out, dx) and torch.equal(dw2, dw)
