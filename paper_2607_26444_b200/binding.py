@@ -490,14 +490,18 @@ def _stride(t, rows: int, cols: int, what: str) -> int:
 
 
 def _scale_stride(t, rows: int) -> int:
-    """Distance of a row's scale to the next one's."""
+    """Distance of a row's scale to the next one's, for at least `rows` fp32 scales that each have a place of their own."""
     n = t.numel()
+    if _types[t.dtype] != STRATA_T_F32:
+        raise ValueError(f"scales are fp32, not {t.dtype}")
+    if n < rows:
+        raise ValueError("one scale per row is needed")
     if t.dim() == 1 or t.is_contiguous():
         stride = t.stride(-1) if t.dim() else 1
     else:
         stride = _strides(t[..., None])[2]
-    if n < rows:
-        raise ValueError("one scale per row is needed")
+    if stride == 0 and rows > 1:
+        raise ValueError("one scale broadcast to all rows (stride 0): pass a tensor that holds one per row")
     return max(1, stride)
 
 
