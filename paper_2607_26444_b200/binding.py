@@ -730,9 +730,11 @@ class MoEContext:
         if not x.is_contiguous():
             x_stride = _strides(x)[2]
         rp = hp = op = qp = sp = q_stride = s_stride = q_type = 0
+        if (residual is None) != (residual_out is None):
+            raise ValueError("residual and residual_out come together")
+        if (q is None) != (q_scale is None):
+            raise ValueError("q comes with q_scale")
         if residual is not None:
-            if residual_out is None:
-                raise ValueError("residual needs residual_out")
             rp, hp = residual.data_ptr(), residual_out.data_ptr()
             if not (residual.numel() == n and residual.is_contiguous() and residual.size(-1) == cols and residual.dtype == dtype):
                 rp, r_stride = _bf16(residual), _stride(residual, rows, cols, "residual")
@@ -744,8 +746,6 @@ class MoEContext:
             if not (out.numel() == n and out.is_contiguous() and out.size(-1) == cols and out.dtype == dtype):
                 op, o_stride = _bf16(out), _stride(out, rows, cols, "out")
         if q is not None:
-            if q_scale is None:
-                raise ValueError("q comes with q_scale")
             qp, q_type, q_stride = q.data_ptr(), _code_type(q), _stride(q, rows, cols, "q")
             sp, s_stride = q_scale.data_ptr(), _scale_stride(q_scale, rows)
         wt = _float_type(weight)

@@ -1,4 +1,6 @@
 """What the torch-level calls of the layer operators refuse before any address reaches the library (no GPU needed)."""
+import types
+
 import pytest
 import torch
 
@@ -22,3 +24,22 @@ def test_broadcast_scales_are_refused():
         B._scale_stride(torch.ones(4, 1).expand(4, 4), 16)
     assert B._scale_stride(torch.ones(1).expand(1), 1) == 1 and B._scale_stride(torch.ones(()), 1) == 1
     assert B._scale_stride(torch.ones(16, 3)[:, 1], 16) == 3 and B._scale_stride(torch.ones(4, 4, 5)[..., 2], 16) == 5
+
+
+def host_context():
+    """The attributes that the calls use, with a library call that must not be reached."""
+    def reached(*args):
+        raise AssertionError("the call reached the library")
+    return types.SimpleNamespace(h=None, _norm=reached, _c=reached, _raw_stream=lambda index: 0, device=torch.device("cuda", 0),
+                                 n_tok=4, n_items=8, E=16)
+
+
+def test_norm_outputs_come_in_pairs():
+    """residual_out without a residual, or a scale without codes, would be left as they were."""
+    x, w = torch.zeros((4, 64), dtype=torch.bfloat16), torch.ones(64)
+    h, scale, q = torch.empty_like(x), torch.empty(4), torch.empty((4, 64), dtype=torch.int8)
+    for kw in (dict(residual_out=h), dict(residual=x), dict(q_scale=scale), dict(q=q)):
+        with pytest.raises(ValueError):
+            B.MoEContext.norm(host_context(), x, w, 1e-6, out=torch.empty_like(x), **kw)
+    with pytest.raises(AssertionError):
+        B.MoEContext.norm(host_context(), x, w, 1e-6, residual=x, residual_out=h, q=q, q_scale=scale)
