@@ -505,13 +505,16 @@ def _scale_stride(t, rows: int) -> int:
     return max(1, stride)
 
 
+_INT32 = -2                          # expert ids: no operand type of the library
+
+
 class _Types(dict):
     """Element types by torch dtype, filled on first use (torch is imported by the callers that need it)."""
 
     def __missing__(self, dtype):
         import torch
         self.update({torch.float32: STRATA_T_F32, torch.bfloat16: STRATA_T_BF16, torch.int16: STRATA_T_BF16,
-                     torch.int8: STRATA_T_INT8, torch.float8_e4m3fn: STRATA_T_E4M3})
+                     torch.int8: STRATA_T_INT8, torch.float8_e4m3fn: STRATA_T_E4M3, torch.int32: _INT32})
         return self.setdefault(dtype, -1)
 
 
@@ -540,10 +543,13 @@ def _bf16(t) -> int:
     return t.data_ptr()
 
 
-def _flat(t, dtype_bytes: int, n: int, what: str) -> int:
-    """Address of a contiguous tensor of n elements."""
-    if t.numel() != n or not t.is_contiguous() or t.element_size() != dtype_bytes:
-        raise ValueError(f"{what}: {n} contiguous elements of {dtype_bytes} bytes are needed")
+_NAMES = {STRATA_T_BF16: "bf16", STRATA_T_F32: "fp32", STRATA_T_INT8: "int8", STRATA_T_E4M3: "e4m3", _INT32: "int32"}
+
+
+def _flat(t, code: int, n: int, what: str) -> int:
+    """Address of a contiguous tensor of n elements of type `code`."""
+    if t.numel() != n or not t.is_contiguous() or _types[t.dtype] != code:
+        raise ValueError(f"{what}: {n} contiguous {_NAMES[code]} elements are needed")
     return t.data_ptr()
 
 
@@ -706,7 +712,8 @@ class MoEContext:
         n = self.n_items
         _check(self._c.strata_moe_route(
             self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, self.n_tok, self.E, "logits"),
-            None if bias is None else _flat(bias, 4, self.E, "bias"), _flat(ids, 4, n, "ids"), _flat(w, 4, n, "w"),
+            None if bias is None else _flat(bias, STRATA_T_F32, self.E, "bias"), _flat(ids, _INT32, n, "ids"),
+            _flat(w, STRATA_T_F32, n, "w"),
             self._stream()), "strata_moe_route")
 
     def route_grad(self, params: strata_route_params, logits, ids, dw, dlogits) -> None:
@@ -716,7 +723,7 @@ class MoEContext:
             raise ValueError("dlogits has the type of logits")
         _check(self._c.strata_moe_route_grad(
             self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, self.n_tok, self.E, "logits"),
-            _flat(ids, 4, n, "ids"), _flat(dw, 4, n, "dw"), dlogits.data_ptr(),
+            _flat(ids, _INT32, n, "ids"), _flat(dw, STRATA_T_F32, n, "dw"), dlogits.data_ptr(),
             _stride(dlogits, self.n_tok, self.E, "dlogits"), self._stream()), "strata_moe_route_grad")
 
     def norm(self, x, weight, eps: float, out=None, residual=None, residual_out=None, q=None, q_scale=None) -> None:
@@ -774,8 +781,8 @@ class MoEContext:
             scratch = self.norm_grad_scratch(rows, cols)
         wt = _float_type(weight)
         _check(self._c.strata_norm_grad(self.h, strata_norm_grad_args(
-            rows, cols, wt, eps, 0, _bf16(dy), _bf16(h), _flat(weight, 4 if wt else 2, cols, "weight"), rp,
-            _bf16(dx), _flat(dweight, 4, cols, "dweight"), scratch.data_ptr(), scratch.nbytes, dy_stride,
+            rows, cols, wt, eps, 0, _bf16(dy), _bf16(h), _flat(weight, wt, cols, "weight"), rp,
+            _bf16(dx), _flat(dweight, STRATA_T_F32, cols, "dweight"), scratch.data_ptr(), scratch.nbytes, dy_stride,
             _stride(h, rows, cols, "h"), r_stride, _stride(dx, rows, cols, "dx")), self._stream()), "strata_norm_grad")
 
     def quantize_rows(self, x, q, q_scale, layout: Optional[Layout] = None) -> None:
@@ -793,10 +800,12 @@ class MoEContext:
         channels = w.size(1)
         if w.dtype != a.dtype or w.dim() != 3:
             raise ValueError("w is [E, channels, inner] of a's type")
+        kind = _code_type(a)
         wide = channels // 2 if gated else channels
         _check(self._c.strata_moe_expert_matmul(self.h, layout.c, strata_matmul_args(
-            _code_type(a), 1 if gated else 0, inner, channels, rows, a.data_ptr(), a_scale.data_ptr(),
-            _flat(w, 1, self.E * channels * inner, "w"), _flat(w_scale, 4, self.E * channels, "w_scale"), _bf16(out),
+            kind, 1 if gated else 0, inner, channels, rows, a.data_ptr(), a_scale.data_ptr(),
+            _flat(w, kind, self.E * channels * inner, "w"), _flat(w_scale, STRATA_T_F32, self.E * channels, "w_scale"),
+            _bf16(out),
             a_stride, _scale_stride(a_scale, rows), _stride(out, rows, wide, "out")), self._stream()),
             "strata_moe_expert_matmul")
 

@@ -30,8 +30,9 @@ def host_context():
     """The attributes that the calls use, with a library call that must not be reached."""
     def reached(*args):
         raise AssertionError("the call reached the library")
-    return types.SimpleNamespace(h=None, _norm=reached, _c=reached, _raw_stream=lambda index: 0, device=torch.device("cuda", 0),
-                                 n_tok=4, n_items=8, E=16)
+    entries = types.SimpleNamespace(strata_moe_route=reached, strata_moe_route_grad=reached)
+    return types.SimpleNamespace(h=None, _norm=reached, _c=entries, _raw_stream=lambda index: 0, _stream=lambda: 0,
+                                 device=torch.device("cuda", 0), n_tok=4, n_items=8, E=16)
 
 
 def test_norm_outputs_come_in_pairs():
@@ -43,3 +44,22 @@ def test_norm_outputs_come_in_pairs():
             B.MoEContext.norm(host_context(), x, w, 1e-6, out=torch.empty_like(x), **kw)
     with pytest.raises(AssertionError):
         B.MoEContext.norm(host_context(), x, w, 1e-6, residual=x, residual_out=h, q=q, q_scale=scale)
+
+
+def test_ids_weights_and_scales_are_of_their_type():
+    """Ids and gate weights have the same shape and element size: swapped, each would be read as the other."""
+    ids, w = torch.zeros((4, 2), dtype=torch.int32), torch.zeros((4, 2))
+    logits = torch.zeros((4, 16))
+    params = B.make_route()
+    for args in ((w, ids), (w, w), (ids, ids), (ids.long(), w), (ids, w.double())):
+        with pytest.raises(ValueError):
+            B.MoEContext.route(host_context(), params, logits, *args)
+        with pytest.raises(ValueError):
+            B.MoEContext.route_grad(host_context(), params, logits, *args, torch.zeros_like(logits))
+    with pytest.raises(ValueError):
+        B.MoEContext.route(host_context(), params, logits, ids, w, bias=torch.zeros(16, dtype=torch.int32))
+    assert B._flat(ids, B._INT32, 8, "ids") == ids.data_ptr() and B._flat(w, B.STRATA_T_F32, 8, "w") == w.data_ptr()
+    with pytest.raises(ValueError):
+        B._float_type(ids)
+    with pytest.raises(ValueError):
+        B._code_type(ids)
