@@ -668,7 +668,10 @@ cudaError_t route_vpl(RouteParams& p, const strata_route_params& r, int n_sm, cu
 {
     const bool by_score = p.bias != nullptr || p.top2;
     constexpr int kVec = BF16 ? 8 : 4;                            // logits in 16 bytes
-    p.fast = !(by_score && r.score == STRATA_SCORE_SOFTMAX);
+    // The shorter way needs every group inside its lanes.  Where the group count is no power of two, lanes stay without a
+    // group, and above 560 experts the others may have more than 32 each: those shapes take the exact path, whose runs cover
+    // all 1,024 whatever the groups.
+    p.fast = !(by_score && r.score == STRATA_SCORE_SOFTMAX) && p.group_size <= p.lanes_per_group * VPL;
     p.run = (p.group_size + p.lanes_per_group - 1) / p.lanes_per_group;
     if (VPL >= kVec) p.run = (p.run + kVec - 1) / kVec * kVec;
     p.fast_vec = p.vec_ok && p.run % kVec == 0 && p.group_size % kVec == 0;
@@ -732,6 +735,7 @@ cudaError_t launch_route(const strata_moe_shape& s, const strata_route_params& r
         case 4: return bf ? route_vpl<4, true>(p, r, n_sm, st) : route_vpl<4, false>(p, r, n_sm, st);
         case 8: return bf ? route_vpl<8, true>(p, r, n_sm, st) : route_vpl<8, false>(p, r, n_sm, st);
         case 16: return bf ? route_vpl<16, true>(p, r, n_sm, st) : route_vpl<16, false>(p, r, n_sm, st);
+        // 32, and what only the exact path holds (see p.fast)
         default: return bf ? route_vpl<32, true>(p, r, n_sm, st) : route_vpl<32, false>(p, r, n_sm, st);
     }
 }

@@ -16,6 +16,25 @@ pytestmark = pytest.mark.gpu
 DEV, U = base.DEV, base.U
 
 
+# ---- router ------------------------------------------------------------------------------------------------------
+
+# Group counts that leave lanes of a warp without a group: a lane would have to hold more than 32 experts.
+WIDE_GROUPS = [(960, 3), (800, 5), (800, 20), (594, 9), (561, 17), (1023, 31)]
+
+
+@pytest.mark.parametrize("n", [7, 5003])
+@pytest.mark.parametrize("E,G", WIDE_GROUPS)
+@pytest.mark.parametrize("score,bias,gs,renorm", [("sigmoid", True, "top2", True), ("sigmoid", False, "max", True),
+                                                  ("softmax", False, "max", False), ("softmax", False, "max", True),
+                                                  ("softmax", True, "max", True)])
+def test_route_considers_every_expert_of_wide_groups(n, E, G, score, bias, gs, renorm):
+    c = dict(n=n, E=E, K=8, score=score, bias=bias, G=G, kg=(G + 1) // 2, gs=gs, renorm=renorm, scale=1.0, dt=torch.float32)
+    ctx, params, logits, b, ids, w = base.route_case(c)
+    ctx.route(params, logits, ids, w, bias=b)
+    assert ctx.device_status() == B.STRATA_OK
+    base.check_route(c, logits, b, ids, w)
+
+
 # ---- norm --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rows,cols", [(9001, 64), (9001, 1024), (7000, 1544)])
