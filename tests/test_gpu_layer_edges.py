@@ -35,6 +35,30 @@ def test_route_considers_every_expert_of_wide_groups(n, E, G, score, bias, gs, r
     base.check_route(c, logits, b, ids, w)
 
 
+# Scores whose sum lies below scale / (largest binary32): sigmoid(-88) = 6.05e-39, so scale / sum is infinite and the weights
+# are not.  Such a score is subnormal: its rounding is within 2^-150, 2^-22 of the smallest here (2.9e-39); exp(88) adds its
+# 2^-23, the sum 1 + exp 2^-24, and the sum of K scores (K - 1) 2^-150 / (K * 2.9e-39) < 2^-22.  A weight is a quotient of two of
+# these, rounded twice: 2 * (2^-22 + 2^-23 + 2^-24) + 2^-22 + 2^-23 < 2^-19.
+TINY = 2.0 ** -19
+
+
+@pytest.mark.parametrize("n", [5, 9501])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("K,scale", [(1, 2.5), (8, 64.0), (8, 1.0), (12, 64.0)])
+def test_route_weights_of_tiny_scores(n, bias, K, scale):
+    E = 64
+    logits = torch.full((n, E), -88.5, device=DEV)
+    logits += 0.5 * torch.rand((n, E), generator=base.gen(3), device=DEV)
+    ctx = B.MoEContext(1, n, 8, E, K)
+    ids, w = torch.empty((n, K), dtype=torch.int32, device=DEV), torch.empty((n, K), device=DEV)
+    b = torch.rand(E, generator=base.gen(4), device=DEV) if bias else None
+    ctx.route(B.make_route("sigmoid", True, scale), logits, ids, w, bias=b)
+    got = base.f64(w)
+    want = ref.route_weights(base.f64(logits), ids.cpu().numpy(), "sigmoid", True, scale)
+    assert np.all(np.isfinite(got))
+    np.testing.assert_allclose(got, want, rtol=TINY)
+
+
 # ---- norm --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rows,cols", [(9001, 64), (9001, 1024), (7000, 1544)])
