@@ -613,15 +613,16 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
         mean = warp_sum(live ? d * softmax_fast(lk, m) * inv : 0.0f);
     } else if constexpr (MODE == kGradSigmoid) {
         const float s = live ? sigmoid_f(lk) : 0.0f;
-        const float slope = live ? s * sigmoid_f(-lk) : 0.0f;     // s * (1 - s) without the cancellation
-        d = p.scale * dw;
+        const float rest = live ? sigmoid_f(-lk) : 0.0f;          // 1 - s without the cancellation
+        d = p.scale * dw * s;
         if (p.renormalise) {
+            // (scale / D) * (dw - dot) * s through the weight s / D: 1 / D overflows where a few tiny scores make up D
             const float total = warp_sum(s);
             const float w = total > 0.0f ? __fdiv_rn(s, total) : 0.0f;
             const float dot = warp_sum(dw * w);
-            d = total > 0.0f ? __fdiv_rn(p.scale * (dw - dot), total) : 0.0f;
+            d = p.scale * (dw - dot) * w;
         }
-        d = live ? d * slope : 0.0f;
+        d *= rest;
     } else {
         m = warp_max(lk);
         float t = live ? softmax_term(lk, m) : 0.0f;

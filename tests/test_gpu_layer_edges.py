@@ -59,6 +59,24 @@ def test_route_weights_of_tiny_scores(n, bias, K, scale):
     np.testing.assert_allclose(got, want, rtol=TINY)
 
 
+@pytest.mark.parametrize("renorm", [True, False])
+def test_route_grad_of_tiny_scores(renorm):
+    n, E, K, scale = 40, 64, 8, 2.5
+    g = base.gen(5)
+    logits = -88.5 + 0.5 * torch.rand((n, E), generator=g, device=DEV)
+    ctx = B.MoEContext(1, n, 8, E, K)
+    ids = torch.argsort(torch.rand((n, E), generator=g, device=DEV), dim=1)[:, :K].to(torch.int32).contiguous()
+    dw = 10 * base.randn(g, n, K)
+    grad = torch.empty_like(logits)
+    ctx.route_grad(B.make_route("sigmoid", renorm, scale), logits, ids, dw, grad)
+    got = base.f64(grad)
+    assert np.all(np.isfinite(got))
+    want = ref.route_grad(base.f64(logits), ids.cpu().numpy().astype(np.int64), base.f64(dw), "sigmoid", renorm, scale)
+    # renormalised: scale * (dw - dot) * weight, terms of scale * max|dw|; otherwise scale * dw * score, subnormal
+    size = scale * float(dw.abs().max())
+    assert np.all(np.abs(got - want) <= (2 * TINY * size if renorm else TINY * np.abs(want) + size * 2.0 ** -148))
+
+
 # ---- norm --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rows,cols", [(9001, 64), (9001, 1024), (7000, 1544)])
