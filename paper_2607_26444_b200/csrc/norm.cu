@@ -299,7 +299,8 @@ __global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : VPT == 8 || (NORM && RE
             }
         }
     }
-    if (QK != kNoCodes && tid == 0) p.q_scale[row * p.q_scale_stride] = __fdiv_rn(top * rstd, QK == kInt8 ? 127.0f : 448.0f);
+    if (QK != kNoCodes && tid == 0)                                  // a zero row has scale 0 also where eps = 0 makes rstd infinite
+        p.q_scale[row * p.q_scale_stride] = top == 0.0f && rstd == INFINITY ? 0.0f : __fdiv_rn(top * rstd, QK == kInt8 ? 127.0f : 448.0f);
 }
 
 constexpr int kMaxStages = 4, kMaxGroups = 8;

@@ -104,3 +104,19 @@ def test_norm_grad_in_place_with_rows_fetched_ahead(rows, cols, residual):
             out = d2 if target == "dy" else r2
             ctx.norm_grad(d2, h, w, 1e-6, out, dw2, dresidual=r2)
             assert torch.equal(out, dx) and torch.equal(dw2, dw)
+
+
+@pytest.mark.parametrize("kind", ["int8", "e4m3"])
+@pytest.mark.parametrize("rows", [3, 2500])
+def test_norm_codes_of_a_zero_row_without_eps(kind, rows):
+    """mean(h^2) + eps = 0: the reciprocal root is infinite, codes and scale of the row are zero all the same."""
+    cols = 1544
+    ctx = B.MoEContext(1, 1, 8, 1, 1)
+    x = base.randn(base.gen(6), rows, cols).to(torch.bfloat16)
+    x[1] = 0
+    weight = torch.ones(cols, device=DEV)
+    for residual in (None, torch.zeros_like(x)):
+        q, scale = torch.empty((rows, cols), dtype=base.CODES[kind], device=DEV), torch.full((rows,), float("nan"), device=DEV)
+        ctx.norm(x, weight, 0.0, residual=residual, residual_out=None if residual is None else torch.empty_like(x), q=q, q_scale=scale)
+        assert not q[1].view(torch.uint8).any() and float(scale[1]) == 0.0
+        assert bool(torch.isfinite(scale).all()) and bool((scale[torch.arange(rows) != 1] > 0).all())
