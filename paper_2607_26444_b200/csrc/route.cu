@@ -16,7 +16,8 @@ struct RouteParams {
     const float* bias;
     int32_t* ids;
     float* w;
-    int n_tok, E, K;
+    unsigned n_tok;        // below 2^31; tokens are counted unsigned, since a warp's stride takes the count past the end
+    int E, K;
     int n_group, topk_group, group_size;
     int renormalise, top2;
     int fast, fast_vec;    // fast = 0: every token takes the exact path
@@ -107,7 +108,7 @@ struct __align__(16) RouteSmem {          // of one warp
 // rounds of a warp-wide maximum take the winners one by one.  1,138 instructions per token at 256 experts in 4 of
 // 8 groups.
 template <int VPL, bool BF16, bool SIGMOID, bool BY_SCORE>
-__device__ __noinline__ void route_exact(const RouteParams& p, int tok, RouteSmem& sm, uint32_t* all)
+__device__ __noinline__ void route_exact(const RouteParams& p, unsigned tok, RouteSmem& sm, uint32_t* all)
 {
     const int lane = (int)threadIdx.x & 31;
     const int e0 = lane * VPL;
@@ -363,8 +364,8 @@ __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) ro
     extern __shared__ uint32_t dyn_keys[];                        // [warps][E], only for groups that split a lane's run
     __shared__ RouteSmem s_route[kRouteWarps];
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int step = (int)gridDim.x * kRouteWarps;
-    int tok = (int)blockIdx.x * kRouteWarps + warp;
+    const unsigned step = gridDim.x * kRouteWarps;
+    unsigned tok = blockIdx.x * kRouteWarps + warp;
     RouteSmem& sm = s_route[warp];
     griddep_wait();
     if (tok >= p.n_tok) return;
@@ -400,7 +401,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) ro
         __syncwarp();                                             // the last batch's candidates have been read
 #pragma unroll 1
         for (int b = 0; b < kBatch; ++b) {
-            const int t = tok + b * step;
+            const unsigned t = tok + b * step;
             if (t >= p.n_tok) {
                 if (mine_b == b) total = -1;
                 break;
@@ -490,7 +491,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32, route_blocks_per_sm(VPL)) ro
             }
         }
         __syncwarp();
-        const int my_tok = tok + mine_b * step;
+        const unsigned my_tok = tok + mine_b * step;
         int id = -1, rank = p.K;
         float lk = 0.0f, s = 0.0f;
         uint32_t key = 0;
@@ -556,7 +557,8 @@ struct RouteGradParams {
     void* dlogits;
     long long dstride;
     int* status;
-    int n_tok, E, K;
+    unsigned n_tok;
+    int E, K;
     int renormalise;
     int vec_ok, dvec_ok;
     float scale;
@@ -573,7 +575,7 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
     extern __shared__ float s_rows[];                             // [warps][32 * VPL]
     constexpr bool kFullRow = MODE == kGradSoftmax;
     const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
-    const int tok = (int)blockIdx.x * kRouteWarps + warp;
+    const unsigned tok = blockIdx.x * kRouteWarps + warp;
     griddep_wait();
     griddep_launch_dependents();
     if (tok >= p.n_tok) return;
@@ -679,10 +681,10 @@ cudaError_t route_vpl(RouteParams& p, const strata_route_params& r, int n_sm, cu
     p.run = (p.group_size + p.lanes_per_group - 1) / p.lanes_per_group;
     if (VPL >= kVec) p.run = (p.run + kVec - 1) / kVec * kVec;
     p.fast_vec = p.vec_ok && p.run % kVec == 0 && p.group_size % kVec == 0;
-    const unsigned grid = (unsigned)min((p.n_tok + kRouteWarps - 1) / kRouteWarps, n_sm * route_blocks_per_sm(VPL));
+    const unsigned grid = min((p.n_tok + kRouteWarps - 1) / kRouteWarps, (unsigned)(n_sm * route_blocks_per_sm(VPL)));
     const size_t smem = p.n_group > 1 && p.group_size % VPL != 0 ? (size_t)kRouteWarps * p.E * sizeof(uint32_t) : 0;
     // two tokens per batch where their candidates (about K + 2) fit 16 lanes, and where a warp has two tokens at all
-    const bool pairs = VPL <= 8 && p.K <= 8 && p.n_tok > (int)grid * kRouteWarps;
+    const bool pairs = VPL <= 8 && p.K <= 8 && p.n_tok > grid * kRouteWarps;
     constexpr int kPairCap = VPL <= 8 ? 16 : 32;
 #define STRATA_ROUTE(SIG, BY)                                                                                            \
     (pairs ? launch_pdl(route_kernel<VPL, BF16, SIG, BY, kPairCap>, grid, kRouteWarps * 32, smem, st, p)                 \
@@ -695,7 +697,7 @@ cudaError_t route_vpl(RouteParams& p, const strata_route_params& r, int n_sm, cu
 template <int VPL, bool BF16>
 cudaError_t route_grad_vpl(const RouteGradParams& p, const strata_route_params& r, cudaStream_t st)
 {
-    const unsigned grid = (unsigned)((p.n_tok + kRouteWarps - 1) / kRouteWarps);
+    const unsigned grid = (p.n_tok + kRouteWarps - 1) / kRouteWarps;
     const size_t smem = (size_t)kRouteWarps * 32 * VPL * sizeof(float);
     if (r.score == STRATA_SCORE_SIGMOID)
         return launch_pdl(route_grad_kernel<VPL, BF16, kGradSigmoid>, grid, kRouteWarps * 32, smem, st, p);
@@ -720,7 +722,7 @@ cudaError_t launch_route(const strata_moe_shape& s, const strata_route_params& r
     p.bias = bias;
     p.ids = ids;
     p.w = w;
-    p.n_tok = s.R * s.T;
+    p.n_tok = (unsigned)s.R * (unsigned)s.T;
     p.E = s.E;
     p.K = s.K;
     p.n_group = r.n_group;
@@ -756,7 +758,7 @@ cudaError_t launch_route_grad(const strata_moe_shape& s, const strata_route_para
     p.dlogits = dlogits;
     p.dstride = dstride;
     p.status = status;
-    p.n_tok = s.R * s.T;
+    p.n_tok = (unsigned)s.R * (unsigned)s.T;
     p.E = s.E;
     p.K = s.K;
     p.vec_ok = rows_on_16(logits, stride, type);

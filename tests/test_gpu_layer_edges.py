@@ -77,6 +77,31 @@ def test_route_grad_of_tiny_scores(renorm):
     assert np.all(np.abs(got - want) <= (2 * TINY * size if renorm else TINY * np.abs(want) + size * 2.0 ** -148))
 
 
+def test_route_of_almost_two_to_the_31_tokens():
+    """The strides of warps take the token count past 2^31.  26 to 35 GB in use, a second or two."""
+    R, T, E, K = 2, 2 ** 30 - 1, 2, 1
+    ctx = B.MoEContext(R, T, 8, E, K)
+    n = R * T
+    logits = torch.zeros((n, E), dtype=torch.bfloat16, device=DEV)
+    logits[::3, 1] = 1.0
+    ids = torch.full((n, K), -7, dtype=torch.int32, device=DEV)
+    w = torch.full((n, K), -7.0, device=DEV)
+    ctx.route(B.make_route("softmax"), logits, ids, w)
+    assert ctx.device_status() == B.STRATA_OK
+    ones = (n + 2) // 3
+    assert bool((ids[::3] == 1).all()) and int(ids.sum(dtype=torch.int64)) == ones and int(ids.min()) == 0
+    assert float(w.min()) == 1.0 and float(w.max()) == 1.0
+    grad = torch.full_like(logits, float("nan"))
+    ctx.route_grad(B.make_route("sigmoid", False, 4.0), logits, ids, w, grad)     # 4 s (1 - s): 1 at a logit of 0, 0.7864 at 1
+    assert ctx.device_status() == B.STRATA_OK
+    want = torch.tensor(4 * 0.7310585786 * (1 - 0.7310585786), device=DEV).to(torch.bfloat16)
+    assert bool((grad[::3, 1] == want).all()) and bool((grad[::3, 0] == 0).all())
+    assert bool((grad[1::3, 0] == 1).all()) and bool((grad[2::3, 0] == 1).all()) and float(grad[:, 1].max()) == float(want)
+    assert not bool(grad[1::3, 1].any()) and not bool(grad[2::3, 1].any())
+    del ctx, logits, ids, w, grad
+    torch.cuda.empty_cache()
+
+
 # ---- norm --------------------------------------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rows,cols", [(9001, 64), (9001, 1024), (7000, 1544)])
