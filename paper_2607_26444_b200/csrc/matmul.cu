@@ -165,6 +165,11 @@ __device__ __forceinline__ void tmem_ld_wait(uint32_t (&r)[16])
 __device__ __forceinline__ void tmem_fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void tmem_fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 
+// Row tiles of `height` over `rows` rows, without the sum that passes 2^31 - 1 where one expert holds nearly as many.
+__host__ __device__ constexpr int tiles_of(int rows, int height) { return rows / height + (rows % height != 0 ? 1 : 0); }
+static_assert(tiles_of(0, 256) == 0 && tiles_of(1, 64) == 1 && tiles_of(64, 64) == 1 && tiles_of(65, 64) == 2, "");
+static_assert(tiles_of(2147483647, 256) == 8388608 && tiles_of(2147483647, 64) == 33554432, "");
+
 struct Work {
     int e, m, row0, rows;               // expert, channel tile, first receive row, rows of the tile
 };
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
     if (warp == 0) {                                                 // prefix of row tiles
         int carry = 0;
         for (int e0 = 0; e0 < p.E; e0 += 32) {
-            const int own = e0 + lane < p.E ? (s_cnt[e0 + lane] + BN - 1) / BN : 0;
+            const int own = e0 + lane < p.E ? tiles_of(s_cnt[e0 + lane], BN) : 0;
             int v = own;
 #pragma unroll
             for (int o = 1; o < 32; o <<= 1) {
