@@ -201,9 +201,11 @@ __device__ __forceinline__ Work find_work(unsigned t, const int* s_base, const i
 }
 
 // Whether both warps of an exchanging pair go on: one vote for all 64 threads, so that neither waits for the other in vain.
+// The vote asks for converged warps, which lanes that left a wait one by one need not be.
 __device__ __forceinline__ bool pair_all(bool ok, int pair)
 {
     uint32_t r;
+    __syncwarp();
     asm volatile(
         "{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\t"
         "bar.red.and.pred q, %2, 64, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
@@ -462,6 +464,7 @@ __global__ void __launch_bounds__(Tile<MB, BN>::threads, 1) expert_matmul_kernel
             uint16_t* out = p.out + (long long)(w.row0 + col0) * p.out_stride;
             int phase = 0;
             for (int c0 = 0; c0 < rows; c0 += 16, phase ^= 1) {
+                __syncwarp();                                        // loads from TMEM ask for converged warps: waits and stores part them
                 float sc[16];
 #pragma unroll
                 for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(&sc[c]) = *reinterpret_cast<const float4*>(&scale[c0 + c]);
