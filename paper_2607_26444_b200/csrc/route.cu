@@ -44,8 +44,13 @@ __device__ __forceinline__ float sigmoid_f(float l) { return __frcp_rn(__fadd_rn
 // exp(l - m) for l <= m; infinities at the maximum count as equal to it
 __device__ __forceinline__ float softmax_term(float l, float m) { return l == m ? 1.0f : expf(l - m); }
 
-// the same through the hardware's power of two: 2^-22 relative and the rounding of its argument, for gradients
-__device__ __forceinline__ float softmax_fast(float l, float m) { return l == m ? 1.0f : __expf(l - m); }
+// The same for gradients.  A bf16 gradient takes the hardware's power of two, whose argument l * log2(e) is rounded: within
+// 2^-22 + |l - m| 2^-23 relative, 2^-16 where the term is still a normal number, against 2^-9 of the result's own rounding.
+template <bool BF16>
+__device__ __forceinline__ float softmax_grad_term(float l, float m)
+{
+    return l == m ? 1.0f : BF16 ? __expf(l - m) : expf(l - m);
+}
 
 __device__ __forceinline__ float warp_sum(float v)
 {
@@ -606,13 +611,13 @@ __global__ void __launch_bounds__(kRouteWarps * 32) route_grad_kernel(const Rout
         float s = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            l[i] = l[i] == -INFINITY ? 0.0f : softmax_fast(l[i], m);
+            l[i] = l[i] == -INFINITY ? 0.0f : softmax_grad_term<BF16>(l[i], m);
             s += l[i];
         }
         s = warp_sum(s);
         inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
         d = p.scale * dw;
-        mean = warp_sum(live ? d * softmax_fast(lk, m) * inv : 0.0f);
+        mean = warp_sum(live ? d * softmax_grad_term<BF16>(lk, m) * inv : 0.0f);
     } else if constexpr (MODE == kGradSigmoid) {
         const float s = live ? sigmoid_f(lk) : 0.0f;
         const float rest = live ? sigmoid_f(-lk) : 0.0f;          // 1 - s without the cancellation

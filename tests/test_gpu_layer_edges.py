@@ -77,6 +77,27 @@ def test_route_grad_of_tiny_scores(renorm):
     assert np.all(np.abs(got - want) <= (2 * TINY * size if renorm else TINY * np.abs(want) + size * 2.0 ** -148))
 
 
+def test_route_grad_of_fp32_logits_keeps_the_exponential_exact():
+    """Far below the largest logit too.  Whole logits, so that differences are exact; of the experts that were not chosen, so that
+    nothing cancels: -s_e * d * s_k.  Relative error, K = 1: expf within 2 ulp (2^-22) in s_e, s_k and each sum; a sum of E/32
+    + 5 terms and its reciprocal, twice; five products: 4 * 2^-22 + (2 * (1 + 5 + 1) + 5) * 2^-24 = 35 u."""
+    n, E = 4000, 32
+    g = base.gen(8)
+    logits = torch.randint(-80, 1, (n, E), generator=g, device=DEV).float()
+    logits[:, 0] = 0
+    ids = torch.randint(1, E, (n, 1), generator=g, device=DEV).to(torch.int32)
+    logits.scatter_(1, ids.long(), -torch.randint(0, 4, (n, 1), generator=g, device=DEV).float())
+    dw = torch.ones((n, 1), device=DEV)
+    grad = torch.empty_like(logits)
+    ctx = B.MoEContext(1, n, 8, E, 1)
+    ctx.route_grad(B.make_route("softmax", False), logits, ids, dw, grad)
+    i64 = ids.cpu().numpy().astype(np.int64)
+    want, got = ref.route_grad(base.f64(logits), i64, base.f64(dw), "softmax", False, 1.0), base.f64(grad)
+    np.put_along_axis(want, i64, 1.0, 1)
+    np.put_along_axis(got, i64, 1.0, 1)
+    np.testing.assert_allclose(got, want, rtol=35 * U)
+
+
 def test_route_of_almost_two_to_the_31_tokens():
     """The strides of warps take the token count past 2^31.  26 to 35 GB in use, a second or two."""
     R, T, E, K = 2, 2 ** 30 - 1, 2, 1
