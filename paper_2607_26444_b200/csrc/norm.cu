@@ -541,16 +541,24 @@ cudaError_t run_rows_v(RowParams& p, cudaStream_t st)
 
 // Vectors per thread.  Eight put twice the loads of a thread in flight and need fewer warps per row (one up to 2048 columns), four
 // spread a row over more threads and leave room to keep h * w between the passes.  Measured, four against eight, us:
-//   quantiser 131,072 x 2048: 148, 119; 30,000 x 4096: 72, 58; 60,000 x 1024: 34, 36
-//   norm without residual to bf16, 30,000 x 4096: 83, 77; 16,384 x 7168: 86, 73; to e4m3, 30,000 x 4096: 84, 95
-//   norm with residual 30,000 x 4096 to bf16: 147, 150; 20,000 x 8800 (four take blocks of 288 threads): 232, 217
-//   128 rows of 7168 with residual to e4m3 (one wave of blocks, latency): 3.6, 5.3
+//   quantiser, eight above 1024 columns: 65,280 x 2056: 119, 87 (half of eight's places hold anything, two thirds of four's);
+//     51,622 x 2600: 100, 77; 32,768 x 4096: 78, 63; 32,704 x 4104: 118, 84; 16,368 x 8200: 97, 85; 4096 x 32768: 110, 70
+//   norm without residual to bf16, the same except from 8200 to 10,240 columns: 65,280 x 2056: 138, 100; 32,768 x 4096: 93, 82;
+//     18,724 x 7168: 98, 81; 16,368 x 8200: 100, 102; 2048 x 8200: 14, 15; 13,107 x 10,240: 89, 90; 10,922 x 12,288: 96, 85
+//   norm without residual to e4m3, four: 65,536 x 2048: 90, 97; 16,384 x 8192: 93, 102
+//   norm with residual to bf16, four: 16,368 x 8200: 162, 179; 8065 x 16,640: 160, 209; 8192 x 16,384: 160, 162
+//   norm with residual to e4m3, eight from 10,248 to 16,384 columns: 4096 x 12,288: 68, 62; 8192 x 12,288: 130, 114; 8192 x 16,384: 160, 152;
+//     outside four: 16,368 x 8200: 175, 174; 2048 x 8200: 24, 26; 18,724 x 7168: 147, 160; 8065 x 16,640: 230, 251
+//   few rows, four: 128 rows of 7168 with residual to e4m3 (one wave of blocks, latency): 3.6, 5.3; with residual to e4m3 2048 x 16,384:
+//     46.0, 46.5; from 2048 rows without one: 2048 x 7168: 10.7, 9.0 (quantiser), 12.6, 11.0 (norm); 2048 x 1032: 8.2, 8.4 and 7.0, 7.1
 template <bool NORM, bool RES, int QK>
 cudaError_t run_rows(RowParams& p, cudaStream_t st)
 {
-    if constexpr (!NORM || RES || QK == kNoCodes) {
-        const int longer = RES ? 8192 / 8 : 1024 / 8;
-        if (p.vecs > longer && p.rows >= 2048) return run_rows_v<NORM, RES, QK, 8>(p, st);
+    if constexpr (NORM && RES && QK != kNoCodes) {
+        if (p.vecs > 10240 / 8 && p.vecs <= 16384 / 8 && p.rows >= 4096) return run_rows_v<NORM, RES, QK, 8>(p, st);
+    } else if constexpr (!NORM || (!RES && QK == kNoCodes)) {
+        const bool four = NORM && p.vecs > 8192 / 8 && p.vecs <= 10240 / 8;
+        if (p.vecs > 1024 / 8 && p.rows >= 2048 && !four) return run_rows_v<NORM, RES, QK, 8>(p, st);
     }
     return run_rows_v<NORM, RES, QK, 4>(p, st);
 }

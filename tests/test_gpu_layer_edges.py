@@ -166,3 +166,12 @@ def test_norm_codes_of_a_zero_row_without_eps(kind, rows):
         ctx.norm(x, weight, 0.0, residual=residual, residual_out=None if residual is None else torch.empty_like(x), q=q, q_scale=scale)
         assert not q[1].view(torch.uint8).any() and float(scale[1]) == 0.0
         assert bool(torch.isfinite(scale).all()) and bool((scale[torch.arange(rows) != 1] > 0).all())
+
+
+# Long rows in both kinds of threads: the rule's edges in columns and rows.
+@pytest.mark.parametrize("rows,cols,residual,out", [
+    (4096, 10240, True, "e4m3"), (4096, 10248, True, "int8"), (4096, 10248, True, "both"), (4095, 10248, True, "e4m3"),
+    (4097, 16384, True, "e4m3"), (4096, 16392, True, "int8"), (2048, 8192, False, "bf16"), (2048, 8200, False, "bf16"),
+    (2048, 10248, False, "bf16"), (2048, 10248, True, "bf16")])
+def test_norm_of_long_rows(rows, cols, residual, out):
+    base.test_norm_against_64_bits(rows, cols, residual, out)
