@@ -23,6 +23,19 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
                                  int* status, WorkQueue wq, int n_sm, cudaStream_t st);
 
 #ifdef __CUDACC__
+// A wait with a limit.  False if it ran out, here or in another thread of the block (`dead`, in shared memory): the status then
+// tells that the results are void, and every role of the block leaves its loop.
+__device__ __forceinline__ bool wait_or_dead(uint64_t* bar, uint32_t parity, volatile int* dead, int* status)
+{
+    for (uint32_t it = 0; it < (uint32_t)(STRATA_WAIT_LIMIT); ++it) {
+        if (mbar_try_wait(bar, parity)) return true;
+        if (*dead) return false;
+    }
+    *dead = 1;
+    report_status(status, STRATA_ERR_TIMEOUT);
+    return false;
+}
+
 __device__ __forceinline__ void unpack_bf16x8(uint4 v, float* f)
 {
     const uint32_t u[4] = {v.x, v.y, v.z, v.w};

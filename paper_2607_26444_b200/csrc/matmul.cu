@@ -77,18 +77,6 @@ struct SmemTail {                       // behind the operand stages
 };
 static_assert(sizeof(SmemTail) % 16 == 0, "the scales behind it are read in vectors");
 
-// ---- waits with a limit: a wait that runs out sets the status and makes every role of the CTA leave its loop ----
-__device__ __forceinline__ bool wait_or_dead(uint64_t* bar, uint32_t parity, volatile int* dead, int* status)
-{
-    for (uint32_t it = 0; it < (uint32_t)(STRATA_WAIT_LIMIT); ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*dead) return false;
-    }
-    *dead = 1;
-    report_status(status, STRATA_ERR_TIMEOUT);
-    return false;
-}
-
 __device__ __forceinline__ void mbar_arrive(uint64_t* bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(smem_addr(bar)) : "memory");

@@ -305,18 +305,6 @@ __global__ void __launch_bounds__(MAXT, MAXT > 256 ? 1 : VPT == 8 || (NORM && RE
 
 constexpr int kMaxStages = 4, kMaxGroups = 8;
 
-// False if the wait ran out, here or in another thread of the block: the status tells that the results are void.
-__device__ __forceinline__ bool ring_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status)
-{
-    for (uint32_t it = 0; it < (uint32_t)(STRATA_WAIT_LIMIT); ++it) {
-        if (mbar_try_wait(bar, parity)) return true;
-        if (*dead) return false;
-    }
-    *dead = 1;
-    report_status(status, STRATA_ERR_TIMEOUT);
-    return false;
-}
-
 struct GradParams {
     const uint16_t* dy;
     const uint16_t* h;
@@ -399,7 +387,7 @@ __global__ void __launch_bounds__(MAXT, MAXT == 128 ? 4 : 1) norm_grad_kernel(co
         const unsigned char* src = my_ring + (size_t)stage * stage_bytes;
         uint4 hv[kVpt], dv[kVpt], rv[kVpt];                          // without a ring; with one they are read where they lie
         if constexpr (RING) {
-            ring_wait(&s_full[sub][stage], parity, &s_dead, p.status);
+            wait_or_dead(&s_full[sub][stage], parity, &s_dead, p.status);
         } else {
 #pragma unroll
             for (int j = 0; j < kVpt; ++j) {
