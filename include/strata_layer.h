@@ -9,6 +9,13 @@
  * a "stride" is the distance between two rows, in elements of that tensor, and may exceed the row's length.
  * Rounding to bf16 and to 8-bit codes is to nearest, ties to even.  All sums, norms, softmax statistics and
  * scales are binary32 (the products of int8 rows accumulate in int32, exactly).
+ * Functions and quotients inside are binary32 as well.  Where they are coarser than expf and a rounded quotient (by CUDA's
+ * bounds, in units of the last place of binary32): the gradient of softmax weights that are not renormalised, for bf16
+ * logits: an exponential within 2 + 1.2 |l - max|; silu in a gated product: an exponential within 2 + 1.2 |g| and a division within
+ * 2, and zero where g is below -87.3; the norm's gradient: a reciprocal square root within 2.  The router decides a token
+ * in one of two ways, whose weights may differ in the last places.
+ * The order of a row's sums depends on the rows and columns of the call: equal calls give equal bits, but the last bit of a row's norm
+ * may differ between a call that holds it among few rows and one that holds it among many.
  */
 #ifndef STRATA_LAYER_H
 #define STRATA_LAYER_H
@@ -77,10 +84,12 @@ strata_status strata_moe_route_grad(strata_ctx *ctx, const strata_route_params *
  * y = (h * weight) * rstd,  rstd = 1 / sqrt(mean(h^2) + eps): the mean is of h as it is stored
  * out  (bf16) = bf16(y), if given
  * q (8 bits)  = codes of y * limit / max|y|, q_scale[row] = max|y| / limit, limit = 127 (int8) or 448 (e4m3), if
- *               given: y is about code * q_scale.  The quotient is one correctly rounded binary32 value before it
- *               becomes a code, so half-way cases go to the even code.  Codes of an all-zero row are zero with scale 0.
+ *               given: y is about code * q_scale.  With bf16 weights the quotient is one correctly rounded binary32 value
+ *               before it becomes a code, so half-way cases go to the even code; with float weights h * weight and its multiple
+ *               by limit are rounded first, 2^-23 relative in all.  Codes of an all-zero row are zero with scale 0, whatever eps.
  *               Codes are of y, not of bf16(y); they do not depend on rstd, which cancels.
- * NaN and infinities follow the formula in `out`; codes and scale of a row that holds one are unspecified.
+ * NaN and infinities follow the formula in `out` (eps = 0 makes rstd infinite where the squares sum to zero or underflow to it);
+ * codes and scale of a row that holds one are unspecified.
  * x, residual, residual_out, out: device bf16, 16-byte aligned, strides multiples of 8; weight: device bf16 or float
  * [cols], 16-byte aligned; q: 8-byte aligned, stride a multiple of 8; q_scale: element `row` at q_scale[row *
  * q_scale_stride].  cols: a multiple of 8, at most 32768.  rows may be 0 (nothing is launched, row
@@ -130,7 +139,7 @@ strata_status strata_norm_grad_scratch_bytes(strata_ctx *ctx, int64_t rows, int3
 strata_status strata_norm_grad(strata_ctx *ctx, const strata_norm_grad_args *args, void *stream);
 
 /* ---- rows to 8 bits -----------------------------------------------------------------------------------------
- * q = codes of x * limit / max|x|, q_scale[row] = max|x| / limit, as in strata_norm.  n_valid: device int32, or NULL;
+ * q = codes of x * limit / max|x|, q_scale[row] = max|x| / limit, as in strata_norm with a weight of 1.  n_valid: device int32, or NULL;
  * if given, only rows below *n_valid are read and written (expert_offset + E of a layout: the rows in use of a
  * receive buffer).  Alignments, strides and limits as in strata_norm.  One launch. */
 strata_status strata_quantize_rows(strata_ctx *ctx, const void *x, int64_t x_stride, int64_t rows, int32_t cols,
@@ -139,7 +148,7 @@ strata_status strata_quantize_rows(strata_ctx *ctx, const void *x, int64_t x_str
 
 /* ---- the experts' products ------------------------------------------------------------------------------------
  * For every expert e and every row r of its segment (expert_offset[e] .. + expert_count[e] of the layout; all
- * R*slot_capacity rows of the segment in the fixed-capacity layout):
+ * R*slot_capacity rows of the segment in the fixed-capacity layout, empty slots too):
  *   y[r, n] = (sum_k a[r,k] * w[e,n,k]) * (a_scale[r] * w_scale[e,n])
  *   out[r, n] = bf16(y[r, n])                                             n < channels, or
  *   out[r, n] = bf16(silu(y[r, n]) * y[r, channels/2 + n])                n < channels/2, if gated

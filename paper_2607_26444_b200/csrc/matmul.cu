@@ -208,6 +208,8 @@ __device__ __forceinline__ float acc_value(uint32_t v)
 {
     return INT8 ? __int2float_rn((int)v) : __uint_as_float(v);
 }
+// silu(g) * u.  The exponential is within 2 + 1.2 |g| ulp (CUDA's bound for __expf), 2^-16 at the most, and the division within 2, against
+// the result's own 2^-9; where 1 + exp(-g) passes 2^126 (g < -87.3) the quotient is zero instead of below 2^-119.
 __device__ __forceinline__ float gate_mul(float g, float u) { return __fdividef(g, 1.0f + __expf(-g)) * u; }
 
 // N columns of 32 channels, lane = channel `ch`: neighbouring lanes exchange, so that one holds two channels of column c and
@@ -648,6 +650,9 @@ cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_lay
     // <1,64> 45 us, <2,128> 42 us; 32 rows each 149, 156 (<2,256> 163); 128 rows 337, 185, 178; 512 rows 1149, 469, 396.
     // Where the weights' way from HBM takes longer than that, smaller tiles spread it better over the SMs: 1.03, 1.08 and 1.13
     // of the bytes at the measured copy rate (149, 156, 163 us against 144 us at 32 rows each).
+    // What the estimate does not see: rows spread around their mean (at a multiple of the height half of the experts spill into one
+    // more tile), that a partly filled tile takes fewer matrix cycles (at 128 rows each it says 155 and 259 us for the two larger
+    // ones, and takes the one that is 4 % slower), and slots that are masked or unrouted (a call's rows are known on the device only).
     struct Cost { int mb, bn; float c, f, hbm; };
     static const Cost costs[3] = {{1, 64, 0.37f, 0.65f, 1.03f}, {2, 128, 0.66f, 1.06f, 1.08f}, {2, 256, 1.22f, 2.78f, 1.13f}};
     constexpr float kHbmBytesPerUs = 6.55e6f;

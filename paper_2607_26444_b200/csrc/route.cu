@@ -1,6 +1,7 @@
 // Router: logits -> top-k expert ids and gate weights, and the gradient of the logits (strata_layer.h has the
-// formulas).  One warp owns one token; lane q holds the logits of experts q*VPL .. q*VPL + VPL-1 in registers, so the
-// order (lane, register) is the order of expert indexes and "ties to the lower index" needs no index in the key.
+// formulas).  One warp owns one token; a lane holds up to VPL logits of neighbouring experts in registers, lanes in the order of
+// the experts, so the order (lane, register) is the order of expert indexes and "ties to the lower index" needs no
+// index in the key.
 #include "layer.cuh"
 
 namespace strata {
@@ -44,8 +45,8 @@ __device__ __forceinline__ float sigmoid_f(float l) { return __frcp_rn(__fadd_rn
 // exp(l - m) for l <= m; infinities at the maximum count as equal to it
 __device__ __forceinline__ float softmax_term(float l, float m) { return l == m ? 1.0f : expf(l - m); }
 
-// The same for gradients.  A bf16 gradient takes the hardware's power of two, whose argument l * log2(e) is rounded: within
-// 2^-22 + |l - m| 2^-23 relative, 2^-16 where the term is still a normal number, against 2^-9 of the result's own rounding.
+// The same for gradients.  A bf16 gradient takes the hardware's power of two, whose argument is rounded: within 2 + 1.2 |l - m| ulp
+// (CUDA's bound for __expf), 2^-16 where the term is still a normal number, against 2^-9 of the result's own rounding.
 template <bool BF16>
 __device__ __forceinline__ float softmax_grad_term(float l, float m)
 {
