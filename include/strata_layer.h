@@ -43,11 +43,12 @@ typedef enum {
  *          (STRATA_GROUP_MAX) or the sum of its two largest (STRATA_GROUP_TOP2); the topk_group best groups
  *          stay, ties to the lower group
  * ids      the K experts of largest c, in decreasing order, ties to the lower index
- * weights  w_k = scale * s[id_k], divided by the sum of the token's K scores if renormalise is set
+ * weights  w_k = scale * s[id_k], divided by the sum of the token's K scores if renormalise is set (for the softmax: scale times
+ *          the softmax over the chosen logits, so that chosen scores below the range of binary32 count as well)
  * An expert whose logit (or whose choice) is NaN or -inf is never chosen, and a NaN or -inf logit counts as a
  * score of zero in the softmax.  A token with fewer than K such experts left gets id -1 and weight 0 in its last
- * slots (the layout treats -1 as "not routed" under STRATA_FLAG_ALLOW_UNROUTED).  If every chosen score is zero,
- * renormalised weights are zero. */
+ * slots (the layout treats -1 as "not routed" under STRATA_FLAG_ALLOW_UNROUTED).  If every chosen sigmoid score is
+ * zero, renormalised weights are zero. */
 #define STRATA_SCORE_SOFTMAX 0
 #define STRATA_SCORE_SIGMOID 1
 #define STRATA_GROUP_MAX 0
@@ -72,7 +73,7 @@ strata_status strata_moe_route(strata_ctx *ctx, const strata_route_params *param
  *   d_k = scale * dw_k, or with renormalised weights (scale / D) * (dw_k - sum_j dw_j s_j / D), D = sum_j s_j
  *   sigmoid: dlogit = d * s * (1 - s);  softmax: dlogit_e = s_e * (d_e - sum_k d_k s_k), d_e = 0 if not chosen
  * topk_ids are the forward call's; -1 is skipped, a repeated id adds up, an id outside [0,E) is skipped and
- * raises BAD_EXPERT_ID.  If D is zero the gradient is zero; a NaN or -inf logit gets zero.  dlogits has the
+ * raises BAD_EXPERT_ID.  If D is zero (sigmoid) the gradient is zero; a NaN or -inf logit gets zero.  dlogits has the
  * type of logits and row stride dlogits_stride; every element of its rows is written.  Needs a workspace (the
  * status word).  One launch. */
 strata_status strata_moe_route_grad(strata_ctx *ctx, const strata_route_params *params, const void *logits,

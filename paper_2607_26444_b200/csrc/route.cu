@@ -289,6 +289,8 @@ __device__ __noinline__ void route_exact(const RouteParams& p, unsigned tok, Rou
         }
     }
     const bool sel = rank < p.K;
+    if constexpr (!SIGMOID)
+        if (p.renormalise) m = warp_max(sel ? lk : -INFINITY);    // weights among the chosen only; a bias or sums may leave the largest out
     float s = 0.0f;
     if (sel) {
         if constexpr (SIGMOID) s = sigmoid_f(lk);

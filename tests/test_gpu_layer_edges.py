@@ -98,6 +98,36 @@ def test_route_grad_of_fp32_logits_keeps_the_exponential_exact():
     np.testing.assert_allclose(got, want, rtol=35 * U)
 
 
+@pytest.mark.parametrize("n", [6, 9501])
+@pytest.mark.parametrize("groups,K", [((1, 1, "max"), 8), ((8, 2, "top2"), 8), ((4, 1, "max"), 3)])
+@pytest.mark.parametrize("depth", [90.0, 300.0, 3.0e38])
+def test_route_renormalised_softmax_far_below_an_expert_that_is_not_chosen(n, groups, K, depth):
+    """The bias chooses experts whose scores are subnormal or zero beside that of the largest logit: their weights are the
+    softmax over the chosen logits all the same, and the gradient is that of these weights.  Relative error of a weight as in
+    test_gpu_layer.py with |l - max| <= 8: 2 u (K + 8 + 8)."""
+    E, scale = 64, 1.5
+    g = base.gen(9)
+    logits = 4 * torch.rand((n, E), generator=g, device=DEV)
+    b = torch.zeros(E, device=DEV)
+    b[16:32] = 4.0 + torch.rand(16, generator=g, device=DEV)       # two of the eight groups, one of the four
+    logits[:, 16:32] = logits[:, 16:32] - depth                     # at 3e38 all of them are equal
+    ctx = B.MoEContext(1, n, 8, E, K)
+    params = B.make_route("softmax", True, scale, *groups)
+    ids, w = torch.empty((n, K), dtype=torch.int32, device=DEV), torch.empty((n, K), device=DEV)
+    ctx.route(params, logits, ids, w, bias=b)
+    i64, l64 = ids.cpu().numpy().astype(np.int64), base.f64(logits)
+    assert np.all((i64 >= 16) & (i64 < 32))
+    chosen = np.take_along_axis(l64, i64, 1)
+    t = np.exp(chosen - chosen.max(1, keepdims=True))
+    t /= t.sum(1, keepdims=True)
+    np.testing.assert_allclose(base.f64(w), scale * t, rtol=2 * U * (K + 16))
+    dw, grad = base.randn(g, n, K), torch.empty_like(logits)
+    ctx.route_grad(params, logits, ids, dw, grad)
+    want = np.zeros((n, E))
+    np.put_along_axis(want, i64, scale * t * (base.f64(dw) - (base.f64(dw) * t).sum(1, keepdims=True)), 1)
+    assert np.all(np.abs(base.f64(grad) - want) <= 8 * U * (K + 16) * scale * float(dw.abs().max()))
+
+
 def test_route_of_almost_two_to_the_31_tokens():
     """The strides of warps take the token count past 2^31.  26 to 35 GB in use, a second or two."""
     R, T, E, K = 2, 2 ** 30 - 1, 2, 1
