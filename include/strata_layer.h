@@ -31,7 +31,9 @@ typedef enum {
     STRATA_T_BF16 = 0,
     STRATA_T_F32 = 1,
     STRATA_T_INT8 = 2,             /* codes -127..127, largest magnitude of a row = 127       */
-    STRATA_T_E4M3 = 3              /* e4m3 ("fn"), largest magnitude of a row = 448           */
+    STRATA_T_E4M3 = 3,             /* e4m3 ("fn"), largest magnitude of a row = 448           */
+    STRATA_T_MXF4 = 4,             /* rows in 4 bits, see strata_rows4                        */
+    STRATA_T_NVF4 = 5
 } strata_type;
 
 /* ---- router ----------------------------------------------------------------------------------------------
@@ -174,6 +176,95 @@ typedef struct {
 } strata_matmul_args;
 strata_status strata_moe_expert_matmul(strata_ctx *ctx, const strata_moe_layout_t *layout,
                                        const strata_matmul_args *args, void *stream);
+
+/* ---- rows in 4 bits ------------------------------------------------------------------------------------------
+ * A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), times the scale of its block, times the scale of its
+ * row if there is one.  Two codes share a byte, the first in its low half.
+ *   MXF4: blocks of 32 values, a scale byte s stands for 2^(s - 127), 255 for NaN (e8m0)
+ *   NVF4: blocks of 16 values, the scale is an e4m3 number
+ * codes: row r at byte r * code_stride, cols / 2 bytes; block: scale bytes, row r at byte r * block_stride, cols / 32 or
+ * cols / 16 bytes; scale: float, row r at scale[r * scale_stride], or NULL (1).  codes and block are 16-byte aligned, their strides
+ * multiples of 16 that hold a row, below 2^40.  cols is a multiple of 32. */
+typedef struct {
+    void *codes;
+    void *block;
+    float *scale;
+    int64_t code_stride, block_stride, scale_stride;
+} strata_rows4;
+
+/* Codes and scales of bf16 rows (M: a block's largest magnitude, A: the row's):
+ *   MXF4: the power of two 2^s, s = floor(log2 M) - 2, and one more where M >= 7 * 2^s; between 2^-127 and 2^125;
+ *         codes of x / 2^s.  scale must be NULL.
+ *   NVF4: scale[row] = A / 2688 (one binary32 division); block scale b = e4m3(448 M / A); codes of 2688 x / (A b), zero where
+ *         b is zero.  scale is required.
+ * Every code and block scale is the nearest to the exact quotient, ties to even, 6 (and 448) at the most.  A block of zeros has zero
+ * codes, with block scale 0.  A block (MXF4) or row (NVF4) that holds a NaN or an infinity stands for NaN throughout; its
+ * codes are unspecified.  Below A = 2688 * 2^-126 the row's scale is a subnormal number and loses places.
+ * n_valid: as in strata_quantize_rows.  x: bf16, 16-byte aligned, stride a multiple of 8.  cols <= 32768.  rows may
+ * be 0.  Outputs may alias no input.  One launch. */
+strata_status strata_quantize_rows4(strata_ctx *ctx, const void *x, int64_t x_stride, int64_t rows, int32_t cols,
+                                    int32_t type, const strata_rows4 *q, const int32_t *n_valid, void *stream);
+
+/* out = the values of 4-bit rows, code * (block scale * scale) with each product rounded to binary32, in bf16 or float (out_type).
+ * out: 16-byte aligned, stride a multiple of 16 bytes.  One launch. */
+strata_status strata_dequantize_rows4(strata_ctx *ctx, const strata_rows4 *q, int64_t rows, int32_t cols, int32_t type,
+                                      void *out, int32_t out_type, int64_t out_stride, const int32_t *n_valid, void *stream);
+
+/* The experts' products over 4-bit rows: as strata_moe_expert_matmul, with
+ *   y[r, n] = (sum_k a[r,k] * w[e,n,k]) * (scale[r] * w.scale[e,n])
+ * where a and w include their block scales.  a: the rows of the receive buffer; w: [E, channels] rows in order (row e * channels
+ * + n), of the same type.  inner: a multiple of 32, at most 131072; channels: any number, an even one if gated.  The sums are
+ * binary32.  Needs a workspace (the status word).  One launch. */
+typedef struct {
+    int32_t type;                  /* STRATA_T_MXF4 or STRATA_T_NVF4, of a and w alike        */
+    int32_t gated;                 /* 0 or 1: w holds the gate's channels/2 rows, then up's   */
+    int32_t inner;
+    int32_t channels;
+    int64_t a_rows;
+    strata_rows4 a, w;
+    void *out;                     /* bf16, as in strata_moe_expert_matmul                    */
+    int64_t out_stride;
+} strata_matmul4_args;
+strata_status strata_moe_expert_matmul4(strata_ctx *ctx, const strata_moe_layout_t *layout,
+                                        const strata_matmul4_args *args, void *stream);
+
+/* ---- balance of the router -------------------------------------------------------------------------------------
+ * The R*T tokens form one group, or one per source rank (per_rank).  A token takes part if one of its K ids is routed (not
+ * -1); the others are padding.  For a group of n such tokens, C[e] slots of them routed to expert e:
+ *   p[t, e] = softmax(logits[t])[e], or the sigmoid scores of the token over their sum
+ *   prob[e] = (sum_t p[t, e]) / n          (0 where n is 0)
+ *   balance = weight * mean over the groups with tokens of  sum_e (E * C[e] / (K * n)) * prob[e]
+ *   z       = z_weight * mean over all tokens that take part of  log(sum_e exp(logits[t, e]))^2
+ * A NaN or -inf logit counts as a score of zero, as in the router; a token without any other logit adds nothing to prob and z.
+ * C is a constant of the gradient.  loss[0] = balance, loss[1] = z; both are 0 where no token takes part.
+ * An id outside [0,E) other than -1 is not counted and raises BAD_EXPERT_ID.  The order of all sums is fixed by the shape. */
+typedef struct {
+    int32_t score;                 /* STRATA_SCORE_*                                          */
+    int32_t per_rank;              /* 0: one group, 1: R groups                               */
+    float weight;                  /* finite                                                  */
+    float z_weight;                /* finite                                                  */
+} strata_balance_params;
+typedef struct {                   /* device, what the gradient needs of the forward call     */
+    int32_t *count;                /* [groups, E]  C                                          */
+    int32_t *tokens;               /* [groups]     n                                          */
+    float *prob;                   /* [groups, E]                                             */
+} strata_balance_stats;
+
+/* logits, topk_ids as in strata_moe_route (logits may be any row-strided bf16 or float rows [R*T, E]); loss: device float
+ * [2]; scratch: device, 16-byte aligned, of strata_moe_balance_scratch_bytes.  Needs a workspace.  Two launches. */
+strata_status strata_moe_balance_scratch_bytes(strata_ctx *ctx, const strata_balance_params *params, size_t *bytes);
+strata_status strata_moe_balance_loss(strata_ctx *ctx, const strata_balance_params *params, const void *logits,
+                                      int32_t logits_type, int64_t logits_stride, const int32_t *topk_ids, float *loss,
+                                      const strata_balance_stats *stats, void *scratch, size_t scratch_bytes, void *stream);
+
+/* dlogits = dloss[0] * d balance / d logits + dloss[1] * d z / d logits + add, of the type of logits.  dloss: device float
+ * [2], or NULL (1, 1); add: a gradient that arrives otherwise (strata_moe_route_grad), of the type of logits, or NULL; dlogits may be
+ * add.  stats: as strata_moe_balance_loss wrote them for the same ids.  Padding tokens and masked logits get `add`, or 0.  Every
+ * element of dlogits' rows is written.  One launch. */
+strata_status strata_moe_balance_grad(strata_ctx *ctx, const strata_balance_params *params, const void *logits,
+                                      int32_t logits_type, int64_t logits_stride, const int32_t *topk_ids,
+                                      const strata_balance_stats *stats, const float *dloss, const void *add,
+                                      int64_t add_stride, void *dlogits, int64_t dlogits_stride, void *stream);
 
 #ifdef __cplusplus
 }

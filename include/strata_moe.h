@@ -56,16 +56,25 @@ typedef enum {
     STRATA_BF16 = 0,               /* dispatch copies bf16 rows bit for bit           */
     STRATA_FP8_E4M3_B128 = 1,      /* dispatch quantises to e4m3, one fp32 scale per
                                       token per block of 128 columns                  */
-    STRATA_Q8_ROW = 2              /* rows that are already 8-bit codes, H bytes, followed by
+    STRATA_Q8_ROW = 2,             /* rows that are already 8-bit codes, H bytes, followed by
                                       STRATA_Q8_TRAILER bytes that start with the row's fp32
                                       scale: dispatch copies them bit for bit         */
+    STRATA_MXF4_ROW = 3,           /* rows that are already 4-bit codes (strata_rows4 of strata_layer.h):
+                                      H/2 bytes of codes, then their block scales; copied bit for bit */
+    STRATA_NVF4_ROW = 4            /* the same with e4m3 block scales, then the row's fp32 scale */
 } strata_dtype;
 /* Bytes behind the H codes of a STRATA_Q8_ROW row (one 32-byte sector, so that rows of H % 32 == 0 stay
  * sector-aligned): the scale travels with its row, and dispatch moves half the bytes of bf16. */
 #define STRATA_Q8_TRAILER 32
+/* Bytes of 4-bit rows: the block scales start at byte H/2, the fp32 scale of a NVF4_ROW at STRATA_NVF4_ROW_SCALE; rows
+ * fill whole 32-byte sectors. */
+#define STRATA_MXF4_ROW_BYTES(H) (((size_t)(H) / 2 + (size_t)(H) / 32 + 31) / 32 * 32)
+#define STRATA_NVF4_ROW_SCALE(H) (((size_t)(H) / 2 + (size_t)(H) / 16 + 15) / 16 * 16)
+#define STRATA_NVF4_ROW_BYTES(H) ((STRATA_NVF4_ROW_SCALE(H) + 4 + 31) / 32 * 32)
 
 /* Problem shape.  Requirements: R,T,H,E,K > 0; E % R == 0; E <= 1024; K <= 32;
- * H % 8 == 0 (rows are whole 16-byte vectors); H % 128 == 0 for FP8; H % 16 == 0 for Q8_ROW;
+ * H % 8 == 0 (rows are whole 16-byte vectors); H % 128 == 0 for FP8; H % 16 == 0 for Q8_ROW; H % 32 == 0 for
+ * MXF4_ROW and NVF4_ROW;
  * R*T*K + E*(segment_align-1) < 2^31.
  * Two production variants of the layout (zero = off, the packed strict layout):
  *  segment_align A > 1: every expert segment starts at a multiple of A rows (what a grouped GEMM
@@ -286,6 +295,8 @@ strata_status strata_moe_layout_noalloc(const strata_moe_shape *shape, const int
  * Q8_ROW: x is uint8 [R,T,H+STRATA_Q8_TRAILER] (what strata_norm writes with q = x, q_stride = H + STRATA_Q8_TRAILER and
  *        the scale of row n at byte H of the row), recv uint8 [capacity_rows, H+STRATA_Q8_TRAILER]; rows are copied
  *        bit for bit; recv_scale must be NULL.
+ * MXF4_ROW, NVF4_ROW: x is uint8 [R,T,STRATA_MXF4_ROW_BYTES(H)] (STRATA_NVF4_ROW_BYTES), what strata_quantize_rows4 writes with
+ *        these strides, recv the same per row; rows are copied bit for bit; recv_scale must be NULL.
  * recv (and recv_scale) must lie inside a registered region (NOT_REGISTERED otherwise); x and recv
  * must be 16-byte aligned, recv_scale 4-byte aligned; capacity_rows >= strata_moe_recv_rows (CAPACITY
  * otherwise).  Items with dst_row = -1 are skipped silently; any other dst_row outside

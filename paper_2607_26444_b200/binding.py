@@ -32,6 +32,8 @@ STRATA_ERR_BAD_ROW = 10
 STRATA_BF16 = 0
 STRATA_FP8_E4M3_B128 = 1
 STRATA_Q8_ROW = 2
+STRATA_MXF4_ROW = 3
+STRATA_NVF4_ROW = 4
 STRATA_Q8_TRAILER = 32               # bytes behind the codes of a Q8_ROW row; the first four are its scale
 STRATA_FLAG_ALLOW_UNROUTED = 1
 
@@ -49,10 +51,12 @@ EXPORTS = [
     "strata_p2p", "strata_alltoallv",
     "strata_moe_route", "strata_moe_route_grad", "strata_norm", "strata_norm_grad_scratch_bytes", "strata_norm_grad",
     "strata_quantize_rows", "strata_moe_expert_matmul",
+    "strata_quantize_rows4", "strata_dequantize_rows4", "strata_moe_expert_matmul4", "strata_moe_balance_scratch_bytes",
+    "strata_moe_balance_loss", "strata_moe_balance_grad",
 ]
 
 # element types and modes of the layer operators (include/strata_layer.h)
-STRATA_T_BF16, STRATA_T_F32, STRATA_T_INT8, STRATA_T_E4M3 = 0, 1, 2, 3
+STRATA_T_BF16, STRATA_T_F32, STRATA_T_INT8, STRATA_T_E4M3, STRATA_T_MXF4, STRATA_T_NVF4 = 0, 1, 2, 3, 4, 5
 STRATA_SCORE_SOFTMAX, STRATA_SCORE_SIGMOID = 0, 1
 STRATA_GROUP_MAX, STRATA_GROUP_TOP2 = 0, 1
 
@@ -132,6 +136,37 @@ class strata_matmul_args(ctypes.Structure):
                 ("a_scale", ctypes.c_void_p), ("w", ctypes.c_void_p), ("w_scale", ctypes.c_void_p),
                 ("out", ctypes.c_void_p), ("a_stride", ctypes.c_int64), ("a_scale_stride", ctypes.c_int64),
                 ("out_stride", ctypes.c_int64)]
+
+
+class strata_rows4(ctypes.Structure):
+    _fields_ = [("codes", ctypes.c_void_p), ("block", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("code_stride", ctypes.c_int64), ("block_stride", ctypes.c_int64), ("scale_stride", ctypes.c_int64)]
+
+
+class strata_matmul4_args(ctypes.Structure):
+    _fields_ = [("type", ctypes.c_int32), ("gated", ctypes.c_int32), ("inner", ctypes.c_int32),
+                ("channels", ctypes.c_int32), ("a_rows", ctypes.c_int64), ("a", strata_rows4), ("w", strata_rows4),
+                ("out", ctypes.c_void_p), ("out_stride", ctypes.c_int64)]
+
+
+class strata_balance_params(ctypes.Structure):
+    _fields_ = [("score", ctypes.c_int32), ("per_rank", ctypes.c_int32), ("weight", ctypes.c_float),
+                ("z_weight", ctypes.c_float)]
+
+
+class strata_balance_stats(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_void_p), ("tokens", ctypes.c_void_p), ("prob", ctypes.c_void_p)]
+
+
+_SCORES = {"softmax": STRATA_SCORE_SOFTMAX, "sigmoid": STRATA_SCORE_SIGMOID}
+
+
+def make_balance(score: str = "softmax", weight: float = 1.0, z_weight: float = 0.0,
+                 per_rank: bool = False) -> strata_balance_params:
+    """score: "softmax" or "sigmoid" (normalised); per_rank: a loss for each source rank's tokens, averaged."""
+    if score not in _SCORES:
+        raise ValueError(f"unknown score {score!r}")
+    return strata_balance_params(_SCORES[score], int(per_rank), weight, z_weight)
 
 
 def make_route(score: str = "softmax", renormalise: bool = True, scale: float = 1.0, n_group: int = 1,
@@ -220,6 +255,13 @@ def lib() -> ctypes.CDLL:
         "strata_norm_grad": [vp, P(strata_norm_grad_args), vp],
         "strata_quantize_rows": [vp, vp, i64, i64, i32, i32, vp, i64, vp, i64, vp, vp],
         "strata_moe_expert_matmul": [vp, P(strata_moe_layout_t), P(strata_matmul_args), vp],
+        "strata_quantize_rows4": [vp, vp, i64, i64, i32, i32, P(strata_rows4), vp, vp],
+        "strata_dequantize_rows4": [vp, P(strata_rows4), i64, i32, i32, vp, i32, i64, vp, vp],
+        "strata_moe_expert_matmul4": [vp, P(strata_moe_layout_t), P(strata_matmul4_args), vp],
+        "strata_moe_balance_scratch_bytes": [vp, P(strata_balance_params), P(sz)],
+        "strata_moe_balance_loss": [vp, P(strata_balance_params), vp, i32, i64, vp, vp, P(strata_balance_stats), vp, sz, vp],
+        "strata_moe_balance_grad": [vp, P(strata_balance_params), vp, i32, i64, vp, P(strata_balance_stats), vp, vp, i64, vp,
+                                    i64, vp],
     }
     for name, args in sigs.items():
         fn = getattr(L, name)
@@ -454,6 +496,41 @@ def strata_moe_expert_matmul(ctx, layout: strata_moe_layout_t, args: strata_matm
     return lib().strata_moe_expert_matmul(ctx, ctypes.byref(layout), ctypes.byref(args), stream)
 
 
+def strata_quantize_rows4(ctx, x: int, x_stride: int, rows: int, cols: int, type_: int, q: strata_rows4,
+                          n_valid: Optional[int], stream: int) -> int:
+    return lib().strata_quantize_rows4(ctx, x, x_stride, rows, cols, type_, ctypes.byref(q), n_valid, stream)
+
+
+def strata_dequantize_rows4(ctx, q: strata_rows4, rows: int, cols: int, type_: int, out: int, out_type: int,
+                            out_stride: int, n_valid: Optional[int], stream: int) -> int:
+    return lib().strata_dequantize_rows4(ctx, ctypes.byref(q), rows, cols, type_, out, out_type, out_stride, n_valid,
+                                         stream)
+
+
+def strata_moe_expert_matmul4(ctx, layout: strata_moe_layout_t, args: strata_matmul4_args, stream: int) -> int:
+    return lib().strata_moe_expert_matmul4(ctx, ctypes.byref(layout), ctypes.byref(args), stream)
+
+
+def strata_moe_balance_scratch_bytes(ctx, params: strata_balance_params) -> Tuple[int, int]:
+    n = ctypes.c_size_t()
+    rc = lib().strata_moe_balance_scratch_bytes(ctx, ctypes.byref(params), ctypes.byref(n))
+    return rc, n.value
+
+
+def strata_moe_balance_loss(ctx, params: strata_balance_params, logits: int, logits_type: int, logits_stride: int,
+                            topk_ids: int, loss: int, stats: strata_balance_stats, scratch: int, scratch_bytes: int,
+                            stream: int) -> int:
+    return lib().strata_moe_balance_loss(ctx, ctypes.byref(params), logits, logits_type, logits_stride, topk_ids, loss,
+                                         ctypes.byref(stats), scratch, scratch_bytes, stream)
+
+
+def strata_moe_balance_grad(ctx, params: strata_balance_params, logits: int, logits_type: int, logits_stride: int,
+                            topk_ids: int, stats: strata_balance_stats, dloss: Optional[int], add: Optional[int],
+                            add_stride: int, dlogits: int, dlogits_stride: int, stream: int) -> int:
+    return lib().strata_moe_balance_grad(ctx, ctypes.byref(params), logits, logits_type, logits_stride, topk_ids,
+                                         ctypes.byref(stats), dloss, add, add_stride, dlogits, dlogits_stride, stream)
+
+
 # ---- convenience wrapper over torch tensors (memory + streams only) ---------
 
 def _check(rc: int, where: str) -> None:
@@ -560,6 +637,84 @@ def q8_rows(buf, code_dtype):
     h = buf.shape[-1] - STRATA_Q8_TRAILER
     scale = buf.view(torch.float32)[..., h // 4]
     return buf[..., :h].view(code_dtype), scale
+
+
+_BLOCK4 = {STRATA_T_MXF4: 32, STRATA_T_NVF4: 16}          # values that share a scale
+_KINDS4 = {"mxfp4": STRATA_T_MXF4, "nvfp4": STRATA_T_NVF4}
+
+
+def _kind4(kind: str) -> int:
+    if kind not in _KINDS4:
+        raise ValueError(f"4-bit rows are mxfp4 or nvfp4, not {kind!r}")
+    return _KINDS4[kind]
+
+
+class Rows4:
+    """Rows in 4 bits: codes uint8 (or torch.float4_e2m1fn_x2) [.., cols / 2], two to a byte and the first in its low half;
+    block scales [.., cols / 32] of torch.float8_e8m0fnu (mxfp4) or [.., cols / 16] of torch.float8_e4m3fn (nvfp4); scales
+    of the rows fp32 [..] or None (1).  Rows of codes and of block scales start on 16 bytes."""
+
+    def __init__(self, codes, block, scale=None):
+        import torch
+        if codes.dtype != torch.uint8 and codes.dtype != torch.float4_e2m1fn_x2:
+            raise ValueError(f"4-bit codes are torch.uint8 or torch.float4_e2m1fn_x2, not {codes.dtype}")
+        if block.dtype != torch.float8_e8m0fnu and block.dtype != torch.float8_e4m3fn:
+            raise ValueError(f"block scales are torch.float8_e8m0fnu or torch.float8_e4m3fn, not {block.dtype}")
+        self.type = STRATA_T_MXF4 if block.dtype == torch.float8_e8m0fnu else STRATA_T_NVF4
+        self.codes, self.block, self.scale = codes, block, scale
+        rows, half, code_stride = _strides(codes)
+        self.rows, self.cols = rows, 2 * half
+        if self.cols % 32:
+            raise ValueError("4-bit rows have a multiple of 32 columns")
+        block_stride = _stride(block, rows, self.cols // _BLOCK4[self.type], "block scales")
+        if rows == 1:                                     # nothing is read between rows that are not there
+            code_stride, block_stride = -(-code_stride // 16) * 16, -(-block_stride // 16) * 16
+        self.c = strata_rows4(codes.data_ptr(), block.data_ptr(), None if scale is None else scale.data_ptr(), code_stride,
+                              block_stride, 0 if scale is None else _scale_stride(scale, rows))
+
+
+def empty_rows4(shape, cols: int, kind: str, device="cuda") -> Rows4:
+    """Uninitialised 4-bit rows [*shape, cols] of kind "mxfp4" or "nvfp4", as quantize_rows4 writes them."""
+    import torch
+    code = _kind4(kind)
+    n = cols // _BLOCK4[code]
+    block = torch.empty((*shape, -(-n // 16) * 16), dtype=torch.uint8, device=device)
+    block = block.view(torch.float8_e8m0fnu if code == STRATA_T_MXF4 else torch.float8_e4m3fn)[..., :n]
+    scale = torch.empty(shape, dtype=torch.float32, device=device) if code == STRATA_T_NVF4 else None
+    return Rows4(torch.empty((*shape, cols // 2), dtype=torch.uint8, device=device), block, scale)
+
+
+def row4_bytes(cols: int, kind: str) -> int:
+    """Bytes of a row of dispatch type STRATA_MXF4_ROW or STRATA_NVF4_ROW."""
+    if _kind4(kind) == STRATA_T_MXF4:
+        return (cols // 2 + cols // 32 + 31) // 32 * 32
+    return ((cols // 2 + cols // 16 + 15) // 16 * 16 + 4 + 31) // 32 * 32
+
+
+def q4_rows(buf, cols: int, kind: str) -> Rows4:
+    """The 4-bit rows in a uint8 buffer [.., row4_bytes(cols, kind)] of STRATA_MXF4_ROW or STRATA_NVF4_ROW rows."""
+    import torch
+    if buf.shape[-1] != row4_bytes(cols, kind):
+        raise ValueError(f"rows of {row4_bytes(cols, kind)} bytes are needed, not of {buf.shape[-1]}")
+    half, n = cols // 2, cols // _BLOCK4[_kind4(kind)]
+    block = buf[..., half:half + n]
+    if kind == "mxfp4":
+        return Rows4(buf[..., :half], block.view(torch.float8_e8m0fnu))
+    return Rows4(buf[..., :half], block.view(torch.float8_e4m3fn), buf.view(torch.float32)[..., (half + n + 15) // 16 * 4])
+
+
+class BalanceStats:
+    """What balance_loss leaves for its gradient and for the books: count int32 and prob fp32 [groups, E], tokens int32
+    [groups]; and its scratch."""
+
+    def __init__(self, groups: int, E: int, scratch_bytes: int, device):
+        import torch
+        self.count = torch.empty((groups, E), dtype=torch.int32, device=device)
+        self.tokens = torch.empty(groups, dtype=torch.int32, device=device)
+        self.prob = torch.empty((groups, E), dtype=torch.float32, device=device)
+        self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=device)
+        self.groups = groups
+        self.c = strata_balance_stats(self.count.data_ptr(), self.tokens.data_ptr(), self.prob.data_ptr())
 
 
 class Layout:
@@ -808,6 +963,65 @@ class MoEContext:
             _bf16(out),
             a_stride, _scale_stride(a_scale, rows), _stride(out, rows, wide, "out")), self._stream()),
             "strata_moe_expert_matmul")
+
+    def quantize_rows4(self, x, q: Rows4, layout: Optional[Layout] = None) -> None:
+        """bf16 rows -> 4-bit codes with their scales; with a layout, only the rows it has in use."""
+        rows, cols, stride = _strides(x)
+        if q.rows != rows or q.cols != cols:
+            raise ValueError(f"q: {rows} rows of {cols} are needed, not {q.rows} of {q.cols}")
+        n_valid = layout.expert_offset.data_ptr() + 4 * self.E if layout is not None else None
+        _check(self._c.strata_quantize_rows4(self.h, _bf16(x), stride, rows, cols, q.type, q.c, n_valid, self._stream()),
+               "strata_quantize_rows4")
+
+    def dequantize_rows4(self, q: Rows4, out, layout: Optional[Layout] = None) -> None:
+        """The values of 4-bit rows in bf16 or fp32; with a layout, only of the rows it has in use."""
+        n_valid = layout.expert_offset.data_ptr() + 4 * self.E if layout is not None else None
+        _check(self._c.strata_dequantize_rows4(self.h, q.c, q.rows, q.cols, q.type, out.data_ptr(), _float_type(out),
+                                               _stride(out, q.rows, q.cols, "out"), n_valid, self._stream()),
+               "strata_dequantize_rows4")
+
+    def expert_matmul4(self, layout: Layout, a: Rows4, w: Rows4, out, gated: bool = False) -> None:
+        """expert_matmul over 4-bit rows a [rows, inner] and 4-bit weights w [E, channels, inner] of the same kind."""
+        if w.codes.dim() != 3 or w.type != a.type or w.cols != a.cols or w.codes.size(0) != self.E:
+            raise ValueError("w is [E, channels, inner] of a's kind")
+        channels = w.codes.size(1)
+        _check(self._c.strata_moe_expert_matmul4(self.h, layout.c, strata_matmul4_args(
+            a.type, 1 if gated else 0, a.cols, channels, a.rows, a.c, w.c, _bf16(out),
+            _stride(out, a.rows, channels // 2 if gated else channels, "out")), self._stream()),
+            "strata_moe_expert_matmul4")
+
+    def balance_stats(self, params: strata_balance_params) -> BalanceStats:
+        """Outputs and scratch of balance_loss for these parameters."""
+        rc, n = strata_moe_balance_scratch_bytes(self.h, params)
+        _check(rc, "strata_moe_balance_scratch_bytes")
+        return BalanceStats(self.R if params.per_rank else 1, self.E, n, self.device)
+
+    def _balance_stats(self, params: strata_balance_params, stats: BalanceStats):
+        if stats.groups != (self.R if params.per_rank else 1) or stats.count.size(1) != self.E:
+            raise ValueError("stats were made for other parameters")
+        return stats.c
+
+    def balance_loss(self, params: strata_balance_params, logits, ids, loss, stats: BalanceStats) -> None:
+        """loss fp32 [2] = the balance loss and the mean square of the logits' log-sum-exp, each with its weight; stats: the
+        counts per expert and the mean scores."""
+        _check(self._c.strata_moe_balance_loss(
+            self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, self.n_tok, self.E, "logits"),
+            _flat(ids, _INT32, self.n_items, "ids"), _flat(loss, STRATA_T_F32, 2, "loss"), self._balance_stats(params, stats),
+            stats.scratch.data_ptr(), stats.scratch.nbytes, self._stream()), "strata_moe_balance_loss")
+
+    def balance_grad(self, params: strata_balance_params, logits, ids, stats: BalanceStats, dlogits, dloss=None,
+                     add=None) -> None:
+        """dlogits (of the type of logits) = the gradient of both losses, times dloss (fp32 [2] on the device, or None: 1), plus
+        `add`, which may be dlogits itself."""
+        if dlogits.dtype != logits.dtype or (add is not None and add.dtype != logits.dtype):
+            raise ValueError("dlogits and add have the type of logits")
+        n, e = self.n_tok, self.E
+        _check(self._c.strata_moe_balance_grad(
+            self.h, params, logits.data_ptr(), _float_type(logits), _stride(logits, n, e, "logits"),
+            _flat(ids, _INT32, self.n_items, "ids"), self._balance_stats(params, stats),
+            None if dloss is None else _flat(dloss, STRATA_T_F32, 2, "dloss"), None if add is None else add.data_ptr(),
+            0 if add is None else _stride(add, n, e, "add"), dlogits.data_ptr(), _stride(dlogits, n, e, "dlogits"),
+            self._stream()), "strata_moe_balance_grad")
 
     def row_experts(self, layout: Layout, out=None):
         """int32 [recv_rows]: the expert of every occupied receive row, -1 for padding and empty rows."""

@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libstrata_moe.so")
 SOURCES = ["api.cu", "layout.cu", "dispatch.cu", "combine.cu", "partition.cu", "collective.cu", "rowmap.cu", "expert.cu",
-           "layer_api.cu", "route.cu", "norm.cu", "matmul.cu"]
+           "layer_api.cu", "route.cu", "norm.cu", "matmul.cu", "rows4.cu", "matmul4.cu", "balance.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-cudart", "static", "--threads", "0"]
 

@@ -12,6 +12,7 @@ cudaError_t configure_partition_kernels();
 cudaError_t configure_collective_kernels();
 cudaError_t configure_matmul_kernels();
 cudaError_t configure_norm_kernels();
+cudaError_t configure_matmul4_kernels();
 }  // namespace strata
 
 namespace {
@@ -25,8 +26,9 @@ strata_status check_shape(const strata_moe_shape* s)
     const strata_status st = check_layout_shape(*s);
     if (st != STRATA_OK) return st;
     if (s->dispatch_dtype != STRATA_BF16 && s->dispatch_dtype != STRATA_FP8_E4M3_B128 &&
-        s->dispatch_dtype != STRATA_Q8_ROW)
+        s->dispatch_dtype != STRATA_Q8_ROW && s->dispatch_dtype != STRATA_MXF4_ROW && s->dispatch_dtype != STRATA_NVF4_ROW)
         return STRATA_ERR_SHAPE;
+    if ((s->dispatch_dtype == STRATA_MXF4_ROW || s->dispatch_dtype == STRATA_NVF4_ROW) && s->H % 32 != 0) return STRATA_ERR_SHAPE;
     if (s->dispatch_dtype == STRATA_Q8_ROW && s->H % 16 != 0) return STRATA_ERR_SHAPE;
     if (s->dispatch_dtype == STRATA_FP8_E4M3_B128 && s->H % 128 != 0) return STRATA_ERR_SHAPE;
     // Dispatch and combine number their work units (a token, or a column piece of one never shorter than
@@ -41,6 +43,8 @@ size_t recv_row_bytes(const strata_moe_shape& s)
     switch (s.dispatch_dtype) {
         case STRATA_FP8_E4M3_B128: return (size_t)s.H;
         case STRATA_Q8_ROW: return (size_t)s.H + STRATA_Q8_TRAILER;
+        case STRATA_MXF4_ROW: return STRATA_MXF4_ROW_BYTES(s.H);
+        case STRATA_NVF4_ROW: return STRATA_NVF4_ROW_BYTES(s.H);
         default: return (size_t)s.H * 2;
     }
 }
@@ -106,7 +110,8 @@ strata_status strata_ctx_create(strata_ctx** out, const strata_moe_shape* shape,
             return STRATA_ERR_CUDA;
         if (configure_layout_kernels() != cudaSuccess || configure_dispatch_kernels() != cudaSuccess ||
             configure_partition_kernels() != cudaSuccess || configure_collective_kernels() != cudaSuccess ||
-            configure_matmul_kernels() != cudaSuccess || configure_norm_kernels() != cudaSuccess) {
+            configure_matmul_kernels() != cudaSuccess || configure_norm_kernels() != cudaSuccess ||
+            configure_matmul4_kernels() != cudaSuccess) {
             cudaGetLastError();
             return STRATA_ERR_CUDA;
         }
@@ -765,8 +770,8 @@ strata_status strata_device_status(strata_ctx* ctx, void* stream, strata_status*
     }
     if (word != 0) {
         // clear the status word; after an error also the ticket and the work-claim counters, which a
-        // kernel that gave up may have left non-zero (header words 0..9)
-        if (cudaMemsetAsync(ctx->ws, 0, 10 * sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
+        // kernel that gave up may have left non-zero (header words 0..10)
+        if (cudaMemsetAsync(ctx->ws, 0, 11 * sizeof(int), st) != cudaSuccess || cudaStreamSynchronize(st) != cudaSuccess) {
             cudaGetLastError();
             return STRATA_ERR_CUDA;
         }

@@ -1,0 +1,418 @@
+// Balance loss of the router with the counts per expert, and its gradient (strata_layer.h has the formulas).  One warp owns a
+// token, lanes hold neighbouring experts (scores.cuh).  All sums run in an order that the shape fixes: a warp's tokens, the
+// warps of a block, the blocks of a group, the groups.
+#include "scores.cuh"
+
+namespace strata {
+
+namespace {
+
+constexpr int kWarps = 8;
+constexpr int kBlocksPerSm = 4;
+constexpr int kSumCols = 32, kSumLanes = 8;    // of balance_sum_kernel
+
+struct BalanceGeom {
+    int groups, slices, col_blocks;
+    long long group_tokens;
+};
+BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params& b, int n_sm)
+{
+    BalanceGeom g;
+    g.groups = b.per_rank ? s.R : 1;
+    g.group_tokens = b.per_rank ? s.T : (long long)s.R * s.T;
+    const long long most = max(1ll, (long long)n_sm * kBlocksPerSm / g.groups);
+    g.slices = (int)min(most, (g.group_tokens + kWarps - 1) / kWarps);
+    g.col_blocks = (s.E + kSumCols - 1) / kSumCols;
+    return g;
+}
+
+struct BalanceParams {
+    const void* logits;
+    long long stride, group_tokens;
+    const int32_t* ids;
+    float* part_p;         // [groups * slices, E]  sums of scores
+    int32_t* part_c;       // [groups * slices, E]  slots
+    int32_t* part_n;       // [groups * slices]     tokens that take part
+    float* part_z;         // [groups * slices]     sums of squares
+    float* part_loss;      // [groups * col_blocks]
+    int32_t* count;
+    int32_t* tokens;
+    float* prob;
+    float* loss;
+    int* status;
+    unsigned* ticket;
+    int E, K, groups, slices, vec_ok;
+    float weight, z_weight;
+};
+
+// The normalised scores of a token, and the softmax and the logarithm of its sum where they are asked for.
+template <int VPL, bool SIGMOID>
+__device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&soft)[VPL], float& lse)
+{
+    lse = 0.0f;
+    if (!SIGMOID || want_soft) {
+        float m = l[0];
+#pragma unroll
+        for (int i = 1; i < VPL; ++i) m = fmaxf(m, l[i]);
+        m = warp_max(m);
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
+            s += soft[i];
+        }
+        s = warp_sum(s);
+        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) soft[i] *= inv;
+        if (s > 0.0f) lse = m + logf(s);
+    }
+    if constexpr (SIGMOID) {
+        float s = 0.0f;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) {
+            p[i] = sigmoid_f(l[i]);
+            s += p[i];
+        }
+        s = warp_sum(s);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) p[i] = s > 0.0f ? __fdiv_rn(p[i], s) : 0.0f;
+    } else {
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) p[i] = soft[i];
+    }
+}
+
+template <int VPL, bool BF16, bool SIGMOID>
+__global__ void __launch_bounds__(kWarps * 32) balance_kernel(const BalanceParams p)
+{
+    extern __shared__ float s_sum[];                              // [warps][32 * VPL]
+    __shared__ int s_count[kMaxExperts];
+    __shared__ float s_z[kWarps];
+    __shared__ int s_n[kWarps];
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, e0 = lane * VPL;
+    const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
+    for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) s_count[e] = 0;
+    __syncthreads();
+    griddep_wait();
+    float sum[VPL], z = 0.0f;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
+    for (long long t = slice * kWarps + warp; t < p.group_tokens; t += p.slices * kWarps) {
+        const long long tok = group * p.group_tokens + t;
+        int id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
+        float l[VPL], q[VPL], soft[VPL], lse;
+        load_logits<VPL, BF16>(l, p.logits, tok * p.stride, e0, p.E, p.vec_ok != 0);
+        if (id < -1 || id >= p.E) {
+            report_status(p.status, STRATA_ERR_BAD_EXPERT_ID);
+            id = -1;
+        }
+        if (!__any_sync(kFull, id >= 0)) continue;
+        if (id >= 0) atomicAdd(&s_count[id], 1);
+        token_scores<VPL, SIGMOID>(l, p.z_weight != 0.0f, q, soft, lse);
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) sum[i] += q[i];
+        z = fmaf(lse, lse, z);
+        ++n;
+    }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) s_sum[warp * 32 * VPL + i * 32 + lane] = sum[i];
+    if (lane == 0) {
+        s_z[warp] = z;
+        s_n[warp] = n;
+    }
+    __syncthreads();
+    griddep_launch_dependents();
+    for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) {
+        const int at = (e % VPL) * 32 + e / VPL;
+        float a = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) a += s_sum[w * 32 * VPL + at];
+        p.part_p[(size_t)blockIdx.x * p.E + e] = a;
+        p.part_c[(size_t)blockIdx.x * p.E + e] = s_count[e];
+    }
+    if (threadIdx.x == 0) {
+        float a = 0.0f;
+        int c = 0;
+        for (int w = 0; w < kWarps; ++w) {
+            a += s_z[w];
+            c += s_n[w];
+        }
+        p.part_z[blockIdx.x] = a;
+        p.part_n[blockIdx.x] = c;
+    }
+}
+
+// Sum over a block's threads in a fixed order; valid in thread 0.
+template <typename V>
+__device__ __forceinline__ V block_sum(V v, V* buf)
+{
+    const int t = (int)threadIdx.x;
+    __syncthreads();
+    buf[t] = v;
+    __syncthreads();
+#pragma unroll
+    for (int o = kSumCols * kSumLanes / 2; o > 0; o >>= 1) {
+        if (t < o) buf[t] += buf[t + o];
+        __syncthreads();
+    }
+    return buf[0];
+}
+
+// Slices to groups: 32 experts of one group per block, each of 8 lanes adding every 8th slice.  The block that draws the last
+// ticket adds up the losses.
+__global__ void __launch_bounds__(kSumCols* kSumLanes) balance_sum_kernel(const BalanceParams p, int col_blocks)
+{
+    __shared__ float s_f[kSumCols * kSumLanes];
+    __shared__ int s_i[kSumCols * kSumLanes];
+    __shared__ bool s_last;
+    const int t = (int)threadIdx.x, cx = t % kSumCols, ly = t / kSumCols;
+    const int group = (int)blockIdx.x / col_blocks, e = ((int)blockIdx.x - group * col_blocks) * kSumCols + cx;
+    griddep_wait();
+    griddep_launch_dependents();
+    const size_t first = (size_t)group * p.slices;
+    int n = 0;
+    for (int i = t; i < p.slices; i += kSumCols * kSumLanes) n += p.part_n[first + i];
+    n = block_sum(n, s_i);
+    float a = 0.0f;
+    int c = 0;
+    if (e < p.E)
+        for (int i = ly; i < p.slices; i += kSumLanes) {
+            a += p.part_p[(first + i) * p.E + e];
+            c += p.part_c[(first + i) * p.E + e];
+        }
+    __syncthreads();
+    s_f[t] = a;
+    s_i[t] = c;
+    __syncthreads();
+#pragma unroll
+    for (int o = kSumLanes / 2; o > 0; o >>= 1) {
+        if (ly < o) {
+            s_f[t] += s_f[t + o * kSumCols];
+            s_i[t] += s_i[t + o * kSumCols];
+        }
+        __syncthreads();
+    }
+    float part = 0.0f;
+    if (ly == 0 && e < p.E) {
+        const float prob = n > 0 ? __fdiv_rn(s_f[t], (float)n) : 0.0f;
+        p.prob[(size_t)group * p.E + e] = prob;
+        p.count[(size_t)group * p.E + e] = s_i[t];
+        part = n > 0 ? (float)s_i[t] * prob : 0.0f;
+    }
+    part = block_sum(part, s_f);
+    if (t == 0) {
+        p.part_loss[blockIdx.x] = n > 0 ? part * __fdiv_rn((float)p.E, (float)p.K * (float)n) : 0.0f;
+        if (blockIdx.x % (unsigned)col_blocks == 0) p.tokens[group] = n;
+        __threadfence();
+        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (!s_last) return;
+    __threadfence();
+    float loss = 0.0f, z = 0.0f;
+    int alive = 0, total = 0;
+    for (int i = t; i < (int)gridDim.x; i += kSumCols * kSumLanes) loss += __ldcg(p.part_loss + i);
+    for (int i = t; i < p.groups; i += kSumCols * kSumLanes) {
+        const int m = __ldcg(p.tokens + i);
+        alive += m > 0;
+        total += m;
+    }
+    for (int i = t; i < p.groups * p.slices; i += kSumCols * kSumLanes) z += p.part_z[i];
+    loss = block_sum(loss, s_f);
+    z = block_sum(z, s_f);
+    alive = block_sum(alive, s_i);
+    total = block_sum(total, s_i);
+    if (t == 0) {
+        p.loss[0] = alive > 0 ? p.weight * __fdiv_rn(loss, (float)alive) : 0.0f;
+        p.loss[1] = total > 0 && p.z_weight != 0.0f ? p.z_weight * __fdiv_rn(z, (float)total) : 0.0f;
+        *p.ticket = 0;
+    }
+}
+
+struct BalanceGradParams {
+    const void* logits;
+    const void* add;
+    void* dlogits;
+    long long stride, add_stride, dstride, group_tokens;
+    const int32_t* ids;
+    const int32_t* count;
+    const int32_t* tokens;
+    const float* dloss;
+    int E, K, groups, slices, vec_ok, add_vec_ok, dvec_ok;
+    float weight, z_weight;
+};
+
+template <int VPL, bool BF16, bool SIGMOID>
+__global__ void __launch_bounds__(kWarps * 32) balance_grad_kernel(const BalanceGradParams p)
+{
+    __shared__ int s_alive, s_total;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, e0 = lane * VPL;
+    const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
+    if (threadIdx.x == 0) s_alive = s_total = 0;
+    __syncthreads();
+    griddep_wait();
+    griddep_launch_dependents();
+    for (int i = (int)threadIdx.x; i < p.groups; i += kWarps * 32) {
+        const int m = p.tokens[i];
+        if (m > 0) {
+            atomicAdd(&s_alive, 1);
+            atomicAdd(&s_total, m);
+        }
+    }
+    __syncthreads();
+    const int n = p.tokens[group];
+    const float d0 = p.dloss ? p.dloss[0] : 1.0f, d1 = p.dloss ? p.dloss[1] : 1.0f;
+    // d balance / d p[t, e] = c[e]
+    const float unit = n > 0 ? d0 * p.weight * __fdiv_rn((float)p.E, (float)s_alive * (float)p.K * (float)n) / (float)n : 0.0f;
+    const float unit_z = n > 0 ? d1 * p.z_weight * 2.0f / (float)s_total : 0.0f;
+    const bool want_z = p.z_weight != 0.0f;
+    float c[VPL];
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) c[i] = e0 + i < p.E ? unit * (float)p.count[(size_t)group * p.E + e0 + i] : 0.0f;
+    for (long long t = slice * kWarps + warp; t < p.group_tokens; t += p.slices * kWarps) {
+        const long long tok = group * p.group_tokens + t;
+        const int id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
+        float l[VPL], q[VPL], soft[VPL], g[VPL], lse;
+        load_logits<VPL, BF16>(l, p.logits, tok * p.stride, e0, p.E, p.vec_ok != 0);
+        if (p.add) load_logits<VPL, BF16, true>(g, p.add, tok * p.add_stride, e0, p.E, p.add_vec_ok != 0);
+        else {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) g[i] = 0.0f;
+        }
+        if (__any_sync(kFull, id >= 0 && id < p.E)) {
+            token_scores<VPL, SIGMOID>(l, want_z, q, soft, lse);
+            float dot = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) dot = fmaf(q[i], c[i], dot);
+            dot = warp_sum(dot);
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) {
+                float d = q[i] * (c[i] - dot);
+                if constexpr (SIGMOID) d *= sigmoid_f(-l[i]);     // 1 - s without the cancellation
+                if (want_z) d = fmaf(unit_z * lse, soft[i], d);
+                if (l[i] == -INFINITY) d = 0.0f;
+                g[i] += d;
+            }
+        }
+        store_row<VPL, BF16>(g, p.dlogits, tok * p.dstride, e0, p.E, p.dvec_ok != 0);
+    }
+}
+
+size_t aligned(size_t n) { return (n + 15) & ~(size_t)15; }
+
+template <int VPL, bool BF16>
+cudaError_t loss_vpl(const BalanceParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
+{
+    const size_t smem = (size_t)kWarps * 32 * VPL * sizeof(float);
+    return sigmoid ? launch_pdl(balance_kernel<VPL, BF16, true>, grid, kWarps * 32, smem, st, p)
+                   : launch_pdl(balance_kernel<VPL, BF16, false>, grid, kWarps * 32, smem, st, p);
+}
+template <int VPL, bool BF16>
+cudaError_t grad_vpl(const BalanceGradParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
+{
+    return sigmoid ? launch_pdl(balance_grad_kernel<VPL, BF16, true>, grid, kWarps * 32, 0, st, p)
+                   : launch_pdl(balance_grad_kernel<VPL, BF16, false>, grid, kWarps * 32, 0, st, p);
+}
+
+}  // namespace
+
+size_t balance_scratch_bytes(const strata_moe_shape& s, const strata_balance_params& b, int n_sm)
+{
+    const BalanceGeom g = balance_geom(s, b, n_sm);
+    const size_t blocks = (size_t)g.groups * g.slices;
+    return 2 * aligned(blocks * s.E * 4) + 2 * aligned(blocks * 4) + aligned((size_t)g.groups * g.col_blocks * 4);
+}
+
+#define STRATA_BY_WIDTH(f, ...)                                                                     \
+    switch (lanes_width(s.E)) {                                                                     \
+        case 1: return bf ? f<1, true>(__VA_ARGS__) : f<1, false>(__VA_ARGS__);                     \
+        case 2: return bf ? f<2, true>(__VA_ARGS__) : f<2, false>(__VA_ARGS__);                     \
+        case 4: return bf ? f<4, true>(__VA_ARGS__) : f<4, false>(__VA_ARGS__);                     \
+        case 8: return bf ? f<8, true>(__VA_ARGS__) : f<8, false>(__VA_ARGS__);                     \
+        case 16: return bf ? f<16, true>(__VA_ARGS__) : f<16, false>(__VA_ARGS__);                  \
+        default: return bf ? f<32, true>(__VA_ARGS__) : f<32, false>(__VA_ARGS__);                  \
+    }
+
+namespace {
+cudaError_t first_pass(const strata_moe_shape& s, const BalanceParams& p, bool bf, bool sigmoid, unsigned grid, cudaStream_t st)
+{
+    STRATA_BY_WIDTH(loss_vpl, p, sigmoid, grid, st)
+}
+}  // namespace
+
+cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_params& b, const void* logits, int type,
+                                long long stride, const int32_t* ids, float* loss, const strata_balance_stats& stats,
+                                void* scratch, int* status, unsigned* ticket, int n_sm, cudaStream_t st, int* n_launches)
+{
+    const BalanceGeom g = balance_geom(s, b, n_sm);
+    const size_t blocks = (size_t)g.groups * g.slices;
+    BalanceParams p{};
+    p.logits = logits;
+    p.stride = stride;
+    p.group_tokens = g.group_tokens;
+    p.ids = ids;
+    char* at = static_cast<char*>(scratch);
+    p.part_p = reinterpret_cast<float*>(at);
+    at += aligned(blocks * s.E * 4);
+    p.part_c = reinterpret_cast<int32_t*>(at);
+    at += aligned(blocks * s.E * 4);
+    p.part_n = reinterpret_cast<int32_t*>(at);
+    at += aligned(blocks * 4);
+    p.part_z = reinterpret_cast<float*>(at);
+    at += aligned(blocks * 4);
+    p.part_loss = reinterpret_cast<float*>(at);
+    p.count = stats.count;
+    p.tokens = stats.tokens;
+    p.prob = stats.prob;
+    p.loss = loss;
+    p.status = status;
+    p.ticket = ticket;
+    p.E = s.E;
+    p.K = s.K;
+    p.groups = g.groups;
+    p.slices = g.slices;
+    p.vec_ok = rows_on_16(logits, stride, type);
+    p.weight = b.weight;
+    p.z_weight = b.z_weight;
+    *n_launches = 1;
+    const cudaError_t err = first_pass(s, p, type == STRATA_T_BF16, b.score == STRATA_SCORE_SIGMOID, (unsigned)blocks, st);
+    if (err != cudaSuccess) return err;
+    *n_launches = 2;
+    return launch_pdl(balance_sum_kernel, (unsigned)(g.groups * g.col_blocks), kSumCols * kSumLanes, 0, st, p, g.col_blocks);
+}
+
+cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_params& b, const void* logits, int type,
+                                long long stride, const int32_t* ids, const strata_balance_stats& stats, const float* dloss,
+                                const void* add, long long add_stride, void* dlogits, long long dstride, int n_sm,
+                                cudaStream_t st)
+{
+    const BalanceGeom g = balance_geom(s, b, n_sm);
+    BalanceGradParams p{};
+    p.logits = logits;
+    p.add = add;
+    p.dlogits = dlogits;
+    p.stride = stride;
+    p.add_stride = add_stride;
+    p.dstride = dstride;
+    p.group_tokens = g.group_tokens;
+    p.ids = ids;
+    p.count = stats.count;
+    p.tokens = stats.tokens;
+    p.dloss = dloss;
+    p.E = s.E;
+    p.K = s.K;
+    p.groups = g.groups;
+    p.slices = g.slices;
+    p.vec_ok = rows_on_16(logits, stride, type);
+    p.add_vec_ok = add && rows_on_16(add, add_stride, type);
+    p.dvec_ok = rows_on_16(dlogits, dstride, type);
+    p.weight = b.weight;
+    p.z_weight = b.z_weight;
+    const bool bf = type == STRATA_T_BF16, sigmoid = b.score == STRATA_SCORE_SIGMOID;
+    const unsigned grid = (unsigned)(g.groups * g.slices);
+    STRATA_BY_WIDTH(grad_vpl, p, sigmoid, grid, st)
+}
+
+}  // namespace strata

@@ -15,6 +15,7 @@ namespace strata {
 // word 1: ticket of the layout kernel (returns to 0 after every call)
 // word 2: work-claim counter of dispatch, word 4: of combine, word 6: of the collectives, word 8: of the experts'
 //         products (each returns to 0 inside the kernel)
+// word 10: ticket of the balance loss (returns to 0 after every call)
 // bytes [256, ...): per-tile, per-expert counts, int32 [n_tiles, E]
 // the last collective_table_bytes() bytes: pair table of all-to-all-v
 constexpr int kWsHeaderBytes = 256;

@@ -21,6 +21,21 @@ cudaError_t launch_quantize(const void* x, long long x_stride, long long rows, i
 cudaError_t configure_matmul_kernels();
 cudaError_t launch_expert_matmul(const strata_moe_shape& s, const strata_moe_layout_t& L, const strata_matmul_args& a,
                                  int* status, WorkQueue wq, int n_sm, cudaStream_t st);
+cudaError_t launch_quantize4(const void* x, long long x_stride, long long rows, int cols, int type, const strata_rows4& q,
+                             const int32_t* n_valid, cudaStream_t st);
+cudaError_t launch_dequantize4(const strata_rows4& q, long long rows, int cols, int type, void* out, int out_type,
+                               long long out_stride, const int32_t* n_valid, cudaStream_t st);
+cudaError_t configure_matmul4_kernels();
+cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_layout_t& L, const strata_matmul4_args& a,
+                                  int* status, WorkQueue wq, int n_sm, cudaStream_t st);
+size_t balance_scratch_bytes(const strata_moe_shape& s, const strata_balance_params& b, int n_sm);
+cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_params& b, const void* logits, int type,
+                                long long stride, const int32_t* ids, float* loss, const strata_balance_stats& stats,
+                                void* scratch, int* status, unsigned* ticket, int n_sm, cudaStream_t st, int* n_launches);
+cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_params& b, const void* logits, int type,
+                                long long stride, const int32_t* ids, const strata_balance_stats& stats, const float* dloss,
+                                const void* add, long long add_stride, void* dlogits, long long dstride, int n_sm,
+                                cudaStream_t st);
 
 #ifdef __CUDACC__
 // A wait with a limit.  False if it ran out, here or in another thread of the block (`dead`, in shared memory): the status then

@@ -1,5 +1,5 @@
 // C ABI of strata_layer.h: argument validation and kernel launches.  Host-side only; the kernels live in route.cu,
-// norm.cu and matmul.cu.
+// norm.cu, matmul.cu, rows4.cu, matmul4.cu and balance.cu.
 #include <cmath>
 
 #include "ctx.cuh"
@@ -11,6 +11,8 @@ using namespace strata;
 
 constexpr int kMaxCols = 32768;          // longest row the norm and the quantiser hold in registers
 constexpr int kMaxInner = 131056;        // 2^31 / 128^2, less one: int8 sums cannot overflow int32
+
+constexpr int kMaxInner4 = 131072;       // of the 4-bit products
 
 WorkQueue matmul_queue(const strata_ctx* c) { return WorkQueue{reinterpret_cast<unsigned int*>(c->ws) + 8}; }
 
@@ -48,6 +50,34 @@ strata_status check_codes(const void* q, int64_t q_stride, const float* q_scale,
 bool bad_extent(int64_t rows, int32_t cols)
 {
     return rows < 0 || rows >= (1ll << 31) || cols < 8 || cols % 8 != 0 || cols > kMaxCols;
+}
+
+// 4-bit rows: what every use of them asks for; `type` decides how many scale bytes a row has
+strata_status check_rows4(const strata_rows4& q, int32_t type, int32_t cols)
+{
+    if (type != STRATA_T_MXF4 && type != STRATA_T_NVF4) return STRATA_ERR_INVALID_ARG;
+    if (!q.codes || !q.block) return STRATA_ERR_INVALID_ARG;
+    if (cols < 32 || cols % 32 != 0) return STRATA_ERR_SHAPE;
+    const int64_t scales = cols / (type == STRATA_T_NVF4 ? 16 : 32);
+    if (q.code_stride < cols / 2 || q.code_stride % 16 != 0 || q.code_stride >= (1ll << 40)) return STRATA_ERR_SHAPE;
+    if (q.block_stride < scales || q.block_stride % 16 != 0 || q.block_stride >= (1ll << 40)) return STRATA_ERR_SHAPE;
+    if (q.scale && q.scale_stride < 1) return STRATA_ERR_SHAPE;
+    return on(q.codes, 16) && on(q.block, 16) && on(q.scale, 4) ? STRATA_OK : STRATA_ERR_ALIGNMENT;
+}
+
+strata_status check_balance(const strata_ctx* ctx, const strata_balance_params* b)
+{
+    if (!ctx || !b) return STRATA_ERR_INVALID_ARG;
+    if (b->score != STRATA_SCORE_SOFTMAX && b->score != STRATA_SCORE_SIGMOID) return STRATA_ERR_INVALID_ARG;
+    if (b->per_rank != 0 && b->per_rank != 1) return STRATA_ERR_INVALID_ARG;
+    if (!std::isfinite(b->weight) || !std::isfinite(b->z_weight)) return STRATA_ERR_INVALID_ARG;
+    return (int64_t)ctx->shape.R * ctx->shape.T < (1ll << 31) ? STRATA_OK : STRATA_ERR_SHAPE;
+}
+strata_status check_logits(const strata_ctx* ctx, const void* p, int32_t type, int64_t stride)
+{
+    if (type != STRATA_T_BF16 && type != STRATA_T_F32) return STRATA_ERR_INVALID_ARG;
+    if (stride < ctx->shape.E) return STRATA_ERR_SHAPE;
+    return on(p, type == STRATA_T_F32 ? 4 : 2) ? STRATA_OK : STRATA_ERR_ALIGNMENT;
 }
 
 #define STRATA_CHECK(call)                          \
@@ -187,6 +217,113 @@ strata_status strata_moe_expert_matmul(strata_ctx* ctx, const strata_moe_layout_
     DeviceGuard g(ctx->device);
     if (!g.ok) return STRATA_ERR_CUDA;
     return launched(ctx, launch_expert_matmul(s, *layout, *a, ctx->ws, matmul_queue(ctx), ctx->n_sm, static_cast<cudaStream_t>(stream)));
+}
+
+strata_status strata_quantize_rows4(strata_ctx* ctx, const void* x, int64_t x_stride, int64_t rows, int32_t cols,
+                                    int32_t type, const strata_rows4* q, const int32_t* n_valid, void* stream)
+{
+    if (!ctx || !q) return STRATA_ERR_INVALID_ARG;
+    if (bad_extent(rows, cols) || cols % 32 != 0) return STRATA_ERR_SHAPE;
+    if (rows == 0) return STRATA_OK;
+    if (!x) return STRATA_ERR_INVALID_ARG;
+    STRATA_CHECK(check_rows4(*q, type, cols));
+    if ((q->scale != nullptr) != (type == STRATA_T_NVF4)) return STRATA_ERR_INVALID_ARG;
+    STRATA_CHECK(check_rows16(x, x_stride, cols));
+    if (!on(n_valid, 4)) return STRATA_ERR_ALIGNMENT;
+    if (ctx->device < 0) return STRATA_ERR_CUDA;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return STRATA_ERR_CUDA;
+    return launched(ctx, launch_quantize4(x, x_stride, rows, cols, type, *q, n_valid, static_cast<cudaStream_t>(stream)));
+}
+
+strata_status strata_dequantize_rows4(strata_ctx* ctx, const strata_rows4* q, int64_t rows, int32_t cols, int32_t type,
+                                      void* out, int32_t out_type, int64_t out_stride, const int32_t* n_valid, void* stream)
+{
+    if (!ctx || !q) return STRATA_ERR_INVALID_ARG;
+    if (bad_extent(rows, cols) || cols % 32 != 0) return STRATA_ERR_SHAPE;
+    if (rows == 0) return STRATA_OK;
+    if (!out || (out_type != STRATA_T_BF16 && out_type != STRATA_T_F32)) return STRATA_ERR_INVALID_ARG;
+    STRATA_CHECK(check_rows4(*q, type, cols));
+    if (out_stride < cols || out_stride % (out_type == STRATA_T_F32 ? 4 : 8) != 0) return STRATA_ERR_SHAPE;
+    if (!on(out, 16) || !on(n_valid, 4)) return STRATA_ERR_ALIGNMENT;
+    if (ctx->device < 0) return STRATA_ERR_CUDA;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return STRATA_ERR_CUDA;
+    return launched(ctx, launch_dequantize4(*q, rows, cols, type, out, out_type, out_stride, n_valid,
+                                            static_cast<cudaStream_t>(stream)));
+}
+
+strata_status strata_moe_expert_matmul4(strata_ctx* ctx, const strata_moe_layout_t* layout, const strata_matmul4_args* a,
+                                        void* stream)
+{
+    if (!ctx || !layout || !a || !a->out) return STRATA_ERR_INVALID_ARG;
+    if (!layout->expert_offset || !layout->expert_count) return STRATA_ERR_INVALID_ARG;
+    if (a->gated != 0 && a->gated != 1) return STRATA_ERR_INVALID_ARG;
+    const strata_moe_shape& s = ctx->shape;
+    if (a->inner < 32 || a->inner % 32 != 0 || a->inner > kMaxInner4) return STRATA_ERR_SHAPE;
+    if (a->channels < 1 || (a->gated && a->channels % 2 != 0) || a->channels > (1 << 24)) return STRATA_ERR_SHAPE;
+    if ((int64_t)a->channels * s.E >= (1ll << 31)) return STRATA_ERR_SHAPE;
+    if (a->a_rows >= (1ll << 31) || a->out_stride < a->channels / (a->gated ? 2 : 1)) return STRATA_ERR_SHAPE;
+    STRATA_CHECK(check_rows4(a->a, a->type, a->inner));
+    STRATA_CHECK(check_rows4(a->w, a->type, a->inner));
+    // a tensor map holds the distance between two experts' weights in 40 bits
+    if (a->w.code_stride * a->channels >= (1ll << 40) || a->w.block_stride * a->channels >= (1ll << 40)) return STRATA_ERR_SHAPE;
+    if (!on(a->out, 2)) return STRATA_ERR_ALIGNMENT;
+    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
+    if (a->a_rows < (int64_t)recv_rows(s)) return STRATA_ERR_CAPACITY;
+    if (ctx->device < 0) return STRATA_ERR_CUDA;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return STRATA_ERR_CUDA;
+    return launched(ctx, launch_expert_matmul4(s, *layout, *a, ctx->ws, matmul_queue(ctx), ctx->n_sm, static_cast<cudaStream_t>(stream)));
+}
+
+strata_status strata_moe_balance_scratch_bytes(strata_ctx* ctx, const strata_balance_params* params, size_t* bytes)
+{
+    STRATA_CHECK(check_balance(ctx, params));
+    if (!bytes) return STRATA_ERR_INVALID_ARG;
+    *bytes = balance_scratch_bytes(ctx->shape, *params, ctx->n_sm_device);
+    return STRATA_OK;
+}
+
+strata_status strata_moe_balance_loss(strata_ctx* ctx, const strata_balance_params* params, const void* logits,
+                                      int32_t logits_type, int64_t logits_stride, const int32_t* topk_ids, float* loss,
+                                      const strata_balance_stats* stats, void* scratch, size_t scratch_bytes, void* stream)
+{
+    STRATA_CHECK(check_balance(ctx, params));
+    if (!logits || !topk_ids || !loss || !stats || !stats->count || !stats->tokens || !stats->prob || !scratch)
+        return STRATA_ERR_INVALID_ARG;
+    STRATA_CHECK(check_logits(ctx, logits, logits_type, logits_stride));
+    if (!on(topk_ids, 4) || !on(loss, 4) || !on(stats->count, 4) || !on(stats->tokens, 4) || !on(stats->prob, 4) || !on(scratch, 16))
+        return STRATA_ERR_ALIGNMENT;
+    if (!ctx->ws) return STRATA_ERR_WORKSPACE;
+    if (scratch_bytes < balance_scratch_bytes(ctx->shape, *params, ctx->n_sm_device)) return STRATA_ERR_CAPACITY;
+    if (ctx->device < 0) return STRATA_ERR_CUDA;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return STRATA_ERR_CUDA;
+    int n = 0;
+    const cudaError_t err =
+        launch_balance_loss(ctx->shape, *params, logits, logits_type, logits_stride, topk_ids, loss, *stats, scratch, ctx->ws,
+                            reinterpret_cast<unsigned*>(ctx->ws) + 10, ctx->n_sm_device, static_cast<cudaStream_t>(stream), &n);
+    return launched(ctx, err, (uint64_t)n);
+}
+
+strata_status strata_moe_balance_grad(strata_ctx* ctx, const strata_balance_params* params, const void* logits,
+                                      int32_t logits_type, int64_t logits_stride, const int32_t* topk_ids,
+                                      const strata_balance_stats* stats, const float* dloss, const void* add,
+                                      int64_t add_stride, void* dlogits, int64_t dlogits_stride, void* stream)
+{
+    STRATA_CHECK(check_balance(ctx, params));
+    if (!logits || !topk_ids || !stats || !stats->count || !stats->tokens || !dlogits) return STRATA_ERR_INVALID_ARG;
+    STRATA_CHECK(check_logits(ctx, logits, logits_type, logits_stride));
+    STRATA_CHECK(check_logits(ctx, dlogits, logits_type, dlogits_stride));
+    if (add) STRATA_CHECK(check_logits(ctx, add, logits_type, add_stride));
+    if (!on(topk_ids, 4) || !on(stats->count, 4) || !on(stats->tokens, 4) || !on(dloss, 4)) return STRATA_ERR_ALIGNMENT;
+    if (ctx->device < 0) return STRATA_ERR_CUDA;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return STRATA_ERR_CUDA;
+    return launched(ctx, launch_balance_grad(ctx->shape, *params, logits, logits_type, logits_stride, topk_ids, *stats, dloss, add,
+                                             add_stride, dlogits, dlogits_stride, ctx->n_sm_device,
+                                             static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"
