@@ -3,44 +3,63 @@
 // formulas).  The matrix instructions take the block scales themselves, from TMEM.
 //
 // As in 8 bits the weights are the M operand and the rows the N operand (matmul.cu).  A stage is 128 bytes of codes of every row, 256
-// values, which is one swizzle span, and a box of 16 scale bytes of every row.  The instructions want the scales of 128 rows as
-// 32 lines of 4 words, one word (4 scales) of rows l, l + 32, l + 64 and l + 96 per line: TMA brings 128 rows of 4 words, and a
-// warp turns them in place, lane l the 4 x 4 words of its four rows.
+// values, which is one swizzle span.  Scales come in groups of 32 or 64 bytes of every row, for several stages: a box of 16
+// bytes per stage took as many requests of the copy engine as the codes themselves.  The instructions want the scales of 128 rows
+// as 32 lines, word (4 scales) by word, of rows l, l + 32, l + 64 and l + 96, in each of TMEM's four quarters: four warps read the rows
+// from shared memory and store them to their quarters.  (tcgen05.cp from lines prepared in shared memory takes about
+// 60 cycles each in which the matrix unit does nothing: a quarter of the time at 512 rows per expert, a third with e4m3 scales.)
+//
+// CG = 2: two CTAs share a tile.  Each holds its own 128 weight rows and half of the tile's rows, and one instruction of the leader
+// multiplies for both; an SM then reads 7 KB of shared memory for what takes it 10 KB alone, and fetches half the rows from L2.
 #include "tiles.cuh"
+
+#ifdef STRATA_TEST_HOOKS
+#include <atomic>
+#endif
 
 namespace strata {
 
 namespace {
 
-constexpr int kM = 128;                 // channels of a matrix instruction
+#ifdef STRATA_TEST_HOOKS
+std::atomic<int> g_inject_short_load4{0};    // see matmul.cu
+#endif
+
+constexpr int kM = 128;                 // channels of a matrix instruction, in one CTA
 constexpr int kKBytes = 128;            // bytes of codes of a row in a stage: one swizzle span, 256 values
 constexpr int kUmmaK = 32;              // the same of a matrix instruction: 64 values
 constexpr int kBlock = kM * kKBytes;    // codes of one 128-row block of weights in a stage
-constexpr int kScaleBox = 16;           // scale bytes of a row in a stage
-constexpr int kScales = kM * kScaleBox; // scales of 128 rows
+constexpr int kChunk = 16;              // scale bytes of a row that TMEM takes at a time: 4 words
+constexpr int kGroups = 2;              // groups of scales in shared memory, chunks of them in TMEM
+constexpr int kScaleWarps = 4;
 
-// A tile is MB blocks of 128 weight rows by up to BN rows of the N operand (see matmul.cu for the gated forms).
-template <bool NV, int MB, int BN>
+// A tile of a CTA is MB blocks of 128 weight rows by up to BN rows of the N operand (see matmul.cu for the gated forms), of which
+// it holds BN / CG.
+template <bool NV, int CG, int MB, int BN>
 struct Tile4 {
-    static constexpr int box_rows = BN >= 192 ? 64 : 32;            // rows of one TMA box of the N operand
-    static constexpr int n_blocks = (BN + 127) / 128;
-    static constexpr int w_stage = MB * kBlock, a_stage = BN * kKBytes;
-    static constexpr int ws_stage = MB * kScales, as_stage = n_blocks * kScales;
-    static constexpr int stage_bytes = w_stage + a_stage + ws_stage + as_stage;
-    static constexpr int stages = 208 * 1024 / stage_bytes < 8 ? 208 * 1024 / stage_bytes : 8;
-    static constexpr int words = NV ? 4 : 2;                        // scale words of a row that a stage uses
-    static constexpr int sw_cols = MB * words * 4, sa_cols = n_blocks * words * 4;    // TMEM columns of a stage's scales
-    static constexpr int scale_cols = 2 * (sw_cols + sa_cols);      // two stages in turn
+    static constexpr int own_rows = BN / CG;                        // rows of the N operand in this CTA
+    static constexpr int box_rows = 32;                             // rows of one TMA box of the N operand
+    static constexpr int w_stage = MB * kBlock, a_stage = own_rows * kKBytes, stage_bytes = w_stage + a_stage;
+    static constexpr int group_bytes = BN <= 64 ? 64 : 32;          // scale bytes of a row in a group
+    static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // stages that a group serves
+    static constexpr int per_chunk = kChunk / (NV ? 16 : 8);
+    static constexpr int words = 4 / per_chunk;                     // scale words of a row that a stage uses
+    static constexpr int ws_group = MB * kM * group_bytes, as_group = BN * group_bytes;
+    static constexpr int a_cols = (BN / 32 + 3) / 4 * 4;            // TMEM columns of a word of the rows' scales
+    static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kGroups * chunk_cols;
     static constexpr int bufs = 2 * MB * BN + scale_cols <= 512 ? 2 : 1;
     static constexpr int acc_cols = bufs * MB * BN;
     static constexpr int used_cols = acc_cols + scale_cols;
     static constexpr int tmem_cols = used_cols <= 128 ? 128 : used_cols <= 256 ? 256 : 512;
-    static constexpr int epi_warps = MB == 2 ? 8 : 4;
-    static constexpr int threads = 128 + 32 * epi_warps;            // warps 0: loads, 1: matrix instructions, 2 and 3: scales
-    static constexpr int cols = BN / (epi_warps / 4);
-    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 8 * 32 : 0;
-    static constexpr size_t data_bytes = (size_t)stages * stage_bytes;
-    static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_stage % 1024 == 0 && data_bytes % 1024 == 0, "");
+    static constexpr int epi_warps = BN > 64 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
+    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 1;
+    static constexpr int threads = 32 * (mma_warp + 1);
+    static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
+    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 8 * 32 : 0;    // exchange of a gated tile
+    static constexpr int ring = (swap_floats > 8 * 1024 / 4 ? 192 : 208) * 1024 - kGroups * (ws_group + as_group);
+    static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
+    static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)kGroups * (ws_group + as_group);
+    static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_stage % 1024 == 0 && own_rows % box_rows == 0, "");
 };
 
 struct Mat4Params {
@@ -56,103 +75,213 @@ struct Mat4Params {
     int E, k_blocks, channels, m_tiles; // channels: rows of w per expert
     int last_steps;                     // matrix instructions of the last inner block
     int out_words;                      // pairs of channels of out lie on 4 bytes
+#ifdef STRATA_TEST_HOOKS
+    int test_flags;
+#endif
 };
 
 constexpr int kClaims = 4;              // tiles that the loading warp may be ahead of the epilogue
 
 struct Smem4Tail {                      // behind the operand stages
-    uint64_t full[8], ready[8], empty[8], tmem_full[2], tmem_empty[2], drain;
+    uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], drain, pad64;
+    uint64_t group_full[kGroups], group_empty[kGroups];          // scales in shared memory
+    uint64_t chunk_full[kGroups], chunk_empty[kGroups];          // scales in TMEM
     uint64_t claim_full[kClaims], claim_empty[kClaims];
     unsigned claim[kClaims];
-    uint32_t tmem_base, issued;
-    int dead, pad[3];
+    uint32_t tmem_base, issued, issued_groups;
+    int dead, pad[4];
 };
 static_assert(sizeof(Smem4Tail) % 16 == 0, "the scales behind it are read in vectors");
 
-// Descriptor of 32 lines of 16 bytes without a swizzle: 128 bytes between groups of eight lines.
-__device__ __forceinline__ uint64_t scale_desc(uint32_t addr)
-{
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (1ull << 16) | (8ull << 32) | (1ull << 46);
-}
-__device__ __forceinline__ void copy_scales(uint32_t tmem, uint64_t desc)
-{
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(tmem), "l"(desc) : "memory");
-}
 // Instruction descriptor: A and B e2m1, K-major; scales e8m0 or e4m3; `id`: first of the instruction's scales in their word.
-template <bool NV>
+template <bool NV, int CG>
 __device__ __forceinline__ uint32_t instr_desc4(int n, int id)
 {
-    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (NV ? 0u : 1u << 23) | ((uint32_t)(kM >> 7) << 27) |
+    return (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (NV ? 0u : 1u << 23) | ((uint32_t)(CG * kM >> 7) << 27) |
            ((uint32_t)id << 4) | ((uint32_t)id << 29);
 }
-template <bool NV>
-__device__ __forceinline__ void mma4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
+// Low words of operand descriptors (tiles.cuh: smem_desc); their high word is the same everywhere.
+constexpr uint32_t kDescHigh = 64u | (1u << 14) | (2u << 29);
+__device__ __forceinline__ uint32_t desc_low(uint32_t addr) { return ((addr & 0x3ffffu) >> 4) | (1u << 16); }
+#define STRATA_MMA4(group, kind, vec)                                                                                           \
+    asm volatile(                                                                                                               \
+        "{\n\t.reg .pred p;\n\t.reg .b64 a, b;\n\tsetp.ne.u32 p, %6, 0;\n\tmov.b64 a, {%1, %7};\n\tmov.b64 b, {%2, %7};\n\t"       \
+        "tcgen05.mma.cta_group::" group ".kind::" kind ".block_scale.scale_vec::" vec " [%0], a, b, %3, [%4], [%5], p;\n\t}" ::"r"( \
+            d),                                                                                                                 \
+        "r"(a), "r"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate), "n"(kDescHigh)                                           \
+        : "memory")
+template <bool NV, int CG>
+__device__ __forceinline__ void mma4(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                      uint32_t accumulate)
 {
-    if constexpr (NV)
+    if constexpr (CG == 1 && NV) STRATA_MMA4("1", "mxf4nvf4", "4X");
+    else if constexpr (CG == 1) STRATA_MMA4("1", "mxf4", "2X");
+    else if constexpr (NV) STRATA_MMA4("2", "mxf4nvf4", "4X");
+    else STRATA_MMA4("2", "mxf4", "2X");
+}
+// One lane of a converged warp, always the same.  The warps that issue loads and matrix instructions stay together but for the
+// instruction itself: their operands must lie in uniform registers, and where a single thread runs the loop each one is
+// moved there every time (90 cycles per load and 100 per matrix instruction).
+__device__ __forceinline__ bool elected()
+{
+    uint32_t r;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(r));
+    return r != 0;
+}
+// Arrives at the barrier (of both CTAs of a pair) when all instructions issued so far are done.
+template <int CG>
+__device__ __forceinline__ void commit4(uint64_t* bar)
+{
+    if constexpr (CG == 1) {
+        mma_commit(bar);
+    } else {
         asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4nvf4.block_scale.scale_vec::4X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(smem_addr(bar)),
+            "h"((uint16_t)3)
             : "memory");
+    }
+}
+
+// The same place in the shared memory of CTA `rank` of the pair.
+__device__ __forceinline__ uint32_t in_cta(const void* p, uint32_t rank)
+{
+    uint32_t a;
+    asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(a) : "r"(smem_addr(p)), "r"(rank));
+    return a;
+}
+// Arrives at the leader's barrier.  No data in memory is handed over with it (TMEM has its own fences), so the arrival releases at
+// CTA scope only: at cluster scope it waits for all that the warp has in flight, 1,300 cycles.
+template <int CG>
+__device__ __forceinline__ void arrive_leader(uint64_t* bar)
+{
+    if constexpr (CG == 1) mbar_arrive(bar);
+    else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_cta(bar, 0)) : "memory");
+}
+// A wait by all lanes of a converged warp, which stay together.  `peeked`: a try made earlier had found the phase complete.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status, bool peeked = false)
+{
+    return peeked || __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, status));
+}
+__device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity)
+{
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok)
+        : "r"(smem_addr(bar)), "r"(parity)
+        : "memory");
+    return __all_sync(0xffffffffu, ok != 0);
+}
+// Loads of codes count at the leader's barrier.
+template <int CG>
+__device__ __forceinline__ void load4_2d(void* dst, const CUtensorMap* map, int x, int y, uint64_t* bar, uint32_t leader_bar)
+{
+    if constexpr (CG == 1) tma_load_2d(dst, map, x, y, bar);
     else
         asm volatile(
-            "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %6, 0;\n\t"
-            "tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n\t}" ::"r"(d),
-            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            "cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3}], "
+            "[%4];" ::"r"(smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(leader_bar)
+            : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void load4_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar, uint32_t leader_bar)
+{
+    if constexpr (CG == 1) tma_load_3d(dst, map, x, y, z, bar);
+    else
+        asm volatile(
+            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], "
+            "[%5];" ::"r"(smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar)
             : "memory");
 }
 
-// 128 rows of four words become, for each of the four, 32 lines of one word of rows l, l + 32, l + 64 and l + 96.  A lane reads
-// and writes the same 64 bytes.
-__device__ __forceinline__ void turn_scales(unsigned char* block, int lane)
+__device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
 {
-    uint4* at = reinterpret_cast<uint4*>(block) + lane;
-    const uint4 a = at[0], b = at[32], c = at[64], d = at[96];
-    at[0] = make_uint4(a.x, b.x, c.x, d.x);
-    at[32] = make_uint4(a.y, b.y, c.y, d.y);
-    at[64] = make_uint4(a.z, b.z, c.z, d.z);
-    at[96] = make_uint4(a.w, b.w, c.w, d.w);
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+        : "memory");
+}
+// Four words of the scales of 128 rows, lane l those of rows l, l + 32, l + 64 and l + 96: `word` columns from one word to the next.
+template <int ROW_BYTES>
+__device__ __forceinline__ void read_scales(const unsigned char* rows, int n, int lane, uint4 (&v)[4])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (32 * j < n) v[j] = *reinterpret_cast<const uint4*>(rows + (lane + 32 * j) * ROW_BYTES);
+        else v[j] = make_uint4(0, 0, 0, 0);
+}
+__device__ __forceinline__ void by_word(const uint4 (&v)[4], uint32_t (&r)[16])
+{
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        r[j] = v[j].x;
+        r[4 + j] = v[j].y;
+        r[8 + j] = v[j].z;
+        r[12 + j] = v[j].w;
+    }
 }
 
+// The n-th tile that the loading warp handed over, by all lanes of a warp, which have all read it when this returns.
 __device__ __forceinline__ bool next_tile(Smem4Tail& tail, uint32_t n, unsigned& t, volatile int* dead, int* status)
 {
-    if (!wait_or_dead(&tail.claim_full[n % kClaims], (n / kClaims) & 1, dead, status)) return false;
-    t = *reinterpret_cast<volatile unsigned*>(&tail.claim[n % kClaims]);
+    if (!warp_wait(&tail.claim_full[n % kClaims], (n / kClaims) & 1, dead, status)) return false;
+    t = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile unsigned*>(&tail.claim[n % kClaims]), 0);
     return true;
 }
-
-template <bool NV, bool GATED, int MB, int BN>
-__global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_kernel(const __grid_constant__ Mat4Params p)
+// claim_unit of common.cuh for `claimers` CTAs, which start on the first tiles
+__device__ __forceinline__ unsigned claim_tile(const WorkQueue& q, unsigned n_units, unsigned claimers, bool& exhausted)
 {
-    using T = Tile4<NV, MB, BN>;
+    if (claimers >= n_units || exhausted) return kNoUnit;
+    const unsigned old = atomicAdd(q.next, 1u);
+    if (claimers + old < n_units) return claimers + old;
+    exhausted = true;
+    if (old == n_units - 1) *q.next = 0;                             // the last of the failed claims, one per claimer
+    return kNoUnit;
+}
+
+template <bool NV, bool GATED, int CG, int MB, int BN>
+__global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matmul4_kernel(const __grid_constant__ Mat4Params p)
+{
+    using T = Tile4<NV, CG, MB, BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
     unsigned char* s_w = smem;                                       // [stages][MB * 128][128]
-    unsigned char* s_a = s_w + T::stages * T::w_stage;               // [stages][BN][128]
-    unsigned char* s_ws = s_a + T::stages * T::a_stage;              // [stages][MB * 128][16]
-    unsigned char* s_as = s_ws + T::stages * T::ws_stage;            // [stages][n_blocks * 128][16]
+    unsigned char* s_a = s_w + T::stages * T::w_stage;               // [stages][own rows][128]
+    unsigned char* s_ws = s_a + T::stages * T::a_stage;              // [groups][MB * 128][group bytes]
+    unsigned char* s_as = s_ws + kGroups * T::ws_group;              // [groups][BN][group bytes]
     Smem4Tail* tail = reinterpret_cast<Smem4Tail*>(smem + T::data_bytes);
     float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
     float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][2][8][32]
     int* s_base = reinterpret_cast<int*>(s_swap + T::swap_floats);   // [E + 1]
     int* s_off = s_base + p.E + 1;                                   // [E]
     int* s_cnt = s_off + p.E;                                        // [E]
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = (int)threadIdx.x & 31;
+    const uint32_t rank = CG == 1 ? 0u : blockIdx.x & 1u;            // place in the pair; 0: the leader
+    const unsigned team = blockIdx.x / CG, teams = gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < T::stages; ++s) {
             mbar_init(&tail->full[s], 1);
-            mbar_init(&tail->ready[s], 2);
             mbar_init(&tail->empty[s], 1);
+        }
+        for (int g = 0; g < kGroups; ++g) {
+            mbar_init(&tail->group_full[g], 1);
+            mbar_init(&tail->group_empty[g], kScaleWarps);
+            mbar_init(&tail->chunk_full[g], CG * kScaleWarps);
+            mbar_init(&tail->chunk_empty[g], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&tail->tmem_full[b], 1);
-            mbar_init(&tail->tmem_empty[b], T::epi_warps);
+            mbar_init(&tail->tmem_empty[b], CG * T::epi_warps);
         }
-        for (int c = 0; c < kClaims; ++c) {
-            mbar_init(&tail->claim_full[c], 1);
-            mbar_init(&tail->claim_empty[c], 3 + T::epi_warps);
+        for (int c = 0; c < kClaims; ++c) {                          // consumers: both loaders but the claiming one, the leader's
+            mbar_init(&tail->claim_full[c], 1);                      // matrix warp, all scale and epilogue warps
+            mbar_init(&tail->claim_empty[c], CG * (1 + kScaleWarps + T::epi_warps));
         }
         mbar_init(&tail->drain, 1);
         tail->dead = 0;
@@ -162,11 +291,18 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
         asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_ws) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_as) : "memory");
     }
-    if (warp == 1) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tail->tmem_base)),
-                     "n"(T::tmem_cols)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    if (warp == T::mma_warp) {
+        if constexpr (CG == 1) {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tail->tmem_base)),
+                         "n"(T::tmem_cols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_addr(&tail->tmem_base)),
+                         "n"(T::tmem_cols)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        }
     }
     griddep_wait();
     // segments, kept inside the buffer whatever the offsets hold
@@ -196,139 +332,248 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
         if (lane == 0) s_base[p.E] = carry;
     }
     __syncthreads();
-    const uint32_t tmem = tail->tmem_base;
+    if constexpr (CG == 2) {                                         // both have their barriers before either touches the other's
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    const uint32_t tmem = __shfl_sync(0xffffffffu, tail->tmem_base, 0);
     const unsigned n_tiles = (unsigned)s_base[p.E] * (unsigned)p.m_tiles;
     volatile int* dead = &tail->dead;
 
-    if (warp == 0) {
-        if (lane == 0) {
-            uint32_t it = 0;
-            bool ok = true, exhausted = false;
-            unsigned t = blockIdx.x < n_tiles ? blockIdx.x : kNoUnit;
-            for (uint32_t n = 0; ok; ++n) {
-                // hand the tile to the other warps (kNoUnit ends their loops), then claim the next one
-                if (!wait_or_dead(&tail->claim_empty[n % kClaims], ((n / kClaims) & 1) ^ 1, dead, p.status)) break;
-                tail->claim[n % kClaims] = t;
-                mbar_arrive(&tail->claim_full[n % kClaims]);
-                if (t == kNoUnit) break;
-                const unsigned next = claim_unit(p.wq, n_tiles, gridDim.x, exhausted);
-                const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
-                const int boxes = (w.rows + T::box_rows - 1) / T::box_rows;
-                const uint32_t bytes = (uint32_t)(T::w_stage + T::ws_stage + boxes * T::box_rows * (kKBytes + kScaleBox));
-                for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                    const uint32_t s = it % T::stages;
-                    if (!wait_or_dead(&tail->empty[s], ((it / T::stages) & 1) ^ 1, dead, p.status)) {
+    if (warp == T::load_warp) {
+        uint32_t it = 0, git = 0, s = 0, phase = 0;
+        bool ok = true, exhausted = false, peeked = false;
+        unsigned t = team < n_tiles ? team : kNoUnit;
+        for (uint32_t n = 0; ok; ++n) {
+            // the leader hands the tile to all others (kNoUnit ends their loops), then claims the next one
+            unsigned next = kNoUnit;
+            if (rank == 0) {
+                if (!warp_wait(&tail->claim_empty[n % kClaims], ((n / kClaims) & 1) ^ 1, dead, p.status)) break;
+                if (lane == 0) {
+                    tail->claim[n % kClaims] = t;
+                    mbar_arrive(&tail->claim_full[n % kClaims]);
+                    if constexpr (CG == 2)
+                        asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(
+                                         in_cta(&tail->claim[n % kClaims], 1)),
+                                     "r"(t), "r"(in_cta(&tail->claim_full[n % kClaims], 1))
+                                     : "memory");
+                    if (t != kNoUnit) next = claim_tile(p.wq, n_tiles, teams, exhausted);
+                }
+            } else {
+                if (lane == 0) mbar_expect_tx(&tail->claim_full[n % kClaims], sizeof(unsigned));    // st.async completes it
+                __syncwarp();
+                if (!next_tile(*tail, n, t, dead, p.status)) break;
+                if (lane == 0) arrive_leader<CG>(&tail->claim_empty[n % kClaims]);
+            }
+            if (t == kNoUnit) break;
+            const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
+            const int expert = __shfl_sync(0xffffffffu, w.e, 0), m = __shfl_sync(0xffffffffu, w.m, 0) * CG + (int)rank;
+            const int first = __shfl_sync(0xffffffffu, w.row0, 0), rows = __shfl_sync(0xffffffffu, w.rows, 0);
+            const int half_n = ((rows + 15) & ~15) / CG;             // rows of the tile in each CTA
+            const int boxes = (half_n + T::box_rows - 1) / T::box_rows, all_boxes = (rows + T::box_rows - 1) / T::box_rows;
+            const int row0 = first + (int)rank * half_n;
+            const uint32_t bytes = (uint32_t)(CG * (T::w_stage + boxes * T::box_rows * kKBytes));
+            const uint32_t scale_bytes = (uint32_t)(T::ws_group + all_boxes * T::box_rows * T::group_bytes);
+            for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+                if (kb % T::per_group == 0) {
+                    const uint32_t g = git % kGroups;
+                    if (!warp_wait(&tail->group_empty[g], ((git / kGroups) & 1) ^ 1, dead, p.status)) {
                         ok = false;
                         break;
                     }
-                    mbar_expect_tx(&tail->full[s], bytes);
-                    unsigned char* dw = s_w + s * T::w_stage;
-                    unsigned char* ds = s_ws + s * T::ws_stage;
-                    const int sx = (NV ? kb : kb >> 1) * kScaleBox;  // two blocks of 256 values share a box of 16 scales of 32
-                    if constexpr (GATED) {                           // [2E][channels / 2][inner]: gate, up
+                    ++git;
+                    uint64_t* bar = &tail->group_full[g];
+                    unsigned char* dw = s_ws + g * T::ws_group;
+                    const int x = kb / T::per_group * T::group_bytes;
+                    if (elected()) {
+                        mbar_expect_tx(bar, scale_bytes);
+                        if constexpr (GATED) {                       // [2E][channels / 2][inner]: gate, up
+                            constexpr int kRows = MB * kM / 2;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+                                tma_load_3d(dw + h * kRows * T::group_bytes, &p.map_ws, x, m * kRows, 2 * expert + h, bar);
+                        } else {
+#pragma unroll
+                            for (int b = 0; b < MB; ++b)
+                                tma_load_3d(dw + b * kM * T::group_bytes, &p.map_ws, x, (m * MB + b) * kM, expert, bar);
+                        }
+                        for (int b = 0; b < all_boxes; ++b)
+                            tma_load_2d(s_as + g * T::as_group + b * T::box_rows * T::group_bytes, &p.map_as, x,
+                                        first + b * T::box_rows, bar);
+                    }
+                    __syncwarp();
+                }
+                if (!warp_wait(&tail->empty[s], phase ^ 1, dead, p.status, peeked)) {
+                    ok = false;
+                    break;
+                }
+                const uint32_t next_s = s + 1 == T::stages ? 0 : s + 1;
+                if (next_s == 0) phase ^= 1;
+                peeked = peek(&tail->empty[next_s], phase ^ 1);
+                uint64_t* bar = &tail->full[s];
+                const uint32_t leader_bar = CG == 1 ? 0u : in_cta(bar, 0);
+                unsigned char* dw = s_w + s * T::w_stage;
+                unsigned char* da = s_a + s * T::a_stage;
+                if (elected()) {
+                    if (rank == 0) {
+                        uint32_t expect = bytes;
+#ifdef STRATA_TEST_HOOKS
+                        if (p.test_flags && blockIdx.x == 0 && it == 0) expect += 16;
+#endif
+                        mbar_expect_tx(bar, expect);
+                    }
+                    if constexpr (GATED) {
                         constexpr int kRows = MB * kM / 2;
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            tma_load_3d(dw + g * kRows * kKBytes, &p.map_w, kb * kKBytes, w.m * kRows, 2 * w.e + g, &tail->full[s]);
-                            tma_load_3d(ds + g * kRows * kScaleBox, &p.map_ws, sx, w.m * kRows, 2 * w.e + g, &tail->full[s]);
-                        }
+                        for (int h = 0; h < 2; ++h)
+                            load4_3d<CG>(dw + h * kRows * kKBytes, &p.map_w, kb * kKBytes, m * kRows, 2 * expert + h, bar, leader_bar);
                     } else {
 #pragma unroll
-                        for (int b = 0; b < MB; ++b) {
-                            tma_load_3d(dw + b * kBlock, &p.map_w, kb * kKBytes, (w.m * MB + b) * kM, w.e, &tail->full[s]);
-                            tma_load_3d(ds + b * kScales, &p.map_ws, sx, (w.m * MB + b) * kM, w.e, &tail->full[s]);
-                        }
+                        for (int b = 0; b < MB; ++b)
+                            load4_3d<CG>(dw + b * kBlock, &p.map_w, kb * kKBytes, (m * MB + b) * kM, expert, bar, leader_bar);
                     }
-                    for (int b = 0; b < boxes; ++b) {
-                        tma_load_2d(s_a + s * T::a_stage + b * T::box_rows * kKBytes, &p.map_a, kb * kKBytes,
-                                    w.row0 + b * T::box_rows, &tail->full[s]);
-                        tma_load_2d(s_as + s * T::as_stage + b * T::box_rows * kScaleBox, &p.map_as, sx, w.row0 + b * T::box_rows,
-                                    &tail->full[s]);
-                    }
+                    for (int b = 0; b < boxes; ++b)
+                        load4_2d<CG>(da + b * T::box_rows * kKBytes, &p.map_a, kb * kKBytes, row0 + b * T::box_rows, bar, leader_bar);
                 }
-                t = next;
+                __syncwarp();
+                s = next_s;
             }
-            tail->issued = it;
+            t = __shfl_sync(0xffffffffu, next, 0);
         }
-    } else if (warp == 1) {
         if (lane == 0) {
-            uint32_t it = 0, use = 0;
-            bool ok = true;
+            tail->issued = it;
+            tail->issued_groups = git;
+        }
+    } else if (warp == T::mma_warp) {
+        if (rank == 0) {
+            uint32_t s = 0, phase = 0, cit = 0, use = 0;
+            bool ok = true, stage_peeked = false, chunk_peeked = false;
+            const uint32_t w_desc = desc_low(smem_addr(s_w)), a_desc = desc_low(smem_addr(s_a));
             for (; ok; ++use) {
                 unsigned t;
                 if (!next_tile(*tail, use, t, dead, p.status)) break;
-                mbar_arrive(&tail->claim_empty[use % kClaims]);
+                if (lane == 0) mbar_arrive(&tail->claim_empty[use % kClaims]);
                 if (t == kNoUnit) break;
                 const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
-                const int n = (w.rows + 15) & ~15;
+                const int n = (__shfl_sync(0xffffffffu, w.rows, 0) + 15) & ~15;
                 const uint32_t buf = use % T::bufs;
-                if (!wait_or_dead(&tail->tmem_empty[buf], ((use / T::bufs) & 1) ^ 1, dead, p.status)) break;
+                if (!warp_wait(&tail->tmem_empty[buf], ((use / T::bufs) & 1) ^ 1, dead, p.status)) break;
                 tmem_fence_after();
                 const uint32_t d = tmem + buf * MB * BN;
-                for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                    const uint32_t s = it % T::stages, parity = (it / T::stages) & 1;
-                    if (!wait_or_dead(&tail->full[s], parity, dead, p.status) || !wait_or_dead(&tail->ready[s], parity, dead, p.status)) {
+                const uint32_t idesc0 = instr_desc4<NV, CG>(n, 0), idesc1 = instr_desc4<NV, CG>(n, NV ? 0 : 2);
+                for (int kb = 0; kb < p.k_blocks; ++kb) {
+                    const uint32_t g = cit % kGroups;
+                    if ((kb % T::per_chunk == 0 &&
+                         !warp_wait(&tail->chunk_full[g], (cit / kGroups) & 1, dead, p.status, chunk_peeked)) ||
+                        !warp_wait(&tail->full[s], phase, dead, p.status, stage_peeked)) {
                         ok = false;
                         break;
                     }
                     tmem_fence_after();
-                    const uint64_t dw = smem_desc(smem_addr(s_w + s * T::w_stage));
-                    const uint64_t da = smem_desc(smem_addr(s_a + s * T::a_stage));
-                    const uint32_t sw = tmem + T::acc_cols + (it & 1) * (T::sw_cols + T::sa_cols), sa = sw + T::sw_cols;
-                    const int first = NV ? 0 : (kb & 1) * 2;         // word of the box that this stage begins with
-                    const uint64_t qw = scale_desc(smem_addr(s_ws + s * T::ws_stage) + first * 512);
-                    const uint64_t qa = scale_desc(smem_addr(s_as + s * T::as_stage) + first * 512);
-#pragma unroll
-                    for (int i = 0; i < T::words; ++i) {
-#pragma unroll
-                        for (int b = 0; b < MB; ++b) copy_scales(sw + (b * T::words + i) * 4, qw + b * (kScales >> 4) + i * (512 >> 4));
-#pragma unroll
-                        for (int b = 0; b < T::n_blocks; ++b)
-                            copy_scales(sa + (i * T::n_blocks + b) * 4, qa + b * (kScales >> 4) + i * (512 >> 4));
+                    const bool last = kb == p.k_blocks - 1, chunk_ends = kb % T::per_chunk == T::per_chunk - 1 || last;
+                    // whether the next stage is there is asked before this one's instructions, which take longer to issue than the
+                    // answer to come
+                    const uint32_t next_s = s + 1 == T::stages ? 0 : s + 1;
+                    if (next_s == 0) phase ^= 1;
+                    stage_peeked = peek(&tail->full[next_s], phase);
+                    if (chunk_ends) {
+                        ++cit;
+                        chunk_peeked = peek(&tail->chunk_full[cit % kGroups], (cit / kGroups) & 1);
                     }
-                    const int steps = kb == p.k_blocks - 1 ? p.last_steps : kKBytes / kUmmaK;
+                    const uint32_t dw = w_desc + s * (T::w_stage >> 4), da = a_desc + s * (T::a_stage >> 4);
+                    const int word = kb % T::per_chunk * T::words;   // of the chunk, where this stage begins
+                    const uint32_t sw = tmem + T::acc_cols + g * T::chunk_cols + word * 4;
+                    const uint32_t sa = tmem + T::acc_cols + g * T::chunk_cols + MB * 16 + word * T::a_cols;
+                    auto multiply = [&](int k) {
+                        const int i = NV ? k : k >> 1;
 #pragma unroll
-                    for (int k = 0; k < kKBytes / kUmmaK; ++k) {
-                        if (k < steps) {
-                            const int i = NV ? k : k >> 1;
-                            const uint32_t idesc = instr_desc4<NV>(n, NV ? 0 : (k & 1) * 2);
+                        for (int b = 0; b < MB; ++b)
+                            mma4<NV, CG>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4),
+                                         (k & 1) ? idesc1 : idesc0, sw + b * 16 + i * 4, sa + i * T::a_cols, (kb | k) != 0);
+                    };
+                    if (elected()) {
+                        if (!last) {
 #pragma unroll
-                            for (int b = 0; b < MB; ++b)
-                                mma4<NV>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4), idesc,
-                                         sw + (b * T::words + i) * 4, sa + i * T::n_blocks * 4, (kb | k) != 0);
+                            for (int k = 0; k < kKBytes / kUmmaK; ++k) multiply(k);
+                        } else {
+#pragma unroll
+                            for (int k = 0; k < kKBytes / kUmmaK; ++k)
+                                if (k < p.last_steps) multiply(k);
                         }
+                        commit4<CG>(&tail->empty[s]);
+                        if (chunk_ends) commit4<CG>(&tail->chunk_empty[g]);
+                        if (last) commit4<CG>(&tail->tmem_full[buf]);
                     }
-                    mma_commit(&tail->empty[s]);
+                    __syncwarp();
+                    s = next_s;
                 }
-                if (ok) mma_commit(&tail->tmem_full[buf]);
             }
-            if (*dead) {                                             // instructions in flight must end before TMEM is freed
-                mma_commit(&tail->drain);
+            if (__any_sync(0xffffffffu, *dead) && elected()) {       // instructions in flight must end before TMEM is freed
+                commit4<CG>(&tail->drain);
                 mbar_wait_bounded(&tail->drain, 0);
             }
+            __syncwarp();
         }
-    } else if (warp < 4) {                                           // warp 2: scales of the weights, warp 3: of the rows
-        uint32_t it = 0, use = 0;
+    } else if (warp < kScaleWarps) {                                 // scales to this warp's quarter of TMEM
+        uint32_t git = 0, cit = 0, use = 0;
         bool ok = true;
-        unsigned char* base = warp == 2 ? s_ws : s_as;
-        const int stage = warp == 2 ? T::ws_stage : T::as_stage;
+        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
         for (; ok; ++use) {
             unsigned t;
-            if (!__all_sync(0xffffffffu, next_tile(*tail, use, t, dead, p.status))) break;
-            if (lane == 0) mbar_arrive(&tail->claim_empty[use % kClaims]);
+            if (!next_tile(*tail, use, t, dead, p.status)) break;
+            if (lane == 0) arrive_leader<CG>(&tail->claim_empty[use % kClaims]);
             if (t == kNoUnit) break;
-            for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
-                const uint32_t s = it % T::stages;
-                ok = __all_sync(0xffffffffu, wait_or_dead(&tail->full[s], (it / T::stages) & 1, dead, p.status));
+            for (int kb = 0; kb < p.k_blocks; kb += T::per_chunk, ++cit) {
+                const uint32_t g = git % kGroups, c = cit % kGroups;
+                const int at = kb % T::per_group / T::per_chunk * kChunk;    // of the chunk in its group's rows
+                if (at == 0) ok = warp_wait(&tail->group_full[g], (git / kGroups) & 1, dead, p.status);
                 if (!ok) break;
-                for (int b = 0; b < stage; b += kScales) turn_scales(base + s * stage + b, lane);
-                fence_async_smem();
+                uint4 vw[MB][4], va[T::a_cols / 4][4];
+#pragma unroll
+                for (int b = 0; b < MB; ++b)
+                    read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes + at, kM, lane, vw[b]);
+#pragma unroll
+                for (int b = 0; b < T::a_cols / 4; ++b)
+                    read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes + at, BN - b * kM, lane, va[b]);
                 __syncwarp();
-                if (lane == 0) mbar_arrive(&tail->ready[s]);
+                if (at == T::group_bytes - kChunk || kb + T::per_chunk >= p.k_blocks) {
+                    if (lane == 0) mbar_arrive(&tail->group_empty[g]);
+                    ++git;
+                }
+                ok = warp_wait(&tail->chunk_empty[c], ((cit / kGroups) & 1) ^ 1, dead, p.status);
+                if (!ok) break;
+                tmem_fence_after();
+                const uint32_t to = tmem + T::acc_cols + c * T::chunk_cols + lanes;
+                uint32_t r[16];
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    by_word(vw[b], r);
+                    tmem_st16(to + b * 16, r);
+                }
+                if constexpr (T::a_cols == 4) {
+                    by_word(va[0], r);
+                    tmem_st16(to + MB * 16, r);
+                } else {                                             // two words of up to 256 rows at a time
+                    uint32_t q[16];
+                    by_word(va[0], r);
+                    by_word(va[T::a_cols / 4 - 1], q);
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t x[16] = {r[8 * h],     r[8 * h + 1], r[8 * h + 2], r[8 * h + 3], q[8 * h],     q[8 * h + 1],
+                                                q[8 * h + 2], q[8 * h + 3], r[8 * h + 4], r[8 * h + 5], r[8 * h + 6], r[8 * h + 7],
+                                                q[8 * h + 4], q[8 * h + 5], q[8 * h + 6], q[8 * h + 7]};
+                        tmem_st16(to + MB * 16 + h * 16, x);
+                    }
+                }
+                asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory");
+                tmem_fence_before();
+                __syncwarp();
+                if (lane == 0) arrive_leader<CG>(&tail->chunk_full[c]);
             }
         }
     } else {
-        const int ew = warp - 4, quad = warp & 3;                    // TMEM lanes 32*quad .. of this warp
+        const int ew = warp - kScaleWarps, quad = warp & 3;          // TMEM lanes 32*quad .. of this warp
+        const int pair = (ew >> 2) * 2 + (quad & 1);                 // of warps that exchange
         const int col0 = (ew >> 2) * T::cols;                        // first column of this warp
         float* scale = s_scale + ew * T::cols;
         const int half = p.channels / 2;
@@ -337,27 +582,27 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
             unsigned t;
             const bool got = next_tile(*tail, use, t, dead, p.status);
             if constexpr (GATED && MB == 1) {                        // the two warps of an exchange leave together
-                if (!pair_all(got, quad & 1)) break;
-            } else if (!__all_sync(0xffffffffu, got)) {
+                if (!pair_all(got, pair)) break;
+            } else if (!got) {
                 break;
             }
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&tail->claim_empty[use % kClaims]);
+            if (lane == 0) arrive_leader<CG>(&tail->claim_empty[use % kClaims]);
             if (t == kNoUnit) break;
             const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
+            const int m = w.m * CG + (int)rank;
             const uint32_t buf = use % T::bufs;
             const int rows = min(T::cols, w.rows - col0);            // of this warp; may be negative
             // channel(s) of w that this lane holds, and the first channel of out
             int ch[2], out_ch[2];
             if constexpr (GATED && MB == 1) {
-                out_ch[0] = w.m * (kM / 2) + (quad & 1) * 32 + lane;
+                out_ch[0] = m * (kM / 2) + (quad & 1) * 32 + lane;
                 ch[0] = out_ch[0] + (quad >> 1) * half;
             } else if constexpr (GATED) {
-                out_ch[0] = ch[0] = w.m * kM + quad * 32 + lane;
+                out_ch[0] = ch[0] = m * kM + quad * 32 + lane;
                 ch[1] = ch[0] + half;
             } else {
 #pragma unroll
-                for (int b = 0; b < MB; ++b) out_ch[b] = ch[b] = (w.m * MB + b) * kM + quad * 32 + lane;
+                for (int b = 0; b < MB; ++b) out_ch[b] = ch[b] = (m * MB + b) * kM + quad * 32 + lane;
             }
             const int limit = GATED ? half : p.channels;
             const bool words = p.out_words != 0;
@@ -371,10 +616,10 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
             for (int c = lane; c < T::cols; c += 32)
                 scale[c] = p.a_scale && c < rows ? p.a_scale[(long long)(w.row0 + col0 + c) * p.a_scale_stride] : 1.0f;
             __syncwarp();
-            const bool ok = wait_or_dead(&tail->tmem_full[buf], (use / T::bufs) & 1, dead, p.status);
+            const bool ok = warp_wait(&tail->tmem_full[buf], (use / T::bufs) & 1, dead, p.status);
             if constexpr (GATED && MB == 1) {
-                if (!pair_all(ok, quad & 1)) break;
-            } else if (!__all_sync(0xffffffffu, ok)) {
+                if (!pair_all(ok, pair)) break;
+            } else if (!ok) {
                 break;
             }
             tmem_fence_after();
@@ -399,7 +644,7 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
                     const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 8 * 32 + lane;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[c] : y[8 + c];
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + (quad & 1)) : "memory");
+                    asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
                     float o[8];
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
@@ -435,7 +680,7 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
             }
             tmem_fence_before();
             __syncwarp();
-            if (lane == 0) mbar_arrive(&tail->tmem_empty[buf]);
+            if (lane == 0) arrive_leader<CG>(&tail->tmem_empty[buf]);
         }
     }
     __syncwarp();
@@ -445,28 +690,42 @@ __global__ void __launch_bounds__(Tile4<NV, MB, BN>::threads, 1) expert_matmul4_
     tmem_fence_after();
     if (threadIdx.x == 0 && *dead) {                                 // loads in flight must land before the CTA leaves
         const uint32_t it = tail->issued, first = it > (uint32_t)T::stages ? it - T::stages : 0;
-        for (uint32_t u = first; u < it; ++u) mbar_wait_bounded(&tail->full[u % T::stages], (u / T::stages) & 1);
+        // the other CTA of a pair may have issued loads that the leader does not expect: it waits out the limit for them
+        for (uint32_t u = first; u < it + (CG == 2 ? 1u : 0u); ++u)
+            mbar_wait_bounded(&tail->full[u % T::stages], (u / T::stages) & 1);
+        const uint32_t groups = tail->issued_groups;
+        for (uint32_t u = groups > kGroups ? groups - kGroups : 0; u < groups; ++u)
+            mbar_wait_bounded(&tail->group_full[u % kGroups], (u / kGroups) & 1);
     }
-    if (warp == 1)
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::tmem_cols) : "memory");
+    if constexpr (CG == 2) {                                         // neither leaves while the other may still reach into it
+        __syncthreads();
+        asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    }
+    if (warp == T::mma_warp) {
+        if constexpr (CG == 1)
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::tmem_cols) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(T::tmem_cols) : "memory");
+    }
 }
 
-template <bool NV, int MB, int BN>
+template <bool NV, int CG, int MB, int BN>
 size_t smem_bytes4(int E)
 {
-    using T = Tile4<NV, MB, BN>;
+    using T = Tile4<NV, CG, MB, BN>;
     return 1024 + T::data_bytes + sizeof(Smem4Tail) + (size_t)(T::epi_warps * T::cols + T::swap_floats) * sizeof(float) +
            (size_t)(3 * E + 1) * sizeof(int);
 }
 
-template <bool NV, int MB, int BN>
+template <bool NV, int CG, int MB, int BN>
 cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Params& p, int n_sm, cudaStream_t st)
 {
-    using T = Tile4<NV, MB, BN>;
+    using T = Tile4<NV, CG, MB, BN>;
     const cuuint64_t groups = (cuuint64_t)s.E * (a.gated ? 2 : 1), rows = (cuuint64_t)a.channels / (a.gated ? 2 : 1);
     const cuuint32_t w_rows = (cuuint32_t)(a.gated ? MB * kM / 2 : kM);
     const cuuint64_t bytes[2] = {(cuuint64_t)a.inner / 2, (cuuint64_t)a.inner / (NV ? 16 : 32)};
-    const cuuint32_t box[2] = {kKBytes, kScaleBox};
+    const cuuint32_t box[2] = {kKBytes, T::group_bytes};
     const strata_rows4* ops[2] = {&a.w, &a.a};
     CUtensorMap* maps[2][2] = {{&p.map_w, &p.map_ws}, {&p.map_a, &p.map_as}};
     for (int o = 0; o < 2; ++o)
@@ -481,23 +740,23 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
                         i == 0 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE))
                 return cudaErrorInvalidValue;
         }
-    const int per_tile = MB * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
+    const int per_tile = CG * MB * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
     p.m_tiles = (wide + per_tile - 1) / per_tile;
     const long long tiles = row_tiles(s, a.a_rows, BN) * p.m_tiles;
     if (tiles >= (1ll << 31)) return cudaErrorInvalidConfiguration;
-    const unsigned grid = (unsigned)min(tiles, (long long)n_sm);
-    const size_t smem = smem_bytes4<NV, MB, BN>(s.E);
-    return a.gated ? launch_pdl(expert_matmul4_kernel<NV, true, MB, BN>, grid, T::threads, smem, st, p)
-                   : launch_pdl(expert_matmul4_kernel<NV, false, MB, BN>, grid, T::threads, smem, st, p);
+    const unsigned grid = CG * (unsigned)min(tiles, (long long)max(1, n_sm / CG));
+    const size_t smem = smem_bytes4<NV, CG, MB, BN>(s.E);
+    return a.gated ? launch_pdl_cluster(expert_matmul4_kernel<NV, true, CG, MB, BN>, grid, T::threads, smem, CG, st, p)
+                   : launch_pdl_cluster(expert_matmul4_kernel<NV, false, CG, MB, BN>, grid, T::threads, smem, CG, st, p);
 }
 
-template <bool NV, int MB, int BN>
+template <bool NV, int CG, int MB, int BN>
 cudaError_t configure4()
 {
-    const void* fns[2] = {(const void*)expert_matmul4_kernel<NV, true, MB, BN>, (const void*)expert_matmul4_kernel<NV, false, MB, BN>};
+    const void* fns[2] = {(const void*)expert_matmul4_kernel<NV, true, CG, MB, BN>, (const void*)expert_matmul4_kernel<NV, false, CG, MB, BN>};
     for (const void* f : fns) {
         const cudaError_t e =
-            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes4<NV, MB, BN>(kMaxExperts));
+            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes4<NV, CG, MB, BN>(kMaxExperts));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -505,9 +764,9 @@ cudaError_t configure4()
 template <bool NV>
 cudaError_t configure4_all()
 {
-    cudaError_t e = configure4<NV, 1, 64>();
-    if (e == cudaSuccess) e = configure4<NV, 2, 96>();
-    if (e == cudaSuccess) e = configure4<NV, 2, 192>();
+    cudaError_t e = configure4<NV, 1, 1, 64>();
+    if (e == cudaSuccess) e = configure4<NV, 1, 2, 96>();
+    if (e == cudaSuccess) e = configure4<NV, 2, 1, 192>();
     return e;
 }
 
@@ -515,9 +774,9 @@ template <bool NV>
 cudaError_t pick4(int v, const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Params& p, int n_sm, cudaStream_t st)
 {
     switch (v) {
-        case 0: return run4<NV, 1, 64>(s, a, p, n_sm, st);
-        case 1: return run4<NV, 2, 96>(s, a, p, n_sm, st);
-        default: return run4<NV, 2, 192>(s, a, p, n_sm, st);
+        case 0: return run4<NV, 1, 1, 64>(s, a, p, n_sm, st);
+        case 1: return run4<NV, 1, 2, 96>(s, a, p, n_sm, st);
+        default: return run4<NV, 2, 1, 192>(s, a, p, n_sm, st);
     }
 }
 
@@ -540,6 +799,9 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     p.out = static_cast<uint16_t*>(a.out);
     p.status = status;
     p.wq = wq;
+#ifdef STRATA_TEST_HOOKS
+    p.test_flags = g_inject_short_load4.exchange(0);
+#endif
     p.a_rows = a.a_rows;
     p.a_scale_stride = a.a.scale_stride;
     p.w_scale_stride = a.w.scale_stride;
@@ -556,3 +818,7 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
 }
 
 }  // namespace strata
+
+#ifdef STRATA_TEST_HOOKS
+extern "C" void strata_test_inject_short_load4(int on) { strata::g_inject_short_load4.store(on); }
+#endif
