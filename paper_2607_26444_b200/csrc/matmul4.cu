@@ -32,18 +32,20 @@ constexpr int kBlock = kM * kKBytes;    // codes of one 128-row block of weights
 constexpr int kChunk = 16;              // scale bytes of a row that TMEM takes at a time: 4 words
 constexpr int kGroups = 2;              // groups of scales in shared memory, chunks of them in TMEM
 constexpr int kScaleWarps = 4;
+constexpr int kBoxRows = 32;            // rows of a TMA box of the N operand where it is not the whole height of a tile
 
 // A tile of a CTA is MB blocks of 128 weight rows by up to BN rows of the N operand (see matmul.cu for the gated forms), of which
 // it holds BN / CG.
 template <bool NV, int CG, int MB, int BN>
 struct Tile4 {
     static constexpr int own_rows = BN / CG;                        // rows of the N operand in this CTA
-    static constexpr int box_rows = 32;                             // rows of one TMA box of the N operand
-    static constexpr int w_stage = MB * kBlock, a_stage = own_rows * kKBytes, stage_bytes = w_stage + a_stage;
+    static constexpr int w_span = MB * kBlock, a_span = own_rows * kKBytes;
+    static constexpr int spans = MB == 1 ? 2 : 1;                   // of a stage
+    static constexpr int stage_bytes = spans * (w_span + a_span);
     static constexpr int group_bytes = BN <= 64 ? 64 : 32;          // scale bytes of a row in a group
-    static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // stages that a group serves
+    static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // spans that a group serves
     static constexpr int per_chunk = kChunk / (NV ? 16 : 8);
-    static constexpr int words = 4 / per_chunk;                     // scale words of a row that a stage uses
+    static constexpr int words = 4 / per_chunk;                     // scale words of a row that a span uses
     static constexpr int ws_group = MB * kM * group_bytes, as_group = BN * group_bytes;
     static constexpr int a_cols = (BN / 32 + 3) / 4 * 4;            // TMEM columns of a word of the rows' scales
     static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kGroups * chunk_cols;
@@ -52,18 +54,19 @@ struct Tile4 {
     static constexpr int used_cols = acc_cols + scale_cols;
     static constexpr int tmem_cols = used_cols <= 128 ? 128 : used_cols <= 256 ? 256 : 512;
     static constexpr int epi_warps = BN > 64 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
-    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 1;
-    static constexpr int threads = 32 * (mma_warp + 1);
+    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 1, deal_warp = load_warp + 2;
+    static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
     static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 8 * 32 : 0;    // exchange of a gated tile
-    static constexpr int ring = (swap_floats > 8 * 1024 / 4 ? 192 : 208) * 1024 - kGroups * (ws_group + as_group);
+    static constexpr int ring = (swap_floats > 8 * 1024 / 4 ? 194 : 212) * 1024 - kGroups * (ws_group + as_group);
     static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
     static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)kGroups * (ws_group + as_group);
-    static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_stage % 1024 == 0 && own_rows % box_rows == 0, "");
+    static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_span % 1024 == 0 && own_rows % kBoxRows == 0 && per_group % spans == 0, "");
 };
 
 struct Mat4Params {
-    CUtensorMap map_w, map_a, map_ws, map_as;
+    CUtensorMap map_w, map_ws;          // weights: codes, scales
+    CUtensorMap map_a[2], map_as[2];    // rows: boxes of kBoxRows, and of a tile's whole height
     const int32_t* expert_count;        // NULL: segments are full (fixed-capacity layout)
     const int32_t* expert_offset;
     const float* a_scale;               // NULL: 1
@@ -72,21 +75,23 @@ struct Mat4Params {
     int* status;
     WorkQueue wq;
     long long a_rows, a_scale_stride, w_scale_stride, out_stride;
-    int E, k_blocks, channels, m_tiles; // channels: rows of w per expert
-    int last_steps;                     // matrix instructions of the last inner block
+    int E, k_spans, channels, m_tiles;  // channels: rows of w per expert
+    int last_steps;                     // matrix instructions of the last span
     int out_words;                      // pairs of channels of out lie on 4 bytes
 #ifdef STRATA_TEST_HOOKS
     int test_flags;
 #endif
 };
 
-constexpr int kClaims = 4;              // tiles that the loading warp may be ahead of the epilogue
+constexpr int kClaims = 4;              // tiles that the dealing warp may be ahead of the epilogue
 
 struct Smem4Tail {                      // behind the operand stages
     uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], drain, pad64;
     uint64_t group_full[kGroups], group_empty[kGroups];          // scales in shared memory
     uint64_t chunk_full[kGroups], chunk_empty[kGroups];          // scales in TMEM
-    uint64_t claim_full[kClaims], claim_empty[kClaims];
+    uint64_t work_full[kClaims], work_empty[kClaims];            // tiles, inside a CTA
+    uint64_t claim_full[kClaims], claim_empty[kClaims];          // tiles, from the leader to the other CTA
+    int4 work[kClaims];                 // expert (-1: no more), channel tile, first row, rows
     unsigned claim[kClaims];
     uint32_t tmem_base, issued, issued_groups;
     int dead, pad[4];
@@ -157,12 +162,13 @@ __device__ __forceinline__ void arrive_leader(uint64_t* bar)
     if constexpr (CG == 1) mbar_arrive(bar);
     else asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(in_cta(bar, 0)) : "memory");
 }
-// A wait by all lanes of a converged warp, which stay together.  `peeked`: a try made earlier had found the phase complete.
-__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status, bool peeked = false)
+// A wait by all lanes of a converged warp, which stay together.  `peeked`: what `peek` said earlier; its answer is first looked at
+// here, so that it comes while other instructions issue.
+__device__ __forceinline__ bool warp_wait(uint64_t* bar, uint32_t parity, volatile int* dead, int* status, uint32_t peeked = 0)
 {
-    return peeked || __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, status));
+    return __all_sync(0xffffffffu, peeked != 0) || __all_sync(0xffffffffu, wait_or_dead(bar, parity, dead, status));
 }
-__device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity)
+__device__ __forceinline__ uint32_t peek(uint64_t* bar, uint32_t parity)
 {
     uint32_t ok;
     asm volatile(
@@ -172,7 +178,7 @@ __device__ __forceinline__ bool peek(uint64_t* bar, uint32_t parity)
         : "=r"(ok)
         : "r"(smem_addr(bar)), "r"(parity)
         : "memory");
-    return __all_sync(0xffffffffu, ok != 0);
+    return ok;
 }
 // Loads of codes count at the leader's barrier.
 template <int CG>
@@ -186,15 +192,23 @@ __device__ __forceinline__ void load4_2d(void* dst, const CUtensorMap* map, int 
             "l"(map), "r"(x), "r"(y), "r"(leader_bar)
             : "memory");
 }
-template <int CG>
-__device__ __forceinline__ void load4_3d(void* dst, const CUtensorMap* map, int x, int y, int z, uint64_t* bar, uint32_t leader_bar)
+__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int w, uint64_t* bar)
 {
-    if constexpr (CG == 1) tma_load_3d(dst, map, x, y, z, bar);
+    asm volatile(
+        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
+            smem_addr(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(0), "r"(w), "r"(smem_addr(bar))
+        : "memory");
+}
+template <int CG>
+__device__ __forceinline__ void load4_4d(void* dst, const CUtensorMap* map, int x, int y, int w, uint64_t* bar, uint32_t leader_bar)
+{
+    if constexpr (CG == 1) tma_load_4d(dst, map, x, y, w, bar);
     else
         asm volatile(
-            "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4}], "
-            "[%5];" ::"r"(smem_addr(dst)),
-            "l"(map), "r"(x), "r"(y), "r"(z), "r"(leader_bar)
+            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, "
+            "%5}], [%6];" ::"r"(smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(0), "r"(w), "r"(leader_bar)
             : "memory");
 }
 
@@ -226,21 +240,27 @@ __device__ __forceinline__ void by_word(const uint4 (&v)[4], uint32_t (&r)[16])
     }
 }
 
-// The n-th tile that the loading warp handed over, by all lanes of a warp, which have all read it when this returns.
-__device__ __forceinline__ bool next_tile(Smem4Tail& tail, uint32_t n, unsigned& t, volatile int* dead, int* status)
+// The n-th tile that the dealing warp handed over, by all lanes of a warp.  False: there is none, or a wait ran out.
+__device__ __forceinline__ bool next_tile(Smem4Tail& tail, uint32_t n, Work& w, int lane, volatile int* dead, int* status)
 {
-    if (!warp_wait(&tail.claim_full[n % kClaims], (n / kClaims) & 1, dead, status)) return false;
-    t = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile unsigned*>(&tail.claim[n % kClaims]), 0);
-    return true;
+    if (!warp_wait(&tail.work_full[n % kClaims], (n / kClaims) & 1, dead, status)) return false;
+    int4 v;
+    asm volatile("ld.shared.v4.s32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(smem_addr(&tail.work[n % kClaims])) : "memory");
+    w.e = __shfl_sync(0xffffffffu, v.x, 0);
+    w.m = __shfl_sync(0xffffffffu, v.y, 0);
+    w.row0 = __shfl_sync(0xffffffffu, v.z, 0);
+    w.rows = __shfl_sync(0xffffffffu, v.w, 0);
+    if (lane == 0) mbar_arrive(&tail.work_empty[n % kClaims]);
+    return w.e >= 0;
 }
-// claim_unit of common.cuh for `claimers` CTAs, which start on the first tiles
-__device__ __forceinline__ unsigned claim_tile(const WorkQueue& q, unsigned n_units, unsigned claimers, bool& exhausted)
+// claim_unit of common.cuh for `claimers` CTAs, which start on the first tiles, in two steps: the counter's answer takes up to a
+// microsecond and a half under load, and is needed a tile later.
+__device__ __forceinline__ unsigned claimed_tile(const WorkQueue& q, unsigned drawn, unsigned n_units, unsigned claimers, bool& exhausted)
 {
-    if (claimers >= n_units || exhausted) return kNoUnit;
-    const unsigned old = atomicAdd(q.next, 1u);
-    if (claimers + old < n_units) return claimers + old;
+    if (exhausted) return kNoUnit;
+    if (drawn < n_units - claimers) return claimers + drawn;
     exhausted = true;
-    if (old == n_units - 1) *q.next = 0;                             // the last of the failed claims, one per claimer
+    if (drawn == n_units - 1) *q.next = 0;                           // the last of the failed claims, one per claimer
     return kNoUnit;
 }
 
@@ -250,9 +270,9 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
     using T = Tile4<NV, CG, MB, BN>;
     extern __shared__ unsigned char smem_raw[];
     unsigned char* smem = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    unsigned char* s_w = smem;                                       // [stages][MB * 128][128]
-    unsigned char* s_a = s_w + T::stages * T::w_stage;               // [stages][own rows][128]
-    unsigned char* s_ws = s_a + T::stages * T::a_stage;              // [groups][MB * 128][group bytes]
+    unsigned char* s_w = smem;                                       // [stages][spans][MB * 128][128]
+    unsigned char* s_a = s_w + T::stages * T::spans * T::w_span;     // [stages][spans][own rows][128]
+    unsigned char* s_ws = s_a + T::stages * T::spans * T::a_span;    // [groups][MB * 128][group bytes]
     unsigned char* s_as = s_ws + kGroups * T::ws_group;              // [groups][BN][group bytes]
     Smem4Tail* tail = reinterpret_cast<Smem4Tail*>(smem + T::data_bytes);
     float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
@@ -279,17 +299,19 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             mbar_init(&tail->tmem_full[b], 1);
             mbar_init(&tail->tmem_empty[b], CG * T::epi_warps);
         }
-        for (int c = 0; c < kClaims; ++c) {                          // consumers: both loaders but the claiming one, the leader's
-            mbar_init(&tail->claim_full[c], 1);                      // matrix warp, all scale and epilogue warps
-            mbar_init(&tail->claim_empty[c], CG * (1 + kScaleWarps + T::epi_warps));
+        for (int c = 0; c < kClaims; ++c) {
+            mbar_init(&tail->work_full[c], 1);
+            mbar_init(&tail->work_empty[c], 1 + (rank == 0 ? 1 : 0) + kScaleWarps + T::epi_warps);   // only the leader multiplies
+            mbar_init(&tail->claim_full[c], 1);
+            mbar_init(&tail->claim_empty[c], 1);
         }
         mbar_init(&tail->drain, 1);
         tail->dead = 0;
         mbar_fence_init();
         asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_w) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_a) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_ws) : "memory");
-        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_as) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_a[0]) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&p.map_as[0]) : "memory");
     }
     if (warp == T::mma_warp) {
         if constexpr (CG == 1) {
@@ -340,41 +362,55 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
     const unsigned n_tiles = (unsigned)s_base[p.E] * (unsigned)p.m_tiles;
     volatile int* dead = &tail->dead;
 
-    if (warp == T::load_warp) {
-        uint32_t it = 0, git = 0, s = 0, phase = 0;
-        bool ok = true, exhausted = false, peeked = false;
+    if (warp == T::deal_warp) {
+        // The leader claims a tile and hands it to the other CTA of the pair; each looks its place up and hands that to its warps.
+        bool exhausted = teams >= n_tiles;
         unsigned t = team < n_tiles ? team : kNoUnit;
-        for (uint32_t n = 0; ok; ++n) {
-            // the leader hands the tile to all others (kNoUnit ends their loops), then claims the next one
-            unsigned next = kNoUnit;
+        for (uint32_t n = 0;; ++n) {
+            const uint32_t c = n % kClaims, parity = (n / kClaims) & 1;
+            unsigned drawn = 0;
             if (rank == 0) {
-                if (!warp_wait(&tail->claim_empty[n % kClaims], ((n / kClaims) & 1) ^ 1, dead, p.status)) break;
-                if (lane == 0) {
-                    tail->claim[n % kClaims] = t;
-                    mbar_arrive(&tail->claim_full[n % kClaims]);
-                    if constexpr (CG == 2)
+                if constexpr (CG == 2) {
+                    if (!warp_wait(&tail->claim_empty[c], parity ^ 1, dead, p.status)) break;
+                    if (lane == 0)
                         asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.u32 [%0], %1, [%2];" ::"r"(
-                                         in_cta(&tail->claim[n % kClaims], 1)),
-                                     "r"(t), "r"(in_cta(&tail->claim_full[n % kClaims], 1))
+                                         in_cta(&tail->claim[c], 1)),
+                                     "r"(t), "r"(in_cta(&tail->claim_full[c], 1))
                                      : "memory");
-                    if (t != kNoUnit) next = claim_tile(p.wq, n_tiles, teams, exhausted);
                 }
+                if (lane == 0 && t != kNoUnit && !exhausted) drawn = atomicAdd(p.wq.next, 1u);
             } else {
-                if (lane == 0) mbar_expect_tx(&tail->claim_full[n % kClaims], sizeof(unsigned));    // st.async completes it
+                if (lane == 0) mbar_expect_tx(&tail->claim_full[c], sizeof(unsigned));    // st.async completes it
                 __syncwarp();
-                if (!next_tile(*tail, n, t, dead, p.status)) break;
-                if (lane == 0) arrive_leader<CG>(&tail->claim_empty[n % kClaims]);
+                if (!warp_wait(&tail->claim_full[c], parity, dead, p.status)) break;
+                asm volatile("ld.shared.u32 %0, [%1];" : "=r"(t) : "r"(smem_addr(&tail->claim[c])) : "memory");
+                t = __shfl_sync(0xffffffffu, t, 0);
+                if (lane == 0) arrive_leader<CG>(&tail->claim_empty[c]);
+            }
+            Work w = {-1, 0, 0, 0};
+            if (t != kNoUnit) w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
+            if (!warp_wait(&tail->work_empty[c], parity ^ 1, dead, p.status)) break;
+            if (lane == 0) {
+                tail->work[c] = make_int4(w.e, w.m, w.row0, w.rows);
+                mbar_arrive(&tail->work_full[c]);
             }
             if (t == kNoUnit) break;
-            const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
-            const int expert = __shfl_sync(0xffffffffu, w.e, 0), m = __shfl_sync(0xffffffffu, w.m, 0) * CG + (int)rank;
-            const int first = __shfl_sync(0xffffffffu, w.row0, 0), rows = __shfl_sync(0xffffffffu, w.rows, 0);
-            const int half_n = ((rows + 15) & ~15) / CG;             // rows of the tile in each CTA
-            const int boxes = (half_n + T::box_rows - 1) / T::box_rows, all_boxes = (rows + T::box_rows - 1) / T::box_rows;
-            const int row0 = first + (int)rank * half_n;
-            const uint32_t bytes = (uint32_t)(CG * (T::w_stage + boxes * T::box_rows * kKBytes));
-            const uint32_t scale_bytes = (uint32_t)(T::ws_group + all_boxes * T::box_rows * T::group_bytes);
-            for (int kb = 0; kb < p.k_blocks; ++kb, ++it) {
+            if (rank == 0 && lane == 0) t = claimed_tile(p.wq, drawn, n_tiles, teams, exhausted);
+            t = __shfl_sync(0xffffffffu, t, 0);
+        }
+    } else if (warp == T::load_warp) {
+        uint32_t it = 0, git = 0, s = 0, phase = 0, peeked = 0;
+        bool ok = true;
+        Work w;
+        for (uint32_t use = 0; ok && next_tile(*tail, use, w, lane, dead, p.status); ++use) {
+            const int half_n = ((w.rows + 15) & ~15) / CG;           // rows of the tile in each CTA
+            const int boxes = (half_n + kBoxRows - 1) / kBoxRows, all_boxes = (w.rows + kBoxRows - 1) / kBoxRows;
+            const bool whole = boxes * kBoxRows == T::own_rows, all_whole = all_boxes * kBoxRows == BN;
+            const int row0 = w.row0 + (int)rank * half_n;
+            const int w_row = (w.m * CG + (int)rank) * MB * kM / (GATED ? 2 : 1);
+            const uint32_t span_bytes = (uint32_t)(CG * (T::w_span + boxes * kBoxRows * kKBytes));
+            const uint32_t scale_bytes = (uint32_t)(T::ws_group + all_boxes * kBoxRows * T::group_bytes);
+            for (int kb = 0; kb < p.k_spans; kb += T::spans, ++it) {
                 if (kb % T::per_group == 0) {
                     const uint32_t g = git % kGroups;
                     if (!warp_wait(&tail->group_empty[g], ((git / kGroups) & 1) ^ 1, dead, p.status)) {
@@ -383,23 +419,15 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     }
                     ++git;
                     uint64_t* bar = &tail->group_full[g];
-                    unsigned char* dw = s_ws + g * T::ws_group;
+                    unsigned char* to = s_as + g * T::as_group;
                     const int x = kb / T::per_group * T::group_bytes;
                     if (elected()) {
                         mbar_expect_tx(bar, scale_bytes);
-                        if constexpr (GATED) {                       // [2E][channels / 2][inner]: gate, up
-                            constexpr int kRows = MB * kM / 2;
-#pragma unroll
-                            for (int h = 0; h < 2; ++h)
-                                tma_load_3d(dw + h * kRows * T::group_bytes, &p.map_ws, x, m * kRows, 2 * expert + h, bar);
-                        } else {
-#pragma unroll
-                            for (int b = 0; b < MB; ++b)
-                                tma_load_3d(dw + b * kM * T::group_bytes, &p.map_ws, x, (m * MB + b) * kM, expert, bar);
-                        }
-                        for (int b = 0; b < all_boxes; ++b)
-                            tma_load_2d(s_as + g * T::as_group + b * T::box_rows * T::group_bytes, &p.map_as, x,
-                                        first + b * T::box_rows, bar);
+                        tma_load_4d(s_ws + g * T::ws_group, &p.map_ws, x, w_row, w.e, bar);
+                        if (all_whole) tma_load_2d(to, &p.map_as[1], x, w.row0, bar);
+                        else
+                            for (int b = 0; b < all_boxes; ++b)
+                                tma_load_2d(to + b * kBoxRows * T::group_bytes, &p.map_as[0], x, w.row0 + b * kBoxRows, bar);
                     }
                     __syncwarp();
                 }
@@ -412,33 +440,32 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                 peeked = peek(&tail->empty[next_s], phase ^ 1);
                 uint64_t* bar = &tail->full[s];
                 const uint32_t leader_bar = CG == 1 ? 0u : in_cta(bar, 0);
-                unsigned char* dw = s_w + s * T::w_stage;
-                unsigned char* da = s_a + s * T::a_stage;
+                unsigned char* dw = s_w + s * (T::spans * T::w_span);
+                unsigned char* da = s_a + s * (T::spans * T::a_span);
+                const int spans = min(T::spans, p.k_spans - kb);
                 if (elected()) {
                     if (rank == 0) {
-                        uint32_t expect = bytes;
+                        uint32_t expect = span_bytes * (uint32_t)spans;
 #ifdef STRATA_TEST_HOOKS
                         if (p.test_flags && blockIdx.x == 0 && it == 0) expect += 16;
 #endif
                         mbar_expect_tx(bar, expect);
                     }
-                    if constexpr (GATED) {
-                        constexpr int kRows = MB * kM / 2;
 #pragma unroll
-                        for (int h = 0; h < 2; ++h)
-                            load4_3d<CG>(dw + h * kRows * kKBytes, &p.map_w, kb * kKBytes, m * kRows, 2 * expert + h, bar, leader_bar);
-                    } else {
-#pragma unroll
-                        for (int b = 0; b < MB; ++b)
-                            load4_3d<CG>(dw + b * kBlock, &p.map_w, kb * kKBytes, (m * MB + b) * kM, expert, bar, leader_bar);
+                    for (int i = 0; i < T::spans; ++i) {
+                        if (i >= spans) break;
+                        const int x = (kb + i) * kKBytes;
+                        load4_4d<CG>(dw + i * T::w_span, &p.map_w, x, w_row, w.e, bar, leader_bar);
+                        if (whole) load4_2d<CG>(da + i * T::a_span, &p.map_a[1], x, row0, bar, leader_bar);
+                        else
+                            for (int b = 0; b < boxes; ++b)
+                                load4_2d<CG>(da + i * T::a_span + b * kBoxRows * kKBytes, &p.map_a[0], x, row0 + b * kBoxRows, bar,
+                                             leader_bar);
                     }
-                    for (int b = 0; b < boxes; ++b)
-                        load4_2d<CG>(da + b * T::box_rows * kKBytes, &p.map_a, kb * kKBytes, row0 + b * T::box_rows, bar, leader_bar);
                 }
                 __syncwarp();
                 s = next_s;
             }
-            t = __shfl_sync(0xffffffffu, next, 0);
         }
         if (lane == 0) {
             tail->issued = it;
@@ -446,65 +473,66 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         }
     } else if (warp == T::mma_warp) {
         if (rank == 0) {
-            uint32_t s = 0, phase = 0, cit = 0, use = 0;
-            bool ok = true, stage_peeked = false, chunk_peeked = false;
+            uint32_t s = 0, phase = 0, cit = 0, stage_peeked = 0, chunk_peeked = 0;
+            bool ok = true;
+            Work w;
             const uint32_t w_desc = desc_low(smem_addr(s_w)), a_desc = desc_low(smem_addr(s_a));
-            for (; ok; ++use) {
-                unsigned t;
-                if (!next_tile(*tail, use, t, dead, p.status)) break;
-                if (lane == 0) mbar_arrive(&tail->claim_empty[use % kClaims]);
-                if (t == kNoUnit) break;
-                const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
-                const int n = (__shfl_sync(0xffffffffu, w.rows, 0) + 15) & ~15;
+            for (uint32_t use = 0; ok && next_tile(*tail, use, w, lane, dead, p.status); ++use) {
+                const int n = (w.rows + 15) & ~15;
                 const uint32_t buf = use % T::bufs;
                 if (!warp_wait(&tail->tmem_empty[buf], ((use / T::bufs) & 1) ^ 1, dead, p.status)) break;
                 tmem_fence_after();
                 const uint32_t d = tmem + buf * MB * BN;
                 const uint32_t idesc0 = instr_desc4<NV, CG>(n, 0), idesc1 = instr_desc4<NV, CG>(n, NV ? 0 : 2);
-                for (int kb = 0; kb < p.k_blocks; ++kb) {
-                    const uint32_t g = cit % kGroups;
-                    if ((kb % T::per_chunk == 0 &&
-                         !warp_wait(&tail->chunk_full[g], (cit / kGroups) & 1, dead, p.status, chunk_peeked)) ||
-                        !warp_wait(&tail->full[s], phase, dead, p.status, stage_peeked)) {
-                        ok = false;
-                        break;
-                    }
-                    tmem_fence_after();
-                    const bool last = kb == p.k_blocks - 1, chunk_ends = kb % T::per_chunk == T::per_chunk - 1 || last;
+                for (int kb0 = 0; ok && kb0 < p.k_spans; kb0 += T::spans) {
+                    ok = warp_wait(&tail->full[s], phase, dead, p.status, stage_peeked);
+                    if (!ok) break;
                     // whether the next stage is there is asked before this one's instructions, which take longer to issue than the
                     // answer to come
                     const uint32_t next_s = s + 1 == T::stages ? 0 : s + 1;
                     if (next_s == 0) phase ^= 1;
                     stage_peeked = peek(&tail->full[next_s], phase);
-                    if (chunk_ends) {
-                        ++cit;
-                        chunk_peeked = peek(&tail->chunk_full[cit % kGroups], (cit / kGroups) & 1);
-                    }
-                    const uint32_t dw = w_desc + s * (T::w_stage >> 4), da = a_desc + s * (T::a_stage >> 4);
-                    const int word = kb % T::per_chunk * T::words;   // of the chunk, where this stage begins
-                    const uint32_t sw = tmem + T::acc_cols + g * T::chunk_cols + word * 4;
-                    const uint32_t sa = tmem + T::acc_cols + g * T::chunk_cols + MB * 16 + word * T::a_cols;
-                    auto multiply = [&](int k) {
-                        const int i = NV ? k : k >> 1;
 #pragma unroll
-                        for (int b = 0; b < MB; ++b)
-                            mma4<NV, CG>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4),
-                                         (k & 1) ? idesc1 : idesc0, sw + b * 16 + i * 4, sa + i * T::a_cols, (kb | k) != 0);
-                    };
-                    if (elected()) {
-                        if (!last) {
-#pragma unroll
-                            for (int k = 0; k < kKBytes / kUmmaK; ++k) multiply(k);
-                        } else {
-#pragma unroll
-                            for (int k = 0; k < kKBytes / kUmmaK; ++k)
-                                if (k < p.last_steps) multiply(k);
+                    for (int i = 0; i < T::spans; ++i) {
+                        const int kb = kb0 + i;
+                        if (kb >= p.k_spans) break;
+                        const uint32_t g = cit % kGroups;
+                        if (kb % T::per_chunk == 0) {
+                            ok = warp_wait(&tail->chunk_full[g], (cit / kGroups) & 1, dead, p.status, chunk_peeked);
+                            if (!ok) break;
                         }
-                        commit4<CG>(&tail->empty[s]);
-                        if (chunk_ends) commit4<CG>(&tail->chunk_empty[g]);
-                        if (last) commit4<CG>(&tail->tmem_full[buf]);
+                        tmem_fence_after();
+                        const bool last = kb == p.k_spans - 1, chunk_ends = kb % T::per_chunk == T::per_chunk - 1 || last;
+                        if (chunk_ends) {
+                            ++cit;
+                            chunk_peeked = peek(&tail->chunk_full[cit % kGroups], (cit / kGroups) & 1);
+                        }
+                        const uint32_t dw = w_desc + (s * T::spans + i) * (T::w_span >> 4), da = a_desc + (s * T::spans + i) * (T::a_span >> 4);
+                        const int word = kb % T::per_chunk * T::words;                   // of the chunk, where this span begins
+                        const uint32_t sw = tmem + T::acc_cols + g * T::chunk_cols + word * 4;
+                        const uint32_t sa = tmem + T::acc_cols + g * T::chunk_cols + MB * 16 + word * T::a_cols;
+                        auto multiply = [&](int k) {
+                            const int j = NV ? k : k >> 1;
+#pragma unroll
+                            for (int b = 0; b < MB; ++b)
+                                mma4<NV, CG>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4),
+                                             (k & 1) ? idesc1 : idesc0, sw + b * 16 + j * 4, sa + j * T::a_cols, (kb | k) != 0);
+                        };
+                        if (elected()) {
+                            if (!last) {
+#pragma unroll
+                                for (int k = 0; k < kKBytes / kUmmaK; ++k) multiply(k);
+                            } else {
+#pragma unroll
+                                for (int k = 0; k < kKBytes / kUmmaK; ++k)
+                                    if (k < p.last_steps) multiply(k);
+                            }
+                            if (i == T::spans - 1 || last) commit4<CG>(&tail->empty[s]);
+                            if (chunk_ends) commit4<CG>(&tail->chunk_empty[g]);
+                            if (last) commit4<CG>(&tail->tmem_full[buf]);
+                        }
+                        __syncwarp();
                     }
-                    __syncwarp();
                     s = next_s;
                 }
             }
@@ -515,31 +543,33 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             __syncwarp();
         }
     } else if (warp < kScaleWarps) {                                 // scales to this warp's quarter of TMEM
-        uint32_t git = 0, cit = 0, use = 0;
+        uint32_t git = 0, cit = 0;
         bool ok = true;
         const uint32_t lanes = (uint32_t)(warp * 32) << 16;
-        for (; ok; ++use) {
-            unsigned t;
-            if (!next_tile(*tail, use, t, dead, p.status)) break;
-            if (lane == 0) arrive_leader<CG>(&tail->claim_empty[use % kClaims]);
-            if (t == kNoUnit) break;
-            for (int kb = 0; kb < p.k_blocks; kb += T::per_chunk, ++cit) {
-                const uint32_t g = git % kGroups, c = cit % kGroups;
-                const int at = kb % T::per_group / T::per_chunk * kChunk;    // of the chunk in its group's rows
-                if (at == 0) ok = warp_wait(&tail->group_full[g], (git / kGroups) & 1, dead, p.status);
-                if (!ok) break;
-                uint4 vw[MB][4], va[T::a_cols / 4][4];
+        Work w;
+        uint4 vw[MB][4], va[T::a_cols / 4][4];
+        // the chunk that begins with span kb, from its group in shared memory
+        auto fetch = [&](int kb) {
+            const uint32_t g = git % kGroups;
+            const int at = kb % T::per_group / T::per_chunk * kChunk;        // of the chunk in its group's rows
+            if (at == 0 && !warp_wait(&tail->group_full[g], (git / kGroups) & 1, dead, p.status)) return false;
 #pragma unroll
-                for (int b = 0; b < MB; ++b)
-                    read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes + at, kM, lane, vw[b]);
+            for (int b = 0; b < MB; ++b)
+                read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes + at, kM, lane, vw[b]);
 #pragma unroll
-                for (int b = 0; b < T::a_cols / 4; ++b)
-                    read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes + at, BN - b * kM, lane, va[b]);
+            for (int b = 0; b < T::a_cols / 4; ++b)
+                read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes + at, BN - b * kM, lane, va[b]);
+            if (at == T::group_bytes - kChunk || kb + T::per_chunk >= p.k_spans) {
                 __syncwarp();
-                if (at == T::group_bytes - kChunk || kb + T::per_chunk >= p.k_blocks) {
-                    if (lane == 0) mbar_arrive(&tail->group_empty[g]);
-                    ++git;
-                }
+                if (lane == 0) mbar_arrive(&tail->group_empty[g]);
+                ++git;
+            }
+            return true;
+        };
+        for (uint32_t use = 0; ok && next_tile(*tail, use, w, lane, dead, p.status); ++use) {
+            ok = fetch(0);
+            for (int kb = 0; ok && kb < p.k_spans; kb += T::per_chunk, ++cit) {
+                const uint32_t c = cit % kGroups;
                 ok = warp_wait(&tail->chunk_empty[c], ((cit / kGroups) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
                 tmem_fence_after();
@@ -569,6 +599,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_leader<CG>(&tail->chunk_full[c]);
+                if (kb + T::per_chunk < p.k_spans) ok = fetch(kb + T::per_chunk);
             }
         }
     } else {
@@ -577,18 +608,15 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         const int col0 = (ew >> 2) * T::cols;                        // first column of this warp
         float* scale = s_scale + ew * T::cols;
         const int half = p.channels / 2;
-        uint32_t use = 0;
-        for (;; ++use) {
-            unsigned t;
-            const bool got = next_tile(*tail, use, t, dead, p.status);
+        const bool scaled = p.a_scale || p.w_scale;
+        Work w;
+        for (uint32_t use = 0;; ++use) {
+            const bool got = next_tile(*tail, use, w, lane, dead, p.status);
             if constexpr (GATED && MB == 1) {                        // the two warps of an exchange leave together
                 if (!pair_all(got, pair)) break;
             } else if (!got) {
                 break;
             }
-            if (lane == 0) arrive_leader<CG>(&tail->claim_empty[use % kClaims]);
-            if (t == kNoUnit) break;
-            const Work w = find_work<BN>(t, s_base, s_off, s_cnt, p.E, p.m_tiles);
             const int m = w.m * CG + (int)rank;
             const uint32_t buf = use % T::bufs;
             const int rows = min(T::cols, w.rows - col0);            // of this warp; may be negative
@@ -626,58 +654,64 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             const uint32_t addr = tmem + buf * MB * BN + ((uint32_t)(quad * 32) << 16) + col0;
             uint16_t* out = p.out + (long long)(w.row0 + col0) * p.out_stride;
             int phase = 0;
+            uint32_t v[MB][16];                                      // the columns to come: loaded while those before are worked on
+            __syncwarp();
+            if (rows > 0) {
+#pragma unroll
+                for (int b = 0; b < MB; ++b) tmem_ld16(v[b], addr + b * BN);
+            }
             for (int c0 = 0; c0 < rows; c0 += 16, phase ^= 1) {
+                float y[MB][16];
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    tmem_ld_wait(v[b]);
+#pragma unroll
+                    for (int c = 0; c < 16; ++c) y[b][c] = __uint_as_float(v[b][c]);
+                }
                 __syncwarp();                                        // loads from TMEM ask for converged warps: waits and stores part them
-                float sc[16];
+                if (c0 + 16 < rows) {
 #pragma unroll
-                for (int c = 0; c < 16; c += 4) *reinterpret_cast<float4*>(&sc[c]) = *reinterpret_cast<const float4*>(&scale[c0 + c]);
+                    for (int b = 0; b < MB; ++b) tmem_ld16(v[b], addr + b * BN + c0 + 16);
+                }
+                if (scaled) {
+                    float sc[16];
+#pragma unroll
+                    for (int c = 0; c < 16; c += 4)
+                        *reinterpret_cast<float4*>(&sc[c]) = *reinterpret_cast<const float4*>(&scale[c0 + c]);
+#pragma unroll
+                    for (int b = 0; b < MB; ++b)
+#pragma unroll
+                        for (int c = 0; c < 16; ++c) y[b][c] *= sc[c] * wsc[b];
+                }
                 if constexpr (GATED && MB == 1) {
-                    uint32_t v[16];
-                    tmem_ld16(v, addr + c0);
-                    tmem_ld_wait(v);
-                    float y[16];
-#pragma unroll
-                    for (int c = 0; c < 16; ++c) y[c] = __uint_as_float(v[c]) * (sc[c] * wsc[0]);
                     // the gate's warp finishes columns 0..7, up's warp columns 8..15
                     const bool up = quad >> 1;
                     float* mine = s_swap + (ew * 2 + phase) * 8 * 32 + lane;
                     const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 8 * 32 + lane;
 #pragma unroll
-                    for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[c] : y[8 + c];
+                    for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[0][c] : y[0][8 + c];
                     asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
                     float o[8];
 #pragma unroll
                     for (int c = 0; c < 8; ++c) {
                         const float other = theirs[c * 32];
-                        o[c] = up ? gate_mul(other, y[8 + c]) : gate_mul(y[c], other);
+                        o[c] = up ? gate_mul(other, y[0][8 + c]) : gate_mul(y[0][c], other);
                     }
                     const int shift = up ? 8 : 0;
                     store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride, p.out_stride, rows - c0 - shift, out_ch[0],
                                    limit, words);
                 } else if constexpr (GATED) {
-                    uint32_t g[16], u[16];
-                    tmem_ld16(g, addr + c0);
-                    tmem_ld16(u, addr + BN + c0);
-                    tmem_ld_wait(g);
-                    tmem_ld_wait(u);
-                    float y[16];
+                    float o[16];
 #pragma unroll
-                    for (int c = 0; c < 16; ++c)
-                        y[c] = gate_mul(__uint_as_float(g[c]) * (sc[c] * wsc[0]), __uint_as_float(u[c]) * (sc[c] * wsc[1]));
-                    store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[0], limit, words);
+                    for (int c = 0; c < 16; ++c) o[c] = gate_mul(y[0][c], y[MB - 1][c]);
+                    store_pairs<16>(o, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[0], limit, words);
                 } else {
 #pragma unroll
-                    for (int b = 0; b < MB; ++b) {
-                        uint32_t v[16];
-                        tmem_ld16(v, addr + b * BN + c0);
-                        tmem_ld_wait(v);
-                        float y[16];
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) y[c] = __uint_as_float(v[c]) * (sc[c] * wsc[b]);
-                        store_pairs<16>(y, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[b], limit, words);
-                    }
+                    for (int b = 0; b < MB; ++b)
+                        store_pairs<16>(y[b], lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[b], limit, words);
                 }
             }
+            __syncwarp();
             tmem_fence_before();
             __syncwarp();
             if (lane == 0) arrive_leader<CG>(&tail->tmem_empty[buf]);
@@ -722,24 +756,26 @@ template <bool NV, int CG, int MB, int BN>
 cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Params& p, int n_sm, cudaStream_t st)
 {
     using T = Tile4<NV, CG, MB, BN>;
-    const cuuint64_t groups = (cuuint64_t)s.E * (a.gated ? 2 : 1), rows = (cuuint64_t)a.channels / (a.gated ? 2 : 1);
-    const cuuint32_t w_rows = (cuuint32_t)(a.gated ? MB * kM / 2 : kM);
-    const cuuint64_t bytes[2] = {(cuuint64_t)a.inner / 2, (cuuint64_t)a.inner / (NV ? 16 : 32)};
-    const cuuint32_t box[2] = {kKBytes, T::group_bytes};
-    const strata_rows4* ops[2] = {&a.w, &a.a};
-    CUtensorMap* maps[2][2] = {{&p.map_w, &p.map_ws}, {&p.map_a, &p.map_as}};
-    for (int o = 0; o < 2; ++o)
-        for (int i = 0; i < 2; ++i) {                                // codes, block scales
-            const void* base = i == 0 ? ops[o]->codes : ops[o]->block;
-            const cuuint64_t stride = (cuuint64_t)(i == 0 ? ops[o]->code_stride : ops[o]->block_stride);
-            // weights: [E][channels]; gated: [2E][channels / 2], gate and up of an expert in turn
-            const cuuint64_t dims[3] = {bytes[i], o == 0 ? rows : (cuuint64_t)a.a_rows, groups};
-            const cuuint64_t strides[2] = {stride, rows * stride};
-            const cuuint32_t boxes[3] = {box[i], o == 0 ? w_rows : (cuuint32_t)T::box_rows, 1};
-            if (!encode(maps[o][i], base, o == 0 ? 3 : 2, dims, strides, boxes,
-                        i == 0 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE))
+    const cuuint64_t parts = a.gated ? 2 : 1, rows = (cuuint64_t)a.channels / parts;
+    for (int i = 0; i < 2; ++i) {                                    // codes, block scales
+        const cuuint64_t bytes = (cuuint64_t)a.inner / (i == 0 ? 2 : NV ? 16 : 32);
+        const cuuint32_t box = i == 0 ? kKBytes : T::group_bytes;
+        const CUtensorMapSwizzle swizzle = i == 0 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
+        {   // weights: [E][channels]; gated: [E][2][channels / 2], gate and up of an expert in one box
+            const cuuint64_t stride = (cuuint64_t)(i == 0 ? a.w.code_stride : a.w.block_stride);
+            const cuuint64_t dims[4] = {bytes, rows, parts, (cuuint64_t)s.E}, strides[3] = {stride, rows * stride, parts * rows * stride};
+            const cuuint32_t boxes[4] = {box, (cuuint32_t)(MB * kM / parts), (cuuint32_t)parts, 1};
+            if (!encode(i == 0 ? &p.map_w : &p.map_ws, i == 0 ? a.w.codes : a.w.block, 4, dims, strides, boxes, swizzle))
                 return cudaErrorInvalidValue;
         }
+        const cuuint64_t dims[2] = {bytes, (cuuint64_t)a.a_rows};
+        const cuuint64_t strides[1] = {(cuuint64_t)(i == 0 ? a.a.code_stride : a.a.block_stride)};
+        for (int whole = 0; whole < 2; ++whole) {
+            const cuuint32_t boxes[2] = {box, (cuuint32_t)(!whole ? kBoxRows : i == 0 ? T::own_rows : BN)};
+            if (!encode(i == 0 ? &p.map_a[whole] : &p.map_as[whole], i == 0 ? a.a.codes : a.a.block, 2, dims, strides, boxes, swizzle))
+                return cudaErrorInvalidValue;
+        }
+    }
     const int per_tile = CG * MB * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1);
     p.m_tiles = (wide + per_tile - 1) / per_tile;
     const long long tiles = row_tiles(s, a.a_rows, BN) * p.m_tiles;
@@ -807,8 +843,8 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     p.w_scale_stride = a.w.scale_stride;
     p.out_stride = a.out_stride;
     p.E = s.E;
-    p.k_blocks = (a.inner / 2 + kKBytes - 1) / kKBytes;
-    p.last_steps = (a.inner / 2 - (p.k_blocks - 1) * kKBytes + kUmmaK - 1) / kUmmaK;
+    p.k_spans = (a.inner / 2 + kKBytes - 1) / kKBytes;
+    p.last_steps = (a.inner / 2 - (p.k_spans - 1) * kKBytes + kUmmaK - 1) / kUmmaK;
     p.channels = a.channels;
     p.out_words = a.channels % (a.gated ? 4 : 2) == 0 && a.out_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
     const long long items = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : (long long)s.R * s.T * s.K;
