@@ -220,13 +220,15 @@ __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16]
         "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
         : "memory");
 }
-// Four words of the scales of 128 rows, lane l those of rows l, l + 32, l + 64 and l + 96: `word` columns from one word to the next.
+// Four words (16 bytes at byte `at`) of the scales of up to 128 rows, lane l those of rows l, l + 32, l + 64 and l + 96.  TMA swizzles
+// the rows, so that eight lanes meet eight different places of the banks: without, they meet two or four times.
 template <int ROW_BYTES>
-__device__ __forceinline__ void read_scales(const unsigned char* rows, int n, int lane, uint4 (&v)[4])
+__device__ __forceinline__ void read_scales(const unsigned char* rows, int at, int n, int lane, uint4 (&v)[4])
 {
+    const int turned = at ^ (ROW_BYTES == 32 ? (lane >> 2 & 1) << 4 : (lane >> 1 & 3) << 4);
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        if (32 * j < n) v[j] = *reinterpret_cast<const uint4*>(rows + (lane + 32 * j) * ROW_BYTES);
+        if (32 * j < n) v[j] = *reinterpret_cast<const uint4*>(rows + (lane + 32 * j) * ROW_BYTES + turned);
         else v[j] = make_uint4(0, 0, 0, 0);
 }
 __device__ __forceinline__ void by_word(const uint4 (&v)[4], uint32_t (&r)[16])
@@ -555,10 +557,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             if (at == 0 && !warp_wait(&tail->group_full[g], (git / kGroups) & 1, dead, p.status)) return false;
 #pragma unroll
             for (int b = 0; b < MB; ++b)
-                read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes + at, kM, lane, vw[b]);
+                read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes, at, kM, lane, vw[b]);
 #pragma unroll
             for (int b = 0; b < T::a_cols / 4; ++b)
-                read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes + at, BN - b * kM, lane, va[b]);
+                read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes, at, BN - b * kM, lane, va[b]);
             if (at == T::group_bytes - kChunk || kb + T::per_chunk >= p.k_spans) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&tail->group_empty[g]);
@@ -760,7 +762,9 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
     for (int i = 0; i < 2; ++i) {                                    // codes, block scales
         const cuuint64_t bytes = (cuuint64_t)a.inner / (i == 0 ? 2 : NV ? 16 : 32);
         const cuuint32_t box = i == 0 ? kKBytes : T::group_bytes;
-        const CUtensorMapSwizzle swizzle = i == 0 ? CU_TENSOR_MAP_SWIZZLE_128B : CU_TENSOR_MAP_SWIZZLE_NONE;
+        const CUtensorMapSwizzle swizzle = i == 0                  ? CU_TENSOR_MAP_SWIZZLE_128B
+                                           : T::group_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
+                                                                  : CU_TENSOR_MAP_SWIZZLE_32B;
         {   // weights: [E][channels]; gated: [E][2][channels / 2], gate and up of an expert in one box
             const cuuint64_t stride = (cuuint64_t)(i == 0 ? a.w.code_stride : a.w.block_stride);
             const cuuint64_t dims[4] = {bytes, rows, parts, (cuuint64_t)s.E}, strides[3] = {stride, rows * stride, parts * rows * stride};
