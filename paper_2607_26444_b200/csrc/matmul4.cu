@@ -30,7 +30,8 @@ constexpr int kKBytes = 128;            // bytes of codes of a row in a stage: o
 constexpr int kUmmaK = 32;              // the same of a matrix instruction: 64 values
 constexpr int kBlock = kM * kKBytes;    // codes of one 128-row block of weights in a stage
 constexpr int kChunk = 16;              // scale bytes of a row that TMEM takes at a time: 4 words
-constexpr int kGroups = 2;              // groups of scales in shared memory, chunks of them in TMEM
+constexpr int kChunks = 2;              // chunks of scales in TMEM
+constexpr int kMaxGroups = 3;           // groups of scales in shared memory, at most
 constexpr int kScaleWarps = 4;
 constexpr int kBoxRows = 32;            // rows of a TMA box of the N operand where it is not the whole height of a tile
 
@@ -46,21 +47,23 @@ struct Tile4 {
     static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // spans that a group serves
     static constexpr int per_chunk = kChunk / (NV ? 16 : 8);
     static constexpr int words = 4 / per_chunk;                     // scale words of a row that a span uses
+    static constexpr int groups = NV && BN > 64 ? 3 : 2;            // as many spans as the ring of codes, at least
     static constexpr int ws_group = MB * kM * group_bytes, as_group = BN * group_bytes;
     static constexpr int a_cols = (BN / 32 + 3) / 4 * 4;            // TMEM columns of a word of the rows' scales
-    static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kGroups * chunk_cols;
+    static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kChunks * chunk_cols;
     static constexpr int bufs = 2 * MB * BN + scale_cols <= 512 ? 2 : 1;
     static constexpr int acc_cols = bufs * MB * BN;
     static constexpr int used_cols = acc_cols + scale_cols;
     static constexpr int tmem_cols = used_cols <= 128 ? 128 : used_cols <= 256 ? 256 : 512;
     static constexpr int epi_warps = BN > 64 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
-    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 1, deal_warp = load_warp + 2;
+    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 2, deal_warp = load_warp + 3;
     static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
-    static constexpr int swap_floats = MB == 1 ? epi_warps * 2 * 8 * 32 : 0;    // exchange of a gated tile
-    static constexpr int ring = (swap_floats > 8 * 1024 / 4 ? 194 : 212) * 1024 - kGroups * (ws_group + as_group);
+    static constexpr int swap_bufs = BN > 64 ? 1 : 2;               // of the exchange of a gated tile
+    static constexpr int swap_floats = MB == 1 ? epi_warps * swap_bufs * 8 * 32 : 0;
+    static constexpr int ring = (MB == 1 ? 202 : 212) * 1024 - groups * (ws_group + as_group);
     static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
-    static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)kGroups * (ws_group + as_group);
+    static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)groups * (ws_group + as_group);
     static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_span % 1024 == 0 && own_rows % kBoxRows == 0 && per_group % spans == 0, "");
 };
 
@@ -86,15 +89,15 @@ struct Mat4Params {
 constexpr int kClaims = 4;              // tiles that the dealing warp may be ahead of the epilogue
 
 struct Smem4Tail {                      // behind the operand stages
-    uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], drain, pad64;
-    uint64_t group_full[kGroups], group_empty[kGroups];          // scales in shared memory
-    uint64_t chunk_full[kGroups], chunk_empty[kGroups];          // scales in TMEM
+    uint64_t full[8], empty[8], tmem_full[2], tmem_empty[2], drain;
+    uint64_t group_full[kMaxGroups], group_empty[kMaxGroups];    // scales in shared memory
+    uint64_t chunk_full[kChunks], chunk_empty[kChunks];          // scales in TMEM
     uint64_t work_full[kClaims], work_empty[kClaims];            // tiles, inside a CTA
     uint64_t claim_full[kClaims], claim_empty[kClaims];          // tiles, from the leader to the other CTA
     int4 work[kClaims];                 // expert (-1: no more), channel tile, first row, rows
     unsigned claim[kClaims];
-    uint32_t tmem_base, issued, issued_groups;
-    int dead, pad[4];
+    uint32_t tmem_base, issued[2], issued_groups[2];
+    int dead;
 };
 static_assert(sizeof(Smem4Tail) % 16 == 0, "the scales behind it are read in vectors");
 
@@ -275,10 +278,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
     unsigned char* s_w = smem;                                       // [stages][spans][MB * 128][128]
     unsigned char* s_a = s_w + T::stages * T::spans * T::w_span;     // [stages][spans][own rows][128]
     unsigned char* s_ws = s_a + T::stages * T::spans * T::a_span;    // [groups][MB * 128][group bytes]
-    unsigned char* s_as = s_ws + kGroups * T::ws_group;              // [groups][BN][group bytes]
+    unsigned char* s_as = s_ws + T::groups * T::ws_group;              // [groups][BN][group bytes]
     Smem4Tail* tail = reinterpret_cast<Smem4Tail*>(smem + T::data_bytes);
     float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
-    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][2][8][32]
+    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][buffers][8][32]
     int* s_base = reinterpret_cast<int*>(s_swap + T::swap_floats);   // [E + 1]
     int* s_off = s_base + p.E + 1;                                   // [E]
     int* s_cnt = s_off + p.E;                                        // [E]
@@ -288,14 +291,16 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < T::stages; ++s) {
-            mbar_init(&tail->full[s], 1);
+            mbar_init(&tail->full[s], 2);                            // both loading warps
             mbar_init(&tail->empty[s], 1);
         }
-        for (int g = 0; g < kGroups; ++g) {
-            mbar_init(&tail->group_full[g], 1);
+        for (int g = 0; g < T::groups; ++g) {
+            mbar_init(&tail->group_full[g], 2);
             mbar_init(&tail->group_empty[g], kScaleWarps);
-            mbar_init(&tail->chunk_full[g], CG * kScaleWarps);
-            mbar_init(&tail->chunk_empty[g], 1);
+        }
+        for (int c = 0; c < kChunks; ++c) {
+            mbar_init(&tail->chunk_full[c], CG * kScaleWarps);
+            mbar_init(&tail->chunk_empty[c], 1);
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(&tail->tmem_full[b], 1);
@@ -303,7 +308,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         }
         for (int c = 0; c < kClaims; ++c) {
             mbar_init(&tail->work_full[c], 1);
-            mbar_init(&tail->work_empty[c], 1 + (rank == 0 ? 1 : 0) + kScaleWarps + T::epi_warps);   // only the leader multiplies
+            mbar_init(&tail->work_empty[c], 2 + (rank == 0 ? 1 : 0) + kScaleWarps + T::epi_warps);   // only the leader multiplies
             mbar_init(&tail->claim_full[c], 1);
             mbar_init(&tail->claim_empty[c], 1);
         }
@@ -400,7 +405,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             if (rank == 0 && lane == 0) t = claimed_tile(p.wq, drawn, n_tiles, teams, exhausted);
             t = __shfl_sync(0xffffffffu, t, 0);
         }
-    } else if (warp == T::load_warp) {
+    } else if (warp == T::load_warp || warp == T::load_warp + 1) {   // weights, rows: a load takes its warp about 100 cycles
+        const bool weights = warp == T::load_warp;
         uint32_t it = 0, git = 0, s = 0, phase = 0, peeked = 0;
         bool ok = true;
         Work w;
@@ -410,12 +416,12 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             const bool whole = boxes * kBoxRows == T::own_rows, all_whole = all_boxes * kBoxRows == BN;
             const int row0 = w.row0 + (int)rank * half_n;
             const int w_row = (w.m * CG + (int)rank) * MB * kM / (GATED ? 2 : 1);
-            const uint32_t span_bytes = (uint32_t)(CG * (T::w_span + boxes * kBoxRows * kKBytes));
-            const uint32_t scale_bytes = (uint32_t)(T::ws_group + all_boxes * kBoxRows * T::group_bytes);
+            const uint32_t span_bytes = (uint32_t)(CG * (weights ? T::w_span : boxes * kBoxRows * kKBytes));
+            const uint32_t scale_bytes = (uint32_t)(weights ? T::ws_group : all_boxes * kBoxRows * T::group_bytes);
             for (int kb = 0; kb < p.k_spans; kb += T::spans, ++it) {
                 if (kb % T::per_group == 0) {
-                    const uint32_t g = git % kGroups;
-                    if (!warp_wait(&tail->group_empty[g], ((git / kGroups) & 1) ^ 1, dead, p.status)) {
+                    const uint32_t g = git % T::groups;
+                    if (!warp_wait(&tail->group_empty[g], ((git / T::groups) & 1) ^ 1, dead, p.status)) {
                         ok = false;
                         break;
                     }
@@ -425,8 +431,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     const int x = kb / T::per_group * T::group_bytes;
                     if (elected()) {
                         mbar_expect_tx(bar, scale_bytes);
-                        tma_load_4d(s_ws + g * T::ws_group, &p.map_ws, x, w_row, w.e, bar);
-                        if (all_whole) tma_load_2d(to, &p.map_as[1], x, w.row0, bar);
+                        if (weights) tma_load_4d(s_ws + g * T::ws_group, &p.map_ws, x, w_row, w.e, bar);
+                        else if (all_whole) tma_load_2d(to, &p.map_as[1], x, w.row0, bar);
                         else
                             for (int b = 0; b < all_boxes; ++b)
                                 tma_load_2d(to + b * kBoxRows * T::group_bytes, &p.map_as[0], x, w.row0 + b * kBoxRows, bar);
@@ -449,7 +455,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     if (rank == 0) {
                         uint32_t expect = span_bytes * (uint32_t)spans;
 #ifdef STRATA_TEST_HOOKS
-                        if (p.test_flags && blockIdx.x == 0 && it == 0) expect += 16;
+                        if (p.test_flags && blockIdx.x == 0 && it == 0 && weights) expect += 16;
 #endif
                         mbar_expect_tx(bar, expect);
                     }
@@ -457,8 +463,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     for (int i = 0; i < T::spans; ++i) {
                         if (i >= spans) break;
                         const int x = (kb + i) * kKBytes;
-                        load4_4d<CG>(dw + i * T::w_span, &p.map_w, x, w_row, w.e, bar, leader_bar);
-                        if (whole) load4_2d<CG>(da + i * T::a_span, &p.map_a[1], x, row0, bar, leader_bar);
+                        if (weights) load4_4d<CG>(dw + i * T::w_span, &p.map_w, x, w_row, w.e, bar, leader_bar);
+                        else if (whole) load4_2d<CG>(da + i * T::a_span, &p.map_a[1], x, row0, bar, leader_bar);
                         else
                             for (int b = 0; b < boxes; ++b)
                                 load4_2d<CG>(da + i * T::a_span + b * kBoxRows * kKBytes, &p.map_a[0], x, row0 + b * kBoxRows, bar,
@@ -470,8 +476,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             }
         }
         if (lane == 0) {
-            tail->issued = it;
-            tail->issued_groups = git;
+            tail->issued[warp - T::load_warp] = it;
+            tail->issued_groups[warp - T::load_warp] = git;
         }
     } else if (warp == T::mma_warp) {
         if (rank == 0) {
@@ -494,43 +500,47 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     const uint32_t next_s = s + 1 == T::stages ? 0 : s + 1;
                     if (next_s == 0) phase ^= 1;
                     stage_peeked = peek(&tail->full[next_s], phase);
+                    constexpr int kPart = T::spans < T::per_chunk ? T::spans : T::per_chunk;     // spans of one stage and one chunk
 #pragma unroll
-                    for (int i = 0; i < T::spans; ++i) {
-                        const int kb = kb0 + i;
-                        if (kb >= p.k_spans) break;
-                        const uint32_t g = cit % kGroups;
-                        if (kb % T::per_chunk == 0) {
-                            ok = warp_wait(&tail->chunk_full[g], (cit / kGroups) & 1, dead, p.status, chunk_peeked);
+                    for (int i0 = 0; i0 < T::spans; i0 += kPart) {
+                        const int kb1 = kb0 + i0;
+                        if (kb1 >= p.k_spans) break;
+                        const uint32_t c = cit % kChunks;
+                        if (kb1 % T::per_chunk == 0) {
+                            ok = warp_wait(&tail->chunk_full[c], (cit / kChunks) & 1, dead, p.status, chunk_peeked);
                             if (!ok) break;
+                            tmem_fence_after();
                         }
-                        tmem_fence_after();
-                        const bool last = kb == p.k_spans - 1, chunk_ends = kb % T::per_chunk == T::per_chunk - 1 || last;
+                        const bool last = kb1 + kPart >= p.k_spans;
+                        const bool chunk_ends = (kb1 + kPart) % T::per_chunk == 0 || last;
                         if (chunk_ends) {
                             ++cit;
-                            chunk_peeked = peek(&tail->chunk_full[cit % kGroups], (cit / kGroups) & 1);
+                            chunk_peeked = peek(&tail->chunk_full[cit % kChunks], (cit / kChunks) & 1);
                         }
-                        const uint32_t dw = w_desc + (s * T::spans + i) * (T::w_span >> 4), da = a_desc + (s * T::spans + i) * (T::a_span >> 4);
-                        const int word = kb % T::per_chunk * T::words;                   // of the chunk, where this span begins
-                        const uint32_t sw = tmem + T::acc_cols + g * T::chunk_cols + word * 4;
-                        const uint32_t sa = tmem + T::acc_cols + g * T::chunk_cols + MB * 16 + word * T::a_cols;
-                        auto multiply = [&](int k) {
-                            const int j = NV ? k : k >> 1;
+                        const uint32_t dw = w_desc + (s * T::spans + i0) * (T::w_span >> 4), da = a_desc + (s * T::spans + i0) * (T::a_span >> 4);
+                        const int word = kb1 % T::per_chunk * T::words;                  // of the chunk, where these spans begin
+                        const uint32_t sw = tmem + T::acc_cols + c * T::chunk_cols + word * 4;
+                        const uint32_t sa = tmem + T::acc_cols + c * T::chunk_cols + MB * 16 + word * T::a_cols;
+                        auto multiply = [&](int k) {                 // the k-th 64 values of these spans
+                            const int i = k / 4, j = k % 4, at = NV ? k : k >> 1;        // span, step inside it, word of scales
 #pragma unroll
                             for (int b = 0; b < MB; ++b)
-                                mma4<NV, CG>(d + b * BN, dw + b * (kBlock >> 4) + k * (kUmmaK >> 4), da + k * (kUmmaK >> 4),
-                                             (k & 1) ? idesc1 : idesc0, sw + b * 16 + j * 4, sa + j * T::a_cols, (kb | k) != 0);
+                                mma4<NV, CG>(d + b * BN, dw + i * (T::w_span >> 4) + b * (kBlock >> 4) + j * (kUmmaK >> 4),
+                                             da + i * (T::a_span >> 4) + j * (kUmmaK >> 4), (k & 1) ? idesc1 : idesc0, sw + b * 16 + at * 4,
+                                             sa + at * T::a_cols, (kb1 | k) != 0);
                         };
                         if (elected()) {
                             if (!last) {
 #pragma unroll
-                                for (int k = 0; k < kKBytes / kUmmaK; ++k) multiply(k);
+                                for (int k = 0; k < 4 * kPart; ++k) multiply(k);
                             } else {
+                                const int steps = (p.k_spans - 1 - kb1) * 4 + p.last_steps;
 #pragma unroll
-                                for (int k = 0; k < kKBytes / kUmmaK; ++k)
-                                    if (k < p.last_steps) multiply(k);
+                                for (int k = 0; k < 4 * kPart; ++k)
+                                    if (k < steps) multiply(k);
                             }
-                            if (i == T::spans - 1 || last) commit4<CG>(&tail->empty[s]);
-                            if (chunk_ends) commit4<CG>(&tail->chunk_empty[g]);
+                            if (i0 + kPart == T::spans || last) commit4<CG>(&tail->empty[s]);
+                            if (chunk_ends) commit4<CG>(&tail->chunk_empty[c]);
                             if (last) commit4<CG>(&tail->tmem_full[buf]);
                         }
                         __syncwarp();
@@ -552,9 +562,9 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         uint4 vw[MB][4], va[T::a_cols / 4][4];
         // the chunk that begins with span kb, from its group in shared memory
         auto fetch = [&](int kb) {
-            const uint32_t g = git % kGroups;
+            const uint32_t g = git % T::groups;
             const int at = kb % T::per_group / T::per_chunk * kChunk;        // of the chunk in its group's rows
-            if (at == 0 && !warp_wait(&tail->group_full[g], (git / kGroups) & 1, dead, p.status)) return false;
+            if (at == 0 && !warp_wait(&tail->group_full[g], (git / T::groups) & 1, dead, p.status)) return false;
 #pragma unroll
             for (int b = 0; b < MB; ++b)
                 read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes, at, kM, lane, vw[b]);
@@ -571,8 +581,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         for (uint32_t use = 0; ok && next_tile(*tail, use, w, lane, dead, p.status); ++use) {
             ok = fetch(0);
             for (int kb = 0; ok && kb < p.k_spans; kb += T::per_chunk, ++cit) {
-                const uint32_t c = cit % kGroups;
-                ok = warp_wait(&tail->chunk_empty[c], ((cit / kGroups) & 1) ^ 1, dead, p.status);
+                const uint32_t c = cit % kChunks;
+                ok = warp_wait(&tail->chunk_empty[c], ((cit / kChunks) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
                 tmem_fence_after();
                 const uint32_t to = tmem + T::acc_cols + c * T::chunk_cols + lanes;
@@ -688,8 +698,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                 if constexpr (GATED && MB == 1) {
                     // the gate's warp finishes columns 0..7, up's warp columns 8..15
                     const bool up = quad >> 1;
-                    float* mine = s_swap + (ew * 2 + phase) * 8 * 32 + lane;
-                    const float* theirs = s_swap + ((ew ^ 2) * 2 + phase) * 8 * 32 + lane;
+                    float* mine = s_swap + (ew * T::swap_bufs + phase % T::swap_bufs) * 8 * 32 + lane;
+                    const float* theirs = s_swap + ((ew ^ 2) * T::swap_bufs + phase % T::swap_bufs) * 8 * 32 + lane;
 #pragma unroll
                     for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[0][c] : y[0][8 + c];
                     asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
@@ -699,6 +709,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                         const float other = theirs[c * 32];
                         o[c] = up ? gate_mul(other, y[0][8 + c]) : gate_mul(y[0][c], other);
                     }
+                    if constexpr (T::swap_bufs == 1) asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
                     const int shift = up ? 8 : 0;
                     store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride, p.out_stride, rows - c0 - shift, out_ch[0],
                                    limit, words);
@@ -725,13 +736,13 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
     __syncthreads();
     tmem_fence_after();
     if (threadIdx.x == 0 && *dead) {                                 // loads in flight must land before the CTA leaves
-        const uint32_t it = tail->issued, first = it > (uint32_t)T::stages ? it - T::stages : 0;
         // the other CTA of a pair may have issued loads that the leader does not expect: it waits out the limit for them
+        const uint32_t it = max(tail->issued[0], tail->issued[1]), first = it > (uint32_t)T::stages ? it - T::stages : 0;
         for (uint32_t u = first; u < it + (CG == 2 ? 1u : 0u); ++u)
             mbar_wait_bounded(&tail->full[u % T::stages], (u / T::stages) & 1);
-        const uint32_t groups = tail->issued_groups;
-        for (uint32_t u = groups > kGroups ? groups - kGroups : 0; u < groups; ++u)
-            mbar_wait_bounded(&tail->group_full[u % kGroups], (u / kGroups) & 1);
+        const uint32_t groups = max(tail->issued_groups[0], tail->issued_groups[1]);
+        for (uint32_t u = groups > T::groups ? groups - T::groups : 0; u < groups; ++u)
+            mbar_wait_bounded(&tail->group_full[u % T::groups], (u / T::groups) & 1);
     }
     if constexpr (CG == 2) {                                         // neither leaves while the other may still reach into it
         __syncthreads();
