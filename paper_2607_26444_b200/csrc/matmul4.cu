@@ -35,8 +35,10 @@ constexpr int kMaxGroups = 3;           // groups of scales in shared memory, at
 constexpr int kScaleWarps = 4;
 constexpr int kBoxRows = 32;            // rows of a TMA box of the N operand where it is not the whole height of a tile
 
-// A tile of a CTA is MB blocks of 128 weight rows by up to BN rows of the N operand (see matmul.cu for the gated forms), of which
-// it holds BN / CG.
+// A tile of a CTA is MB blocks of 128 weight rows by up to BN rows of the N operand, of which it holds BN / CG.
+// Gated, MB = 1: eight gate channels, the same eight of up, and so on: TMEM hands 16 lanes at a time to a warp, a thread the
+//                lanes i and i + 8, so that gate and up of a channel meet in a thread.
+// Gated, MB = 2: two accumulators that share the rows, 128 gate channels and the same of up.
 template <bool NV, int CG, int MB, int BN>
 struct Tile4 {
     static constexpr int own_rows = BN / CG;                        // rows of the N operand in this CTA
@@ -47,7 +49,7 @@ struct Tile4 {
     static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // spans that a group serves
     static constexpr int per_chunk = kChunk / (NV ? 16 : 8);
     static constexpr int words = 4 / per_chunk;                     // scale words of a row that a span uses
-    static constexpr int groups = NV && BN > 64 ? 3 : 2;            // as many spans as the ring of codes, at least
+    static constexpr int groups = NV && BN > 96 ? 3 : 2;            // as many spans as the ring of codes, at least
     static constexpr int ws_group = MB * kM * group_bytes, as_group = BN * group_bytes;
     static constexpr int a_cols = (BN / 32 + 3) / 4 * 4;            // TMEM columns of a word of the rows' scales
     static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kChunks * chunk_cols;
@@ -59,9 +61,8 @@ struct Tile4 {
     static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 2, deal_warp = load_warp + 3;
     static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
-    static constexpr int swap_bufs = BN > 64 ? 1 : 2;               // of the exchange of a gated tile
-    static constexpr int swap_floats = MB == 1 ? epi_warps * swap_bufs * 8 * 32 : 0;
-    static constexpr int ring = (MB == 1 ? 202 : 212) * 1024 - groups * (ws_group + as_group);
+    static constexpr int stage_out = epi_warps * 1024;              // bytes: 32 rows of 16 channels or 16 of 32 of every warp
+    static constexpr int ring = 202 * 1024 - groups * (ws_group + as_group);
     static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
     static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)groups * (ws_group + as_group);
     static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_span % 1024 == 0 && own_rows % kBoxRows == 0 && per_group % spans == 0, "");
@@ -80,7 +81,7 @@ struct Mat4Params {
     long long a_rows, a_scale_stride, w_scale_stride, out_stride;
     int E, k_spans, channels, m_tiles;  // channels: rows of w per expert
     int last_steps;                     // matrix instructions of the last span
-    int out_words;                      // pairs of channels of out lie on 4 bytes
+    int out_vec;                        // eight channels of out lie on 16 bytes
 #ifdef STRATA_TEST_HOOKS
     int test_flags;
 #endif
@@ -195,24 +196,63 @@ __device__ __forceinline__ void load4_2d(void* dst, const CUtensorMap* map, int 
             "l"(map), "r"(x), "r"(y), "r"(leader_bar)
             : "memory");
 }
-__device__ __forceinline__ void tma_load_4d(void* dst, const CUtensorMap* map, int x, int y, int w, uint64_t* bar)
+// Weights: rows from y, or groups of eight of the interleaved gate and up from z, of expert e.
+__device__ __forceinline__ void tma_load_5d(void* dst, const CUtensorMap* map, int x, int y, int z, int e, uint64_t* bar)
 {
     asm volatile(
-        "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(
-            smem_addr(dst)),
-        "l"(map), "r"(x), "r"(y), "r"(0), "r"(w), "r"(smem_addr(bar))
+        "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5, %6}], "
+        "[%7];" ::"r"(smem_addr(dst)),
+        "l"(map), "r"(x), "r"(y), "r"(0), "r"(z), "r"(e), "r"(smem_addr(bar))
         : "memory");
 }
 template <int CG>
-__device__ __forceinline__ void load4_4d(void* dst, const CUtensorMap* map, int x, int y, int w, uint64_t* bar, uint32_t leader_bar)
+__device__ __forceinline__ void load4_5d(void* dst, const CUtensorMap* map, int x, int y, int z, int e, uint64_t* bar, uint32_t leader_bar)
 {
-    if constexpr (CG == 1) tma_load_4d(dst, map, x, y, w, bar);
+    if constexpr (CG == 1) tma_load_5d(dst, map, x, y, z, e, bar);
     else
         asm volatile(
-            "cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, "
-            "%5}], [%6];" ::"r"(smem_addr(dst)),
-            "l"(map), "r"(x), "r"(y), "r"(0), "r"(w), "r"(leader_bar)
+            "cp.async.bulk.tensor.5d.shared::cluster.global.tile.mbarrier::complete_tx::bytes.cta_group::2 [%0], [%1, {%2, %3, %4, "
+            "%5, %6}], [%7];" ::"r"(smem_addr(dst)),
+            "l"(map), "r"(x), "r"(y), "r"(0), "r"(z), "r"(e), "r"(leader_bar)
             : "memory");
+}
+
+// 16 lanes of TMEM by 8 * N columns: thread i holds lanes i / 4 (v[.][0], v[.][1]) and i / 4 + 8 (v[.][2], v[.][3]), of every eight
+// columns the two from 2 * (i % 4) on.
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t (&v)[4][4], uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.16x256b.x4.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(v[0][0]), "=r"(v[0][1]), "=r"(v[0][2]), "=r"(v[0][3]), "=r"(v[1][0]), "=r"(v[1][1]), "=r"(v[1][2]), "=r"(v[1][3]),
+          "=r"(v[2][0]), "=r"(v[2][1]), "=r"(v[2][2]), "=r"(v[2][3]), "=r"(v[3][0]), "=r"(v[3][1]), "=r"(v[3][2]), "=r"(v[3][3])
+        : "r"(addr));
+}
+__device__ __forceinline__ void tmem_ld_16x32(uint32_t (&v)[2][4], uint32_t addr)
+{
+    asm volatile("tcgen05.ld.sync.aligned.16x256b.x2.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(v[0][0]), "=r"(v[0][1]), "=r"(v[0][2]), "=r"(v[0][3]), "=r"(v[1][0]), "=r"(v[1][1]), "=r"(v[1][2]),
+                   "=r"(v[1][3])
+                 : "r"(addr));
+}
+// the loaded registers are tied to the wait, so that no use of them moves in front of it
+template <int N>
+__device__ __forceinline__ void tmem_ld_wait4(uint32_t (&v)[N][4])
+{
+    asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+#pragma unroll
+    for (int j = 0; j < N; ++j) asm volatile("" : "+r"(v[j][0]), "+r"(v[j][1]), "+r"(v[j][2]), "+r"(v[j][3])::"memory");
+}
+// N matrices of eight channels (a thread's lane) by eight rows of out (its columns), stored row by row of out: 16 bytes at the
+// address that lane 8 * j + i gives for row i of matrix j.
+__device__ __forceinline__ void store_turned(uint32_t addr, const uint32_t (&r)[4])
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x4.trans.shared.b16 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(r[0]), "r"(r[1]), "r"(r[2]),
+                 "r"(r[3])
+                 : "memory");
+}
+__device__ __forceinline__ void store_turned(uint32_t addr, const uint32_t (&r)[2])
+{
+    asm volatile("stmatrix.sync.aligned.m8n8.x2.trans.shared.b16 [%0], {%1,%2};" ::"r"(addr), "r"(r[0]), "r"(r[1]) : "memory");
 }
 
 __device__ __forceinline__ void tmem_st16(uint32_t addr, const uint32_t (&r)[16])
@@ -281,8 +321,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
     unsigned char* s_as = s_ws + T::groups * T::ws_group;              // [groups][BN][group bytes]
     Smem4Tail* tail = reinterpret_cast<Smem4Tail*>(smem + T::data_bytes);
     float* s_scale = reinterpret_cast<float*>(tail + 1);             // [epilogue warps][cols]
-    float* s_swap = s_scale + T::epi_warps * T::cols;                // [epilogue warps][buffers][8][32]
-    int* s_base = reinterpret_cast<int*>(s_swap + T::swap_floats);   // [E + 1]
+    unsigned char* s_out = reinterpret_cast<unsigned char*>(s_scale + T::epi_warps * T::cols);    // [epilogue warps][1024]
+    int* s_base = reinterpret_cast<int*>(s_out + T::stage_out);      // [E + 1]
     int* s_off = s_base + p.E + 1;                                   // [E]
     int* s_cnt = s_off + p.E;                                        // [E]
     const int warp = __shfl_sync(0xffffffffu, (int)threadIdx.x >> 5, 0), lane = (int)threadIdx.x & 31;
@@ -415,7 +455,8 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             const int boxes = (half_n + kBoxRows - 1) / kBoxRows, all_boxes = (w.rows + kBoxRows - 1) / kBoxRows;
             const bool whole = boxes * kBoxRows == T::own_rows, all_whole = all_boxes * kBoxRows == BN;
             const int row0 = w.row0 + (int)rank * half_n;
-            const int w_row = (w.m * CG + (int)rank) * MB * kM / (GATED ? 2 : 1);
+            const int m = w.m * CG + (int)rank;
+            const int w_row = GATED && MB == 1 ? 0 : m * MB * kM / (GATED ? 2 : 1), w_group = GATED && MB == 1 ? m * 8 : 0;
             const uint32_t span_bytes = (uint32_t)(CG * (weights ? T::w_span : boxes * kBoxRows * kKBytes));
             const uint32_t scale_bytes = (uint32_t)(weights ? T::ws_group : all_boxes * kBoxRows * T::group_bytes);
             for (int kb = 0; kb < p.k_spans; kb += T::spans, ++it) {
@@ -431,7 +472,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     const int x = kb / T::per_group * T::group_bytes;
                     if (elected()) {
                         mbar_expect_tx(bar, scale_bytes);
-                        if (weights) tma_load_4d(s_ws + g * T::ws_group, &p.map_ws, x, w_row, w.e, bar);
+                        if (weights) tma_load_5d(s_ws + g * T::ws_group, &p.map_ws, x, w_row, w_group, w.e, bar);
                         else if (all_whole) tma_load_2d(to, &p.map_as[1], x, w.row0, bar);
                         else
                             for (int b = 0; b < all_boxes; ++b)
@@ -463,7 +504,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                     for (int i = 0; i < T::spans; ++i) {
                         if (i >= spans) break;
                         const int x = (kb + i) * kKBytes;
-                        if (weights) load4_4d<CG>(dw + i * T::w_span, &p.map_w, x, w_row, w.e, bar, leader_bar);
+                        if (weights) load4_5d<CG>(dw + i * T::w_span, &p.map_w, x, w_row, w_group, w.e, bar, leader_bar);
                         else if (whole) load4_2d<CG>(da + i * T::a_span, &p.map_a[1], x, row0, bar, leader_bar);
                         else
                             for (int b = 0; b < boxes; ++b)
@@ -616,115 +657,129 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         }
     } else {
         const int ew = warp - kScaleWarps, quad = warp & 3;          // TMEM lanes 32*quad .. of this warp
-        const int pair = (ew >> 2) * 2 + (quad & 1);                 // of warps that exchange
         const int col0 = (ew >> 2) * T::cols;                        // first column of this warp
+        // A step: 32 columns of 16 channels, or 16 of 32; OB blocks of out per step and accumulators
+        constexpr bool kTight = GATED && MB == 1;
+        constexpr int kStep = kTight ? 32 : 16, kEights = kStep / 8, kPitch = kTight ? 32 : 64, OB = GATED ? 1 : MB;
         float* scale = s_scale + ew * T::cols;
-        const int half = p.channels / 2;
-        const bool scaled = p.a_scale || p.w_scale;
+        unsigned char* mine = s_out + ew * 1024;
+        // 16-byte places of a row of the staged step, turned so that eight rows meet eight different places of the banks
+        auto place = [&](int row, int chunk) {
+            return row * kPitch + ((kTight ? chunk ^ (row >> 2 & 1) : chunk ^ (row >> 1 & 3)) << 4);
+        };
+        const int half = p.channels / 2, limit = GATED ? half : p.channels;
+        const bool scaled = p.a_scale || p.w_scale, vec = p.out_vec != 0;
         Work w;
-        for (uint32_t use = 0;; ++use) {
-            const bool got = next_tile(*tail, use, w, lane, dead, p.status);
-            if constexpr (GATED && MB == 1) {                        // the two warps of an exchange leave together
-                if (!pair_all(got, pair)) break;
-            } else if (!got) {
-                break;
-            }
+        for (uint32_t use = 0; next_tile(*tail, use, w, lane, dead, p.status); ++use) {
             const int m = w.m * CG + (int)rank;
             const uint32_t buf = use % T::bufs;
             const int rows = min(T::cols, w.rows - col0);            // of this warp; may be negative
-            // channel(s) of w that this lane holds, and the first channel of out
-            int ch[2], out_ch[2];
-            if constexpr (GATED && MB == 1) {
-                out_ch[0] = m * (kM / 2) + (quad & 1) * 32 + lane;
-                ch[0] = out_ch[0] + (quad >> 1) * half;
-            } else if constexpr (GATED) {
-                out_ch[0] = ch[0] = m * kM + quad * 32 + lane;
-                ch[1] = ch[0] + half;
-            } else {
+            const int ch0 = kTight ? m * (kM / 2) + quad * 16 : GATED ? m * kM + quad * 32 : m * MB * kM + quad * 32;   // of out
+            float wsc[MB][2][2];                                     // of lanes 16 * h + i / 4 and + 8 of accumulator b
+            if (scaled) {
 #pragma unroll
-                for (int b = 0; b < MB; ++b) out_ch[b] = ch[b] = (m * MB + b) * kM + quad * 32 + lane;
-            }
-            const int limit = GATED ? half : p.channels;
-            const bool words = p.out_words != 0;
-            float wsc[2];
+                for (int b = 0; b < MB; ++b)
 #pragma unroll
-            for (int b = 0; b < MB; ++b)
-                wsc[b] = p.w_scale && out_ch[GATED ? 0 : b] < limit
-                             ? p.w_scale[((long long)w.e * p.channels + ch[b]) * p.w_scale_stride]
-                             : 1.0f;
-            __syncwarp();
-            for (int c = lane; c < T::cols; c += 32)
-                scale[c] = p.a_scale && c < rows ? p.a_scale[(long long)(w.row0 + col0 + c) * p.a_scale_stride] : 1.0f;
-            __syncwarp();
-            const bool ok = warp_wait(&tail->tmem_full[buf], (use / T::bufs) & 1, dead, p.status);
-            if constexpr (GATED && MB == 1) {
-                if (!pair_all(ok, pair)) break;
-            } else if (!ok) {
-                break;
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const int c = ch0 + (kTight ? h * 8 : h * 16 + u * 8) + (GATED ? 0 : b * kM) + (lane >> 2);
+                            const int up = kTight ? u : GATED ? b : 0;
+                            wsc[b][h][u] = p.w_scale && c < limit
+                                               ? p.w_scale[((long long)w.e * p.channels + c + up * half) * p.w_scale_stride]
+                                               : 1.0f;
+                        }
+                __syncwarp();
+                for (int c = lane; c < T::cols; c += 32)
+                    scale[c] = p.a_scale && c < rows ? p.a_scale[(long long)(w.row0 + col0 + c) * p.a_scale_stride] : 1.0f;
+                __syncwarp();
             }
+            if (!warp_wait(&tail->tmem_full[buf], (use / T::bufs) & 1, dead, p.status)) break;
             tmem_fence_after();
             const uint32_t addr = tmem + buf * MB * BN + ((uint32_t)(quad * 32) << 16) + col0;
             uint16_t* out = p.out + (long long)(w.row0 + col0) * p.out_stride;
-            int phase = 0;
-            uint32_t v[MB][16];                                      // the columns to come: loaded while those before are worked on
+            uint32_t v[MB][2][kEights][4];                           // the step to come: loaded while the one before is worked on
+            auto load = [&](int c0) {
+#pragma unroll
+                for (int b = 0; b < MB; ++b)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) tmem_ld_16x32(v[b][h], addr + b * BN + ((uint32_t)(16 * h) << 16) + c0);
+            };
             __syncwarp();
-            if (rows > 0) {
+            if (rows > 0) load(0);
+            for (int c0 = 0; c0 < rows; c0 += kStep) {
+                float y[MB][2][kEights][4];
 #pragma unroll
-                for (int b = 0; b < MB; ++b) tmem_ld16(v[b], addr + b * BN);
-            }
-            for (int c0 = 0; c0 < rows; c0 += 16, phase ^= 1) {
-                float y[MB][16];
+                for (int b = 0; b < MB; ++b)
 #pragma unroll
-                for (int b = 0; b < MB; ++b) {
-                    tmem_ld_wait(v[b]);
+                    for (int h = 0; h < 2; ++h) {
+                        tmem_ld_wait4(v[b][h]);
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) y[b][c] = __uint_as_float(v[b][c]);
-                }
-                __syncwarp();                                        // loads from TMEM ask for converged warps: waits and stores part them
-                if (c0 + 16 < rows) {
+                        for (int j = 0; j < kEights; ++j)
 #pragma unroll
-                    for (int b = 0; b < MB; ++b) tmem_ld16(v[b], addr + b * BN + c0 + 16);
-                }
-                if (scaled) {
-                    float sc[16];
-#pragma unroll
-                    for (int c = 0; c < 16; c += 4)
-                        *reinterpret_cast<float4*>(&sc[c]) = *reinterpret_cast<const float4*>(&scale[c0 + c]);
-#pragma unroll
-                    for (int b = 0; b < MB; ++b)
-#pragma unroll
-                        for (int c = 0; c < 16; ++c) y[b][c] *= sc[c] * wsc[b];
-                }
-                if constexpr (GATED && MB == 1) {
-                    // the gate's warp finishes columns 0..7, up's warp columns 8..15
-                    const bool up = quad >> 1;
-                    float* mine = s_swap + (ew * T::swap_bufs + phase % T::swap_bufs) * 8 * 32 + lane;
-                    const float* theirs = s_swap + ((ew ^ 2) * T::swap_bufs + phase % T::swap_bufs) * 8 * 32 + lane;
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) mine[c * 32] = up ? y[0][c] : y[0][8 + c];
-                    asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
-                    float o[8];
-#pragma unroll
-                    for (int c = 0; c < 8; ++c) {
-                        const float other = theirs[c * 32];
-                        o[c] = up ? gate_mul(other, y[0][8 + c]) : gate_mul(y[0][c], other);
+                            for (int i = 0; i < 4; ++i) y[b][h][j][i] = __uint_as_float(v[b][h][j][i]);
                     }
-                    if constexpr (T::swap_bufs == 1) asm volatile("bar.sync %0, 64;" ::"r"(1 + pair) : "memory");
-                    const int shift = up ? 8 : 0;
-                    store_pairs<8>(o, lane, out + (long long)(c0 + shift) * p.out_stride, p.out_stride, rows - c0 - shift, out_ch[0],
-                                   limit, words);
-                } else if constexpr (GATED) {
-                    float o[16];
+                if (c0 + kStep < rows) load(c0 + kStep);
+                if (scaled) {
 #pragma unroll
-                    for (int c = 0; c < 16; ++c) o[c] = gate_mul(y[0][c], y[MB - 1][c]);
-                    store_pairs<16>(o, lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[0], limit, words);
-                } else {
+                    for (int j = 0; j < kEights; ++j) {
+                        const float2 sc = *reinterpret_cast<const float2*>(&scale[c0 + j * 8 + (lane & 3) * 2]);
 #pragma unroll
-                    for (int b = 0; b < MB; ++b)
-                        store_pairs<16>(y[b], lane, out + (long long)c0 * p.out_stride, p.out_stride, rows - c0, out_ch[b], limit, words);
+                        for (int b = 0; b < MB; ++b)
+#pragma unroll
+                            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) y[b][h][j][i] *= (i & 1 ? sc.y : sc.x) * wsc[b][h][i >> 1];
+                    }
+                }
+#pragma unroll
+                for (int b = 0; b < OB; ++b) {
+                    // stage: lane 8 * j + i gives the place of row i of the j-th eight rows
+                    const int row = lane % kStep;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        if constexpr (kTight) {
+                            uint32_t r[kEights];
+#pragma unroll
+                            for (int j = 0; j < kEights; ++j)
+                                r[j] = pack_bf16x2(gate_mul(y[0][h][j][0], y[0][h][j][2]), gate_mul(y[0][h][j][1], y[0][h][j][3]));
+                            store_turned(smem_addr(mine + place(row, h)), r);
+                        } else {
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                uint32_t r[kEights];
+#pragma unroll
+                                for (int j = 0; j < kEights; ++j) {
+                                    if constexpr (GATED)
+                                        r[j] = pack_bf16x2(gate_mul(y[0][h][j][2 * u], y[MB - 1][h][j][2 * u]),
+                                                           gate_mul(y[0][h][j][2 * u + 1], y[MB - 1][h][j][2 * u + 1]));
+                                    else r[j] = pack_bf16x2(y[b][h][j][2 * u], y[b][h][j][2 * u + 1]);
+                                }
+                                store_turned(smem_addr(mine + place(row, h * 2 + u)), r);
+                            }
+                        }
+                    }
+                    __syncwarp();
+                    constexpr int kChunks16 = kPitch / 16, kRowsAt = 32 / kChunks16;     // 16-byte chunks of a row, rows at a time
+#pragma unroll
+                    for (int i = 0; i < kStep / kRowsAt; ++i) {
+                        const int row2 = i * kRowsAt + lane / kChunks16, chunk = lane % kChunks16;
+                        const int ch = ch0 + b * kM + chunk * 8;
+                        const uint4 q = *reinterpret_cast<const uint4*>(mine + place(row2, chunk));
+                        if (c0 + row2 < rows) {
+                            uint16_t* at = out + (long long)(c0 + row2) * p.out_stride + ch;
+                            if (vec && ch + 8 <= limit) *reinterpret_cast<uint4*>(at) = q;
+                            else {
+                                const uint32_t words[4] = {q.x, q.y, q.z, q.w};
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    if (ch + e < limit) at[e] = (uint16_t)(words[e >> 1] >> (16 * (e & 1)));
+                            }
+                        }
+                    }
+                    __syncwarp();
                 }
             }
-            __syncwarp();
             tmem_fence_before();
             __syncwarp();
             if (lane == 0) arrive_leader<CG>(&tail->tmem_empty[buf]);
@@ -758,10 +813,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
 }
 
 template <bool NV, int CG, int MB, int BN>
-size_t smem_bytes4(int E)
+constexpr size_t smem_bytes4(int E)
 {
     using T = Tile4<NV, CG, MB, BN>;
-    return 1024 + T::data_bytes + sizeof(Smem4Tail) + (size_t)(T::epi_warps * T::cols + T::swap_floats) * sizeof(float) +
+    return 1024 + T::data_bytes + sizeof(Smem4Tail) + (size_t)(T::epi_warps * T::cols) * sizeof(float) + T::stage_out +
            (size_t)(3 * E + 1) * sizeof(int);
 }
 
@@ -776,11 +831,13 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
         const CUtensorMapSwizzle swizzle = i == 0                  ? CU_TENSOR_MAP_SWIZZLE_128B
                                            : T::group_bytes == 64 ? CU_TENSOR_MAP_SWIZZLE_64B
                                                                   : CU_TENSOR_MAP_SWIZZLE_32B;
-        {   // weights: [E][channels]; gated: [E][2][channels / 2], gate and up of an expert in one box
+        {   // weights: [E][channels]; gated: [E][2][channels / 2], gate and up in one box, in turn by eights where MB is 1
             const cuuint64_t stride = (cuuint64_t)(i == 0 ? a.w.code_stride : a.w.block_stride);
-            const cuuint64_t dims[4] = {bytes, rows, parts, (cuuint64_t)s.E}, strides[3] = {stride, rows * stride, parts * rows * stride};
-            const cuuint32_t boxes[4] = {box, (cuuint32_t)(MB * kM / parts), (cuuint32_t)parts, 1};
-            if (!encode(i == 0 ? &p.map_w : &p.map_ws, i == 0 ? a.w.codes : a.w.block, 4, dims, strides, boxes, swizzle))
+            const bool eights = a.gated && MB == 1;
+            const cuuint64_t dims[5] = {bytes, eights ? 8 : rows, parts, eights ? rows / 8 : 1, (cuuint64_t)s.E};
+            const cuuint64_t strides[4] = {stride, rows * stride, 8 * stride, parts * rows * stride};
+            const cuuint32_t boxes[5] = {box, (cuuint32_t)(eights ? 8 : MB * kM / parts), (cuuint32_t)parts, eights ? 8u : 1u, 1};
+            if (!encode(i == 0 ? &p.map_w : &p.map_ws, i == 0 ? a.w.codes : a.w.block, 5, dims, strides, boxes, swizzle))
                 return cudaErrorInvalidValue;
         }
         const cuuint64_t dims[2] = {bytes, (cuuint64_t)a.a_rows};
@@ -804,6 +861,7 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
 template <bool NV, int CG, int MB, int BN>
 cudaError_t configure4()
 {
+    static_assert(smem_bytes4<NV, CG, MB, BN>(kMaxExperts) <= 227 * 1024, "");
     const void* fns[2] = {(const void*)expert_matmul4_kernel<NV, true, CG, MB, BN>, (const void*)expert_matmul4_kernel<NV, false, CG, MB, BN>};
     for (const void* f : fns) {
         const cudaError_t e =
@@ -861,10 +919,11 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     p.k_spans = (a.inner / 2 + kKBytes - 1) / kKBytes;
     p.last_steps = (a.inner / 2 - (p.k_spans - 1) * kKBytes + kUmmaK - 1) / kUmmaK;
     p.channels = a.channels;
-    p.out_words = a.channels % (a.gated ? 4 : 2) == 0 && a.out_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 3u) == 0;
+    p.out_vec = a.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
     const long long items = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : (long long)s.R * s.T * s.K;
     const long long mean = (items + s.E - 1) / s.E;
-    const int v = (int)tune("STRATA_MM4", mean <= 64 ? 0 : mean <= 192 ? 1 : 2);
+    int v = (int)tune("STRATA_MM4", mean <= 64 ? 0 : mean <= 192 ? 1 : 2);
+    if (a.gated && a.channels % 16 != 0) v = 1;                      // the others take gate and up by eights
     return a.type == STRATA_T_NVF4 ? pick4<true>(v, s, a, p, n_sm, st) : pick4<false>(v, s, a, p, n_sm, st);
 }
 

@@ -160,7 +160,7 @@ inline EncodeFn encode_fn()
 inline bool encode(CUtensorMap* map, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
                    const cuuint32_t* box, CUtensorMapSwizzle swizzle = CU_TENSOR_MAP_SWIZZLE_128B)
 {
-    const cuuint32_t ones[4] = {1, 1, 1, 1};
+    const cuuint32_t ones[5] = {1, 1, 1, 1, 1};
     EncodeFn fn = encode_fn();
     return fn && fn(map, CU_TENSOR_MAP_DATA_TYPE_UINT8, (cuuint32_t)rank, const_cast<void*>(base), dims, strides, box, ones,
                     CU_TENSOR_MAP_INTERLEAVE_NONE, swizzle, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
