@@ -1,5 +1,6 @@
 // Balance loss of the router with the counts per expert, and its gradient (strata_layer.h has the formulas).  One warp owns a
-// token, lanes hold neighbouring experts (scores.cuh).  All sums run in an order that the shape fixes: a warp's tokens, the
+// token; its lanes hold vectors of 16 bytes in turn (scores.cuh gives a lane its experts in one run: two loads of half a sector each).
+// All sums run in an order that the shape fixes: a warp's tokens, the
 // warps of a block, the blocks of a group, the groups.
 #include "scores.cuh"
 
@@ -8,20 +9,21 @@ namespace strata {
 namespace {
 
 constexpr int kWarps = 8;
-constexpr int kBlocksPerSm = 4;
-constexpr int kSumCols = 32, kSumLanes = 8;    // of balance_sum_kernel
+constexpr int kSumCols = 8;            // experts of a block of balance_sum_kernel, one per warp
+// Blocks that an SM holds at a time, by the registers that VPL logits per lane take: grids are one wave of them.
+constexpr int loss_blocks(int vpl) { return vpl <= 8 ? 4 : vpl == 16 ? 2 : 1; }
+constexpr int grad_blocks(int vpl) { return vpl <= 4 ? 4 : vpl == 8 ? 3 : vpl == 16 ? 2 : 1; }
 
 struct BalanceGeom {
     int groups, slices, col_blocks;
     long long group_tokens;
 };
-BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params& b, int n_sm)
+BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params& b, int blocks)
 {
     BalanceGeom g;
     g.groups = b.per_rank ? s.R : 1;
     g.group_tokens = b.per_rank ? s.T : (long long)s.R * s.T;
-    const long long most = max(1ll, (long long)n_sm * kBlocksPerSm / g.groups);
-    g.slices = (int)min(most, (g.group_tokens + kWarps - 1) / kWarps);
+    g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + kWarps - 1) / kWarps);
     g.col_blocks = (s.E + kSumCols - 1) / kSumCols;
     return g;
 }
@@ -45,52 +47,107 @@ struct BalanceParams {
     float weight, z_weight;
 };
 
-// The normalised scores of a token, and the softmax and the logarithm of its sum where they are asked for.
+// Expert of register r of a lane.
+template <int VPL, bool BF16>
+__device__ __forceinline__ int expert_of(int lane, int r)
+{
+    constexpr int VW = BF16 ? 8 : 4;
+    if constexpr (VPL >= VW) return r / VW * (32 * VW) + lane * VW + r % VW;
+    else return lane * VPL + r;
+}
+// A token's logits (NaN and places beyond E: -inf), or RAW values (places beyond E: 0).
+template <int VPL, bool BF16, bool RAW = false>
+__device__ __forceinline__ void load_token(float (&l)[VPL], const void* base, long long row_off, int lane, int E, bool vec_ok)
+{
+    constexpr int VW = VPL < (BF16 ? 8 : 4) ? VPL : BF16 ? 8 : 4;
+#pragma unroll
+    for (int j = 0; j < VPL; j += VW) {
+        float(&part)[VW] = *reinterpret_cast<float(*)[VW]>(&l[j]);
+        load_logits<VW, BF16, RAW>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+    }
+}
+template <int VPL, bool BF16>
+__device__ __forceinline__ void store_token(const float (&g)[VPL], void* base, long long row_off, int lane, int E, bool vec_ok)
+{
+    constexpr int VW = VPL < (BF16 ? 8 : 4) ? VPL : BF16 ? 8 : 4;
+#pragma unroll
+    for (int j = 0; j < VPL; j += VW) {
+        const float(&part)[VW] = *reinterpret_cast<const float(*)[VW]>(&g[j]);
+        store_row<VW, BF16>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+    }
+}
+
+// within 2^-23
+__device__ __forceinline__ float approx_rcp(float v)
+{
+    float d;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(d) : "f"(v));
+    return d;
+}
+
+// The normalised scores p of a token; rest: 1 - s of the sigmoid, without the cancellation; where they are asked for, the softmax and
+// the logarithm of its sum.  One exponential per logit gives the sigmoid on both sides, 1 / (1 + e) and e / (1 + e) with e = exp(-|l|),
+// and exp(l) itself, which the softmax takes as long as no logit of the token passes 60.  Reciprocals are within 2^-23.
 template <int VPL, bool SIGMOID>
-__device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&soft)[VPL], float& lse)
+__device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&rest)[VPL],
+                                             float (&soft)[VPL], float& lse)
 {
     lse = 0.0f;
-    if (!SIGMOID || want_soft) {
-        float m = l[0];
-#pragma unroll
-        for (int i = 1; i < VPL; ++i) m = fmaxf(m, l[i]);
-        m = warp_max(m);
-        float s = 0.0f;
+    if constexpr (SIGMOID) {
+        float s = 0.0f, total = 0.0f, top = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
-            s += soft[i];
+            const float e = expf(-fabsf(l[i])), r = approx_rcp(1.0f + e), small = e * r;
+            p[i] = l[i] >= 0.0f ? r : small;
+            rest[i] = l[i] >= 0.0f ? small : r;
+            soft[i] = l[i] >= 0.0f ? approx_rcp(e) : e;
+            s += p[i];
+            total += soft[i];
+            top = fmaxf(top, l[i] == -INFINITY ? 0.0f : fabsf(l[i]));
         }
         s = warp_sum(s);
         const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) soft[i] *= inv;
-        if (s > 0.0f) lse = m + logf(s);
-    }
-    if constexpr (SIGMOID) {
-        float s = 0.0f;
+        for (int i = 0; i < VPL; ++i) p[i] *= inv;
+        if (!want_soft) return;
+        if (__all_sync(kFull, top <= 60.0f)) {
+            total = warp_sum(total);
+            const float inv_total = total > 0.0f ? __frcp_rn(total) : 0.0f;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) {
-            p[i] = sigmoid_f(l[i]);
-            s += p[i];
+            for (int i = 0; i < VPL; ++i) soft[i] *= inv_total;
+            if (total > 0.0f) lse = logf(total);
+            return;
         }
-        s = warp_sum(s);
+    }
+    float m = l[0];
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) p[i] = s > 0.0f ? __fdiv_rn(p[i], s) : 0.0f;
-    } else {
+    for (int i = 1; i < VPL; ++i) m = fmaxf(m, l[i]);
+    m = warp_max(m);
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) {
+        soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
+        s += soft[i];
+    }
+    s = warp_sum(s);
+    const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) soft[i] *= inv;
+    if (s > 0.0f) lse = m + logf(s);
+    if constexpr (!SIGMOID) {
 #pragma unroll
         for (int i = 0; i < VPL; ++i) p[i] = soft[i];
     }
 }
 
 template <int VPL, bool BF16, bool SIGMOID>
-__global__ void __launch_bounds__(kWarps * 32) balance_kernel(const BalanceParams p)
+__global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(const BalanceParams p)
 {
     extern __shared__ float s_sum[];                              // [warps][32 * VPL]
     __shared__ int s_count[kMaxExperts];
     __shared__ float s_z[kWarps];
     __shared__ int s_n[kWarps];
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, e0 = lane * VPL;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
     for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) s_count[e] = 0;
     __syncthreads();
@@ -99,25 +156,37 @@ __global__ void __launch_bounds__(kWarps * 32) balance_kernel(const BalanceParam
     int n = 0;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
-    for (long long t = slice * kWarps + warp; t < p.group_tokens; t += p.slices * kWarps) {
-        const long long tok = group * p.group_tokens + t;
-        int id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
-        float l[VPL], q[VPL], soft[VPL], lse;
-        load_logits<VPL, BF16>(l, p.logits, tok * p.stride, e0, p.E, p.vec_ok != 0);
+    const long long step = (long long)p.slices * kWarps, first = (long long)group * p.group_tokens;
+    long long t = slice * kWarps + warp;
+    float next[VPL];
+    int next_id = -1;
+    auto load = [&] {                                             // a token ahead: its way from memory is longer than one token's work
+        const long long tok = first + t;
+        next_id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
+        load_token<VPL, BF16>(next, p.logits, tok * p.stride, lane, p.E, p.vec_ok != 0);
+    };
+    if (t < p.group_tokens) load();
+    while (t < p.group_tokens) {
+        float l[VPL], q[VPL], rest[VPL], soft[VPL], lse;
+        int id = next_id;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) l[i] = next[i];
+        t += step;
+        if (t < p.group_tokens) load();
         if (id < -1 || id >= p.E) {
             report_status(p.status, STRATA_ERR_BAD_EXPERT_ID);
             id = -1;
         }
         if (!__any_sync(kFull, id >= 0)) continue;
         if (id >= 0) atomicAdd(&s_count[id], 1);
-        token_scores<VPL, SIGMOID>(l, p.z_weight != 0.0f, q, soft, lse);
+        token_scores<VPL, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) sum[i] += q[i];
         z = fmaf(lse, lse, z);
         ++n;
     }
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) s_sum[warp * 32 * VPL + i * 32 + lane] = sum[i];
+    for (int i = 0; i < VPL; ++i) s_sum[warp * 32 * VPL + expert_of<VPL, BF16>(lane, i)] = sum[i];
     if (lane == 0) {
         s_z[warp] = z;
         s_n[warp] = n;
@@ -125,10 +194,9 @@ __global__ void __launch_bounds__(kWarps * 32) balance_kernel(const BalanceParam
     __syncthreads();
     griddep_launch_dependents();
     for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) {
-        const int at = (e % VPL) * 32 + e / VPL;
         float a = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) a += s_sum[w * 32 * VPL + at];
+        for (int w = 0; w < kWarps; ++w) a += s_sum[w * 32 * VPL + e];
         p.part_p[(size_t)blockIdx.x * p.E + e] = a;
         p.part_c[(size_t)blockIdx.x * p.E + e] = s_count[e];
     }
@@ -144,66 +212,45 @@ __global__ void __launch_bounds__(kWarps * 32) balance_kernel(const BalanceParam
     }
 }
 
-// Sum over a block's threads in a fixed order; valid in thread 0.
-template <typename V>
-__device__ __forceinline__ V block_sum(V v, V* buf)
-{
-    const int t = (int)threadIdx.x;
-    __syncthreads();
-    buf[t] = v;
-    __syncthreads();
-#pragma unroll
-    for (int o = kSumCols * kSumLanes / 2; o > 0; o >>= 1) {
-        if (t < o) buf[t] += buf[t + o];
-        __syncthreads();
-    }
-    return buf[0];
-}
+__device__ __forceinline__ int warp_count(int v) { return __reduce_add_sync(kFull, v); }
 
-// Slices to groups: 32 experts of one group per block, each of 8 lanes adding every 8th slice.  The block that draws the last
-// ticket adds up the losses.
-__global__ void __launch_bounds__(kSumCols* kSumLanes) balance_sum_kernel(const BalanceParams p, int col_blocks)
+// Slices to groups: 8 experts of one group per block, one per warp, whose lanes add every 32nd slice.  The block that draws the
+// last ticket adds up the losses.
+__global__ void __launch_bounds__(kSumCols * 32) balance_sum_kernel(const BalanceParams p, int col_blocks)
 {
-    __shared__ float s_f[kSumCols * kSumLanes];
-    __shared__ int s_i[kSumCols * kSumLanes];
+    __shared__ float s_f[kSumCols], s_z[kSumCols];
+    __shared__ int s_alive[kSumCols], s_total[kSumCols];
     __shared__ bool s_last;
-    const int t = (int)threadIdx.x, cx = t % kSumCols, ly = t / kSumCols;
-    const int group = (int)blockIdx.x / col_blocks, e = ((int)blockIdx.x - group * col_blocks) * kSumCols + cx;
+    const int t = (int)threadIdx.x, lane = t & 31, warp = t >> 5;
+    const int group = (int)blockIdx.x / col_blocks, e = ((int)blockIdx.x - group * col_blocks) * kSumCols + warp;
     griddep_wait();
     griddep_launch_dependents();
     const size_t first = (size_t)group * p.slices;
-    int n = 0;
-    for (int i = t; i < p.slices; i += kSumCols * kSumLanes) n += p.part_n[first + i];
-    n = block_sum(n, s_i);
     float a = 0.0f;
-    int c = 0;
-    if (e < p.E)
-        for (int i = ly; i < p.slices; i += kSumLanes) {
-            a += p.part_p[(first + i) * p.E + e];
-            c += p.part_c[(first + i) * p.E + e];
-        }
-    __syncthreads();
-    s_f[t] = a;
-    s_i[t] = c;
-    __syncthreads();
-#pragma unroll
-    for (int o = kSumLanes / 2; o > 0; o >>= 1) {
-        if (ly < o) {
-            s_f[t] += s_f[t + o * kSumCols];
-            s_i[t] += s_i[t + o * kSumCols];
-        }
-        __syncthreads();
+    int c = 0, n = 0;
+    const int col = min(e, p.E - 1);
+#pragma unroll 4
+    for (int i = lane; i < p.slices; i += 32) {
+        n += p.part_n[first + i];
+        a += p.part_p[(first + i) * p.E + col];
+        c += p.part_c[(first + i) * p.E + col];
     }
-    float part = 0.0f;
-    if (ly == 0 && e < p.E) {
-        const float prob = n > 0 ? __fdiv_rn(s_f[t], (float)n) : 0.0f;
-        p.prob[(size_t)group * p.E + e] = prob;
-        p.count[(size_t)group * p.E + e] = s_i[t];
-        part = n > 0 ? (float)s_i[t] * prob : 0.0f;
+    n = warp_count(n);
+    c = warp_count(c);
+    a = warp_sum(a);
+    if (lane == 0) {
+        const float prob = n > 0 ? __fdiv_rn(a, (float)n) : 0.0f;
+        if (e < p.E) {
+            p.prob[(size_t)group * p.E + e] = prob;
+            p.count[(size_t)group * p.E + e] = c;
+        }
+        s_f[warp] = e < p.E && n > 0 ? (float)c * prob * __fdiv_rn((float)p.E, (float)p.K * (float)n) : 0.0f;
     }
-    part = block_sum(part, s_f);
+    __syncthreads();
     if (t == 0) {
-        p.part_loss[blockIdx.x] = n > 0 ? part * __fdiv_rn((float)p.E, (float)p.K * (float)n) : 0.0f;
+        float part = 0.0f;
+        for (int w = 0; w < kSumCols; ++w) part += s_f[w];
+        p.part_loss[blockIdx.x] = part;
         if (blockIdx.x % (unsigned)col_blocks == 0) p.tokens[group] = n;
         __threadfence();
         s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
@@ -213,22 +260,36 @@ __global__ void __launch_bounds__(kSumCols* kSumLanes) balance_sum_kernel(const 
     __threadfence();
     float loss = 0.0f, z = 0.0f;
     int alive = 0, total = 0;
-    for (int i = t; i < (int)gridDim.x; i += kSumCols * kSumLanes) loss += __ldcg(p.part_loss + i);
-    for (int i = t; i < p.groups; i += kSumCols * kSumLanes) {
+#pragma unroll 4
+    for (int i = t; i < (int)gridDim.x; i += kSumCols * 32) loss += __ldcg(p.part_loss + i);
+#pragma unroll 4
+    for (int i = t; i < p.groups * p.slices; i += kSumCols * 32) z += p.part_z[i];
+    for (int i = t; i < p.groups; i += kSumCols * 32) {
         const int m = __ldcg(p.tokens + i);
         alive += m > 0;
         total += m;
     }
-    for (int i = t; i < p.groups * p.slices; i += kSumCols * kSumLanes) z += p.part_z[i];
-    loss = block_sum(loss, s_f);
-    z = block_sum(z, s_f);
-    alive = block_sum(alive, s_i);
-    total = block_sum(total, s_i);
-    if (t == 0) {
-        p.loss[0] = alive > 0 ? p.weight * __fdiv_rn(loss, (float)alive) : 0.0f;
-        p.loss[1] = total > 0 && p.z_weight != 0.0f ? p.z_weight * __fdiv_rn(z, (float)total) : 0.0f;
-        *p.ticket = 0;
+    loss = warp_sum(loss);
+    z = warp_sum(z);
+    alive = warp_count(alive);
+    total = warp_count(total);
+    if (lane == 0) {
+        s_f[warp] = loss;
+        s_z[warp] = z;
+        s_alive[warp] = alive;
+        s_total[warp] = total;
     }
+    __syncthreads();
+    if (t != 0) return;
+    for (int w = 1; w < kSumCols; ++w) {
+        loss += s_f[w];
+        z += s_z[w];
+        alive += s_alive[w];
+        total += s_total[w];
+    }
+    p.loss[0] = alive > 0 ? p.weight * __fdiv_rn(loss, (float)alive) : 0.0f;
+    p.loss[1] = total > 0 && p.z_weight != 0.0f ? p.z_weight * __fdiv_rn(z, (float)total) : 0.0f;
+    *p.ticket = 0;
 }
 
 struct BalanceGradParams {
@@ -245,10 +306,10 @@ struct BalanceGradParams {
 };
 
 template <int VPL, bool BF16, bool SIGMOID>
-__global__ void __launch_bounds__(kWarps * 32) balance_grad_kernel(const BalanceGradParams p)
+__global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_kernel(const BalanceGradParams p)
 {
     __shared__ int s_alive, s_total;
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, e0 = lane * VPL;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
     const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
     if (threadIdx.x == 0) s_alive = s_total = 0;
     __syncthreads();
@@ -270,19 +331,35 @@ __global__ void __launch_bounds__(kWarps * 32) balance_grad_kernel(const Balance
     const bool want_z = p.z_weight != 0.0f;
     float c[VPL];
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) c[i] = e0 + i < p.E ? unit * (float)p.count[(size_t)group * p.E + e0 + i] : 0.0f;
-    for (long long t = slice * kWarps + warp; t < p.group_tokens; t += p.slices * kWarps) {
-        const long long tok = group * p.group_tokens + t;
-        const int id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
-        float l[VPL], q[VPL], soft[VPL], g[VPL], lse;
-        load_logits<VPL, BF16>(l, p.logits, tok * p.stride, e0, p.E, p.vec_ok != 0);
-        if (p.add) load_logits<VPL, BF16, true>(g, p.add, tok * p.add_stride, e0, p.E, p.add_vec_ok != 0);
+    for (int i = 0; i < VPL; ++i) {
+        const int e = expert_of<VPL, BF16>(lane, i);
+        c[i] = e < p.E ? unit * (float)p.count[(size_t)group * p.E + e] : 0.0f;
+    }
+    const long long step = (long long)p.slices * kWarps, first = (long long)group * p.group_tokens;
+    long long t = slice * kWarps + warp;
+    float next[VPL];
+    int next_id = -1;
+    auto load = [&] {                                             // a token ahead, as above
+        const long long tok = first + t;
+        next_id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
+        load_token<VPL, BF16>(next, p.logits, tok * p.stride, lane, p.E, p.vec_ok != 0);
+    };
+    if (t < p.group_tokens) load();
+    while (t < p.group_tokens) {
+        const long long tok = first + t;
+        const int id = next_id;
+        float l[VPL], q[VPL], rest[VPL], soft[VPL], g[VPL], lse;
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) l[i] = next[i];
+        if (p.add) load_token<VPL, BF16, true>(g, p.add, tok * p.add_stride, lane, p.E, p.add_vec_ok != 0);
         else {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) g[i] = 0.0f;
         }
+        t += step;
+        if (t < p.group_tokens) load();
         if (__any_sync(kFull, id >= 0 && id < p.E)) {
-            token_scores<VPL, SIGMOID>(l, want_z, q, soft, lse);
+            token_scores<VPL, SIGMOID>(l, want_z, q, rest, soft, lse);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) dot = fmaf(q[i], c[i], dot);
@@ -290,13 +367,13 @@ __global__ void __launch_bounds__(kWarps * 32) balance_grad_kernel(const Balance
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
                 float d = q[i] * (c[i] - dot);
-                if constexpr (SIGMOID) d *= sigmoid_f(-l[i]);     // 1 - s without the cancellation
+                if constexpr (SIGMOID) d *= rest[i];
                 if (want_z) d = fmaf(unit_z * lse, soft[i], d);
                 if (l[i] == -INFINITY) d = 0.0f;
                 g[i] += d;
             }
         }
-        store_row<VPL, BF16>(g, p.dlogits, tok * p.dstride, e0, p.E, p.dvec_ok != 0);
+        store_token<VPL, BF16>(g, p.dlogits, tok * p.dstride, lane, p.E, p.dvec_ok != 0);
     }
 }
 
@@ -320,7 +397,7 @@ cudaError_t grad_vpl(const BalanceGradParams& p, bool sigmoid, unsigned grid, cu
 
 size_t balance_scratch_bytes(const strata_moe_shape& s, const strata_balance_params& b, int n_sm)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm);
+    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(lanes_width(s.E)));
     const size_t blocks = (size_t)g.groups * g.slices;
     return 2 * aligned(blocks * s.E * 4) + 2 * aligned(blocks * 4) + aligned((size_t)g.groups * g.col_blocks * 4);
 }
@@ -346,7 +423,7 @@ cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_
                                 long long stride, const int32_t* ids, float* loss, const strata_balance_stats& stats,
                                 void* scratch, int* status, unsigned* ticket, int n_sm, cudaStream_t st, int* n_launches)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm);
+    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(lanes_width(s.E)));
     const size_t blocks = (size_t)g.groups * g.slices;
     BalanceParams p{};
     p.logits = logits;
@@ -380,7 +457,7 @@ cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_
     const cudaError_t err = first_pass(s, p, type == STRATA_T_BF16, b.score == STRATA_SCORE_SIGMOID, (unsigned)blocks, st);
     if (err != cudaSuccess) return err;
     *n_launches = 2;
-    return launch_pdl(balance_sum_kernel, (unsigned)(g.groups * g.col_blocks), kSumCols * kSumLanes, 0, st, p, g.col_blocks);
+    return launch_pdl(balance_sum_kernel, (unsigned)(g.groups * g.col_blocks), kSumCols * 32, 0, st, p, g.col_blocks);
 }
 
 cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_params& b, const void* logits, int type,
@@ -388,7 +465,7 @@ cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_
                                 const void* add, long long add_stride, void* dlogits, long long dstride, int n_sm,
                                 cudaStream_t st)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm);
+    const BalanceGeom g = balance_geom(s, b, n_sm * grad_blocks(lanes_width(s.E)));
     BalanceGradParams p{};
     p.logits = logits;
     p.add = add;

@@ -107,7 +107,7 @@ struct Rows4Params {
     long long x_stride, code_stride, block_stride, scale_stride, out_stride;
     long long rows;
     int vecs;              // units of eight values in a row
-    int tpr;               // threads of one row, a multiple of 32; a block holds blockDim.x / tpr rows
+    int tpr;               // threads of one row: 4, 8, 16 or a multiple of 32; a block holds blockDim.x / tpr rows
     int out_f32;
 };
 
@@ -131,7 +131,9 @@ __global__ void __launch_bounds__(MAXT) quantize4_kernel(const Rows4Params p)
     const long long row = (long long)blockIdx.x * ((int)blockDim.x / p.tpr) + sub;
     griddep_wait();
     griddep_launch_dependents();
-    if (row >= p.rows || (p.n_valid && row >= *p.n_valid)) return;
+    const bool live = row < p.rows && !(p.n_valid && row >= *p.n_valid);
+    if (!live && p.tpr >= 32) return;                               // rows that share a warp stay for its exchanges
+    const int vecs = live ? p.vecs : 0;
     const uint16_t* x = p.x + row * p.x_stride;
     uint8_t* codes = p.codes + row * p.code_stride;
     uint8_t* block = p.block + row * p.block_stride;
@@ -139,7 +141,7 @@ __global__ void __launch_bounds__(MAXT) quantize4_kernel(const Rows4Params p)
 #pragma unroll
     for (int j = 0; j < VPT; ++j) {
         const int c = tid + j * p.tpr;
-        v[j] = c < p.vecs ? ld_stream16(x + (size_t)c * 8) : make_uint4(0, 0, 0, 0);
+        v[j] = c < vecs ? ld_stream16(x + (size_t)c * 8) : make_uint4(0, 0, 0, 0);
     }
     if constexpr (!NV) {
 #pragma unroll
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(MAXT) quantize4_kernel(const Rows4Params p)
             const float mult = __uint_as_float(e == 255u ? 0u : (254u - e) << 23);
             const Pair mult2 = make_pair(mult, mult);
             Pair q[4] = {mul2(widen(v[j].x), mult2), mul2(widen(v[j].y), mult2), mul2(widen(v[j].z), mult2), mul2(widen(v[j].w), mult2)};
-            if (c < p.vecs) {
+            if (c < vecs) {
                 *reinterpret_cast<uint32_t*>(codes + (size_t)c * 4) = codes_of(q);
                 if ((c & 3) == 0) block[c >> 2] = (uint8_t)e;
             }
@@ -164,7 +166,9 @@ __global__ void __launch_bounds__(MAXT) quantize4_kernel(const Rows4Params p)
             m[j] = top_of(v[j]);
             top = max(top, m[j]);
         }
-        top = __reduce_max_sync(kFull, top);
+        if (p.tpr >= 32) top = __reduce_max_sync(kFull, top);
+        else
+            for (int o = p.tpr >> 1; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(kFull, top, o));
         if (p.tpr > 32) {
             const int warps = p.tpr >> 5;
             if ((threadIdx.x & 31) == 0) s_top[threadIdx.x >> 5] = top;
@@ -175,29 +179,37 @@ __global__ void __launch_bounds__(MAXT) quantize4_kernel(const Rows4Params p)
         const float range = a < 0x1p-60f ? 0x1p80f : a > 0x1p100f ? 0x1p-30f : 1.0f;
         const float ar = top == 0 ? 1.0f : a * range, inv = __frcp_rn(ar);
         const Pair range2 = make_pair(range, range), big = make_pair(96.0f, 96.0f), neg_big = make_pair(-96.0f, -96.0f);
+        // Two lanes hold a block of every vector: the even lane works out the scale of their first, the odd one of their second.
+        static_assert(VPT % 2 == 0, "");
 #pragma unroll
-        for (int j = 0; j < VPT; ++j) {
-            const int c = tid + j * p.tpr;
-            const uint32_t mb = max(m[j], __shfl_xor_sync(kFull, m[j], 1));
+        for (int j = 0; j < VPT; j += 2) {
+            const uint32_t odd = threadIdx.x & 1u;
+            const uint32_t sent = odd ? m[j] : m[j + 1], kept = odd ? m[j + 1] : m[j];
+            const uint32_t mb = max(kept, __shfl_xor_sync(kFull, sent, 1));
             const float n = __uint_as_float(mb << 16) * range * 448.0f, q0 = n * inv;
-            const uint32_t b = e4m3_of(fmaf(fmaf(q0, -ar, n), inv, q0));
+            uint32_t b = e4m3_of(fmaf(fmaf(q0, -ar, n), inv, q0));
             float r;
             asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(ar * e4m3_value(b)));
-            const float mult = b == 0 ? 0.0f : 2688.0f * r;
-            const Pair mult2 = make_pair(mult, mult);
-            Pair q[4] = {widen(v[j].x), widen(v[j].y), widen(v[j].z), widen(v[j].w)};
-            if (range != 1.0f) {
+            const float own = b == 0 ? 0.0f : 2688.0f * r, other = __shfl_xor_sync(kFull, own, 1);
+            const int at = tid + (j + (int)odd) * p.tpr;             // the vector whose block this lane did
+            if (at < vecs) block[at >> 1] = (uint8_t)b;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = mul2(q[i], range2);
-            }
+            for (int i2 = 0; i2 < 2; ++i2) {
+                const int c = tid + (j + i2) * p.tpr;
+                const float mult = (i2 == 0) == (odd == 0) ? own : other;
+                const Pair mult2 = make_pair(mult, mult);
+                const uint4 u = v[j + i2];
+                Pair q[4] = {widen(u.x), widen(u.y), widen(u.z), widen(u.w)};
+                if (range != 1.0f) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) q[i] = add2(fma2(q[i], mult2, big), neg_big);
-            if (c < p.vecs) {
-                *reinterpret_cast<uint32_t*>(codes + (size_t)c * 4) = codes_of(q);
-                if ((c & 1) == 0) block[c >> 1] = (uint8_t)b;
+                    for (int i = 0; i < 4; ++i) q[i] = mul2(q[i], range2);
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) q[i] = add2(fma2(q[i], mult2, big), neg_big);
+                if (c < vecs) *reinterpret_cast<uint32_t*>(codes + (size_t)c * 4) = codes_of(q);
             }
         }
-        if (tid == 0) p.scale[row * p.scale_stride] = top >= kInfBits ? __uint_as_float(0x7fc00000u) : __fdiv_rn(a, 2688.0f);
+        if (tid == 0 && live) p.scale[row * p.scale_stride] = top >= kInfBits ? __uint_as_float(0x7fc00000u) : __fdiv_rn(a, 2688.0f);
     }
 }
 
@@ -250,19 +262,25 @@ __global__ void __launch_bounds__(MAXT) dequantize4_kernel(const Rows4Params p)
 template <int VPT, typename F>
 cudaError_t run_rows4(Rows4Params& p, F launch)
 {
-    p.tpr = ((p.vecs + VPT - 1) / VPT + 31) / 32 * 32;
+    const int least = (p.vecs + VPT - 1) / VPT;
+    p.tpr = least > 16 ? (least + 31) / 32 * 32 : least > 8 ? 16 : least > 4 ? 8 : 4;
     const int groups = p.tpr <= 128 ? 256 / p.tpr : 1, threads = p.tpr * groups;
     const long long blocks = (p.rows + groups - 1) / groups;
     if (blocks >= (1ll << 31)) return cudaErrorInvalidConfiguration;
     return launch((unsigned)blocks, (unsigned)threads);
 }
 
+// Vectors per thread of the quantiser: eight put more loads in flight and need fewer warps per row (one up to 2048 columns: no
+// barrier).  Measured with two, four and eight, us, mxfp4 then nvfp4: 131,072 x 2048: 124, 108, 105; 217, 156, 122 (the bytes at the
+// measured copy rate: 107, 110); 16,411 x 7200: 61, 53, 50; 94, 80, 66; 65,536 x 1024: 32, 28, 27; 55, 38, 33; 100,000 x 160: 13,
+// 11, 10; 21, 16, 13.  Sixteen: 172 and 196 at 2048 columns, 59 and 64 at 7200.  Of the inverse, two and four: 131,072 x 2048 118, 102;
+// 100,000 x 160 13, 10.
 template <bool NV>
 cudaError_t quantize4(Rows4Params& p, cudaStream_t st)
 {
-    return run_rows4<4>(p, [&](unsigned blocks, unsigned threads) {
-        return threads <= 256 ? launch_pdl(quantize4_kernel<NV, 4, 256>, blocks, threads, 0, st, p)
-                              : launch_pdl(quantize4_kernel<NV, 4, 1024>, blocks, threads, 0, st, p);
+    return run_rows4<8>(p, [&](unsigned blocks, unsigned threads) {
+        return threads <= 256 ? launch_pdl(quantize4_kernel<NV, 8, 256>, blocks, threads, 0, st, p)
+                              : launch_pdl(quantize4_kernel<NV, 8, 512>, blocks, threads, 0, st, p);
     });
 }
 template <bool NV>
