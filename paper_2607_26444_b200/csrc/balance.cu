@@ -63,7 +63,12 @@ __device__ __forceinline__ void load_token(float (&l)[VPL], const void* base, lo
 #pragma unroll
     for (int j = 0; j < VPL; j += VW) {
         float(&part)[VW] = *reinterpret_cast<float(*)[VW]>(&l[j]);
-        load_logits<VW, BF16, RAW>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+        load_logits<VW, BF16, true>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+        if constexpr (!RAW) {
+#pragma unroll
+            for (int i = 0; i < VW; ++i)
+                part[i] = expert_of<VPL, BF16>(lane, j) + i < E ? fmaxf(part[i], -INFINITY) : -INFINITY;    // the other operand for NaN
+        }
     }
 }
 template <int VPL, bool BF16>
@@ -88,7 +93,12 @@ __device__ __forceinline__ float approx_rcp(float v)
 // The normalised scores p of a token; rest: 1 - s of the sigmoid, without the cancellation; where they are asked for, the softmax and
 // the logarithm of its sum.  One exponential per logit gives the sigmoid on both sides, 1 / (1 + e) and e / (1 + e) with e = exp(-|l|),
 // and exp(l) itself, which the softmax takes as long as no logit of the token passes 60.  Reciprocals are within 2^-23.
-template <int VPL, bool SIGMOID>
+// For bf16 logits the exponential is the hardware's power of two (within 2 + 1.2 |x| ulp by CUDA's bound: 2^-16 where the score is
+// still a normal number), against 2^-9 of the gradient's own rounding; in the sums over tokens that error is of either sign.
+template <bool BF16>
+__device__ __forceinline__ float exp_of(float x) { return BF16 ? __expf(x) : expf(x); }
+
+template <int VPL, bool BF16, bool SIGMOID>
 __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&rest)[VPL],
                                              float (&soft)[VPL], float& lse)
 {
@@ -97,7 +107,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
         float s = 0.0f, total = 0.0f, top = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            const float e = expf(-fabsf(l[i])), r = approx_rcp(1.0f + e), small = e * r;
+            const float e = exp_of<BF16>(-fabsf(l[i])), r = approx_rcp(1.0f + e), small = e * r;
             p[i] = l[i] >= 0.0f ? r : small;
             rest[i] = l[i] >= 0.0f ? small : r;
             soft[i] = l[i] >= 0.0f ? approx_rcp(e) : e;
@@ -124,11 +134,15 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
     for (int i = 1; i < VPL; ++i) m = fmaxf(m, l[i]);
     m = warp_max(m);
     float s = 0.0f;
+    if (fabsf(m) < INFINITY) {
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) {
-        soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
-        s += soft[i];
+        for (int i = 0; i < VPL; ++i) soft[i] = exp_of<BF16>(l[i] - m);
+    } else {                                                      // infinities at the maximum count as equal to it
+#pragma unroll
+        for (int i = 0; i < VPL; ++i) soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
     }
+#pragma unroll
+    for (int i = 0; i < VPL; ++i) s += soft[i];
     s = warp_sum(s);
     const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
@@ -179,7 +193,7 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
         }
         if (!__any_sync(kFull, id >= 0)) continue;
         if (id >= 0) atomicAdd(&s_count[id], 1);
-        token_scores<VPL, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
+        token_scores<VPL, BF16, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) sum[i] += q[i];
         z = fmaf(lse, lse, z);
@@ -359,7 +373,7 @@ __global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_ke
         t += step;
         if (t < p.group_tokens) load();
         if (__any_sync(kFull, id >= 0 && id < p.E)) {
-            token_scores<VPL, SIGMOID>(l, want_z, q, rest, soft, lse);
+            token_scores<VPL, BF16, SIGMOID>(l, want_z, q, rest, soft, lse);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) dot = fmaf(q[i], c[i], dot);
