@@ -1,13 +1,18 @@
-"""One feed-forward layer of a mixture of experts on one GPU, forward pass, experts in 8 bits:
+"""One feed-forward layer of a mixture of experts on one GPU, forward pass, experts in 8 or in 4 bits:
 
     residual addition + RMS norm -> router -> routing layout -> dispatch -> gate and up products -> silu(gate) * up
-    -> rows to 8 bits -> down product -> gate-weighted combine
+    -> rows to 8 (4) bits -> down product -> gate-weighted combine
 
-The hidden states leave the norm twice: in bf16 for the router, and as 8-bit rows that carry their scale, which dispatch
-moves (half the bytes of bf16).  The receive buffer is what the experts' products read; nothing is copied in between, and no
-step waits for the host.
+In 8 bits the hidden states leave the norm twice: in bf16 for the router, and as 8-bit rows that carry their scale, which
+dispatch moves (half the bytes of bf16).  In 4 bits (mxfp4, nvfp4) the quantiser makes the rows that dispatch moves, a
+quarter of the bytes, with their block scales.  The receive buffer is what the experts' products read; nothing is copied
+in between, and no step waits for the host.
 
-    python examples/moe_layer.py [--tokens 128] [--hidden 1024] [--inner 512] [--experts 32] [--topk 4] [--kind int8|e4m3]
+balance() adds what training asks of the router: the balance loss of the batch, the counts per expert, and the gradient of
+the logits from the loss and from the gate weights together.
+
+    python examples/moe_layer.py [--tokens 128] [--hidden 1024] [--inner 512] [--experts 32] [--topk 4]
+                                 [--kind int8|e4m3|mxfp4|nvfp4]
 """
 import argparse
 import os
@@ -19,6 +24,7 @@ sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 from paper_2607_26444_b200 import binding as B  # noqa: E402
 
 CODES = {"int8": torch.int8, "e4m3": torch.float8_e4m3fn}
+ROWS4 = {"mxfp4": B.STRATA_MXF4_ROW, "nvfp4": B.STRATA_NVF4_ROW}
 
 
 def to_codes(weight, kind):
@@ -38,44 +44,78 @@ class MoELayer:
 
         def normal(*shape):
             return torch.randn(shape, generator=g, device=device)
-        self.ctx = B.MoEContext(R, T, hidden, experts, topk, dispatch_dtype=B.STRATA_Q8_ROW, allow_unrouted=True)
+        self.kind, self.four = kind, kind in ROWS4
+        self.ctx = B.MoEContext(R, T, hidden, experts, topk, dispatch_dtype=ROWS4.get(kind, B.STRATA_Q8_ROW),
+                                allow_unrouted=True)
         self.norm_weight = 1.0 + 0.1 * normal(hidden)
         self.router = (normal(experts, hidden) / hidden ** 0.5).to(torch.bfloat16)
         self.bias = 0.01 * normal(experts)
         self.gate_up = normal(experts, 2 * inner, hidden) / hidden ** 0.5
         self.down = normal(experts, hidden, inner) / inner ** 0.5
-        self.w1, self.s1 = to_codes(self.gate_up, kind)
-        self.w2, self.s2 = to_codes(self.down, kind)
+        if self.four:
+            self.w1, self.w2 = self.to_rows4(self.gate_up), self.to_rows4(self.down)
+        else:
+            self.w1, self.s1 = to_codes(self.gate_up, kind)
+            self.w2, self.s2 = to_codes(self.down, kind)
         self.params = B.make_route("sigmoid", renormalise=True, scale=1.0, n_group=4, topk_group=2, group_score="top2")
         rows, bf = self.ctx.recv_rows, dict(dtype=torch.bfloat16, device=device)
         self.h, self.y, self.out = (torch.empty((R, T, hidden), **bf) for _ in range(3))
-        self.sent = torch.zeros((R, T, hidden + B.STRATA_Q8_TRAILER), dtype=torch.uint8, device=device)
-        self.recv = torch.zeros((rows, hidden + B.STRATA_Q8_TRAILER), dtype=torch.uint8, device=device)
+        row_bytes = B.row4_bytes(hidden, kind) if self.four else hidden + B.STRATA_Q8_TRAILER
+        self.sent = torch.zeros((R, T, row_bytes), dtype=torch.uint8, device=device)
+        self.recv = torch.zeros((rows, row_bytes), dtype=torch.uint8, device=device)
         self.ctx.register(self.recv)
         self.ids = torch.empty((R, T, topk), dtype=torch.int32, device=device)
         self.gate = torch.empty((R, T, topk), dtype=torch.float32, device=device)
         self.mid = torch.empty((rows, inner), **bf)
-        self.mid_q = torch.empty((rows, inner), dtype=CODES[kind], device=device)
-        self.mid_scale = torch.empty(rows, dtype=torch.float32, device=device)
+        if self.four:
+            self.sent4, self.recv4 = B.q4_rows(self.sent, hidden, kind), B.q4_rows(self.recv, hidden, kind)
+            self.mid4 = B.empty_rows4((rows,), inner, kind, device)
+        else:
+            self.mid_q = torch.empty((rows, inner), dtype=CODES[kind], device=device)
+            self.mid_scale = torch.empty(rows, dtype=torch.float32, device=device)
         self.back = torch.empty((rows, hidden), **bf)
         self.lay = self.ctx.new_layout()
-        self.kind = kind
+        self.balance_params = B.make_balance("sigmoid", weight=0.01, z_weight=0.001, per_rank=True)
+        self.stats = self.ctx.balance_stats(self.balance_params)
+        self.loss = torch.empty(2, dtype=torch.float32, device=device)
+
+    def to_rows4(self, weight):
+        """4-bit weights [E, channels, inner], made once when the weights are loaded."""
+        q = B.empty_rows4(weight.shape[:-1], weight.shape[-1], self.kind, weight.device)
+        self.ctx.quantize_rows4(weight.to(torch.bfloat16), q)
+        return q
 
     def forward(self, x, residual):
         """x, residual: bf16 [R, T, hidden].  Returns the experts' combined output; the new residual is self.h."""
         ctx = self.ctx
-        q, q_scale = B.q8_rows(self.sent, CODES[self.kind])
+        q, q_scale = (None, None) if self.four else B.q8_rows(self.sent, CODES[self.kind])
         ctx.norm(x, self.norm_weight, 1e-6, out=self.y, residual=residual, residual_out=self.h, q=q, q_scale=q_scale)
-        logits = torch.matmul(self.y, self.router.t())
-        ctx.route(self.params, logits, self.ids, self.gate, bias=self.bias)
+        if self.four:
+            ctx.quantize_rows4(self.y, self.sent4)
+        self.logits = torch.matmul(self.y, self.router.t())
+        ctx.route(self.params, self.logits, self.ids, self.gate, bias=self.bias)
         ctx.layout(self.ids, self.lay)
         ctx.dispatch(self.lay, self.sent, self.recv)
-        a, a_scale = B.q8_rows(self.recv, CODES[self.kind])
-        ctx.expert_matmul(self.lay, a, a_scale, self.w1, self.s1, self.mid, gated=True)
-        ctx.quantize_rows(self.mid, self.mid_q, self.mid_scale, layout=self.lay)
-        ctx.expert_matmul(self.lay, self.mid_q, self.mid_scale, self.w2, self.s2, self.back)
+        if self.four:
+            ctx.expert_matmul4(self.lay, self.recv4, self.w1, self.mid, gated=True)
+            ctx.quantize_rows4(self.mid, self.mid4, layout=self.lay)
+            ctx.expert_matmul4(self.lay, self.mid4, self.w2, self.back)
+        else:
+            a, a_scale = B.q8_rows(self.recv, CODES[self.kind])
+            ctx.expert_matmul(self.lay, a, a_scale, self.w1, self.s1, self.mid, gated=True)
+            ctx.quantize_rows(self.mid, self.mid_q, self.mid_scale, layout=self.lay)
+            ctx.expert_matmul(self.lay, self.mid_q, self.mid_scale, self.w2, self.s2, self.back)
         ctx.combine(self.lay, self.back, self.gate, self.out)
         return self.out
+
+    def balance(self, dgate):
+        """After forward: the losses (self.loss), the counts (self.stats.count) and the gradient of the logits, from the
+        losses and from the gradient of the gate weights together."""
+        dlogits = torch.empty_like(self.logits)
+        self.ctx.route_grad(self.params, self.logits, self.ids, dgate, dlogits)
+        self.ctx.balance_loss(self.balance_params, self.logits, self.ids, self.loss, self.stats)
+        self.ctx.balance_grad(self.balance_params, self.logits, self.ids, self.stats, dlogits, add=dlogits)
+        return dlogits
 
     def reference(self, x, residual):
         """The same layer in fp32 from the unquantised weights, with the ids that the router chose."""
@@ -96,7 +136,7 @@ def main(argv=None):
     ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
     for name, default in (("ranks", 2), ("tokens", 128), ("hidden", 1024), ("inner", 512), ("experts", 32), ("topk", 4), ("steps", 20)):
         ap.add_argument(f"--{name}", type=int, default=default)
-    ap.add_argument("--kind", choices=list(CODES), default="int8")
+    ap.add_argument("--kind", choices=[*CODES, *ROWS4], default="int8")
     a = ap.parse_args(argv)
     layer = MoELayer(a.ranks, a.tokens, a.hidden, a.inner, a.experts, a.topk, a.kind)
     x, residual = (torch.randn((a.ranks, a.tokens, a.hidden), device="cuda:0").to(torch.bfloat16) for _ in range(2))

@@ -543,6 +543,8 @@ def _strides(t):
     cols = t.size(-1)
     if t.is_contiguous():
         return (t.numel() // cols if cols else 0), cols, cols
+    if t.dim() == 2 and t.stride(1) == 1:
+        return t.size(0), cols, (t.stride(0) if t.size(0) > 1 else cols)
     stride, rows = cols, 1
     for d in range(t.dim() - 2, -1, -1):
         if t.shape[d] > 1:
@@ -649,28 +651,50 @@ def _kind4(kind: str) -> int:
     return _KINDS4[kind]
 
 
+class _Blocks4(dict):
+    """(type, values per scale) by the torch dtype of block scales, filled on first use."""
+
+    def __missing__(self, dtype):
+        import torch
+        self.update({torch.float8_e8m0fnu: (STRATA_T_MXF4, 32), torch.float8_e4m3fn: (STRATA_T_NVF4, 16)})
+        _codes4.update((torch.uint8, torch.float4_e2m1fn_x2))
+        if dtype not in self:
+            raise ValueError(f"block scales are torch.float8_e8m0fnu or torch.float8_e4m3fn, not {dtype}")
+        return self[dtype]
+
+
+_blocks4 = _Blocks4()
+_codes4 = set()
+
+
 class Rows4:
     """Rows in 4 bits: codes uint8 (or torch.float4_e2m1fn_x2) [.., cols / 2], two to a byte and the first in its low half;
     block scales [.., cols / 32] of torch.float8_e8m0fnu (mxfp4) or [.., cols / 16] of torch.float8_e4m3fn (nvfp4); scales
     of the rows fp32 [..] or None (1).  Rows of codes and of block scales start on 16 bytes."""
 
     def __init__(self, codes, block, scale=None):
-        import torch
-        if codes.dtype != torch.uint8 and codes.dtype != torch.float4_e2m1fn_x2:
+        self.type, per = _blocks4[block.dtype]
+        if codes.dtype not in _codes4:
             raise ValueError(f"4-bit codes are torch.uint8 or torch.float4_e2m1fn_x2, not {codes.dtype}")
-        if block.dtype != torch.float8_e8m0fnu and block.dtype != torch.float8_e4m3fn:
-            raise ValueError(f"block scales are torch.float8_e8m0fnu or torch.float8_e4m3fn, not {block.dtype}")
-        self.type = STRATA_T_MXF4 if block.dtype == torch.float8_e8m0fnu else STRATA_T_NVF4
         self.codes, self.block, self.scale = codes, block, scale
-        rows, half, code_stride = _strides(codes)
-        self.rows, self.cols = rows, 2 * half
-        if self.cols % 32:
+        if codes.is_contiguous():
+            code_stride = codes.size(-1)
+            rows = codes.numel() // code_stride if code_stride else 0
+            cols = 2 * code_stride
+        else:
+            rows, half, code_stride = _strides(codes)
+            cols = 2 * half
+        if cols % 32:
             raise ValueError("4-bit rows have a multiple of 32 columns")
-        block_stride = _stride(block, rows, self.cols // _BLOCK4[self.type], "block scales")
+        block_stride = _stride(block, rows, cols // per, "block scales")
         if rows == 1:                                     # nothing is read between rows that are not there
             code_stride, block_stride = -(-code_stride // 16) * 16, -(-block_stride // 16) * 16
-        self.c = strata_rows4(codes.data_ptr(), block.data_ptr(), None if scale is None else scale.data_ptr(), code_stride,
-                              block_stride, 0 if scale is None else _scale_stride(scale, rows))
+        self.rows, self.cols = rows, cols
+        if scale is None:
+            self.c = strata_rows4(codes.data_ptr(), block.data_ptr(), None, code_stride, block_stride, 0)
+        else:
+            self.c = strata_rows4(codes.data_ptr(), block.data_ptr(), scale.data_ptr(), code_stride, block_stride,
+                                  _scale_stride(scale, rows))
 
 
 def empty_rows4(shape, cols: int, kind: str, device="cuda") -> Rows4:

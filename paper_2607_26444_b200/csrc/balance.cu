@@ -23,7 +23,8 @@ BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params&
     BalanceGeom g;
     g.groups = b.per_rank ? s.R : 1;
     g.group_tokens = b.per_rank ? s.T : (long long)s.R * s.T;
-    g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + kWarps - 1) / kWarps);
+    // four tokens per warp, at least: more slices are more to add up
+    g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + 4 * kWarps - 1) / (4 * kWarps));
     g.col_blocks = (s.E + kSumCols - 1) / kSumCols;
     return g;
 }
@@ -32,8 +33,8 @@ struct BalanceParams {
     const void* logits;
     long long stride, group_tokens;
     const int32_t* ids;
-    float* part_p;         // [groups * slices, E]  sums of scores
-    int32_t* part_c;       // [groups * slices, E]  slots
+    float* part_p;         // [groups, E, slices]   sums of scores
+    int32_t* part_c;       // [groups, E, slices]   slots
     int32_t* part_n;       // [groups * slices]     tokens that take part
     float* part_z;         // [groups * slices]     sums of squares
     float* part_loss;      // [groups * col_blocks]
@@ -211,8 +212,9 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
         float a = 0.0f;
 #pragma unroll
         for (int w = 0; w < kWarps; ++w) a += s_sum[w * 32 * VPL + e];
-        p.part_p[(size_t)blockIdx.x * p.E + e] = a;
-        p.part_c[(size_t)blockIdx.x * p.E + e] = s_count[e];
+        const size_t to = ((size_t)group * p.E + e) * p.slices + slice;
+        p.part_p[to] = a;
+        p.part_c[to] = s_count[e];
     }
     if (threadIdx.x == 0) {
         float a = 0.0f;
@@ -242,12 +244,12 @@ __global__ void __launch_bounds__(kSumCols * 32) balance_sum_kernel(const Balanc
     const size_t first = (size_t)group * p.slices;
     float a = 0.0f;
     int c = 0, n = 0;
-    const int col = min(e, p.E - 1);
-#pragma unroll 4
+    const size_t from = ((size_t)group * p.E + min(e, p.E - 1)) * p.slices;
+#pragma unroll 10
     for (int i = lane; i < p.slices; i += 32) {
         n += p.part_n[first + i];
-        a += p.part_p[(first + i) * p.E + col];
-        c += p.part_c[(first + i) * p.E + col];
+        a += p.part_p[from + i];
+        c += p.part_c[from + i];
     }
     n = warp_count(n);
     c = warp_count(c);

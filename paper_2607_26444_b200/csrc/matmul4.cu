@@ -32,7 +32,6 @@ constexpr int kBlock = kM * kKBytes;    // codes of one 128-row block of weights
 constexpr int kChunk = 16;              // scale bytes of a row that TMEM takes at a time: 4 words
 constexpr int kChunks = 2;              // chunks of scales in TMEM
 constexpr int kMaxGroups = 3;           // groups of scales in shared memory, at most
-constexpr int kScaleWarps = 4;
 constexpr int kBoxRows = 32;            // rows of a TMA box of the N operand where it is not the whole height of a tile
 
 // A tile of a CTA is MB blocks of 128 weight rows by up to BN rows of the N operand, of which it holds BN / CG.
@@ -58,7 +57,10 @@ struct Tile4 {
     static constexpr int used_cols = acc_cols + scale_cols;
     static constexpr int tmem_cols = used_cols <= 128 ? 128 : used_cols <= 256 ? 256 : 512;
     static constexpr int epi_warps = BN > 64 ? 8 : 4;               // a multiple of four: warp & 3 selects the TMEM lanes
-    static constexpr int load_warp = kScaleWarps + epi_warps, mma_warp = load_warp + 2, deal_warp = load_warp + 3;
+    // Warps that bring scales to TMEM, in sets of four that take the chunks in turn: one set works about 550 cycles on a chunk, which
+    // at 16 values per scale is one span, 400 cycles of matrix instructions.
+    static constexpr int scale_warps = MB == 1 ? 8 : 4;
+    static constexpr int load_warp = scale_warps + epi_warps, mma_warp = load_warp + 2, deal_warp = load_warp + 3;
     static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
     static constexpr int stage_out = epi_warps * 1024;              // bytes: 32 rows of 16 channels or 16 of 32 of every warp
@@ -336,10 +338,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         }
         for (int g = 0; g < T::groups; ++g) {
             mbar_init(&tail->group_full[g], 2);
-            mbar_init(&tail->group_empty[g], kScaleWarps);
+            mbar_init(&tail->group_empty[g], T::scale_warps);
         }
         for (int c = 0; c < kChunks; ++c) {
-            mbar_init(&tail->chunk_full[c], CG * kScaleWarps);
+            mbar_init(&tail->chunk_full[c], CG * 4);
             mbar_init(&tail->chunk_empty[c], 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -348,7 +350,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
         }
         for (int c = 0; c < kClaims; ++c) {
             mbar_init(&tail->work_full[c], 1);
-            mbar_init(&tail->work_empty[c], 2 + (rank == 0 ? 1 : 0) + kScaleWarps + T::epi_warps);   // only the leader multiplies
+            mbar_init(&tail->work_empty[c], 2 + (rank == 0 ? 1 : 0) + T::scale_warps + T::epi_warps);   // only the leader multiplies
             mbar_init(&tail->claim_full[c], 1);
             mbar_init(&tail->claim_empty[c], 1);
         }
@@ -595,23 +597,27 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             }
             __syncwarp();
         }
-    } else if (warp < kScaleWarps) {                                 // scales to this warp's quarter of TMEM
+    } else if (warp < T::scale_warps) {                                 // scales to this warp's quarter of TMEM
         uint32_t git = 0, cit = 0;
         bool ok = true;
-        const uint32_t lanes = (uint32_t)(warp * 32) << 16;
+        const uint32_t lanes = (uint32_t)((warp & 3) * 32) << 16;
+        constexpr uint32_t kSets = T::scale_warps / 4;
+        const uint32_t set = (uint32_t)warp >> 2;
         Work w;
         uint4 vw[MB][4], va[T::a_cols / 4][4];
-        // the chunk that begins with span kb, from its group in shared memory
-        auto fetch = [&](int kb) {
+        // the chunk that begins with span kb, from its group in shared memory; `mine`: it is this set's
+        auto fetch = [&](int kb, bool mine) {
             const uint32_t g = git % T::groups;
             const int at = kb % T::per_group / T::per_chunk * kChunk;        // of the chunk in its group's rows
             if (at == 0 && !warp_wait(&tail->group_full[g], (git / T::groups) & 1, dead, p.status)) return false;
+            if (mine) {
 #pragma unroll
-            for (int b = 0; b < MB; ++b)
-                read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes, at, kM, lane, vw[b]);
+                for (int b = 0; b < MB; ++b)
+                    read_scales<T::group_bytes>(s_ws + g * T::ws_group + b * kM * T::group_bytes, at, kM, lane, vw[b]);
 #pragma unroll
-            for (int b = 0; b < T::a_cols / 4; ++b)
-                read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes, at, BN - b * kM, lane, va[b]);
+                for (int b = 0; b < T::a_cols / 4; ++b)
+                    read_scales<T::group_bytes>(s_as + g * T::as_group + b * kM * T::group_bytes, at, BN - b * kM, lane, va[b]);
+            }
             if (at == T::group_bytes - kChunk || kb + T::per_chunk >= p.k_spans) {
                 __syncwarp();
                 if (lane == 0) mbar_arrive(&tail->group_empty[g]);
@@ -620,8 +626,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             return true;
         };
         for (uint32_t use = 0; ok && next_tile(*tail, use, w, lane, dead, p.status); ++use) {
-            ok = fetch(0);
             for (int kb = 0; ok && kb < p.k_spans; kb += T::per_chunk, ++cit) {
+                const bool mine = cit % kSets == set;
+                ok = fetch(kb, mine);
+                if (!ok || !mine) continue;
                 const uint32_t c = cit % kChunks;
                 ok = warp_wait(&tail->chunk_empty[c], ((cit / kChunks) & 1) ^ 1, dead, p.status);
                 if (!ok) break;
@@ -652,11 +660,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                 tmem_fence_before();
                 __syncwarp();
                 if (lane == 0) arrive_leader<CG>(&tail->chunk_full[c]);
-                if (kb + T::per_chunk < p.k_spans) ok = fetch(kb + T::per_chunk);
             }
         }
     } else {
-        const int ew = warp - kScaleWarps, quad = warp & 3;          // TMEM lanes 32*quad .. of this warp
+        const int ew = warp - T::scale_warps, quad = warp & 3;          // TMEM lanes 32*quad .. of this warp
         const int col0 = (ew >> 2) * T::cols;                        // first column of this warp
         // A step: 32 columns of 16 channels, or 16 of 32; OB blocks of out per step and accumulators
         constexpr bool kTight = GATED && MB == 1;
