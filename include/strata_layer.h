@@ -251,7 +251,7 @@ typedef struct {                   /* device, what the gradient needs of the for
 } strata_balance_stats;
 
 /* logits, topk_ids as in strata_moe_route (logits may be any row-strided bf16 or float rows [R*T, E]); loss: device float
- * [2]; scratch: device, 16-byte aligned, of strata_moe_balance_scratch_bytes.  Needs a workspace.  Two launches. */
+ * [2]; scratch: device, 16-byte aligned, of strata_moe_balance_scratch_bytes.  Needs a workspace.  One launch for small batches, else two. */
 strata_status strata_moe_balance_scratch_bytes(strata_ctx *ctx, const strata_balance_params *params, size_t *bytes);
 strata_status strata_moe_balance_loss(strata_ctx *ctx, const strata_balance_params *params, const void *logits,
                                       int32_t logits_type, int64_t logits_stride, const int32_t *topk_ids, float *loss,

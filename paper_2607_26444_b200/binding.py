@@ -737,7 +737,7 @@ class BalanceStats:
         self.tokens = torch.empty(groups, dtype=torch.int32, device=device)
         self.prob = torch.empty((groups, E), dtype=torch.float32, device=device)
         self.scratch = torch.empty(scratch_bytes, dtype=torch.uint8, device=device)
-        self.groups = groups
+        self.groups, self.E = groups, E
         self.c = strata_balance_stats(self.count.data_ptr(), self.tokens.data_ptr(), self.prob.data_ptr())
 
 
@@ -1021,7 +1021,7 @@ class MoEContext:
         return BalanceStats(self.R if params.per_rank else 1, self.E, n, self.device)
 
     def _balance_stats(self, params: strata_balance_params, stats: BalanceStats):
-        if stats.groups != (self.R if params.per_rank else 1) or stats.count.size(1) != self.E:
+        if stats.groups != (self.R if params.per_rank else 1) or stats.E != self.E:
             raise ValueError("stats were made for other parameters")
         return stats.c
 

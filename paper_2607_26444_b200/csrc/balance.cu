@@ -45,6 +45,7 @@ struct BalanceParams {
     int* status;
     unsigned* ticket;
     int E, K, groups, slices, vec_ok;
+    int finish;            // the first kernel adds the slices up itself
     float weight, z_weight;
 };
 
@@ -155,6 +156,60 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
     }
 }
 
+__device__ __forceinline__ int warp_count(int v) { return __reduce_add_sync(kFull, v); }
+
+// The two losses from the groups' sum (`loss`, of this thread) and the blocks' squares, by a whole block; the ticket is returned.
+__device__ __forceinline__ void finish_losses(const BalanceParams& p, float loss)
+{
+    __shared__ float s_f[kWarps], s_z[kWarps];
+    __shared__ int s_alive[kWarps], s_total[kWarps];
+    const int t = (int)threadIdx.x, lane = t & 31, warp = t >> 5;
+    float z = 0.0f;
+    int alive = 0, total = 0;
+#pragma unroll 4
+    for (int i = t; i < p.groups * p.slices; i += kWarps * 32) z += __ldcg(p.part_z + i);
+    for (int i = t; i < p.groups; i += kWarps * 32) {
+        const int m = __ldcg(p.tokens + i);
+        alive += m > 0;
+        total += m;
+    }
+    loss = warp_sum(loss);
+    z = warp_sum(z);
+    alive = warp_count(alive);
+    total = warp_count(total);
+    if (lane == 0) {
+        s_f[warp] = loss;
+        s_z[warp] = z;
+        s_alive[warp] = alive;
+        s_total[warp] = total;
+    }
+    __syncthreads();
+    if (t != 0) return;
+    for (int w = 1; w < kWarps; ++w) {
+        loss += s_f[w];
+        z += s_z[w];
+        alive += s_alive[w];
+        total += s_total[w];
+    }
+    p.loss[0] = alive > 0 ? p.weight * __fdiv_rn(loss, (float)alive) : 0.0f;
+    p.loss[1] = total > 0 && p.z_weight != 0.0f ? p.z_weight * __fdiv_rn(z, (float)total) : 0.0f;
+    *p.ticket = 0;
+}
+// Whether this block is the last of the grid to come here; what the others wrote before is visible to it.
+__device__ __forceinline__ bool last_block(const BalanceParams& p)
+{
+    __shared__ bool s_last;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
+    }
+    __syncthreads();
+    if (s_last) __threadfence();
+    return s_last;
+}
+static_assert(kSumCols == kWarps, "both kernels finish with blocks of as many warps");
+
 template <int VPL, bool BF16, bool SIGMOID>
 __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(const BalanceParams p)
 {
@@ -226,17 +281,36 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
         p.part_z[blockIdx.x] = a;
         p.part_n[blockIdx.x] = c;
     }
+    if (!p.finish) return;
+    // small batches: the last block adds the slices up, a thread per group and expert
+    __threadfence();
+    if (!last_block(p)) return;
+    float loss = 0.0f;
+    for (int i = (int)threadIdx.x; i < p.groups * p.E; i += kWarps * 32) {
+        const int g = i / p.E, e = i - g * p.E;
+        float a = 0.0f;
+        int c = 0, m = 0;
+        for (int s = 0; s < p.slices; ++s) {
+            a += __ldcg(p.part_p + (size_t)i * p.slices + s);
+            c += __ldcg(p.part_c + (size_t)i * p.slices + s);
+            m += __ldcg(p.part_n + g * p.slices + s);
+        }
+        const float prob = m > 0 ? __fdiv_rn(a, (float)m) : 0.0f;
+        p.prob[i] = prob;
+        p.count[i] = c;
+        if (e == 0) p.tokens[g] = m;
+        if (m > 0) loss += (float)c * prob * __fdiv_rn((float)p.E, (float)p.K * (float)m);
+    }
+    __threadfence();
+    __syncthreads();                                              // the tokens of the groups
+    finish_losses(p, loss);
 }
-
-__device__ __forceinline__ int warp_count(int v) { return __reduce_add_sync(kFull, v); }
 
 // Slices to groups: 8 experts of one group per block, one per warp, whose lanes add every 32nd slice.  The block that draws the
 // last ticket adds up the losses.
 __global__ void __launch_bounds__(kSumCols * 32) balance_sum_kernel(const BalanceParams p, int col_blocks)
 {
-    __shared__ float s_f[kSumCols], s_z[kSumCols];
-    __shared__ int s_alive[kSumCols], s_total[kSumCols];
-    __shared__ bool s_last;
+    __shared__ float s_f[kSumCols];
     const int t = (int)threadIdx.x, lane = t & 31, warp = t >> 5;
     const int group = (int)blockIdx.x / col_blocks, e = ((int)blockIdx.x - group * col_blocks) * kSumCols + warp;
     griddep_wait();
@@ -268,44 +342,12 @@ __global__ void __launch_bounds__(kSumCols * 32) balance_sum_kernel(const Balanc
         for (int w = 0; w < kSumCols; ++w) part += s_f[w];
         p.part_loss[blockIdx.x] = part;
         if (blockIdx.x % (unsigned)col_blocks == 0) p.tokens[group] = n;
-        __threadfence();
-        s_last = atomicAdd(p.ticket, 1u) == gridDim.x - 1;
     }
-    __syncthreads();
-    if (!s_last) return;
-    __threadfence();
-    float loss = 0.0f, z = 0.0f;
-    int alive = 0, total = 0;
+    if (!last_block(p)) return;
+    float loss = 0.0f;
 #pragma unroll 4
     for (int i = t; i < (int)gridDim.x; i += kSumCols * 32) loss += __ldcg(p.part_loss + i);
-#pragma unroll 4
-    for (int i = t; i < p.groups * p.slices; i += kSumCols * 32) z += p.part_z[i];
-    for (int i = t; i < p.groups; i += kSumCols * 32) {
-        const int m = __ldcg(p.tokens + i);
-        alive += m > 0;
-        total += m;
-    }
-    loss = warp_sum(loss);
-    z = warp_sum(z);
-    alive = warp_count(alive);
-    total = warp_count(total);
-    if (lane == 0) {
-        s_f[warp] = loss;
-        s_z[warp] = z;
-        s_alive[warp] = alive;
-        s_total[warp] = total;
-    }
-    __syncthreads();
-    if (t != 0) return;
-    for (int w = 1; w < kSumCols; ++w) {
-        loss += s_f[w];
-        z += s_z[w];
-        alive += s_alive[w];
-        total += s_total[w];
-    }
-    p.loss[0] = alive > 0 ? p.weight * __fdiv_rn(loss, (float)alive) : 0.0f;
-    p.loss[1] = total > 0 && p.z_weight != 0.0f ? p.z_weight * __fdiv_rn(z, (float)total) : 0.0f;
-    *p.ticket = 0;
+    finish_losses(p, loss);
 }
 
 struct BalanceGradParams {
@@ -469,9 +511,11 @@ cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_
     p.vec_ok = rows_on_16(logits, stride, type);
     p.weight = b.weight;
     p.z_weight = b.z_weight;
+    // A second launch costs its 2 us on the host and the GPU alike; a thread adds a slice in half a microsecond at worst.
+    p.finish = blocks * s.E <= 4096;
     *n_launches = 1;
     const cudaError_t err = first_pass(s, p, type == STRATA_T_BF16, b.score == STRATA_SCORE_SIGMOID, (unsigned)blocks, st);
-    if (err != cudaSuccess) return err;
+    if (err != cudaSuccess || p.finish) return err;
     *n_launches = 2;
     return launch_pdl(balance_sum_kernel, (unsigned)(g.groups * g.col_blocks), kSumCols * 32, 0, st, p, g.col_blocks);
 }
