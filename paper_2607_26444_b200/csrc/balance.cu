@@ -65,7 +65,16 @@ __device__ __forceinline__ void load_token(float (&l)[VPL], const void* base, lo
 #pragma unroll
     for (int j = 0; j < VPL; j += VW) {
         float(&part)[VW] = *reinterpret_cast<float(*)[VW]>(&l[j]);
-        load_logits<VW, BF16, true>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+        const int e0 = expert_of<VPL, BF16>(lane, j);
+        if (BF16 && VW == 4 && vec_ok && e0 + VW <= E) {          // rows too short for 16 bytes a lane
+            const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row_off + e0);
+            part[0] = __uint_as_float(v.x << 16);
+            part[1 % VW] = __uint_as_float(v.x & 0xffff0000u);
+            part[2 % VW] = __uint_as_float(v.y << 16);
+            part[3 % VW] = __uint_as_float(v.y & 0xffff0000u);
+        } else {
+            load_logits<VW, BF16, true>(part, base, row_off, e0, E, vec_ok);
+        }
         if constexpr (!RAW) {
 #pragma unroll
             for (int i = 0; i < VW; ++i)
@@ -80,7 +89,11 @@ __device__ __forceinline__ void store_token(const float (&g)[VPL], void* base, l
 #pragma unroll
     for (int j = 0; j < VPL; j += VW) {
         const float(&part)[VW] = *reinterpret_cast<const float(*)[VW]>(&g[j]);
-        store_row<VW, BF16>(part, base, row_off, expert_of<VPL, BF16>(lane, j), E, vec_ok);
+        const int e0 = expert_of<VPL, BF16>(lane, j);
+        if (BF16 && VW == 4 && vec_ok && e0 + VW <= E)
+            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + row_off + e0) =
+                make_uint2(pack_bf16x2(part[0], part[1 % VW]), pack_bf16x2(part[2 % VW], part[3 % VW]));
+        else store_row<VW, BF16>(part, base, row_off, e0, E, vec_ok);
     }
 }
 
