@@ -48,7 +48,7 @@ struct Tile4 {
     static constexpr int per_group = group_bytes / (NV ? 16 : 8);   // spans that a group serves
     static constexpr int per_chunk = kChunk / (NV ? 16 : 8);
     static constexpr int words = 4 / per_chunk;                     // scale words of a row that a span uses
-    static constexpr int groups = NV && BN > 96 ? 3 : 2;            // as many spans as the ring of codes, at least
+    static constexpr int groups = NV && BN > 96 && MB == 1 ? 3 : 2;            // as many spans as the ring of codes, at least
     static constexpr int ws_group = MB * kM * group_bytes, as_group = BN * group_bytes;
     static constexpr int a_cols = (BN / 32 + 3) / 4 * 4;            // TMEM columns of a word of the rows' scales
     static constexpr int chunk_cols = 4 * (MB * 4 + a_cols), scale_cols = kChunks * chunk_cols;
@@ -64,7 +64,8 @@ struct Tile4 {
     static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
     static constexpr int stage_out = epi_warps * 1024;              // bytes: 32 rows of 16 channels or 16 of 32 of every warp
-    static constexpr int ring = 202 * 1024 - groups * (ws_group + as_group);
+    static constexpr int max_experts = CG * MB == 4 ? 512 : kMaxExperts;     // what their tables leave of shared memory
+    static constexpr int ring = (CG * MB == 4 ? 204 : 202) * 1024 - groups * (ws_group + as_group);
     static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
     static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)groups * (ws_group + as_group);
     static_assert(used_cols <= 512 && stages >= 2 && cols % 16 == 0 && a_span % 1024 == 0 && own_rows % kBoxRows == 0 && per_group % spans == 0, "");
@@ -868,11 +869,11 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
 template <bool NV, int CG, int MB, int BN>
 cudaError_t configure4()
 {
-    static_assert(smem_bytes4<NV, CG, MB, BN>(kMaxExperts) <= 227 * 1024, "");
+    static_assert(smem_bytes4<NV, CG, MB, BN>(Tile4<NV, CG, MB, BN>::max_experts) <= 227 * 1024, "");
     const void* fns[2] = {(const void*)expert_matmul4_kernel<NV, true, CG, MB, BN>, (const void*)expert_matmul4_kernel<NV, false, CG, MB, BN>};
     for (const void* f : fns) {
         const cudaError_t e =
-            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes4<NV, CG, MB, BN>(kMaxExperts));
+            cudaFuncSetAttribute(f, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes4<NV, CG, MB, BN>(Tile4<NV, CG, MB, BN>::max_experts));
         if (e != cudaSuccess) return e;
     }
     return cudaSuccess;
@@ -883,6 +884,7 @@ cudaError_t configure4_all()
     cudaError_t e = configure4<NV, 1, 1, 64>();
     if (e == cudaSuccess) e = configure4<NV, 1, 2, 96>();
     if (e == cudaSuccess) e = configure4<NV, 2, 1, 192>();
+    if (e == cudaSuccess) e = configure4<NV, 2, 2, 192>();
     return e;
 }
 
@@ -892,7 +894,8 @@ cudaError_t pick4(int v, const strata_moe_shape& s, const strata_matmul4_args& a
     switch (v) {
         case 0: return run4<NV, 1, 1, 64>(s, a, p, n_sm, st);
         case 1: return run4<NV, 1, 2, 96>(s, a, p, n_sm, st);
-        default: return run4<NV, 2, 1, 192>(s, a, p, n_sm, st);
+        case 2: return run4<NV, 2, 1, 192>(s, a, p, n_sm, st);
+        default: return run4<NV, 2, 2, 192>(s, a, p, n_sm, st);
     }
 }
 
