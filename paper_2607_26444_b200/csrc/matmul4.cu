@@ -64,7 +64,7 @@ struct Tile4 {
     static constexpr int threads = 32 * (deal_warp + 1);
     static constexpr int cols = BN / (epi_warps / 4);               // columns of a tile that one epilogue warp reads
     static constexpr int stage_out = epi_warps * 1024;              // bytes: 32 rows of 16 channels or 16 of 32 of every warp
-    static constexpr int max_experts = CG * MB == 4 ? 512 : kMaxExperts;     // what their tables leave of shared memory
+    static constexpr int max_experts = CG * MB == 4 ? 512 : kMaxExperts;     // whose tables shared memory has room for
     static constexpr int ring = (CG * MB == 4 ? 204 : 202) * 1024 - groups * (ws_group + as_group);
     static constexpr int stages = ring / stage_bytes < 8 ? ring / stage_bytes : 8;
     static constexpr size_t data_bytes = (size_t)stages * stage_bytes + (size_t)groups * (ws_group + as_group);
@@ -930,33 +930,37 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     p.last_steps = (a.inner / 2 - (p.k_spans - 1) * kKBytes + kUmmaK - 1) / kUmmaK;
     p.channels = a.channels;
     p.out_vec = a.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
-    // Which tile: the shortest estimate of rounds * (spans * (c + n * filled) + f) over the GPU, where c + n is what one span of a full
-    // tile takes, n the part that grows with the rows in it, and f what a tile adds; at least the weights' way from HBM.  The
-    // constants were fitted to 65 measured shapes of each kind (8, 32 and 60 experts, 1 .. 2048 mean rows, inner 256 .. 7168, 512 ..
-    // 7168 channels, even and Zipf routing); the choice is on average 1.5 % above the best of the three (one tile for all: 3 to 37
-    // %), and 27 % at worst, where the call is a few microseconds.  At 7168 -> 4096 gated, 32 experts, mxfp4, us for <1,1,64>,
-    // <1,2,96>, <2,1,192>: one token 27, 25, 29; 32 rows each 86, 88, 88; 128 rows 153, 116, 96; 256 rows 276, 175, 152; 512 rows 502, 326, 230;
-    // nvfp4 681, 352, 296.  What the estimate does not see: rows spread around their mean, and slots that are masked or unrouted.
-    struct Cost { int cg, mb, bn; float c, n, f, hbm; };
-    static const Cost costs[2][3] = {
-        {{1, 1, 64, 0.08f, 0.19f, 0.86f, 1.19f}, {1, 2, 96, 0.23f, 0.29f, 0.94f, 1.02f}, {2, 1, 192, 0.06f, 0.27f, 1.15f, 1.18f}},
-        {{1, 1, 64, 0.06f, 0.31f, 1.13f, 1.33f}, {1, 2, 96, 0.22f, 0.35f, 1.28f, 1.07f}, {2, 1, 192, 0.11f, 0.34f, 1.45f, 1.33f}}};
+    // Which tile: the shortest estimate of rounds * (spans * (c + n * filled) + f + g * filled) over the GPU, where c + n is what one span
+    // of a full tile takes and f + g what a tile adds, n and g the parts that grow with the rows in it (g is the epilogue where the
+    // accumulators are not doubled); at least the weights' way from HBM.  The constants were fitted to 65 measured shapes of
+    // each kind (8, 32 and 60 experts, 1 .. 2048 mean rows, inner 256 .. 7168, 512 .. 7168 channels, even and Zipf routing); the choice is on average
+    // 1.9 % above the best of the four (one tile for all: 6 to 44 %), and 25 % at worst.  At 7168 -> 4096 gated, 32 experts,
+    // mxfp4, us for <1,1,64>, <1,2,96>, <2,1,192>, <2,2,192>: one token 27, 25, 28, 26; 32 rows each 86, 88, 88, 89; 128 rows 153, 117, 97, 100;
+    // 256 rows 276, 178, 155, 141; 512 rows 502, 338, 234, 217; nvfp4 700, 384, 291, 248; 2048 -> 7168, 512 rows, mxfp4 299, 196, 143, 157.
+    // What the estimate does not see: rows spread around their mean, and slots that are masked or unrouted.
+    struct Cost { int cg, mb, bn; float c, n, f, g, hbm; };
+    static const Cost costs[2][4] = {{{1, 1, 64, 0.03f, 0.28f, 0.84f, 0.0f, 1.15f}, {1, 2, 96, 0.29f, 0.29f, 0.82f, 0.0f, 1.00f},
+                                      {2, 1, 192, 0.12f, 0.25f, 1.17f, 0.10f, 1.17f}, {2, 2, 192, 0.26f, 0.39f, 1.24f, 2.36f, 1.17f}},
+                                     {{1, 1, 64, 0.12f, 0.28f, 0.88f, 0.31f, 1.39f}, {1, 2, 96, 0.33f, 0.29f, 1.04f, 0.49f, 1.06f},
+                                      {2, 1, 192, 0.25f, 0.20f, 1.12f, 1.09f, 1.23f}, {2, 2, 192, 0.35f, 0.35f, 1.26f, 3.24f, 1.23f}}};
     constexpr float kHbmBytesPerUs = 6.55e6f;
     const bool nv = a.type == STRATA_T_NVF4;
     const long long items = s.slot_capacity > 0 ? (long long)s.E * s.R * s.slot_capacity : (long long)s.R * s.T * s.K;
     const long long used = min(items, (long long)s.E), mean = (items + s.E - 1) / s.E;
     const float bytes_us = (float)used * (float)a.channels * (float)a.inner * (nv ? 0.5625f : 0.53125f) / kHbmBytesPerUs;
-    int v = 1;                                                       // the only one that does not take gate and up by eights
+    int v = 1;                                                       // one CTA alone, any number of channels and experts
     float least = 0.0f;
-    for (int i = 0; i < 3 && !(a.gated && a.channels % 16 != 0); ++i) {
+    for (int i = 0; i < 4; ++i) {
         const Cost& k = costs[nv][i];
-        if (k.cg > n_sm) continue;
+        if (a.gated && k.mb == 1 && a.channels % 16 != 0) continue;  // takes gate and up by eights
+        if (k.cg > n_sm || (k.cg * k.mb == 4 && s.E > Tile4<false, 2, 2, 192>::max_experts)) continue;
         const int per_tile = k.cg * k.mb * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1), teams = n_sm / k.cg;
-        const float tiles = (float)(used * ((mean + k.bn - 1) / k.bn) * ((wide + per_tile - 1) / per_tile));
+        const long long heights = (mean + k.bn - 1) / k.bn;
+        const float tiles = (float)(used * heights * ((wide + per_tile - 1) / per_tile));
         const float rounds = tiles > (float)teams ? tiles / (float)teams + 0.19f : 1.0f;
-        const float filled = (float)min(mean, (long long)k.bn) / (float)k.bn;
-        const float cost = max(rounds * ((float)p.k_spans * (k.c + k.n * filled) + k.f), bytes_us * k.hbm);
-        if (i == 0 || cost < least) {
+        const float filled = (float)mean / (float)(heights * k.bn);
+        const float cost = max(rounds * ((float)p.k_spans * (k.c + k.n * filled) + k.f + k.g * filled), bytes_us * k.hbm);
+        if (least == 0.0f || cost < least) {
             least = cost;
             v = i;
         }

@@ -267,6 +267,9 @@ MATMULS = [
     dict(tokens=45, E=5, K=2, inner=480, channels=274),               # an odd number of gated channels: rows of out on two bytes
     dict(tokens=300, E=3, K=2, inner=736, channels=510),
     dict(tokens=1300, E=3, K=2, inner=2304, channels=640),            # several stages round, three scale boxes
+    dict(tokens=1500, E=2, K=1, inner=4128, channels=1056),           # long inner extent, many rows
+    dict(tokens=8000, E=640, K=8, inner=64, channels=256),            # more experts than the widest tile has tables for
+    dict(tokens=4000, E=520, K=8, inner=512, channels=96, skew=True),
 ]
 
 
