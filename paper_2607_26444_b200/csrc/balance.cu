@@ -24,7 +24,8 @@ BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params&
     g.groups = b.per_rank ? s.R : 1;
     g.group_tokens = b.per_rank ? s.T : (long long)s.R * s.T;
     // four tokens per warp, at least: more slices are more to add up
-    g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + 4 * kWarps - 1) / (4 * kWarps));
+    const int least = (int)tune("STRATA_BAL", 4) * kWarps;
+    g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + least - 1) / least);
     g.col_blocks = (s.E + kSumCols - 1) / kSumCols;
     return g;
 }

@@ -2,15 +2,21 @@
 // values of a row, grouped by expert as the routing layout orders them, times each expert's 4-bit weights (strata_layer.h has the
 // formulas).  The matrix instructions take the block scales themselves, from TMEM.
 //
-// As in 8 bits the weights are the M operand and the rows the N operand (matmul.cu).  A stage is 128 bytes of codes of every row, 256
-// values, which is one swizzle span.  Scales come in groups of 32 or 64 bytes of every row, for several stages: a box of 16
-// bytes per stage took as many requests of the copy engine as the codes themselves.  The instructions want the scales of 128 rows
-// as 32 lines, word (4 scales) by word, of rows l, l + 32, l + 64 and l + 96, in each of TMEM's four quarters: four warps read the rows
-// from shared memory and store them to their quarters.  (tcgen05.cp from lines prepared in shared memory takes about
-// 60 cycles each in which the matrix unit does nothing: a quarter of the time at 512 rows per expert, a third with e4m3 scales.)
+// As in 8 bits the weights are the M operand and the rows the N operand (matmul.cu).  A span is 128 bytes of codes of every row, 256
+// values, one swizzle span; a stage is one or two of them.  Scales come in groups of 32 or 64 bytes of every row, for several
+// spans: a box of 16 bytes per span took as many requests of the copy engine as the codes themselves.  The instructions want
+// the scales of 128 rows as 32 lines, word (4 scales) by word, of rows l, l + 32, l + 64 and l + 96, in each of TMEM's four quarters:
+// warps read the rows from shared memory and store them to their quarters, a chunk of four words at a time.  (tcgen05.cp from
+// lines prepared in shared memory took about 60 cycles each in which the matrix unit did nothing: 324 us with, 251 without the
+// copies at 512 rows per expert, 405 and 262 with e4m3 scales.)
 //
-// CG = 2: two CTAs share a tile.  Each holds its own 128 weight rows and half of the tile's rows, and one instruction of the leader
+// CG = 2: two CTAs share a tile.  Each holds its own weight rows and half of the tile's rows, and one instruction of the leader
 // multiplies for both; an SM then reads 7 KB of shared memory for what takes it 10 KB alone, and fetches half the rows from L2.
+//
+// What bounds it (7168 -> 2 x 2048, 32 experts): few rows, the weights' way from HBM (32 rows each: 498 MB in 86 us, 5.9 TB/s); many,
+// the way from L2 to an SM: a pair of <2,1,192> needs 32 KB a span and SM, at the 52 bytes a cycle that loads alone reach 600 cycles, where
+// the instructions take 400; <2,2,192> needs 47 KB for twice the instructions, 900 for 800, but has no second set of accumulators,
+// and its epilogue (28 of 217 us) stands alone.
 #include "tiles.cuh"
 
 #ifdef STRATA_TEST_HOOKS
@@ -843,7 +849,7 @@ cudaError_t run4(const strata_moe_shape& s, const strata_matmul4_args& a, Mat4Pa
             const cuuint64_t stride = (cuuint64_t)(i == 0 ? a.w.code_stride : a.w.block_stride);
             const bool eights = a.gated && MB == 1;
             const cuuint64_t dims[5] = {bytes, eights ? 8 : rows, parts, eights ? rows / 8 : 1, (cuuint64_t)s.E};
-            const cuuint64_t strides[4] = {stride, rows * stride, 8 * stride, parts * rows * stride};
+            const cuuint64_t strides[4] = {stride, rows * stride, eights ? 8 * stride : stride, parts * rows * stride};
             const cuuint32_t boxes[5] = {box, (cuuint32_t)(eights ? 8 : MB * kM / parts), (cuuint32_t)parts, eights ? 8u : 1u, 1};
             if (!encode(i == 0 ? &p.map_w : &p.map_ws, i == 0 ? a.w.codes : a.w.block, 5, dims, strides, boxes, swizzle))
                 return cudaErrorInvalidValue;

@@ -96,6 +96,73 @@ def test_layer_is_captured_and_replayed(kind):
     assert int(layer.stats.count.sum()) == 2 * 40 * 2
 
 
+def product(tokens, inner, seed, kind="mxfp4", E=4, K=2, channels=544):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    ctx = B.MoEContext(1, tokens, 8, E, K)
+    ids = torch.argsort(torch.rand((tokens, E), generator=g, device=DEV), dim=1)[:, :K].to(torch.int32).contiguous()
+    lay = ctx.layout(ids)
+    a, w = B.empty_rows4((tokens * K,), inner, kind), B.empty_rows4((E, channels), inner, kind)
+    x = torch.randn((tokens * K, inner), generator=g, device=DEV).to(torch.bfloat16)
+    ctx.quantize_rows4(torch.randn((E, channels, inner), generator=g, device=DEV).to(torch.bfloat16), w)
+    out = torch.zeros((tokens * K, channels // 2), dtype=torch.bfloat16, device=DEV)
+
+    def call():
+        ctx.quantize_rows4(x, a)
+        ctx.expert_matmul4(lay, a, w, out, gated=True)
+        return out
+    return ctx, call, x
+
+
+@pytest.mark.parametrize("tokens,inner", [(20, 1024), (500, 512), (3000, 1024), (3000, 4608)])
+def test_products_are_captured_and_replayed(tokens, inner):
+    """One CTA per tile and pairs of them, in a graph beside the calls one by one."""
+    ctx, call, x = product(tokens, inner, 5)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = call()
+    x.copy_(torch.randn(x.shape, device=DEV).to(torch.bfloat16))
+    for _ in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    got = out.clone()
+    assert torch.equal(call(), got) and bool(got.any())
+    assert ctx.device_status() == B.STRATA_OK
+
+
+def test_products_on_two_streams_at_once():
+    """Two contexts, each with its own workspace, on two streams: pairs of CTAs of both share the GPU."""
+    cases = [product(3000, 2048, 1), product(2500, 4352, 2, "nvfp4")]
+    want = []
+    for _, call, _ in cases:
+        want.append(call().clone())
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in cases]
+    for _ in range(5):
+        for stream, (_, call, _) in zip(streams, cases):
+            with torch.cuda.stream(stream):
+                call()
+    torch.cuda.synchronize()
+    for (ctx, call, _), w in zip(cases, want):
+        assert ctx.device_status() == B.STRATA_OK
+        assert torch.equal(call(), w)
+
+
+def test_products_in_a_budget_of_sms():
+    """Grids for 1, 2, 3 and 20 SMs (an odd number leaves one without a partner) give the same rows."""
+    for tokens, inner in ((40, 512), (2000, 1024)):
+        ctx, call, _ = product(tokens, inner, 9)
+        want = call().clone()
+        for n in (1, 2, 3, 20, 0):
+            ctx.sm_budget(n)
+            got = call()
+            # another tile shape sums in another order: binary32 roundings, then one to bf16
+            assert torch.allclose(got.float(), want.float(), rtol=2.0 ** -7, atol=2.0 ** -9 * float(want.float().abs().max()))
+        assert ctx.device_status() == B.STRATA_OK
+
+
 def test_router_gradient_of_loss_and_gate_weights_together():
     """balance() = the gradient of the gate weights plus that of the losses, each against the 64-bit formulas."""
     import layer_reference
