@@ -1,7 +1,7 @@
-// Balance loss of the router with the counts per expert, and its gradient (strata_layer.h has the formulas).  One warp owns a
-// token; its lanes hold vectors of 16 bytes in turn (scores.cuh gives a lane its experts in one run: two loads of half a sector each).
-// All sums run in an order that the shape fixes: a warp's tokens, the
-// warps of a block, the blocks of a group, the groups.
+// Balance loss of the router with the counts per expert, and its gradient (strata_layer.h has the formulas).  LPT lanes of a warp own a
+// token, 4 to 32 by the number of experts, each VPL logits in vectors of 16 bytes in turn (scores.cuh gives a lane its experts in one
+// run: two loads of half a sector each).  All sums run in an order that the shape fixes: the tokens of a run of lanes, the runs of
+// a block, the blocks of a group, the groups.
 #include "scores.cuh"
 
 namespace strata {
@@ -10,21 +10,28 @@ namespace {
 
 constexpr int kWarps = 8;
 constexpr int kSumCols = 8;            // experts of a block of balance_sum_kernel, one per warp
+// Tokens of a run of lanes, at least.  More slices finish sooner and are more to add up: 16,384 x 128 takes 15.8, 15.2, 13.1 and 14.0 us
+// with 1, 2, 4 and 8, the gradient, which adds nothing up, 7.1, 7.1, 9.5 and 12.1.
+constexpr int kLossTokens = 4, kGradTokens = 2;
+// Logits per lane and lanes per token.  Several tokens in a warp share its exchanges: 65,536 x 64, loss and gradient, 24 + 16 us with a
+// warp per token, 17 + 11 with eight lanes.
+constexpr int width_of(int E) { return E <= 256 ? 8 : E <= 512 ? 16 : 32; }
+constexpr int lanes_of(int E) { return E <= 32 ? 4 : E <= 64 ? 8 : E <= 128 ? 16 : 32; }
 // Blocks that an SM holds at a time, by the registers that VPL logits per lane take: grids are one wave of them.
-constexpr int loss_blocks(int vpl) { return vpl <= 8 ? 4 : vpl == 16 ? 2 : 1; }
-constexpr int grad_blocks(int vpl) { return vpl <= 4 ? 4 : vpl == 8 ? 3 : vpl == 16 ? 2 : 1; }
+constexpr int loss_blocks(int vpl) { return vpl == 8 ? 4 : vpl == 16 ? 2 : 1; }
+constexpr int grad_blocks(int vpl) { return vpl == 8 ? 3 : vpl == 16 ? 2 : 1; }
 
 struct BalanceGeom {
     int groups, slices, col_blocks;
     long long group_tokens;
 };
-BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params& b, int blocks)
+// At least `tokens` of them for every run of lanes.
+BalanceGeom balance_geom(const strata_moe_shape& s, const strata_balance_params& b, int blocks, int tokens)
 {
     BalanceGeom g;
     g.groups = b.per_rank ? s.R : 1;
     g.group_tokens = b.per_rank ? s.T : (long long)s.R * s.T;
-    // four tokens per warp, at least: more slices are more to add up
-    const int least = (int)tune("STRATA_BAL", 4) * kWarps;
+    const int least = tokens * kWarps * (32 / lanes_of(s.E));
     g.slices = (int)min((long long)max(1, blocks / g.groups), (g.group_tokens + least - 1) / least);
     g.col_blocks = (s.E + kSumCols - 1) / kSumCols;
     return g;
@@ -50,52 +57,67 @@ struct BalanceParams {
     float weight, z_weight;
 };
 
-// Expert of register r of a lane.
-template <int VPL, bool BF16>
-__device__ __forceinline__ int expert_of(int lane, int r)
+// Sum and maximum over the LPT lanes of a token.
+template <int LPT>
+__device__ __forceinline__ float token_sum(float v)
+{
+#pragma unroll
+    for (int o = LPT / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+    return v;
+}
+template <int LPT>
+__device__ __forceinline__ float token_max(float v)
+{
+#pragma unroll
+    for (int o = LPT / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(kFull, v, o));
+    return v;
+}
+// Expert of register r of the token's lane `at`.
+template <int LPT, bool BF16>
+__device__ __forceinline__ int expert_of(int at, int r)
 {
     constexpr int VW = BF16 ? 8 : 4;
-    if constexpr (VPL >= VW) return r / VW * (32 * VW) + lane * VW + r % VW;
-    else return lane * VPL + r;
+    return r / VW * (LPT * VW) + at * VW + r % VW;
 }
 // A token's logits (NaN and places beyond E: -inf), or RAW values (places beyond E: 0).
-template <int VPL, bool BF16, bool RAW = false>
-__device__ __forceinline__ void load_token(float (&l)[VPL], const void* base, long long row_off, int lane, int E, bool vec_ok)
+template <int LPT, int VPL, bool BF16, bool RAW = false>
+__device__ __forceinline__ void load_token(float (&l)[VPL], const void* base, long long row_off, int at, int E, bool vec_ok)
 {
-    constexpr int VW = VPL < (BF16 ? 8 : 4) ? VPL : BF16 ? 8 : 4;
+    constexpr int VW = BF16 ? 8 : 4;
 #pragma unroll
     for (int j = 0; j < VPL; j += VW) {
         float(&part)[VW] = *reinterpret_cast<float(*)[VW]>(&l[j]);
-        const int e0 = expert_of<VPL, BF16>(lane, j);
-        if (BF16 && VW == 4 && vec_ok && e0 + VW <= E) {          // rows too short for 16 bytes a lane
-            const uint2 v = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(base) + row_off + e0);
-            part[0] = __uint_as_float(v.x << 16);
-            part[1 % VW] = __uint_as_float(v.x & 0xffff0000u);
-            part[2 % VW] = __uint_as_float(v.y << 16);
-            part[3 % VW] = __uint_as_float(v.y & 0xffff0000u);
-        } else {
-            load_logits<VW, BF16, true>(part, base, row_off, e0, E, vec_ok);
-        }
+        const int e0 = expert_of<LPT, BF16>(at, j);
+        load_logits<VW, BF16, true>(part, base, row_off, e0, E, vec_ok);
         if constexpr (!RAW) {
 #pragma unroll
-            for (int i = 0; i < VW; ++i)
-                part[i] = expert_of<VPL, BF16>(lane, j) + i < E ? fmaxf(part[i], -INFINITY) : -INFINITY;    // the other operand for NaN
+            for (int i = 0; i < VW; ++i) part[i] = e0 + i < E ? fmaxf(part[i], -INFINITY) : -INFINITY;    // the other operand for NaN
         }
     }
 }
-template <int VPL, bool BF16>
-__device__ __forceinline__ void store_token(const float (&g)[VPL], void* base, long long row_off, int lane, int E, bool vec_ok)
+template <int LPT, int VPL, bool BF16>
+__device__ __forceinline__ void store_token(const float (&g)[VPL], void* base, long long row_off, int at, int E, bool vec_ok)
 {
-    constexpr int VW = VPL < (BF16 ? 8 : 4) ? VPL : BF16 ? 8 : 4;
+    constexpr int VW = BF16 ? 8 : 4;
 #pragma unroll
     for (int j = 0; j < VPL; j += VW) {
         const float(&part)[VW] = *reinterpret_cast<const float(*)[VW]>(&g[j]);
-        const int e0 = expert_of<VPL, BF16>(lane, j);
-        if (BF16 && VW == 4 && vec_ok && e0 + VW <= E)
-            *reinterpret_cast<uint2*>(static_cast<uint16_t*>(base) + row_off + e0) =
-                make_uint2(pack_bf16x2(part[0], part[1 % VW]), pack_bf16x2(part[2 % VW], part[3 % VW]));
-        else store_row<VW, BF16>(part, base, row_off, e0, E, vec_ok);
+        store_row<VW, BF16>(part, base, row_off, expert_of<LPT, BF16>(at, j), E, vec_ok);
     }
+}
+// A token's ids, up to 32 / LPT in each of its lanes.
+template <int LPT>
+__device__ __forceinline__ void load_ids(int (&id)[32 / LPT], const int32_t* ids, int at, int K)
+{
+#pragma unroll
+    for (int s = 0; s < 32 / LPT; ++s) id[s] = s * LPT + at < K ? ids[s * LPT + at] : -1;
+}
+// Whether any of a token's lanes says so.
+template <int LPT>
+__device__ __forceinline__ bool token_any(bool v, int lane)
+{
+    const unsigned all = __ballot_sync(kFull, v);
+    return LPT == 32 ? all != 0 : (all >> (lane / LPT * LPT) & ((1u << (LPT & 31)) - 1u)) != 0;
 }
 
 // within 2^-23
@@ -114,7 +136,7 @@ __device__ __forceinline__ float approx_rcp(float v)
 template <bool BF16>
 __device__ __forceinline__ float exp_of(float x) { return BF16 ? __expf(x) : expf(x); }
 
-template <int VPL, bool BF16, bool SIGMOID>
+template <int LPT, int VPL, bool BF16, bool SIGMOID>
 __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&rest)[VPL],
                                              float (&soft)[VPL], float& lse)
 {
@@ -131,13 +153,13 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
             total += soft[i];
             top = fmaxf(top, l[i] == -INFINITY ? 0.0f : fabsf(l[i]));
         }
-        s = warp_sum(s);
+        s = token_sum<LPT>(s);
         const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) p[i] *= inv;
         if (!want_soft) return;
         if (__all_sync(kFull, top <= 60.0f)) {
-            total = warp_sum(total);
+            total = token_sum<LPT>(total);
             const float inv_total = total > 0.0f ? __frcp_rn(total) : 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) soft[i] *= inv_total;
@@ -148,7 +170,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
     float m = l[0];
 #pragma unroll
     for (int i = 1; i < VPL; ++i) m = fmaxf(m, l[i]);
-    m = warp_max(m);
+    m = token_max<LPT>(m);
     float s = 0.0f;
     if (fabsf(m) < INFINITY) {
 #pragma unroll
@@ -159,7 +181,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
     }
 #pragma unroll
     for (int i = 0; i < VPL; ++i) s += soft[i];
-    s = warp_sum(s);
+    s = token_sum<LPT>(s);
     const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) soft[i] *= inv;
@@ -224,14 +246,16 @@ __device__ __forceinline__ bool last_block(const BalanceParams& p)
 }
 static_assert(kSumCols == kWarps, "both kernels finish with blocks of as many warps");
 
-template <int VPL, bool BF16, bool SIGMOID>
+// Bound by issue and latency: at 65,536 x 256 (sigmoid, per rank) 31 us on the device for 67 MB, 295 instructions a token, and 8 us for the sums.
+template <int LPT, int VPL, bool BF16, bool SIGMOID>
 __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(const BalanceParams p)
 {
-    extern __shared__ float s_sum[];                              // [warps][32 * VPL]
+    constexpr int kRuns = 32 / LPT, kSlots = LPT * VPL;           // runs of lanes of a warp; places for experts
+    extern __shared__ float s_sum[];                              // [warps * runs][slots]
     __shared__ int s_count[kMaxExperts];
-    __shared__ float s_z[kWarps];
-    __shared__ int s_n[kWarps];
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    __shared__ float s_z[kWarps * kRuns];
+    __shared__ int s_n[kWarps * kRuns];
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, at = lane % LPT, run = warp * kRuns + lane / LPT;
     const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
     for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) s_count[e] = 0;
     __syncthreads();
@@ -240,47 +264,61 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
     int n = 0;
 #pragma unroll
     for (int i = 0; i < VPL; ++i) sum[i] = 0.0f;
-    const long long step = (long long)p.slices * kWarps, first = (long long)group * p.group_tokens;
-    long long t = slice * kWarps + warp;
+    const long long step = (long long)p.slices * kWarps * kRuns, first = (long long)group * p.group_tokens;
+    long long t = (long long)(slice * kWarps + warp) * kRuns;     // the warp's first token; run r has t + r
     float next[VPL];
-    int next_id = -1;
+    int next_id[kRuns];
     auto load = [&] {                                             // a token ahead: its way from memory is longer than one token's work
-        const long long tok = first + t;
-        next_id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
-        load_token<VPL, BF16>(next, p.logits, tok * p.stride, lane, p.E, p.vec_ok != 0);
+        const long long mine = t + lane / LPT, tok = first + min(mine, p.group_tokens - 1);
+        load_ids<LPT>(next_id, p.ids + tok * p.K, at, mine < p.group_tokens ? p.K : 0);
+        load_token<LPT, VPL, BF16>(next, p.logits, tok * p.stride, at, p.E, p.vec_ok != 0);
     };
     if (t < p.group_tokens) load();
     while (t < p.group_tokens) {
         float l[VPL], q[VPL], rest[VPL], soft[VPL], lse;
-        int id = next_id;
+        int id[kRuns];
 #pragma unroll
         for (int i = 0; i < VPL; ++i) l[i] = next[i];
+#pragma unroll
+        for (int s = 0; s < kRuns; ++s) id[s] = next_id[s];
         t += step;
         if (t < p.group_tokens) load();
-        if (id < -1 || id >= p.E) {
-            report_status(p.status, STRATA_ERR_BAD_EXPERT_ID);
-            id = -1;
-        }
-        if (!__any_sync(kFull, id >= 0)) continue;
-        if (id >= 0) atomicAdd(&s_count[id], 1);
-        token_scores<VPL, BF16, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
+        bool routed = false;
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) sum[i] += q[i];
-        z = fmaf(lse, lse, z);
-        ++n;
+        for (int s = 0; s < kRuns; ++s) {
+            if (id[s] < -1 || id[s] >= p.E) {
+                report_status(p.status, STRATA_ERR_BAD_EXPERT_ID);
+                id[s] = -1;
+            }
+            if (id[s] >= 0) {
+                atomicAdd(&s_count[id[s]], 1);
+                routed = true;
+            }
+        }
+        __syncwarp();
+        routed = token_any<LPT>(routed, lane);
+        if (!__any_sync(kFull, routed)) continue;
+        token_scores<LPT, VPL, BF16, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
+        if (routed) {
+#pragma unroll
+            for (int i = 0; i < VPL; ++i) sum[i] += q[i];
+            z = fmaf(lse, lse, z);
+            ++n;
+        }
+        __syncwarp();
     }
 #pragma unroll
-    for (int i = 0; i < VPL; ++i) s_sum[warp * 32 * VPL + expert_of<VPL, BF16>(lane, i)] = sum[i];
-    if (lane == 0) {
-        s_z[warp] = z;
-        s_n[warp] = n;
+    for (int i = 0; i < VPL; ++i) s_sum[run * kSlots + expert_of<LPT, BF16>(at, i)] = sum[i];
+    if (at == 0) {
+        s_z[run] = z;
+        s_n[run] = n;
     }
     __syncthreads();
     griddep_launch_dependents();
     for (int e = (int)threadIdx.x; e < p.E; e += kWarps * 32) {
         float a = 0.0f;
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) a += s_sum[w * 32 * VPL + e];
+        for (int w = 0; w < kWarps * kRuns; ++w) a += s_sum[w * kSlots + e];
         const size_t to = ((size_t)group * p.E + e) * p.slices + slice;
         p.part_p[to] = a;
         p.part_c[to] = s_count[e];
@@ -288,7 +326,7 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
     if (threadIdx.x == 0) {
         float a = 0.0f;
         int c = 0;
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kWarps * kRuns; ++w) {
             a += s_z[w];
             c += s_n[w];
         }
@@ -377,11 +415,13 @@ struct BalanceGradParams {
     float weight, z_weight;
 };
 
-template <int VPL, bool BF16, bool SIGMOID>
+// The same case: 43 us, 400 instructions a token, 134 MB (21 us of HBM); a third block per SM keeps it at 80 registers.
+template <int LPT, int VPL, bool BF16, bool SIGMOID>
 __global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_kernel(const BalanceGradParams p)
 {
+    constexpr int kRuns = 32 / LPT;
     __shared__ int s_alive, s_total;
-    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31;
+    const int warp = (int)threadIdx.x >> 5, lane = (int)threadIdx.x & 31, at = lane % LPT;
     const int group = (int)blockIdx.x / p.slices, slice = (int)blockIdx.x - group * p.slices;
     if (threadIdx.x == 0) s_alive = s_total = 0;
     __syncthreads();
@@ -404,90 +444,96 @@ __global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_ke
     float c[VPL];
 #pragma unroll
     for (int i = 0; i < VPL; ++i) {
-        const int e = expert_of<VPL, BF16>(lane, i);
+        const int e = expert_of<LPT, BF16>(at, i);
         c[i] = e < p.E ? unit * (float)p.count[(size_t)group * p.E + e] : 0.0f;
     }
-    const long long step = (long long)p.slices * kWarps, first = (long long)group * p.group_tokens;
-    long long t = slice * kWarps + warp;
+    const long long step = (long long)p.slices * kWarps * kRuns, first = (long long)group * p.group_tokens;
+    long long t = (long long)(slice * kWarps + warp) * kRuns;
     float next[VPL];
-    int next_id = -1;
+    int next_id[kRuns];
     auto load = [&] {                                             // a token ahead, as above
-        const long long tok = first + t;
-        next_id = lane < p.K ? p.ids[tok * p.K + lane] : -1;
-        load_token<VPL, BF16>(next, p.logits, tok * p.stride, lane, p.E, p.vec_ok != 0);
+        const long long mine = t + lane / LPT, tok = first + min(mine, p.group_tokens - 1);
+        load_ids<LPT>(next_id, p.ids + tok * p.K, at, mine < p.group_tokens ? p.K : 0);
+        load_token<LPT, VPL, BF16>(next, p.logits, tok * p.stride, at, p.E, p.vec_ok != 0);
     };
     if (t < p.group_tokens) load();
     while (t < p.group_tokens) {
-        const long long tok = first + t;
-        const int id = next_id;
+        const long long mine = t + lane / LPT, tok = first + mine;
+        const bool live = mine < p.group_tokens;
         float l[VPL], q[VPL], rest[VPL], soft[VPL], g[VPL], lse;
+        bool routed = false;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) l[i] = next[i];
-        if (p.add) load_token<VPL, BF16, true>(g, p.add, tok * p.add_stride, lane, p.E, p.add_vec_ok != 0);
+#pragma unroll
+        for (int s = 0; s < kRuns; ++s) routed |= next_id[s] >= 0 && next_id[s] < p.E;
+        if (p.add && live) load_token<LPT, VPL, BF16, true>(g, p.add, tok * p.add_stride, at, p.E, p.add_vec_ok != 0);
         else {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) g[i] = 0.0f;
         }
         t += step;
         if (t < p.group_tokens) load();
-        if (__any_sync(kFull, id >= 0 && id < p.E)) {
-            token_scores<VPL, BF16, SIGMOID>(l, want_z, q, rest, soft, lse);
+        __syncwarp();
+        routed = token_any<LPT>(routed, lane);
+        if (__any_sync(kFull, routed)) {
+            token_scores<LPT, VPL, BF16, SIGMOID>(l, want_z, q, rest, soft, lse);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) dot = fmaf(q[i], c[i], dot);
-            dot = warp_sum(dot);
+            dot = token_sum<LPT>(dot);
 #pragma unroll
             for (int i = 0; i < VPL; ++i) {
                 float d = q[i] * (c[i] - dot);
                 if constexpr (SIGMOID) d *= rest[i];
                 if (want_z) d = fmaf(unit_z * lse, soft[i], d);
                 if (l[i] == -INFINITY) d = 0.0f;
-                g[i] += d;
+                if (routed) g[i] += d;
             }
         }
-        store_token<VPL, BF16>(g, p.dlogits, tok * p.dstride, lane, p.E, p.dvec_ok != 0);
+        if (live) store_token<LPT, VPL, BF16>(g, p.dlogits, tok * p.dstride, at, p.E, p.dvec_ok != 0);
+        __syncwarp();
     }
 }
 
 size_t aligned(size_t n) { return (n + 15) & ~(size_t)15; }
 
-template <int VPL, bool BF16>
-cudaError_t loss_vpl(const BalanceParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
+template <int LPT, int VPL, bool BF16>
+cudaError_t loss_width(const BalanceParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
 {
     const size_t smem = (size_t)kWarps * 32 * VPL * sizeof(float);
-    return sigmoid ? launch_pdl(balance_kernel<VPL, BF16, true>, grid, kWarps * 32, smem, st, p)
-                   : launch_pdl(balance_kernel<VPL, BF16, false>, grid, kWarps * 32, smem, st, p);
+    return sigmoid ? launch_pdl(balance_kernel<LPT, VPL, BF16, true>, grid, kWarps * 32, smem, st, p)
+                   : launch_pdl(balance_kernel<LPT, VPL, BF16, false>, grid, kWarps * 32, smem, st, p);
 }
-template <int VPL, bool BF16>
-cudaError_t grad_vpl(const BalanceGradParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
+template <int LPT, int VPL, bool BF16>
+cudaError_t grad_width(const BalanceGradParams& p, bool sigmoid, unsigned grid, cudaStream_t st)
 {
-    return sigmoid ? launch_pdl(balance_grad_kernel<VPL, BF16, true>, grid, kWarps * 32, 0, st, p)
-                   : launch_pdl(balance_grad_kernel<VPL, BF16, false>, grid, kWarps * 32, 0, st, p);
+    return sigmoid ? launch_pdl(balance_grad_kernel<LPT, VPL, BF16, true>, grid, kWarps * 32, 0, st, p)
+                   : launch_pdl(balance_grad_kernel<LPT, VPL, BF16, false>, grid, kWarps * 32, 0, st, p);
 }
 
 }  // namespace
 
 size_t balance_scratch_bytes(const strata_moe_shape& s, const strata_balance_params& b, int n_sm)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(lanes_width(s.E)));
+    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(width_of(s.E)), kLossTokens);
     const size_t blocks = (size_t)g.groups * g.slices;
     return 2 * aligned(blocks * s.E * 4) + 2 * aligned(blocks * 4) + aligned((size_t)g.groups * g.col_blocks * 4);
 }
 
-#define STRATA_BY_WIDTH(f, ...)                                                                     \
-    switch (lanes_width(s.E)) {                                                                     \
-        case 1: return bf ? f<1, true>(__VA_ARGS__) : f<1, false>(__VA_ARGS__);                     \
-        case 2: return bf ? f<2, true>(__VA_ARGS__) : f<2, false>(__VA_ARGS__);                     \
-        case 4: return bf ? f<4, true>(__VA_ARGS__) : f<4, false>(__VA_ARGS__);                     \
-        case 8: return bf ? f<8, true>(__VA_ARGS__) : f<8, false>(__VA_ARGS__);                     \
-        case 16: return bf ? f<16, true>(__VA_ARGS__) : f<16, false>(__VA_ARGS__);                  \
-        default: return bf ? f<32, true>(__VA_ARGS__) : f<32, false>(__VA_ARGS__);                  \
+#define STRATA_BY_WIDTH(f, ...)                                                                                    \
+    switch (s.E <= 256 ? lanes_of(s.E) : width_of(s.E) * 4) {                                                      \
+        case 4: return bf ? f<4, 8, true>(__VA_ARGS__) : f<4, 8, false>(__VA_ARGS__);                              \
+        case 8: return bf ? f<8, 8, true>(__VA_ARGS__) : f<8, 8, false>(__VA_ARGS__);                              \
+        case 16: return bf ? f<16, 8, true>(__VA_ARGS__) : f<16, 8, false>(__VA_ARGS__);                           \
+        case 32: return bf ? f<32, 8, true>(__VA_ARGS__) : f<32, 8, false>(__VA_ARGS__);                           \
+        case 64: return bf ? f<32, 16, true>(__VA_ARGS__) : f<32, 16, false>(__VA_ARGS__);                         \
+        default: return bf ? f<32, 32, true>(__VA_ARGS__) : f<32, 32, false>(__VA_ARGS__);                         \
     }
 
 namespace {
 cudaError_t first_pass(const strata_moe_shape& s, const BalanceParams& p, bool bf, bool sigmoid, unsigned grid, cudaStream_t st)
 {
-    STRATA_BY_WIDTH(loss_vpl, p, sigmoid, grid, st)
+    STRATA_BY_WIDTH(loss_width, p, sigmoid, grid, st)
 }
 }  // namespace
 
@@ -495,7 +541,7 @@ cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_
                                 long long stride, const int32_t* ids, float* loss, const strata_balance_stats& stats,
                                 void* scratch, int* status, unsigned* ticket, int n_sm, cudaStream_t st, int* n_launches)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(lanes_width(s.E)));
+    const BalanceGeom g = balance_geom(s, b, n_sm * loss_blocks(width_of(s.E)), kLossTokens);
     const size_t blocks = (size_t)g.groups * g.slices;
     BalanceParams p{};
     p.logits = logits;
@@ -539,7 +585,7 @@ cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_
                                 const void* add, long long add_stride, void* dlogits, long long dstride, int n_sm,
                                 cudaStream_t st)
 {
-    const BalanceGeom g = balance_geom(s, b, n_sm * grad_blocks(lanes_width(s.E)));
+    const BalanceGeom g = balance_geom(s, b, n_sm * grad_blocks(width_of(s.E)), kGradTokens);
     BalanceGradParams p{};
     p.logits = logits;
     p.add = add;
@@ -563,7 +609,7 @@ cudaError_t launch_balance_grad(const strata_moe_shape& s, const strata_balance_
     p.z_weight = b.z_weight;
     const bool bf = type == STRATA_T_BF16, sigmoid = b.score == STRATA_SCORE_SIGMOID;
     const unsigned grid = (unsigned)(g.groups * g.slices);
-    STRATA_BY_WIDTH(grad_vpl, p, sigmoid, grid, st)
+    STRATA_BY_WIDTH(grad_width, p, sigmoid, grid, st)
 }
 
 }  // namespace strata
