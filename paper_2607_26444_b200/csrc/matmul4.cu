@@ -17,6 +17,8 @@
 // the way from L2 to an SM: a pair of <2,1,192> needs 32 KB a span and SM, at the 52 bytes a cycle that loads alone reach 600 cycles, where
 // the instructions take 400; <2,2,192> needs 47 KB for twice the instructions, 900 for 800, but has no second set of accumulators,
 // and its epilogue (28 of 217 us) stands alone.
+#include <type_traits>
+
 #include "tiles.cuh"
 
 #ifdef STRATA_TEST_HOOKS
@@ -90,7 +92,7 @@ struct Mat4Params {
     long long a_rows, a_scale_stride, w_scale_stride, out_stride;
     int E, k_spans, channels, m_tiles;  // channels: rows of w per expert
     int last_steps;                     // matrix instructions of the last span
-    int out_vec;                        // eight channels of out lie on 16 bytes
+    int out_piece;                      // 16, 8, 4 or 2 bytes: what every row of out starts on
 #ifdef STRATA_TEST_HOOKS
     int test_flags;
 #endif
@@ -682,7 +684,7 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
             return row * kPitch + ((kTight ? chunk ^ (row >> 2 & 1) : chunk ^ (row >> 1 & 3)) << 4);
         };
         const int half = p.channels / 2, limit = GATED ? half : p.channels;
-        const bool scaled = p.a_scale || p.w_scale, vec = p.out_vec != 0;
+        const bool scaled = p.a_scale || p.w_scale;
         Work w;
         for (uint32_t use = 0; next_tile(*tail, use, w, lane, dead, p.status); ++use) {
             const int m = w.m * CG + (int)rank;
@@ -718,6 +720,27 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                 for (int b = 0; b < MB; ++b)
 #pragma unroll
                     for (int h = 0; h < 2; ++h) tmem_ld_16x32(v[b][h], addr + b * BN + ((uint32_t)(16 * h) << 16) + c0);
+            };
+            // the staged step to out, in pieces of W bytes that every row starts on, neighbouring lanes along a row (16,384 rows,
+            // 2048 -> 7164 nvfp4, 8 bytes: 201 us; element by element from 16-byte pieces 557; 7168 channels 178)
+            auto flush = [&](auto piece, int c0, int block) {
+                constexpr int W = decltype(piece)::value, kPieces = kPitch / W, kRowsAt = 32 / kPieces;
+#pragma unroll 4
+                for (int i = 0; i < kStep / kRowsAt; ++i) {
+                    const int row = i * kRowsAt + lane / kPieces, at = lane % kPieces * W;
+                    const int ch = ch0 + block + at / 2;
+                    if (c0 + row >= rows || ch >= limit) continue;
+                    const unsigned char* from = mine + place(row, at >> 4) + (at & 15);
+                    uint16_t* to = out + (long long)(c0 + row) * p.out_stride + ch;
+                    if (ch + W / 2 <= limit) {
+                        if constexpr (W == 16) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+                        else if constexpr (W == 8) *reinterpret_cast<uint2*>(to) = *reinterpret_cast<const uint2*>(from);
+                        else if constexpr (W == 4) *reinterpret_cast<uint32_t*>(to) = *reinterpret_cast<const uint32_t*>(from);
+                        else *to = *reinterpret_cast<const uint16_t*>(from);
+                    } else {
+                        for (int e = 0; ch + e < limit; ++e) to[e] = reinterpret_cast<const uint16_t*>(from)[e];
+                    }
+                }
             };
             __syncwarp();
             if (rows > 0) load(0);
@@ -774,23 +797,10 @@ __global__ void __launch_bounds__(Tile4<NV, CG, MB, BN>::threads, 1) expert_matm
                         }
                     }
                     __syncwarp();
-                    constexpr int kChunks16 = kPitch / 16, kRowsAt = 32 / kChunks16;     // 16-byte chunks of a row, rows at a time
-#pragma unroll
-                    for (int i = 0; i < kStep / kRowsAt; ++i) {
-                        const int row2 = i * kRowsAt + lane / kChunks16, chunk = lane % kChunks16;
-                        const int ch = ch0 + b * kM + chunk * 8;
-                        const uint4 q = *reinterpret_cast<const uint4*>(mine + place(row2, chunk));
-                        if (c0 + row2 < rows) {
-                            uint16_t* at = out + (long long)(c0 + row2) * p.out_stride + ch;
-                            if (vec && ch + 8 <= limit) *reinterpret_cast<uint4*>(at) = q;
-                            else {
-                                const uint32_t words[4] = {q.x, q.y, q.z, q.w};
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (ch + e < limit) at[e] = (uint16_t)(words[e >> 1] >> (16 * (e & 1)));
-                            }
-                        }
-                    }
+                    if (p.out_piece == 16) flush(std::integral_constant<int, 16>(), c0, b * kM);
+                    else if (p.out_piece == 8) flush(std::integral_constant<int, 8>(), c0, b * kM);
+                    else if (p.out_piece == 4) flush(std::integral_constant<int, 4>(), c0, b * kM);
+                    else flush(std::integral_constant<int, 2>(), c0, b * kM);
                     __syncwarp();
                 }
             }
@@ -935,7 +945,9 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     p.k_spans = (a.inner / 2 + kKBytes - 1) / kKBytes;
     p.last_steps = (a.inner / 2 - (p.k_spans - 1) * kKBytes + kUmmaK - 1) / kUmmaK;
     p.channels = a.channels;
-    p.out_vec = a.out_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.out) & 15u) == 0;
+    const uintptr_t at = reinterpret_cast<uintptr_t>(a.out);
+    p.out_piece = 16;
+    while (p.out_piece > 2 && (a.out_stride * 2 % p.out_piece != 0 || at % p.out_piece != 0)) p.out_piece /= 2;
     // Which tile: the shortest estimate of rounds * (spans * (c + n * filled) + f + g * filled) over the GPU, where c + n is what one span
     // of a full tile takes and f + g what a tile adds, n and g the parts that grow with the rows in it (g is the epilogue where the
     // accumulators are not doubled); at least the weights' way from HBM.  The constants were fitted to 65 measured shapes of

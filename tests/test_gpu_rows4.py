@@ -340,3 +340,20 @@ def test_rows_and_blocks_that_are_not_a_number_stay_apart():
     keep = torch.arange(a.rows, device=DEV) != 3
     assert bool(torch.isnan(out[3]).all()) and torch.equal(out[keep], want[keep])
     assert ctx.device_status() == B.STRATA_OK
+
+
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("rows", [30, 400])
+def test_rows_of_out_that_start_on_fewer_than_16_bytes(rows, gated):
+    """Every start of a row of out (16, 8, 4 and 2 bytes), with channels that end inside a piece; what lies around is left alone."""
+    for channels in (96, 100, 102) if gated else (96, 100, 101):
+        for stride, first in ((128, 0), (132, 0), (130, 0), (129, 0), (128, 4), (128, 2), (128, 1)):
+            ctx, lay, a, w, out = matmul_case(rows, 3, 2, 96, channels, gated, "mxfp4", 3)
+            wide = channels // 2 if gated else channels
+            buf = torch.full((a.rows * stride + 8,), 99.0, dtype=torch.bfloat16, device=DEV)
+            view = buf[first:first + a.rows * stride].view(a.rows, stride)[:, :wide]
+            ctx.expert_matmul4(lay, a, w, view, gated=gated)
+            check_products(lay, a, w, view, gated)
+            around = buf.clone()
+            around[first:first + a.rows * stride].view(a.rows, stride)[:, :wide] = 99.0
+            assert bool((around == 99.0).all())
