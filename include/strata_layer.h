@@ -182,7 +182,7 @@ strata_status strata_moe_expert_matmul(strata_ctx *ctx, const strata_moe_layout_
  * A value is an e2m1 code (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives), times the scale of its block, times the scale of its
  * row if there is one.  Two codes share a byte, the first in its low half.
  *   MXF4: blocks of 32 values, a scale byte s stands for 2^(s - 127), 255 for NaN (e8m0)
- *   NVF4: blocks of 16 values, the scale is an e4m3 number
+ *   NVF4: blocks of 16 values, the scale is an e4m3 number, not negative
  * codes: row r at byte r * code_stride, cols / 2 bytes; block: scale bytes, row r at byte r * block_stride, cols / 32 or
  * cols / 16 bytes; scale: float, row r at scale[r * scale_stride], or NULL (1).  codes and block are 16-byte aligned, their strides
  * multiples of 16 that hold a row, below 2^40.  cols is a multiple of 32. */
