@@ -130,7 +130,9 @@ __device__ __forceinline__ float approx_rcp(float v)
 
 // The normalised scores p of a token; rest: 1 - s of the sigmoid, without the cancellation; where they are asked for, the softmax and
 // the logarithm of its sum.  One exponential per logit gives the sigmoid on both sides, 1 / (1 + e) and e / (1 + e) with e = exp(-|l|),
-// and exp(l) itself, which the softmax takes as long as no logit of the token passes 60.  Reciprocals are within 2^-23.
+// and exp(l) itself, which the softmax takes as long as no logit of the token passes 60.  Reciprocals are within 2^-23.  Sigmoid scores
+// that add up to less than 2^-100 are their exponentials to within that, so their quotients are the softmax, whose sum is at least 1: the
+// reciprocal of their own would pass binary32, or they would have vanished.
 // For bf16 logits the exponential is the hardware's power of two (within 2 + 1.2 |x| ulp by CUDA's bound: 2^-16 where the score is
 // still a normal number), against 2^-9 of the gradient's own rounding; in the sums over tokens that error is of either sign.
 template <bool BF16>
@@ -141,6 +143,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
                                              float (&soft)[VPL], float& lse)
 {
     lse = 0.0f;
+    bool tiny = false;
     if constexpr (SIGMOID) {
         float s = 0.0f, total = 0.0f, top = 0.0f;
 #pragma unroll
@@ -154,11 +157,13 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
             top = fmaxf(top, l[i] == -INFINITY ? 0.0f : fabsf(l[i]));
         }
         s = token_sum<LPT>(s);
-        const float inv = s > 0.0f ? __frcp_rn(s) : 0.0f;
+        tiny = s < 0x1p-100f;
+        const float inv = tiny ? 0.0f : __frcp_rn(s);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) p[i] *= inv;
-        if (!want_soft) return;
-        if (__all_sync(kFull, top <= 60.0f)) {
+        const bool any_tiny = __any_sync(kFull, tiny);
+        if (!want_soft && !any_tiny) return;
+        if (!any_tiny && __all_sync(kFull, top <= 60.0f)) {
             total = token_sum<LPT>(total);
             const float inv_total = total > 0.0f ? __frcp_rn(total) : 0.0f;
 #pragma unroll
@@ -186,7 +191,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
 #pragma unroll
     for (int i = 0; i < VPL; ++i) soft[i] *= inv;
     if (s > 0.0f) lse = m + logf(s);
-    if constexpr (!SIGMOID) {
+    if (!SIGMOID || tiny) {
 #pragma unroll
         for (int i = 0; i < VPL; ++i) p[i] = soft[i];
     }

@@ -122,6 +122,21 @@ def test_balance_masked_logits(score, z_weight):
     assert not dlogits[7].any() and not dlogits[9].any() and float(dlogits[4, 5]) == 0
 
 
+@pytest.mark.parametrize("shift", [-60.0, -80.0, -95.0, -200.0])
+@pytest.mark.parametrize("experts", [40, 256])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_balance_tiny_scores(shift, experts, dtype):
+    """Tokens whose sigmoid scores add up to a subnormal number, or to less than binary32 holds, beside ordinary ones: their
+    quotients are those of the exponentials (the scores are, within 2^-86 of themselves)."""
+    ctx, logits, ids = case(2, 30, experts, 3, dtype, 4, False)
+    logits[1::2] += shift
+    logits[5, 3:] = -float("inf")
+    for z_weight in (0.0, 0.1):
+        params = B.make_balance("sigmoid", weight=1.0, z_weight=z_weight)
+        loss, stats, dlogits = run(ctx, params, logits, ids)
+        check(ctx, params, "sigmoid", 1.0, z_weight, logits, ids, loss, stats, dlogits)
+
+
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 def test_balance_incoming_gradients(dtype):
     ctx, logits, ids = case(3, 50, 96, 4, dtype, 8, True)
