@@ -267,7 +267,8 @@ strata_status strata_moe_expert_matmul4(strata_ctx* ctx, const strata_moe_layout
     STRATA_CHECK(check_rows4(a->a, a->type, a->inner));
     STRATA_CHECK(check_rows4(a->w, a->type, a->inner));
     // a tensor map holds the distance between two experts' weights in 40 bits
-    if (a->w.code_stride * a->channels >= (1ll << 40) || a->w.block_stride * a->channels >= (1ll << 40)) return STRATA_ERR_SHAPE;
+    const int64_t widest = ((1ll << 40) - 1) / a->channels;
+    if (a->w.code_stride > widest || a->w.block_stride > widest) return STRATA_ERR_SHAPE;
     if (!on(a->out, 2)) return STRATA_ERR_ALIGNMENT;
     if (!ctx->ws) return STRATA_ERR_WORKSPACE;
     if (a->a_rows < (int64_t)recv_rows(s)) return STRATA_ERR_CAPACITY;

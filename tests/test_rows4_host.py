@@ -98,7 +98,9 @@ def test_dequantize_refusals(ctx, change, want):
     (dict(inner=240), SHAPE), (dict(inner=0), SHAPE), (dict(inner=131104), SHAPE), (dict(channels=0), SHAPE),
     (dict(channels=127, gated=1), SHAPE), (dict(channels=(1 << 24) + 2), SHAPE), (dict(out_stride=127), SHAPE),
     (dict(gated=1, out_stride=64), CUDA), (dict(a_rows=511), CAP), (dict(a_rows=1 << 31), SHAPE),
-    (dict(w=rows4(code_stride=1 << 36)), SHAPE), (dict(w=rows4(block_stride=1 << 36)), SHAPE)])
+    (dict(w=rows4(code_stride=1 << 36)), SHAPE), (dict(w=rows4(block_stride=1 << 36)), SHAPE),
+    (dict(w=rows4(code_stride=1 << 39), channels=1 << 24, out_stride=1 << 24), SHAPE),             # their product is 2^63
+    (dict(w=rows4(block_stride=(1 << 40) - 16), channels=1 << 24, out_stride=1 << 24), SHAPE)])
 def test_matmul_refusals(ctx, change, want):
     kw = dict(type=MX, gated=0, inner=256, channels=128, a_rows=512, a=rows4(), w=rows4(), out=P, out_stride=128)
     kw.update(change)
