@@ -575,8 +575,10 @@ def _scale_stride(t, rows: int) -> int:
         raise ValueError(f"scales are fp32, not {t.dtype}")
     if n < rows:
         raise ValueError("one scale per row is needed")
-    if t.dim() == 1 or t.is_contiguous():
-        stride = t.stride(-1) if t.dim() else 1
+    if t.dim() == 1:
+        stride = t.stride(0)
+    elif t.is_contiguous():
+        stride = 1                                        # a last dimension of one element may have any stride of its own
     else:
         stride = _strides(t[..., None])[2]
     if stride == 0 and rows > 1:
