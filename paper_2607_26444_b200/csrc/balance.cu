@@ -133,13 +133,14 @@ __device__ __forceinline__ float approx_rcp(float v)
 // and exp(l) itself, which the softmax takes as long as no logit of the token passes 60.  Reciprocals are within 2^-23.  Sigmoid scores
 // that add up to less than 2^-100 are their exponentials to within that, so their quotients are the softmax, whose sum is at least 1: the
 // reciprocal of their own would pass binary32, or they would have vanished.
+// Tokens that share a warp choose together; those that are not routed have no vote, and their results, whatever they are, are not used.
 // For bf16 logits the exponential is the hardware's power of two (within 2 + 1.2 |x| ulp by CUDA's bound: 2^-16 where the score is
 // still a normal number), against 2^-9 of the gradient's own rounding; in the sums over tokens that error is of either sign.
 template <bool BF16>
 __device__ __forceinline__ float exp_of(float x) { return BF16 ? __expf(x) : expf(x); }
 
 template <int LPT, int VPL, bool BF16, bool SIGMOID>
-__device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_soft, float (&p)[VPL], float (&rest)[VPL],
+__device__ __forceinline__ void token_scores(const float (&l)[VPL], bool routed, bool want_soft, float (&p)[VPL], float (&rest)[VPL],
                                              float (&soft)[VPL], float& lse)
 {
     lse = 0.0f;
@@ -157,13 +158,13 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool want_so
             top = fmaxf(top, l[i] == -INFINITY ? 0.0f : fabsf(l[i]));
         }
         s = token_sum<LPT>(s);
-        tiny = s < 0x1p-100f;
+        tiny = routed && s < 0x1p-100f;
         const float inv = tiny ? 0.0f : __frcp_rn(s);
 #pragma unroll
         for (int i = 0; i < VPL; ++i) p[i] *= inv;
         const bool any_tiny = __any_sync(kFull, tiny);
         if (!want_soft && !any_tiny) return;
-        if (!any_tiny && __all_sync(kFull, top <= 60.0f)) {
+        if (!any_tiny && __all_sync(kFull, top <= 60.0f || !routed)) {
             total = token_sum<LPT>(total);
             const float inv_total = total > 0.0f ? __frcp_rn(total) : 0.0f;
 #pragma unroll
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
         __syncwarp();
         routed = token_any<LPT>(routed, lane);
         if (!__any_sync(kFull, routed)) continue;
-        token_scores<LPT, VPL, BF16, SIGMOID>(l, p.z_weight != 0.0f, q, rest, soft, lse);
+        token_scores<LPT, VPL, BF16, SIGMOID>(l, routed, p.z_weight != 0.0f, q, rest, soft, lse);
         if (routed) {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) sum[i] += q[i];
@@ -481,7 +482,7 @@ __global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_ke
         __syncwarp();
         routed = token_any<LPT>(routed, lane);
         if (__any_sync(kFull, routed)) {
-            token_scores<LPT, VPL, BF16, SIGMOID>(l, want_z, q, rest, soft, lse);
+            token_scores<LPT, VPL, BF16, SIGMOID>(l, routed, want_z, q, rest, soft, lse);
             float dot = 0.0f;
 #pragma unroll
             for (int i = 0; i < VPL; ++i) dot = fmaf(q[i], c[i], dot);

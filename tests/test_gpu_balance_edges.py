@@ -1,0 +1,57 @@
+"""Balance loss and gradient on the GPU where they can go wrong: padding beside live tokens, far-apart bf16 logits, long sums of few
+experts, and every entry of the gradient.  Tolerances are derived beside each test before its first run (u = 2^-24)."""
+import os
+import sys
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2607_26444_b200 import binding as B
+
+sys.path.insert(0, os.path.dirname(os.path.abspath(__file__)))
+import rows4_reference as ref  # noqa: E402
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+U = 2.0 ** -24
+
+
+def f64(t):
+    return t.float().cpu().numpy().astype(np.float64)
+
+
+def make(R, T, E, K, dtype, seed, spread=2.0):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    logits = (spread * torch.randn((R * T, E), generator=g, device=DEV)).to(dtype)
+    ids = torch.argsort(torch.rand((R * T, E), generator=g, device=DEV), dim=1)[:, :K].to(torch.int32).reshape(R, T, K).contiguous()
+    return B.MoEContext(R, T, 8, E, K, allow_unrouted=True), logits, ids
+
+
+def run(ctx, params, logits, ids):
+    stats = ctx.balance_stats(params)
+    loss, dlogits = torch.empty(2, device=DEV), torch.empty_like(logits)
+    ctx.balance_loss(params, logits, ids, loss, stats)
+    ctx.balance_grad(params, logits, ids, stats, dlogits)
+    assert ctx.device_status() == B.STRATA_OK
+    return loss, stats, dlogits
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts", [8, 60, 128, 256])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_padding_changes_no_bit(score, experts, dtype):
+    """What stands in the logits of padding tokens, which may share a warp with live ones, shows nowhere."""
+    ctx, logits, ids = make(2, 51, experts, 4, dtype, experts)
+    ids.view(102, 4)[1::2] = -1
+    ids.view(102, 4)[70:] = -1
+    live = (ids.view(102, 4) >= 0).any(1)
+    params = B.make_balance(score, weight=1.0, z_weight=0.1)
+    loss, stats, dlogits = run(ctx, params, logits, ids)
+    for value in (float("nan"), float("inf"), -float("inf"), 1e4, -1e4):
+        other = logits.clone()
+        other[~live] = value
+        loss2, stats2, dlogits2 = run(ctx, params, other, ids)
+        assert torch.equal(loss, loss2) and torch.equal(stats.prob, stats2.prob) and torch.equal(stats.count, stats2.count)
+        assert torch.equal(dlogits, dlogits2) and not bool(dlogits2[~live].any())
