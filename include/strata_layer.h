@@ -12,8 +12,8 @@
  * Functions and quotients inside are binary32 as well.  Where they are coarser than expf and a rounded quotient (by CUDA's
  * bounds, in units of the last place of binary32): the gradient of softmax weights that are not renormalised, for bf16
  * logits: an exponential within 2 + 1.2 |l - max|; silu in a gated product: an exponential within 2 + 1.2 |g| and a division within
- * 2, and zero where g is below -87.3; the norm's gradient: a reciprocal square root within 2; the balance loss: a sigmoid's reciprocal
- * within 1, and for bf16 logits an exponential as in the router's gradient.  The router decides a token
+ * 2, and zero where g is below -87.3; the norm's gradient: a reciprocal square root within 2; the balance loss and
+ * its gradient: a sigmoid's reciprocal within 1; the gradient alone, for bf16 logits: an exponential as in the router's.  The router decides a token
  * in one of two ways, whose weights may differ in the last places.
  * The order of a row's sums depends on the rows and columns of the call: equal calls give equal bits, but the last bit of a row's norm
  * may differ between a call that holds it among few rows and one that holds it among many.

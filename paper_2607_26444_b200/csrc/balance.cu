@@ -134,12 +134,12 @@ __device__ __forceinline__ float approx_rcp(float v)
 // that add up to less than 2^-100 are their exponentials to within that, so their quotients are the softmax, whose sum is at least 1: the
 // reciprocal of their own would pass binary32, or they would have vanished.
 // Tokens that share a warp choose together; those that are not routed have no vote, and their results, whatever they are, are not used.
-// For bf16 logits the exponential is the hardware's power of two (within 2 + 1.2 |x| ulp by CUDA's bound: 2^-16 where the score is
-// still a normal number), against 2^-9 of the gradient's own rounding; in the sums over tokens that error is of either sign.
-template <bool BF16>
-__device__ __forceinline__ float exp_of(float x) { return BF16 ? __expf(x) : expf(x); }
+// FAST, for gradients in bf16: the exponential is the hardware's power of two (within 2 + 1.2 |x| ulp by CUDA's bound: 2^-16 where the
+// score is still a normal number), against 2^-9 of the gradient's own rounding.  The loss and the mean scores are binary32 and take expf.
+template <bool FAST>
+__device__ __forceinline__ float exp_of(float x) { return FAST ? __expf(x) : expf(x); }
 
-template <int LPT, int VPL, bool BF16, bool SIGMOID>
+template <int LPT, int VPL, bool FAST, bool SIGMOID>
 __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool routed, bool want_soft, float (&p)[VPL], float (&rest)[VPL],
                                              float (&soft)[VPL], float& lse)
 {
@@ -149,7 +149,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool routed,
         float s = 0.0f, total = 0.0f, top = 0.0f;
 #pragma unroll
         for (int i = 0; i < VPL; ++i) {
-            const float e = exp_of<BF16>(-fabsf(l[i])), r = approx_rcp(1.0f + e), small = e * r;
+            const float e = exp_of<FAST>(-fabsf(l[i])), r = approx_rcp(1.0f + e), small = e * r;
             p[i] = l[i] >= 0.0f ? r : small;
             rest[i] = l[i] >= 0.0f ? small : r;
             soft[i] = l[i] >= 0.0f ? approx_rcp(e) : e;
@@ -180,7 +180,7 @@ __device__ __forceinline__ void token_scores(const float (&l)[VPL], bool routed,
     float s = 0.0f;
     if (fabsf(m) < INFINITY) {
 #pragma unroll
-        for (int i = 0; i < VPL; ++i) soft[i] = exp_of<BF16>(l[i] - m);
+        for (int i = 0; i < VPL; ++i) soft[i] = exp_of<FAST>(l[i] - m);
     } else {                                                      // infinities at the maximum count as equal to it
 #pragma unroll
         for (int i = 0; i < VPL; ++i) soft[i] = l[i] == -INFINITY ? 0.0f : softmax_term(l[i], m);
@@ -304,7 +304,7 @@ __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(
         __syncwarp();
         routed = token_any<LPT>(routed, lane);
         if (!__any_sync(kFull, routed)) continue;
-        token_scores<LPT, VPL, BF16, SIGMOID>(l, routed, p.z_weight != 0.0f, q, rest, soft, lse);
+        token_scores<LPT, VPL, false, SIGMOID>(l, routed, p.z_weight != 0.0f, q, rest, soft, lse);
         if (routed) {
 #pragma unroll
             for (int i = 0; i < VPL; ++i) sum[i] += q[i];

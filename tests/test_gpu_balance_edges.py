@@ -55,3 +55,27 @@ def test_padding_changes_no_bit(score, experts, dtype):
         loss2, stats2, dlogits2 = run(ctx, params, other, ids)
         assert torch.equal(loss, loss2) and torch.equal(stats.prob, stats2.prob) and torch.equal(stats.count, stats2.count)
         assert torch.equal(dlogits, dlogits2) and not bool(dlogits2[~live].any())
+
+
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("experts", [40, 96, 160, 400])
+def test_mean_scores_of_far_apart_bf16_logits(score, experts):
+    """One token, so that the mean scores are its scores: they are as exact for bf16 logits as for binary32.
+
+    Logits are multiples of 1/2 from 0 to -80 (bf16 holds them, and their differences are exact).  Roundings of a score, in u: its
+    exponential 4 (2 ulp); the exponentials of the sum 4; the sum, 8 or 16 terms in a lane and 5 exchanges, 21; its reciprocal and the product
+    2; for a sigmoid a sum (1), a reciprocal within an ulp (2) and a product (1), once for the score and once for the sum, 8.  The
+    log-sum-exp is between 0 and 7 and takes the sum's 25 u and 2 ulp of itself; its square twice that, and a rounding."""
+    ctx, _, ids = make(1, 1, experts, 3, torch.bfloat16, 1)
+    g = torch.Generator().manual_seed(experts)
+    logits = (-0.5 * torch.randint(0, 161, (1, experts), generator=g))
+    logits[0, torch.randperm(experts, generator=g)[0]] = 0
+    logits = logits.to(torch.bfloat16).to(DEV)
+    params = B.make_balance(score, weight=1.0, z_weight=1.0)
+    loss, stats, _ = run(ctx, params, logits, ids)
+    want, _, _, prob, _, _ = ref.balance(f64(logits)[None], ids.cpu().numpy(), score, 1.0, 1.0)
+    normal = prob > 2.0 ** -120
+    assert normal.sum() > experts // 2
+    np.testing.assert_allclose(f64(stats.prob)[normal], prob[normal], rtol=(31 + (8 if score == "sigmoid" else 0)) * U)
+    lse = np.sqrt(want[1])
+    np.testing.assert_allclose(f64(loss)[1], want[1], rtol=0, atol=2 * lse * (25 + 4 * max(lse, 1)) * U + 2 * U * want[1])
