@@ -577,8 +577,11 @@ cudaError_t launch_balance_loss(const strata_moe_shape& s, const strata_balance_
     p.vec_ok = rows_on_16(logits, stride, type);
     p.weight = b.weight;
     p.z_weight = b.z_weight;
-    // A second launch costs its 2 us on the host and the GPU alike; a thread adds a slice in half a microsecond at worst.
-    p.finish = blocks * s.E <= 4096;
+    // A second launch costs 0.5 to 1 us on the GPU and 2 us on the host.  Without it a thread of the last block adds all slices of its
+    // expert up: us with two launches and with one, softmax, fp32, at 1, 8, 16, 32, 64 and 256 slices: 256 x 8 9.6, 8.8; 2048 x 8 9.7,
+    // 9.3; 4096 x 8 10.1, 9.5; 8192 x 8 10.0, 10.6; 16,384 x 8 10.7, 12.1; 65,536 x 8 13.7, 21.7; where a thread has several experts,
+    // at 8, 16 and 32: 8 groups of 2048 x 8 9.8, 9.9; 16 groups of 4096 x 16 12.6, 14.6; 8 groups of 8192 x 8 10.4, 15.5.
+    p.finish = g.slices <= 8 && blocks * s.E <= 4096;
     *n_launches = 1;
     const cudaError_t err = first_pass(s, p, type == STRATA_T_BF16, b.score == STRATA_SCORE_SIGMOID, (unsigned)blocks, st);
     if (err != cudaSuccess || p.finish) return err;

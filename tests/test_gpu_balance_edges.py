@@ -79,3 +79,30 @@ def test_mean_scores_of_far_apart_bf16_logits(score, experts):
     np.testing.assert_allclose(f64(stats.prob)[normal], prob[normal], rtol=(31 + (8 if score == "sigmoid" else 0)) * U)
     lse = np.sqrt(want[1])
     np.testing.assert_allclose(f64(loss)[1], want[1], rtol=0, atol=2 * lse * (25 + 4 * max(lse, 1)) * U + 2 * U * want[1])
+
+
+@pytest.mark.parametrize("R,T,E,per_rank,launches", [
+    (1, 300, 8, False, 1), (4, 96, 60, True, 1), (1, 1024, 60, False, 1), (1, 2049, 16, False, 2), (1, 16384, 16, False, 2),
+    (1, 65537, 8, False, 2), (1, 70000, 4, False, 2), (8, 8192, 8, True, 2), (2, 3000, 128, True, 2)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+def test_long_sums_of_few_experts(R, T, E, per_rank, launches, score):
+    """Many partial sums per expert are added up by a launch of their own, few by the first one's last block.
+
+    A mean score is a sum of positive terms: each within 40 u + 2 u max|l| (a score), added up by at most T / 64 tokens in a run of
+    lanes, 64 runs, 19 slices in a lane and 5 exchanges; a division.  A loss adds E and R terms and two roundings of its factors.
+    A log-sum-exp (its mean square is above 1) is off by 40 u and 4 u of itself, the mean of its squares twice that and the sums' roundings."""
+    ctx, logits, ids = make(R, T, E, min(3, E), torch.float32, E)
+    params = B.make_balance(score, weight=0.5, z_weight=0.25, per_rank=per_rank)
+    stats, loss = ctx.balance_stats(params), torch.empty(2, device=DEV)
+    before = ctx.launch_count()
+    ctx.balance_loss(params, logits, ids, loss, stats)
+    assert ctx.launch_count() - before == launches
+    groups = R if per_rank else 1
+    want, count, tokens, prob, _, _ = ref.balance(f64(logits).reshape(groups, -1, E), ids.cpu().numpy().reshape(groups, -1, ctx.K),
+                                                  score, 0.5, 0.25)
+    assert np.array_equal(stats.count.cpu().numpy(), count) and np.array_equal(stats.tokens.cpu().numpy(), tokens)
+    rel = (40 + 2 * float(logits.abs().max()) + T * R / groups / 64 + 90) * U
+    np.testing.assert_allclose(f64(stats.prob), prob, rtol=rel)
+    np.testing.assert_allclose(f64(loss)[0], want[0], rtol=rel + (E + R + 8) * U)
+    np.testing.assert_allclose(f64(loss)[1], want[1], rtol=2 * rel + 16 * U)
+    assert ctx.device_status() == B.STRATA_OK
