@@ -31,6 +31,7 @@ namespace {
 
 #ifdef STRATA_TEST_HOOKS
 std::atomic<int> g_inject_short_load4{0};    // see matmul.cu
+std::atomic<int> g_tile4{-1}, g_last_tile4{-1};    // the tile to take instead of the estimate's (-1: none); the one taken last
 #endif
 
 constexpr int kM = 128;                 // channels of a matrix instruction, in one CTA
@@ -968,10 +969,13 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     const float bytes_us = (float)used * (float)a.channels * (float)a.inner * (nv ? 0.5625f : 0.53125f) / kHbmBytesPerUs;
     int v = 1;                                                       // one CTA alone, any number of channels and experts
     float least = 0.0f;
+    auto takes = [&](const Cost& k) {
+        if (a.gated && k.mb == 1 && a.channels % 16 != 0) return false;      // takes gate and up by eights
+        return k.cg <= n_sm && (k.cg * k.mb < 4 || s.E <= Tile4<false, 2, 2, 192>::max_experts);
+    };
     for (int i = 0; i < 4; ++i) {
         const Cost& k = costs[nv][i];
-        if (a.gated && k.mb == 1 && a.channels % 16 != 0) continue;  // takes gate and up by eights
-        if (k.cg > n_sm || (k.cg * k.mb == 4 && s.E > Tile4<false, 2, 2, 192>::max_experts)) continue;
+        if (!takes(k)) continue;
         const int per_tile = k.cg * k.mb * kM / (a.gated ? 2 : 1), wide = a.channels / (a.gated ? 2 : 1), teams = n_sm / k.cg;
         const long long heights = (mean + k.bn - 1) / k.bn;
         const float tiles = (float)(used * heights * ((wide + per_tile - 1) / per_tile));
@@ -984,6 +988,13 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
         }
     }
     v = (int)tune("STRATA_MM4", v);
+#ifdef STRATA_TEST_HOOKS
+    if (const int forced = g_tile4.load(); forced >= 0) {
+        if (forced > 3 || !takes(costs[nv][forced])) return cudaErrorInvalidValue;
+        v = forced;
+    }
+    g_last_tile4.store(v);
+#endif
     return nv ? pick4<true>(v, s, a, p, n_sm, st) : pick4<false>(v, s, a, p, n_sm, st);
 }
 
@@ -991,4 +1002,6 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
 
 #ifdef STRATA_TEST_HOOKS
 extern "C" void strata_test_inject_short_load4(int on) { strata::g_inject_short_load4.store(on); }
+extern "C" void strata_test_tile4(int tile) { strata::g_tile4.store(tile); }
+extern "C" int strata_test_last_tile4(void) { return strata::g_last_tile4.load(); }
 #endif
