@@ -1,7 +1,8 @@
 """Child process of tests/test_gpu_matmul4_tiles.py: runs with STRATA_MOE_LIB pointing at the test-hooks build.
 
 Every product runs on the tile that the command line names (-1: the one that the library chooses), against the 64-bit form and the
-tolerances of test_gpu_rows4.py.  Prints one JSON line: {case: "ok", "refused" or what went wrong}."""
+tolerances of test_gpu_rows4.py.  Prints one JSON line: {case: ["ok", "refused" or what went wrong, a digest of the rows]}; with a second argument "timeout"
+what became of a wait that ran out."""
 import ctypes
 import hashlib
 import json
@@ -87,11 +88,35 @@ def capacity(kind, gated):
     return out
 
 
-def main(tile):
+def timeout(L):
+    """The first load of one launch is expected to bring 16 bytes more than it does (see rows4_timeout_child.py)."""
+    hook = L.strata_test_inject_short_load4
+    hook.argtypes, hook.restype = [ctypes.c_int], None
+    ctx, lay, a, w, out = t.matmul_case(1400, 2, 1, 2048, 1024, False, "nvfp4", 7)
+
+    def call():
+        ctx.expert_matmul4(lay, a, w, out)
+        return out.clone()
+    want = call()
+    res = {"before": ctx.device_status()}
+    hook(1)
+    call()
+    res["after_injection"] = ctx.device_status()
+    res["header_words"] = ctx.workspace[:44].view(torch.int32).cpu().tolist()
+    res["same_afterwards"] = bool(torch.equal(call(), want))
+    res["after_normal_call"] = ctx.device_status()
+    res["tile"] = L.strata_test_last_tile4()
+    return res
+
+
+def main(tile, what=""):
     L = B.lib()
     L.strata_test_tile4.argtypes, L.strata_test_tile4.restype = [ctypes.c_int], None
     L.strata_test_last_tile4.restype = ctypes.c_int
     L.strata_test_tile4(tile)
+    if what == "timeout":
+        print(json.dumps(timeout(L)), flush=True)
+        return
     res = {}
 
     def run(name, f, *args):
@@ -124,4 +149,4 @@ def main(tile):
 
 
 if __name__ == "__main__":
-    main(int(sys.argv[1]))
+    main(int(sys.argv[1]), *sys.argv[2:])
