@@ -106,3 +106,46 @@ def test_long_sums_of_few_experts(R, T, E, per_rank, launches, score):
     np.testing.assert_allclose(f64(loss)[0], want[0], rtol=rel + (E + R + 8) * U)
     np.testing.assert_allclose(f64(loss)[1], want[1], rtol=2 * rel + 16 * U)
     assert ctx.device_status() == B.STRATA_OK
+
+
+@pytest.mark.parametrize("R,T,E,K,dtype", [
+    (1, 3, 8, 2, torch.float32), (4, 33, 60, 4, torch.float32), (2, 300, 128, 8, torch.bfloat16), (8, 57, 256, 8, torch.float32),
+    (2, 40, 1000, 32, torch.float32), (16, 700, 384, 7, torch.float32), (4, 50, 500, 5, torch.bfloat16)])
+@pytest.mark.parametrize("score", ["softmax", "sigmoid"])
+@pytest.mark.parametrize("z_weight", [0.0, 0.5])
+def test_every_entry_of_the_gradient(R, T, E, K, dtype, score, z_weight):
+    """Entry e of a token is p (c - sum p c) times 1 - s for a sigmoid, and 2 z lse softmax / N, so that its error has the factor p too.
+
+    Relative to itself, in u: a score s = 2 (E / 32 + 16 + 2.4 max|l|) (exponentials of 2 ulp, or 2 + 1.2 |l - max| for bf16, arguments'
+    roundings, a sum of E / 32 + 5 terms, reciprocals, products); c 8; 1 - s 14 + 4.8 max|l| at most; the product 4.  The sum p c is off by s + E / 32 + 13 of
+    sum p |c|; log-sum-exp by s, and 4 of itself.  Half a step of the stored type is 2^-9 of the power of two above (bf16) or u.
+    The check itself is checked: zeros, an expectation with the scores of another expert, and one without the factor 1 - s fail it."""
+    ctx, logits, ids = make(R, T, E, K, dtype, E + K)
+    params = B.make_balance(score, weight=0.25, z_weight=z_weight, per_rank=True)
+    got = f64(run(ctx, params, logits, ids)[2]).reshape(R, T, E)
+    l = f64(logits).reshape(R, T, E)
+    _, count, tokens, _, db, dz = ref.balance(l, ids.cpu().numpy(), score, 0.25, z_weight)
+    want, top = db + dz, np.abs(l).max()
+    ex = np.exp(l - l.max(2, keepdims=True))
+    soft = ex / ex.sum(2, keepdims=True)
+    lse = l.max(2, keepdims=True) + np.log(ex.sum(2, keepdims=True))
+    p, slope = soft, np.ones_like(soft)
+    if score == "sigmoid":
+        p = 1 / (1 + np.exp(-l))
+        p, slope = p / p.sum(2, keepdims=True), 1 - p
+    c = (0.25 / R * count * E / (K * tokens[:, None] ** 2.0))[:, None]
+    dot = (p * c).sum(2, keepdims=True)
+    s = 2 * (E / 32 + 16 + 2.4 * top)
+    tol = p * slope * U * ((s + 8 + 14 + 4.8 * top + 4) * np.abs(c - dot) + 8 * c + (s + E / 32 + 21) * dot)
+    tol = tol + 2 * z_weight / tokens.sum() * soft * U * (s + (s + 12) * np.abs(lse))
+    step = np.ldexp(1.0, np.maximum(np.frexp(want)[1], -125) - 9) if dtype == torch.bfloat16 else U * np.abs(want)
+    tol = tol + step + 1e-40
+    bad = ~(np.abs(got - want) <= tol)
+    assert not bad.any(), (int(bad.sum()), got[bad][:4], want[bad][:4], tol[bad][:4])
+    norm = np.linalg.norm
+    assert norm(tol) <= (2.0 ** -7 if dtype == torch.bfloat16 else 2.0 ** -11) * norm(want)
+    wrong = [np.zeros_like(want), np.roll(p, 1, axis=2) * slope * (c - dot) + np.roll(dz, 1, axis=2)]
+    if score == "sigmoid" and z_weight == 0:                  # beside the z term in bf16 the factor need not show
+        wrong.append(p * (c - dot))
+    for other in wrong:
+        assert (np.abs(got - other) > tol).mean() > 0.75
