@@ -17,6 +17,8 @@
  * in one of two ways, whose weights may differ in the last places.
  * The order of a row's sums depends on the rows and columns of the call: equal calls give equal bits, but the last bit of a row's norm
  * may differ between a call that holds it among few rows and one that holds it among many.
+ * strata_ctx_set_sm_budget bounds the grids of the experts' products, which choose their tile by it as well; in int8 and in 4 bits that
+ * does not show in the results.  The other operators size their grids for the whole GPU.
  */
 #ifndef STRATA_LAYER_H
 #define STRATA_LAYER_H
@@ -214,8 +216,9 @@ strata_status strata_dequantize_rows4(strata_ctx *ctx, const strata_rows4 *q, in
 /* The experts' products over 4-bit rows: as strata_moe_expert_matmul, with
  *   y[r, n] = (sum_k a[r,k] * w[e,n,k]) * (scale[r] * w.scale[e,n])
  * where a and w include their block scales.  a: the rows of the receive buffer; w: [E, channels] rows in order (row e * channels
- * + n), of the same type.  inner: a multiple of 32, at most 131072; channels: any number, an even one if gated.  The sums are
- * binary32.  Needs a workspace (the status word).  One launch. */
+ * + n), of the same type, with a scale per channel (a scale per expert is spread over its channels) or none.  inner: a multiple of
+ * 32, at most 131072; channels: any number, an even one if gated.  The sums are binary32.  Needs a workspace (the status word).
+ * One launch. */
 typedef struct {
     int32_t type;                  /* STRATA_T_MXF4 or STRATA_T_NVF4, of a and w alike        */
     int32_t gated;                 /* 0 or 1: w holds the gate's channels/2 rows, then up's   */
@@ -252,7 +255,8 @@ typedef struct {                   /* device, what the gradient needs of the for
 } strata_balance_stats;
 
 /* logits, topk_ids as in strata_moe_route (logits may be any row-strided bf16 or float rows [R*T, E]); loss: device float
- * [2]; scratch: device, 16-byte aligned, of strata_moe_balance_scratch_bytes.  Needs a workspace.  One launch for small batches, else two. */
+ * [2]; scratch: device, 16-byte aligned, of strata_moe_balance_scratch_bytes.  Needs a workspace.  One launch where an expert
+ * has few partial sums (groups of up to 2,048 tokens at 32 experts or fewer, of 256 above 128), else two. */
 strata_status strata_moe_balance_scratch_bytes(strata_ctx *ctx, const strata_balance_params *params, size_t *bytes);
 strata_status strata_moe_balance_loss(strata_ctx *ctx, const strata_balance_params *params, const void *logits,
                                       int32_t logits_type, int64_t logits_stride, const int32_t *topk_ids, float *loss,

@@ -253,6 +253,8 @@ __device__ __forceinline__ bool last_block(const BalanceParams& p)
 static_assert(kSumCols == kWarps, "both kernels finish with blocks of as many warps");
 
 // Bound by issue and latency: at 65,536 x 256 (sigmoid, per rank) 31 us on the device for 67 MB, 295 instructions a token, and 8 us for the sums.
+// expf instead of the hardware's power of two for bf16 logits: 34.2 and 35.5 us there with the sums, softmax 28.8 and 30.5.  64 registers spill
+// 24 bytes a thread for fp32 logits with four lanes per token.
 template <int LPT, int VPL, bool BF16, bool SIGMOID>
 __global__ void __launch_bounds__(kWarps * 32, loss_blocks(VPL)) balance_kernel(const BalanceParams p)
 {
@@ -421,7 +423,8 @@ struct BalanceGradParams {
     float weight, z_weight;
 };
 
-// The same case: 43 us, 400 instructions a token, 134 MB (21 us of HBM); a third block per SM keeps it at 80 registers.
+// The same case: 43 us, 400 instructions a token, 134 MB (21 us of HBM); a third block per SM keeps it at 80 registers.  That spills 20 to 48
+// bytes a thread for a sigmoid, or with four lanes per token; at 1024 experts 255 registers spill 24 to 88 for a sigmoid.
 template <int LPT, int VPL, bool BF16, bool SIGMOID>
 __global__ void __launch_bounds__(kWarps * 32, grad_blocks(VPL)) balance_grad_kernel(const BalanceGradParams p)
 {

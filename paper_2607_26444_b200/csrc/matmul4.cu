@@ -956,7 +956,9 @@ cudaError_t launch_expert_matmul4(const strata_moe_shape& s, const strata_moe_la
     // 1.9 % above the best of the four (one tile for all: 6 to 44 %), and 25 % at worst.  At 7168 -> 4096 gated, 32 experts,
     // mxfp4, us for <1,1,64>, <1,2,96>, <2,1,192>, <2,2,192>: one token 27, 25, 28, 26; 32 rows each 86, 88, 88, 89; 128 rows 153, 117, 97, 100;
     // 256 rows 276, 178, 155, 141; 512 rows 502, 338, 234, 217; nvfp4 700, 384, 291, 248; 2048 -> 7168, 512 rows, mxfp4 299, 196, 143, 157.
-    // What the estimate does not see: rows spread around their mean, and slots that are masked or unrouted.
+    // What the estimate does not see: rows spread around their mean, and slots that are masked or unrouted.  7,422 rows over 60 experts, 1440 ->
+    // 2040 nvfp4, us for the four: even 58, 45, 40, 45, Zipf 60, 45, 46, 49; it takes <2,2,192> for both and expects 23 of it: some rounds of
+    // tiles of unlike height, dealt in the order of the experts.  What a tile is does not show in the results: all four sum in the same order.
     struct Cost { int cg, mb, bn; float c, n, f, g, hbm; };
     static const Cost costs[2][4] = {{{1, 1, 64, 0.03f, 0.28f, 0.84f, 0.0f, 1.15f}, {1, 2, 96, 0.29f, 0.29f, 0.82f, 0.0f, 1.00f},
                                       {2, 1, 192, 0.12f, 0.25f, 1.17f, 0.10f, 1.17f}, {2, 2, 192, 0.26f, 0.39f, 1.24f, 2.36f, 1.17f}},
